@@ -317,6 +317,103 @@ int cct_softmax_loss_backward(int32_t N, int32_t C, const float* prob, const int
                               float* dx, void* hip_stream);
 
 /*
+ * Feed-forward blocks: matrix products with their activation and additions in one kernel, in training and in
+ * serving.  (The paper's fully connected layers are cct_conv_* with K == H == W, fp32, bias only; these take 16-bit
+ * tensors too, rows of any stride, and what lies around the product.)  x is M x K (M tokens or images), a weight is
+ * N x K, both with consecutive values along K; a row begins `ld` elements behind the one before (ld >= the row's
+ * length; any element-aligned pointer and any such ld are accepted, rows that begin at multiples of 16 bytes are the
+ * fastest).  All tensors of a call have the descriptor's type.  Sums are fp32 (the matrix cores'), activations are
+ * computed in fp32, a result is rounded once.
+ */
+typedef enum { CCT_TYPE_F32 = 0, CCT_TYPE_BF16 = 1, CCT_TYPE_F16 = 2 } cct_type_t;
+typedef enum {
+  CCT_ACT_NONE = 0,
+  CCT_ACT_RELU = 1,     /* max(z, 0), NaN stays NaN; derivative 1 where z > 0, else 0               */
+  CCT_ACT_SILU = 2,     /* z / (1 + exp(-z))                                                        */
+  CCT_ACT_GELU = 3,     /* z * Phi(z), Phi the normal distribution function                         */
+  CCT_ACT_GELU_TANH = 4 /* z * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3))) / 2                      */
+} cct_activation_t;
+
+/* Host structs.  `type` holds a cct_type_t, `activation` a cct_activation_t.  M >= 0, the others >= 1; M == 0 is an
+ * empty batch: nothing is read, gradients of weights are zero. */
+typedef struct {
+  int32_t M, N, K; /* x: M x K, w: N x K, y: M x N */
+  int32_t type, activation;
+} cct_linear_desc_t;
+typedef struct {
+  int32_t M, F, K; /* x: M x K, wg and wu: F x K, h: M x F */
+  int32_t type, activation;
+} cct_gated_desc_t;
+
+/* Workspace of a call; backward == 0: the forward pass.  It must be 256-byte aligned; a smaller one is CCT_EWORKSPACE,
+ * whether or not the call at hand would need it all (operands whose rows are not 16-byte aligned are copied there). */
+int cct_linear_workspace_bytes(const cct_linear_desc_t* desc, int32_t backward, size_t* bytes);
+int cct_gated_workspace_bytes(const cct_gated_desc_t* desc, int32_t backward, size_t* bytes);
+
+/*
+ * z = x w^T + bias,  y = act(z) + residual.  bias (N values) and residual (M x N) may be NULL.  z may be NULL; a
+ * training program keeps it for the backward pass (it is not needed there for CCT_ACT_NONE).  y may be the residual
+ * itself (same pointer and ldr == ldy); nothing else may overlap.
+ */
+int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                       const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * dz = dy * act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum of dz over its rows; the residual's gradient is dy.
+ * Any of dx, dw, dbias may be NULL: it is not computed then, and w is not read without dx, x not without dw (both
+ * may be NULL then).  z may be NULL for CCT_ACT_NONE.  Sums run in a fixed order (bit-reproducible).  16-bit types:
+ * dz is rounded to the type before the products, as the matrix cores take it, and summed unrounded for dbias.
+ */
+int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                        const void* z, int64_t ldz, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dw,
+                        int64_t lddw, void* dbias, void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * The first half of a gated feed-forward block: g = x wg^T,  u = x wu^T,  h = act(g) * u, from the unrounded g and u.
+ * g and u may be NULL (both or neither); a training program keeps them.  The block's second half is
+ * cct_linear_forward on h, with the residual.
+ */
+int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
+                      const void* wu, int64_t ldwu, void* h, int64_t ldh, void* g, int64_t ldg, void* u, int64_t ldu,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+/*
+ * dg = dh * u * act'(g),  du = dh * act(g),  dx = dg wg + du wu (one sum),  dwg = dg^T x,  dwu = du^T x.
+ * dx may be NULL, and dwg and dwu together.  16-bit types: dg and du are rounded to the type before the products.
+ */
+int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
+                       const void* wu, int64_t ldwu, const void* g, int64_t ldg, const void* u, int64_t ldu,
+                       const void* dh, int64_t lddh, void* dx, int64_t lddx, void* dwg, int64_t lddwg, void* dwu,
+                       int64_t lddwu, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * From gradients to new weights, over lists of tensors (host arrays; the tensors they name are contiguous device
+ * memory, element-aligned).  The lists are read during the call only.
+ *
+ * cct_grad_norm: clip[0] = 2-norm of all values of all tensors, clip[1] = what the gradients are multiplied by:
+ * max_norm / norm where the norm exceeds max_norm, else 1 (Caffe's rule for clip_gradients; an infinite norm gives 0,
+ * a NaN NaN).  max_norm > 0, infinity for no limit.  clip: device, 2 floats.  The sum is carried in 64 bits and runs
+ * in a fixed order.
+ * cct_grad_scale: out[i] = grads[i] * clip[1], of the same sizes and types; out may be the gradients themselves, which
+ * are not touched then if clip[1] is 1.
+ * cct_sgd_update: Caffe's rule, v = momentum * v + rate * (clip[1] * g + decay * w),  w = w - v.  weights and
+ * moments are fp32, gradients of any type; clip may be NULL (1).  copies (may be NULL): w rounded to the type of the
+ * tensor given, which the products of the next step read.
+ */
+typedef struct {
+  void* data;
+  int64_t n;    /* values, may be 0 */
+  int32_t type; /* cct_type_t */
+  int32_t reserved;
+} cct_tensor_t;
+int cct_grad_norm_workspace_bytes(const cct_tensor_t* grads, int32_t count, size_t* bytes);
+int cct_grad_norm(const cct_tensor_t* grads, int32_t count, float max_norm, float* clip, void* workspace,
+                  size_t workspace_bytes, void* hip_stream);
+int cct_grad_scale(const cct_tensor_t* grads, int32_t count, const float* clip, const cct_tensor_t* out,
+                   void* hip_stream);
+int cct_sgd_update(const cct_tensor_t* grads, int32_t count, const float* clip, const cct_tensor_t* weights,
+                   const cct_tensor_t* moments, const cct_tensor_t* copies, float rate, float momentum, float decay,
+                   void* hip_stream);
+
+/*
  * Measurement aid (used by bench.py for the per-kernel roofline figures).  While enabled,
  * every kernel launch of the library is bracketed by two HIP events on the launching stream.
  * This is the one place where the library creates HIP objects (events, host side only); it

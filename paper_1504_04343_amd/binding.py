@@ -26,6 +26,9 @@ _lib = ctypes.CDLL(LIB_PATH)
 LOWER_AUTO, LOWER_TYPE1, LOWER_TYPE2, LOWER_TYPE3, LOWER_FUSED = 0, 1, 2, 3, 4
 PREC_F32, PREC_BF16_IN_F32_ACC = 0, 1
 PASS_FORWARD, PASS_BACKWARD_DATA, PASS_BACKWARD_WEIGHTS = 0, 1, 2
+PASS_BACKWARD = 3  # of the feed-forward operators, whose gradients are one call
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 OK, EINVAL, EWORKSPACE, EUNSUPPORTED, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5
 STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -38,7 +41,9 @@ EXPORTS = [
     "cct_relu_forward", "cct_relu_backward", "cct_pool_output_dims", "cct_maxpool_forward",
     "cct_maxpool_backward", "cct_lrn_forward", "cct_lrn_backward",
     "cct_dropout_forward", "cct_dropout_backward", "cct_softmax_loss_forward",
-    "cct_softmax_loss_backward",
+    "cct_softmax_loss_backward", "cct_linear_workspace_bytes", "cct_gated_workspace_bytes",
+    "cct_linear_forward", "cct_linear_backward", "cct_gated_forward", "cct_gated_backward",
+    "cct_grad_norm_workspace_bytes", "cct_grad_norm", "cct_grad_scale", "cct_sgd_update",
 ]
 
 
@@ -98,6 +103,36 @@ _lib.cct_dropout_forward.argtypes = [_vp, _vp, ctypes.c_float, _vp, _i64, _vp]
 _lib.cct_dropout_backward.argtypes = [_vp, _vp, ctypes.c_float, _vp, _i64, _vp]
 _lib.cct_softmax_loss_forward.argtypes = [_i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.cct_softmax_loss_backward.argtypes = [_i32, _i32, _vp, _vp, _vp, _vp]
+
+
+class LinearDesc(ctypes.Structure):
+    """cct_linear_desc_t."""
+    _fields_ = [(k, ctypes.c_int32) for k in ("M", "N", "K", "type", "activation")]
+
+
+class GatedDesc(ctypes.Structure):
+    """cct_gated_desc_t."""
+    _fields_ = [(k, ctypes.c_int32) for k in ("M", "F", "K", "type", "activation")]
+
+
+class Tensor(ctypes.Structure):
+    """cct_tensor_t."""
+    _fields_ = [("data", _vp), ("n", _i64), ("type", _i32), ("reserved", _i32)]
+
+
+_lp, _gp, _tp = ctypes.POINTER(LinearDesc), ctypes.POINTER(GatedDesc), ctypes.POINTER(Tensor)
+_f32 = ctypes.c_float
+_lib.cct_linear_workspace_bytes.argtypes = [_lp, _i32, ctypes.POINTER(_sz)]
+_lib.cct_gated_workspace_bytes.argtypes = [_gp, _i32, ctypes.POINTER(_sz)]
+_lib.cct_linear_forward.argtypes = [_lp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _sz, _vp]
+_lib.cct_linear_backward.argtypes = [_lp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp,
+                                     _sz, _vp]
+_lib.cct_gated_forward.argtypes = [_gp] + [_vp, _i64] * 6 + [_vp, _sz, _vp]
+_lib.cct_gated_backward.argtypes = [_gp] + [_vp, _i64] * 9 + [_vp, _sz, _vp]
+_lib.cct_grad_norm_workspace_bytes.argtypes = [_tp, _i32, ctypes.POINTER(_sz)]
+_lib.cct_grad_norm.argtypes = [_tp, _i32, _f32, _vp, _vp, _sz, _vp]
+_lib.cct_grad_scale.argtypes = [_tp, _i32, _vp, _tp, _vp]
+_lib.cct_sgd_update.argtypes = [_tp, _i32, _vp, _tp, _tp, _tp, _f32, _f32, _f32, _vp]
 
 
 class ProfileEntry(ctypes.Structure):
@@ -399,3 +434,175 @@ def cct_softmax_loss_backward(prob, label, dx) -> None:
     N, C = prob.shape
     _check(_lib.cct_softmax_loss_backward(N, C, _ptr(prob, "prob"), _iptr(label, "label", (N,)),
                                           _ptr(dx, "dx", (N, C)), _stream()), "cct_softmax_loss_backward")
+
+
+# ---- feed-forward blocks ----------------------------------------------------------------------
+# A matrix is a two-dimensional tensor whose values are consecutive along a row; its rows may lie further apart.
+
+_DTYPES = (torch.float32, torch.bfloat16, torch.float16)  # by TYPE_*
+
+
+def make_linear_desc(M, N, K, type=TYPE_F32, activation=ACT_NONE) -> LinearDesc:
+    return LinearDesc(M, N, K, type, activation)
+
+
+def make_gated_desc(M, F, K, type=TYPE_F32, activation=ACT_SILU) -> GatedDesc:
+    return GatedDesc(M, F, K, type, activation)
+
+
+def cct_linear_workspace_bytes(desc: LinearDesc, pass_: int) -> int:
+    out = _sz()
+    _check(_lib.cct_linear_workspace_bytes(ctypes.byref(desc), int(pass_ != PASS_FORWARD), ctypes.byref(out)),
+           "cct_linear_workspace_bytes")
+    return out.value
+
+
+def cct_gated_workspace_bytes(desc: GatedDesc, pass_: int) -> int:
+    out = _sz()
+    _check(_lib.cct_gated_workspace_bytes(ctypes.byref(desc), int(pass_ != PASS_FORWARD), ctypes.byref(out)),
+           "cct_gated_workspace_bytes")
+    return out.value
+
+
+def alloc_linear_workspace(desc: LinearDesc, pass_: int):
+    return torch.empty(cct_linear_workspace_bytes(desc, pass_), dtype=torch.uint8, device="cuda")
+
+
+def alloc_gated_workspace(desc: GatedDesc, pass_: int):
+    return torch.empty(cct_gated_workspace_bytes(desc, pass_), dtype=torch.uint8, device="cuda")
+
+
+def _mat(t, name, rows, cols, dtype, optional=False):
+    """Address and row stride of a matrix."""
+    if t is None:
+        if optional:
+            return None, 0
+        raise ValueError("%s is required" % name)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a torch tensor on the GPU" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.shape != (rows, cols):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (rows, cols)))
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise TypeError("%s must have consecutive values along a row" % name)
+    if rows <= 1:
+        ld = cols
+    elif ld < cols:
+        raise TypeError("%s has rows that overlap" % name)
+    return t.data_ptr(), ld
+
+
+def _vec(t, name, n, dtype):
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or t.shape != (n,) or \
+            not t.is_contiguous():
+        raise TypeError("%s must be a contiguous %s GPU tensor of shape (%d,)" % (name, dtype, n))
+    return t.data_ptr()
+
+
+def _dtype_of(desc):
+    if not 0 <= desc.type < len(_DTYPES):
+        raise CctError(EINVAL, "type %d" % desc.type)
+    return _DTYPES[desc.type]
+
+
+def cct_linear_forward(desc: LinearDesc, x, w, bias, residual, y, z, workspace) -> None:
+    """y = act(x w^T + bias) + residual; bias, residual and z (the product before the activation) may be None."""
+    M, N, K, dt = desc.M, desc.N, desc.K, _dtype_of(desc)
+    _check(_lib.cct_linear_forward(
+        ctypes.byref(desc), *_mat(x, "x", M, K, dt), *_mat(w, "w", N, K, dt), _vec(bias, "bias", N, dt),
+        *_mat(residual, "residual", M, N, dt, True), *_mat(y, "y", M, N, dt), *_mat(z, "z", M, N, dt, True),
+        *_ws(workspace), _stream()), "cct_linear_forward")
+
+
+def cct_linear_backward(desc: LinearDesc, x, w, z, dy, dx, dw, dbias, workspace) -> None:
+    """dx, dw and dbias from dy; each may be None, then x (without dw) and w (without dx) may be too."""
+    M, N, K, dt = desc.M, desc.N, desc.K, _dtype_of(desc)
+    _check(_lib.cct_linear_backward(
+        ctypes.byref(desc), *_mat(x, "x", M, K, dt, dw is None), *_mat(w, "w", N, K, dt, dx is None),
+        *_mat(z, "z", M, N, dt, True), *_mat(dy, "dy", M, N, dt), *_mat(dx, "dx", M, K, dt, True),
+        *_mat(dw, "dw", N, K, dt, True), _vec(dbias, "dbias", N, dt), *_ws(workspace), _stream()),
+        "cct_linear_backward")
+
+
+def cct_gated_forward(desc: GatedDesc, x, wg, wu, h, g, u, workspace) -> None:
+    """h = act(x wg^T) * (x wu^T); g and u, the two products, are kept if given."""
+    M, F, K, dt = desc.M, desc.F, desc.K, _dtype_of(desc)
+    _check(_lib.cct_gated_forward(
+        ctypes.byref(desc), *_mat(x, "x", M, K, dt), *_mat(wg, "wg", F, K, dt), *_mat(wu, "wu", F, K, dt),
+        *_mat(h, "h", M, F, dt), *_mat(g, "g", M, F, dt, True), *_mat(u, "u", M, F, dt, True), *_ws(workspace),
+        _stream()), "cct_gated_forward")
+
+
+def cct_gated_backward(desc: GatedDesc, x, wg, wu, g, u, dh, dx, dwg, dwu, workspace) -> None:
+    """dx, dwg and dwu from dh and the products that the forward pass kept."""
+    M, F, K, dt = desc.M, desc.F, desc.K, _dtype_of(desc)
+    none = dx is None
+    _check(_lib.cct_gated_backward(
+        ctypes.byref(desc), *_mat(x, "x", M, K, dt, dwg is None), *_mat(wg, "wg", F, K, dt, none),
+        *_mat(wu, "wu", F, K, dt, none), *_mat(g, "g", M, F, dt), *_mat(u, "u", M, F, dt), *_mat(dh, "dh", M, F, dt),
+        *_mat(dx, "dx", M, K, dt, True), *_mat(dwg, "dwg", F, K, dt, True), *_mat(dwu, "dwu", F, K, dt, True),
+        *_ws(workspace), _stream()), "cct_gated_backward")
+
+
+# ---- gradient norm and weight update ------------------------------------------------------------
+
+class TensorList:
+    """The tensors of a list and their descriptors, made once and passed to any number of calls.  The tensors are
+    held: their addresses stay valid as long as the list lives (do not resize them)."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        for i, t in enumerate(self.tensors):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise TypeError("tensor %d must be a torch tensor on the GPU" % i)
+            if t.dtype not in _DTYPES or not t.is_contiguous():
+                raise TypeError("tensor %d must be contiguous fp32, bf16 or fp16" % i)
+        self.count = len(self.tensors)
+        self.array = (Tensor * max(1, self.count))(
+            *(Tensor(t.data_ptr(), t.numel(), _DTYPES.index(t.dtype), 0) for t in self.tensors))
+
+
+def make_tensor_list(tensors) -> TensorList:
+    return TensorList(tensors)
+
+
+def cct_grad_norm_workspace_bytes(grads: TensorList) -> int:
+    out = _sz()
+    _check(_lib.cct_grad_norm_workspace_bytes(grads.array, grads.count, ctypes.byref(out)),
+           "cct_grad_norm_workspace_bytes")
+    return out.value
+
+
+def alloc_norm_workspace(grads: TensorList):
+    return torch.empty(cct_grad_norm_workspace_bytes(grads), dtype=torch.uint8, device="cuda")
+
+
+def _same(a: TensorList, b: TensorList, name):
+    if b.count != a.count:
+        raise ValueError("%s has %d tensors, expected %d" % (name, b.count, a.count))
+    return b.array
+
+
+def cct_grad_norm(grads: TensorList, max_norm, clip, workspace) -> None:
+    """clip (2 fp32 values on the GPU): the norm of all gradients, and what they are to be multiplied by."""
+    _check(_lib.cct_grad_norm(grads.array, grads.count, max_norm, _ptr(clip, "clip", (2,)), *_ws(workspace),
+                              _stream()), "cct_grad_norm")
+
+
+def cct_grad_scale(grads: TensorList, clip, out: TensorList) -> None:
+    """out = grads * clip[1]; out may be grads itself."""
+    _check(_lib.cct_grad_scale(grads.array, grads.count, _ptr(clip, "clip", (2,)), _same(grads, out, "out"),
+                               _stream()), "cct_grad_scale")
+
+
+def cct_sgd_update(grads: TensorList, clip, weights: TensorList, moments: TensorList, copies, rate, momentum=0.9,
+                   decay=0.0) -> None:
+    """One step of the weights, in place; clip may be None, copies too (else: the weights in other types)."""
+    _check(_lib.cct_sgd_update(grads.array, grads.count, _ptr(clip, "clip", (2,), optional=True),
+                               _same(grads, weights, "weights"), _same(grads, moments, "moments"),
+                               None if copies is None else _same(grads, copies, "copies"), rate, momentum, decay,
+                               _stream()), "cct_sgd_update")

@@ -1,0 +1,86 @@
+// Activations of the feed-forward operators and their derivatives, in fp32.
+#pragma once
+#include "cct_internal.h"
+
+namespace cct {
+namespace {
+
+// 1 / (1 + exp(-z)); both ends are exact (exp overflows to infinity, its reciprocal is 0)
+__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + expf(-z)); }
+
+constexpr float kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
+constexpr float kTanhC = 0.79788456080286536f, kTanhD = 0.044715f;
+
+// act(z) for several values: one uniform branch for all of them
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&z)[N]) {
+  switch (act) {
+    case CCT_ACT_RELU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) z[e] = z[e] < 0.f ? 0.f : z[e];  // NaN stays
+      break;
+    case CCT_ACT_SILU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) z[e] *= logistic(z[e]);
+      break;
+    case CCT_ACT_GELU:  // erfc, not 1 + erf: the left tail keeps its digits
+#pragma unroll
+      for (int e = 0; e < N; ++e) z[e] *= 0.5f * erfcf(-kSqrtHalf * z[e]);
+      break;
+    case CCT_ACT_GELU_TANH:  // (1 + tanh(a)) / 2 is the logistic function of 2 a
+#pragma unroll
+      for (int e = 0; e < N; ++e) z[e] *= logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z[e] * z[e]));
+      break;
+    default: break;
+  }
+}
+
+// act(z) and act'(z)
+template <int N>
+__device__ __forceinline__ void activate_both(int act, const float (&z)[N], float (&a)[N], float (&d)[N]) {
+  switch (act) {
+    case CCT_ACT_RELU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        a[e] = z[e] < 0.f ? 0.f : z[e];
+        d[e] = z[e] > 0.f ? 1.f : 0.f;
+      }
+      break;
+    case CCT_ACT_SILU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float s = logistic(z[e]);
+        a[e] = z[e] * s;
+        d[e] = s * (1.f + z[e] * (1.f - s));
+      }
+      break;
+    case CCT_ACT_GELU:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float phi = 0.5f * erfcf(-kSqrtHalf * z[e]);
+        a[e] = z[e] * phi;
+        d[e] = phi + z[e] * (kInvSqrt2Pi * expf(-0.5f * z[e] * z[e]));
+      }
+      break;
+    case CCT_ACT_GELU_TANH:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float z2 = z[e] * z[e], s = logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z2));
+        const float slope = 2.f * s * (1.f - s);  // 0 where z2 overflows: no infinity times 0
+        a[e] = z[e] * s;
+        d[e] = s + (slope == 0.f ? 0.f : z[e] * slope * (kTanhC * (1.f + 3.f * kTanhD * z2)));
+      }
+      break;
+    default:
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        a[e] = z[e];
+        d[e] = 1.f;
+      }
+  }
+}
+
+inline bool activation_known(int act) { return act >= CCT_ACT_NONE && act <= CCT_ACT_GELU_TANH; }
+
+}  // namespace
+}  // namespace cct

@@ -1,0 +1,57 @@
+// What the translation units of the feed-forward operators share.
+#pragma once
+#include "cct_internal.h"
+#include "number_types.h"
+
+namespace cct {
+
+// One matrix product of a feed-forward operator: sum over segments s and k of A_s(m, k) B_s(n, k), M x N results, and what
+// becomes of them.  An operand's element (row, k) lies at p + row * rs + k * ks elements; one of rs and ks is 1.
+struct FfOperand {
+  const void* p;
+  long long rs, ks;
+};
+enum FfEpilogue {
+  kFfLinear,  // z = sum + bias (kept if z is there), out = act(z) + residual
+  kFfGated    // two products of the same A: g and u (kept if z and z2 are there), out = act(g) * u
+};
+struct FfProduct {
+  int M, N, K;
+  int type;
+  int segments;        // 1 or 2: contractions that are summed; kFfGated: B[0] and B[1] are the two products'
+  FfOperand A[2], B[2];
+  int epilogue, activation;
+  const void* bias;
+  const void* residual;
+  long long ldr;
+  void* out;
+  long long ldo;
+  void *z, *z2;
+  long long ldz, ldz2;
+};
+int launch_ff_product(const FfProduct& p, hipStream_t st);
+
+// dz = dy * act'(z) into rows of ld values (a multiple of 8; zeros behind the N values of a row), and the column sums of the
+// unrounded dz; any of the two may be missing.  z NULL: dz = dy.  `part`: ff_sum_rows(M) * N floats.
+struct FfDz {
+  int M, N, type, activation;
+  const void *dy, *z;
+  long long lddy, ldz;
+  void* dz;
+  long long ld;
+  void* dbias;
+  float* part;
+};
+int ff_sum_rows(int M);
+int launch_ff_dz(const FfDz& p, hipStream_t st);
+// dg = dh * u * act'(g), du = dh * act(g), both with rows of ld values as dz above.
+struct FfGatedDz {
+  int M, F, type, activation;
+  const void *dh, *g, *u;
+  long long lddh, ldg, ldu;
+  void *dg, *du;
+  long long ld;
+};
+int launch_ff_gated_dz(const FfGatedDz& p, hipStream_t st);
+
+}  // namespace cct

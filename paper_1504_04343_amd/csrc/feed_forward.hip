@@ -1,0 +1,253 @@
+// The feed-forward operators' entry points (cct_linear_*, cct_gated_*): checks of arguments, workspace layouts, and which
+// kernels a call runs.
+#include <algorithm>
+
+#include "activation.h"
+#include "feed_forward.h"
+
+namespace cct {
+namespace {
+
+long long up(long long v, long long to) { return (v + to - 1) / to * to; }
+
+// Parts of a workspace, one behind the other.
+struct Layout {
+  long long total = 0;
+  long long take(long long bytes) {
+    const long long at = total;
+    total += up(bytes, 256);
+    return at;
+  }
+};
+
+struct Matrix {
+  const void* p;
+  long long ld;
+};
+// A tensor of rows x cols of a type: there, aligned to a value, rows that do not overlap.
+bool matrix_ok(const Matrix& m, long long rows, long long cols, int type) {
+  if (!m.p || ((uintptr_t)m.p & (type_bytes(type) - 1)) || m.ld < 0) return false;
+  return rows <= 1 || m.ld >= cols;
+}
+bool vector_ok(const void* p, int type) { return !((uintptr_t)p & (type_bytes(type) - 1)); }
+
+// Sizes up to which no product of two of them, a stride and a value's bytes passes 63 bits, and a launch's workgroups 31.
+int dims_ok(int32_t M, int32_t N, int32_t K, int32_t type, int32_t activation) {
+  if (M < 0 || N < 1 || K < 1 || !type_known(type) || !activation_known(activation)) return CCT_EINVAL;
+  const long long tiles = up(M, 64) / 64 * (up(N, 64) / 64), back = up(std::max(N, K), 64) / 64 * (up(std::max(M, N), 64) / 64);
+  return tiles < 0x7fffffffLL && back < 0x7fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
+}
+int workspace_ok(const void* workspace, size_t have, long long need) {
+  if (!workspace || ((uintptr_t)workspace & 255)) return CCT_EINVAL;
+  return have >= (size_t)need ? CCT_OK : CCT_EWORKSPACE;
+}
+
+struct LinearBackward {
+  long long dz, part, ld, total;
+};
+LinearBackward linear_backward_layout(const cct_linear_desc_t& d) {
+  Layout l;
+  LinearBackward b;
+  b.ld = up(d.N, 8);
+  b.dz = l.take((long long)d.M * b.ld * type_bytes(d.type));
+  b.part = l.take((long long)ff_sum_rows(d.M) * d.N * 4);
+  b.total = std::max(l.total, 256LL);
+  return b;
+}
+struct GatedBackward {
+  long long dg, du, ld, total;
+};
+GatedBackward gated_backward_layout(const cct_gated_desc_t& d) {
+  Layout l;
+  GatedBackward b;
+  b.ld = up(d.F, 8);
+  b.dg = l.take((long long)d.M * b.ld * type_bytes(d.type));
+  b.du = l.take((long long)d.M * b.ld * type_bytes(d.type));
+  b.total = std::max(l.total, 256LL);
+  return b;
+}
+
+FfOperand rows_of(const void* p, long long ld) { return {p, ld, 1}; }
+FfOperand columns_of(const void* p, long long ld) { return {p, 1, ld}; }
+
+// out (rows x cols) = sum over segments of A_s B_s^T, rounded, nothing else
+FfProduct plain_product(int type, int rows, int cols, int k, void* out, long long ldo) {
+  FfProduct p = {};
+  p.M = rows;
+  p.N = cols;
+  p.K = k;
+  p.type = type;
+  p.segments = 1;
+  p.epilogue = kFfLinear;
+  p.activation = CCT_ACT_NONE;
+  p.out = out;
+  p.ldo = ldo;
+  return p;
+}
+
+}  // namespace
+}  // namespace cct
+
+using namespace cct;
+
+extern "C" {
+
+int cct_linear_workspace_bytes(const cct_linear_desc_t* desc, int32_t backward, size_t* bytes) {
+  if (!desc || !bytes) return CCT_EINVAL;
+  const cct_linear_desc_t& d = *desc;
+  const int rc = dims_ok(d.M, d.N, d.K, d.type, d.activation);
+  if (rc != CCT_OK) return rc;
+  *bytes = backward ? (size_t)linear_backward_layout(d).total : 256;
+  return CCT_OK;
+}
+
+int cct_gated_workspace_bytes(const cct_gated_desc_t* desc, int32_t backward, size_t* bytes) {
+  if (!desc || !bytes) return CCT_EINVAL;
+  const cct_gated_desc_t& d = *desc;
+  const int rc = dims_ok(d.M, d.F, d.K, d.type, d.activation);
+  if (rc != CCT_OK) return rc;
+  *bytes = backward ? (size_t)gated_backward_layout(d).total : 256;
+  return CCT_OK;
+}
+
+int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                       const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz,
+                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!desc) return CCT_EINVAL;
+  const cct_linear_desc_t& d = *desc;
+  int rc = dims_ok(d.M, d.N, d.K, d.type, d.activation);
+  if (rc != CCT_OK) return rc;
+  if (d.M == 0) return CCT_OK;
+  if (!matrix_ok({x, ldx}, d.M, d.K, d.type) || !matrix_ok({w, ldw}, d.N, d.K, d.type) ||
+      !matrix_ok({y, ldy}, d.M, d.N, d.type) || !vector_ok(bias, d.type) ||
+      (residual && !matrix_ok({residual, ldr}, d.M, d.N, d.type)) || (z && !matrix_ok({z, ldz}, d.M, d.N, d.type)))
+    return CCT_EINVAL;
+  rc = workspace_ok(workspace, workspace_bytes, 256);
+  if (rc != CCT_OK) return rc;
+  FfProduct p = plain_product(d.type, d.M, d.N, d.K, y, ldy);
+  p.A[0] = rows_of(x, ldx);
+  p.B[0] = rows_of(w, ldw);
+  p.activation = d.activation;
+  p.bias = bias;
+  p.residual = residual;
+  p.ldr = ldr;
+  p.z = z;
+  p.ldz = ldz;
+  return launch_ff_product(p, (hipStream_t)hip_stream);
+}
+
+int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                        const void* z, int64_t ldz, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dw,
+                        int64_t lddw, void* dbias, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!desc) return CCT_EINVAL;
+  const cct_linear_desc_t& d = *desc;
+  int rc = dims_ok(d.M, d.N, d.K, d.type, d.activation);
+  if (rc != CCT_OK) return rc;
+  const bool act = d.activation != CCT_ACT_NONE;
+  // an empty batch's tensors have no address; gradients of weights are written all the same
+  if (d.M > 0 && ((dw && !matrix_ok({x, ldx}, d.M, d.K, d.type)) || (act && !matrix_ok({z, ldz}, d.M, d.N, d.type)) ||
+                  !matrix_ok({dy, lddy}, d.M, d.N, d.type) || (dx && !matrix_ok({w, ldw}, d.N, d.K, d.type)) ||
+                  (dx && !matrix_ok({dx, lddx}, d.M, d.K, d.type))))
+    return CCT_EINVAL;
+  if ((dw && !matrix_ok({dw, lddw}, d.N, d.K, d.type)) || !vector_ok(dbias, d.type)) return CCT_EINVAL;
+  const LinearBackward b = linear_backward_layout(d);
+  rc = workspace_ok(workspace, workspace_bytes, b.total);
+  if (rc != CCT_OK) return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  char* ws = (char*)workspace;
+  const bool copy = act && (dx || dw);
+  if (copy || dbias) {
+    FfDz q = {d.M, d.N, d.type, d.activation, dy, act ? z : nullptr, lddy, ldz, copy ? ws + b.dz : nullptr, b.ld, dbias,
+              (float*)(ws + b.part)};
+    rc = launch_ff_dz(q, st);
+    if (rc != CCT_OK) return rc;
+  }
+  const void* dz = copy ? ws + b.dz : dy;
+  const long long ld = copy ? b.ld : lddy;
+  if (dx && d.M > 0) {
+    FfProduct p = plain_product(d.type, d.M, d.K, d.N, dx, lddx);
+    p.A[0] = rows_of(dz, ld);
+    p.B[0] = columns_of(w, ldw);
+    rc = launch_ff_product(p, st);
+    if (rc != CCT_OK) return rc;
+  }
+  if (dw) {
+    FfProduct p = plain_product(d.type, d.N, d.K, d.M, dw, lddw);
+    p.A[0] = columns_of(dz, ld);
+    p.B[0] = columns_of(x, ldx);
+    rc = launch_ff_product(p, st);
+  }
+  return rc;
+}
+
+int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
+                      const void* wu, int64_t ldwu, void* h, int64_t ldh, void* g, int64_t ldg, void* u, int64_t ldu,
+                      void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!desc) return CCT_EINVAL;
+  const cct_gated_desc_t& d = *desc;
+  int rc = dims_ok(d.M, d.F, d.K, d.type, d.activation);
+  if (rc != CCT_OK) return rc;
+  if (d.M == 0) return CCT_OK;
+  if (!matrix_ok({x, ldx}, d.M, d.K, d.type) || !matrix_ok({wg, ldwg}, d.F, d.K, d.type) ||
+      !matrix_ok({wu, ldwu}, d.F, d.K, d.type) || !matrix_ok({h, ldh}, d.M, d.F, d.type) || (!g != !u) ||
+      (g && (!matrix_ok({g, ldg}, d.M, d.F, d.type) || !matrix_ok({u, ldu}, d.M, d.F, d.type))))
+    return CCT_EINVAL;
+  rc = workspace_ok(workspace, workspace_bytes, 256);
+  if (rc != CCT_OK) return rc;
+  FfProduct p = plain_product(d.type, d.M, d.F, d.K, h, ldh);
+  p.epilogue = kFfGated;
+  p.activation = d.activation;
+  p.A[0] = rows_of(x, ldx);
+  p.B[0] = rows_of(wg, ldwg);
+  p.B[1] = rows_of(wu, ldwu);
+  p.z = g;
+  p.ldz = ldg;
+  p.z2 = u;
+  p.ldz2 = ldu;
+  return launch_ff_product(p, (hipStream_t)hip_stream);
+}
+
+int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
+                       const void* wu, int64_t ldwu, const void* g, int64_t ldg, const void* u, int64_t ldu,
+                       const void* dh, int64_t lddh, void* dx, int64_t lddx, void* dwg, int64_t lddwg, void* dwu,
+                       int64_t lddwu, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!desc) return CCT_EINVAL;
+  const cct_gated_desc_t& d = *desc;
+  int rc = dims_ok(d.M, d.F, d.K, d.type, d.activation);
+  if (rc != CCT_OK) return rc;
+  if (!dwg != !dwu) return CCT_EINVAL;
+  if (d.M > 0 && ((dwg && !matrix_ok({x, ldx}, d.M, d.K, d.type)) || !matrix_ok({g, ldg}, d.M, d.F, d.type) ||
+                  !matrix_ok({u, ldu}, d.M, d.F, d.type) || !matrix_ok({dh, lddh}, d.M, d.F, d.type) ||
+                  (dx && (!matrix_ok({wg, ldwg}, d.F, d.K, d.type) || !matrix_ok({wu, ldwu}, d.F, d.K, d.type) ||
+                          !matrix_ok({dx, lddx}, d.M, d.K, d.type)))))
+    return CCT_EINVAL;
+  if (dwg && (!matrix_ok({dwg, lddwg}, d.F, d.K, d.type) || !matrix_ok({dwu, lddwu}, d.F, d.K, d.type))) return CCT_EINVAL;
+  const GatedBackward b = gated_backward_layout(d);
+  rc = workspace_ok(workspace, workspace_bytes, b.total);
+  if (rc != CCT_OK) return rc;
+  if (!dx && !dwg) return CCT_OK;
+  hipStream_t st = (hipStream_t)hip_stream;
+  void *dg = (char*)workspace + b.dg, *du = (char*)workspace + b.du;
+  rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, dg, du, b.ld}, st);
+  if (rc != CCT_OK) return rc;
+  if (dx && d.M > 0) {
+    FfProduct p = plain_product(d.type, d.M, d.K, d.F, dx, lddx);
+    p.segments = 2;
+    p.A[0] = rows_of(dg, b.ld);
+    p.A[1] = rows_of(du, b.ld);
+    p.B[0] = columns_of(wg, ldwg);
+    p.B[1] = columns_of(wu, ldwu);
+    rc = launch_ff_product(p, st);
+    if (rc != CCT_OK) return rc;
+  }
+  for (int i = 0; i < 2 && dwg; ++i) {
+    FfProduct p = plain_product(d.type, d.F, d.K, d.M, i ? dwu : dwg, i ? lddwu : lddwg);
+    p.A[0] = columns_of(i ? du : dg, b.ld);
+    p.B[0] = columns_of(x, ldx);
+    rc = launch_ff_product(p, st);
+    if (rc != CCT_OK) return rc;
+  }
+  return CCT_OK;
+}
+
+}  // extern "C"

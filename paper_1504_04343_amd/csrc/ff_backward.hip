@@ -1,0 +1,164 @@
+// The elementwise half of the feed-forward operators' backward passes:
+//   linear  dz = dy act'(z), and dbias = column sums of dz;
+//   gated   dg = dh u act'(g), du = dh act(g).
+// Each input is read once and each output written once; the rounding of dz, dg and du to 16 bits is the matrix cores', which
+// take no more of an operand (2^-9 of a value at most for bf16, the same as the operands themselves were rounded by).
+//
+// A workgroup takes 256 columns x kRows rows, a thread 8 neighbouring columns of every eighth row: its column sums stay in
+// registers, meet in LDS in a fixed order and leave as one row of partial sums per workgroup, which a second kernel adds in
+// order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
+#include <algorithm>
+
+#include "activation.h"
+#include "feed_forward.h"
+
+namespace cct {
+namespace {
+
+constexpr int NT = 256, kCols = 256, kRows = 64;
+
+template <class F>
+void with_type(int type, F f) {
+  if (type == CCT_TYPE_F32)
+    f(std::integral_constant<int, CCT_TYPE_F32>());
+  else if (type == CCT_TYPE_BF16)
+    f(std::integral_constant<int, CCT_TYPE_BF16>());
+  else
+    f(std::integral_constant<int, CCT_TYPE_F16>());
+}
+
+// 8 values from column c on of a row of n, those past its end zero
+template <int TYPE>
+__device__ __forceinline__ void load_columns(float (&v)[8], const void* p, long long row, int c, int n) {
+  if (c + 8 <= n) {
+    const f32x8 all = load8<TYPE>(p, row + c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = all[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < n ? load1<TYPE>(p, row + c + e) : 0.f;
+  }
+}
+// into a row that has room for whole eights
+template <int TYPE>
+__device__ __forceinline__ void store_columns(void* p, long long at, const float (&v)[8]) {
+  f32x8 all;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) all[e] = v[e];
+  store8<TYPE>(p, at, all);
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(NT) void ff_dz_kernel(FfDz p) {
+  const int wide = (p.N + kCols - 1) / kCols, down = blockIdx.x / wide, c0 = (blockIdx.x - down * wide) * kCols;
+  const int c = c0 + (threadIdx.x & 31) * 8, lane_row = threadIdx.x >> 5;
+  const int r0 = down * kRows, r1 = min(r0 + kRows, p.M);
+  float sum[8] = {};
+  if (c < p.N)
+    for (int r = r0 + lane_row; r < r1; r += NT / 32) {
+      float v[8];
+      load_columns<TYPE>(v, p.dy, r * p.lddy, c, p.N);
+      if (p.z) {
+        float z[8], a[8], d[8];
+        load_columns<TYPE>(z, p.z, r * p.ldz, c, p.N);
+        activate_both(p.activation, z, a, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= d[e];
+      }
+      if (p.dz) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e >= p.N) v[e] = 0.f;
+        store_columns<TYPE>(p.dz, r * p.ld + c, v);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+    }
+  if (!p.dbias) return;
+  __shared__ float sums[NT / 32][kCols];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[lane_row][(threadIdx.x & 31) * 8 + e] = sum[e];
+  __syncthreads();
+  const int col = c0 + threadIdx.x;
+  if (col >= p.N) return;
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < NT / 32; ++k) s += sums[k][threadIdx.x];
+  p.part[(long long)down * p.N + col] = s;
+}
+
+// dbias from the rows of partial sums: 64 columns per workgroup, four runs of rows that meet in LDS
+template <int TYPE>
+__global__ __launch_bounds__(NT) void ff_bias_sum_kernel(const float* __restrict__ part, int rows, int N, void* dbias) {
+  const int col = blockIdx.x * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
+  const int per = (rows + 3) / 4, end = min(rows, (q + 1) * per);
+  float s = 0.f;
+  if (col < N)
+    for (int r = q * per; r < end; ++r) s += part[(long long)r * N + col];
+  __shared__ float sums[4][64];
+  sums[q][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (q == 0 && col < N)
+    store1<TYPE>(dbias, col, (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]));
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p) {
+  const int wide = (p.F + kCols - 1) / kCols, down = blockIdx.x / wide;
+  const int c = (blockIdx.x - down * wide) * kCols + (threadIdx.x & 31) * 8;
+  const int r0 = down * kRows, r1 = min(r0 + kRows, p.M);
+  if (c >= p.F) return;
+  for (int r = r0 + (threadIdx.x >> 5); r < r1; r += NT / 32) {
+    float dh[8], g[8], u[8], a[8], d[8];
+    load_columns<TYPE>(dh, p.dh, r * p.lddh, c, p.F);
+    load_columns<TYPE>(g, p.g, r * p.ldg, c, p.F);
+    load_columns<TYPE>(u, p.u, r * p.ldu, c, p.F);
+    activate_both(p.activation, g, a, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      d[e] = c + e < p.F ? dh[e] * u[e] * d[e] : 0.f;
+      a[e] = c + e < p.F ? dh[e] * a[e] : 0.f;
+    }
+    store_columns<TYPE>(p.dg, r * p.ld + c, d);
+    store_columns<TYPE>(p.du, r * p.ld + c, a);
+  }
+}
+
+}  // namespace
+
+int ff_sum_rows(int M) { return (M + kRows - 1) / kRows; }
+
+int launch_ff_dz(const FfDz& p, hipStream_t st) {
+  const int rows = ff_sum_rows(p.M);
+  const double n = (double)p.M * p.N, e = type_bytes(p.type);
+  const char* const names[] = {"ff_dz_kernel<f32>", "ff_dz_kernel<bf16>", "ff_dz_kernel<f16>"};
+  with_type(p.type, [&](auto type) {
+    ProfScope ps(names[p.type], 2.0 * n, e * n * (1 + (p.z != nullptr) + (p.dz != nullptr)), st);
+    if (p.M > 0)
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_dz_kernel<decltype(type)::value>), dim3((p.N + kCols - 1) / kCols * rows), dim3(NT), 0, st,
+                         p);
+  });
+  CCT_CHECK_LAUNCH();
+  if (!p.dbias) return CCT_OK;
+  with_type(p.type, [&](auto type) {
+    ProfScope ps("ff_bias_sum_kernel", (double)rows * p.N, 4.0 * rows * p.N, st);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((p.N + 63) / 64), dim3(NT), 0, st,
+                       p.part, rows, p.N, p.dbias);
+  });
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+int launch_ff_gated_dz(const FfGatedDz& p, hipStream_t st) {
+  if (p.M == 0) return CCT_OK;
+  const double n = (double)p.M * p.F, e = type_bytes(p.type);
+  with_type(p.type, [&](auto type) {
+    ProfScope ps("ff_gated_dz_kernel", 6.0 * n, 5.0 * e * n, st);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_gated_dz_kernel<decltype(type)::value>),
+                       dim3((p.F + kCols - 1) / kCols * ff_sum_rows(p.M)), dim3(NT), 0, st, p);
+  });
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+}  // namespace cct

@@ -1,0 +1,363 @@
+// From gradients to new weights over lists of tensors: the 2-norm of all gradients, the gradients scaled down to a largest
+// norm, and the step with momentum and weight decay (Caffe's rules, as the other layers').
+//
+//   norm    n = sqrt(sum g^2), s = max_norm / n where n > max_norm, else 1
+//   scale   out = s g
+//   update  v = momentum v + rate (s g + decay w),  w = w - v,  copy = w rounded
+//
+// All of it is memory: the norm reads every gradient once, scaling reads and writes each, the update reads gradient, weight
+// and moment and writes the latter two.  A model's list holds hundreds of tensors, most of them small, so that a launch
+// takes as many as its arguments hold (4 KiB; nothing is uploaded or kept); a workgroup takes up to kRun values of one of
+// them.  Scaling and updating walk the lists from the end: what the norm read last is what the 256 MiB cache behind the
+// eight L2s still holds.
+//
+// The squares are summed in 64 bits: with 2^-53 per addition no order matters to the fp32 result, 3e38 squared does not
+// overflow, and the kernel waits for memory all the same (4 conversions and fused multiply-adds per 16 bytes).  Every
+// workgroup leaves one sum; one workgroup adds them in a fixed order, so that the norm is bit-reproducible.
+#include <algorithm>
+#include <cmath>
+
+#include "cct_internal.h"
+#include "number_types.h"
+
+namespace cct {
+namespace {
+
+constexpr int NT = 256;
+constexpr int kRun = 8192;  // values per workgroup: 4 of its 8-value steps per thread
+
+// What a launch is told: tensors with P pointers each, and at which workgroup each begins.
+template <int P, int COUNT>
+struct ListArgs {
+  static constexpr int kCount = COUNT;
+  void* p[P][COUNT];
+  long long n[COUNT];
+  int first[COUNT + 1];
+  unsigned char type[COUNT], other[COUNT];  // of p[0] and of the last pointer
+  int count;
+};
+typedef ListArgs<1, 160> NormArgs;
+typedef ListArgs<2, 120> ScaleArgs;
+typedef ListArgs<4, 72> UpdateArgs;
+static_assert(sizeof(NormArgs) < 3900 && sizeof(ScaleArgs) < 3900 && sizeof(UpdateArgs) < 3900, "a launch's arguments");
+
+// which tensor workgroup b of the launch belongs to
+template <class Args>
+__device__ __forceinline__ int tensor_of(const Args& a, int b) {
+  int lo = 0, hi = a.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.first[mid] <= b)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+template <class F>
+__device__ __forceinline__ void with_type(int type, F f) {
+  if (type == CCT_TYPE_F32)
+    f(std::integral_constant<int, CCT_TYPE_F32>());
+  else if (type == CCT_TYPE_BF16)
+    f(std::integral_constant<int, CCT_TYPE_BF16>());
+  else
+    f(std::integral_constant<int, CCT_TYPE_F16>());
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+__global__ __launch_bounds__(NT) void grad_norm_kernel(NormArgs a, double* __restrict__ part) {
+  const int i = tensor_of(a, blockIdx.x);
+  const long long at = (long long)((int)blockIdx.x - a.first[i]) * kRun;
+  const int n = (int)min((long long)kRun, a.n[i] - at);
+  double sum = 0.0;
+  with_type(a.type[i], [&](auto type) {
+    constexpr int TYPE = decltype(type)::value;
+    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
+    auto add = [&](float v) { sum = fma((double)v, (double)v, sum); };
+    if (n == kRun) {
+      f32x8 v[kRun / NT / 8];
+#pragma unroll
+      for (int u = 0; u < kRun / NT / 8; ++u) v[u] = load8<TYPE>(g, (u * NT + threadIdx.x) * 8);
+#pragma unroll
+      for (int u = 0; u < kRun / NT / 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) add(v[u][e]);
+    } else {
+      for (int k = threadIdx.x * 8; k < n; k += NT * 8)
+        if (k + 8 <= n) {
+          const f32x8 v = load8<TYPE>(g, k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) add(v[e]);
+        } else {
+          for (int e = k; e < n; ++e) add(load1<TYPE>(g, e));
+        }
+    }
+  });
+  __shared__ double sums[NT / 64];
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+constexpr int kFinalThreads = 1024;
+__global__ __launch_bounds__(kFinalThreads) void grad_norm_final_kernel(const double* __restrict__ part, int n,
+                                                                        float max_norm, float* __restrict__ clip) {
+  double sum = 0.0;
+  for (int k = threadIdx.x; k < n; k += kFinalThreads) sum += part[k];
+  __shared__ double sums[kFinalThreads / 64];
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < kFinalThreads / 64; ++w) sum += sums[w];
+  const double norm = sqrt(sum);
+  clip[0] = (float)norm;
+  clip[1] = norm != norm ? (float)norm : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+}
+
+__global__ __launch_bounds__(NT) void grad_scale_kernel(ScaleArgs a, const float* __restrict__ clip) {
+  const int b = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(a, b);
+  const float s = clip[1];
+  if (a.p[0][i] == a.p[1][i] && s == 1.f) return;
+  const long long at = (long long)(b - a.first[i]) * kRun;
+  const int n = (int)min((long long)kRun, a.n[i] - at);
+  with_type(a.type[i], [&](auto type) {
+    constexpr int TYPE = decltype(type)::value;
+    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
+    void* out = (typename Number<TYPE>::T*)a.p[1][i] + at;
+    if (n == kRun) {
+      f32x8 v[kRun / NT / 8];
+#pragma unroll
+      for (int u = 0; u < kRun / NT / 8; ++u) v[u] = load8<TYPE>(g, (u * NT + threadIdx.x) * 8);
+#pragma unroll
+      for (int u = 0; u < kRun / NT / 8; ++u) store8<TYPE>(out, (u * NT + threadIdx.x) * 8, v[u] * s);
+    } else {
+      for (int k = threadIdx.x * 8; k < n; k += NT * 8)
+        if (k + 8 <= n)
+          store8<TYPE>(out, k, load8<TYPE>(g, k) * s);
+        else
+          for (int e = k; e < n; ++e) store1<TYPE>(out, e, load1<TYPE>(g, e) * s);
+    }
+  });
+}
+
+struct StepRule {
+  float rate, momentum, decay;
+};
+
+template <int TYPE, int COPY>  // COPY: the copy's type, -1 for none
+__device__ __forceinline__ void update_run(const void* g, float* w, float* v, void* copy, int n, float s, StepRule r) {
+  auto step = [&](float gr, float& wt, float& mo) {
+    mo = r.momentum * mo + r.rate * (s * gr + r.decay * wt);
+    wt -= mo;
+  };
+  for (int k = threadIdx.x * 8; k < n; k += NT * 8)
+    if (k + 8 <= n) {
+      const f32x8 gr = load8<TYPE>(g, k);
+      f32x8 wt = load8<CCT_TYPE_F32>(w, k), mo = load8<CCT_TYPE_F32>(v, k);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float a = wt[e], b = mo[e];
+        step(gr[e], a, b);
+        wt[e] = a;
+        mo[e] = b;
+      }
+      store8<CCT_TYPE_F32>(v, k, mo);
+      store8<CCT_TYPE_F32>(w, k, wt);
+      if constexpr (COPY >= 0) store8<COPY>(copy, k, wt);
+    } else {
+      for (int e = k; e < n; ++e) {
+        float wt = w[e], mo = v[e];
+        step(load1<TYPE>(g, e), wt, mo);
+        v[e] = mo;
+        w[e] = wt;
+        if constexpr (COPY >= 0) store1<COPY>(copy, e, wt);
+      }
+    }
+}
+
+__global__ __launch_bounds__(NT) void sgd_update_kernel(UpdateArgs a, const float* __restrict__ clip, StepRule r) {
+  const int b = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(a, b);
+  const float s = clip ? clip[1] : 1.f;
+  const long long at = (long long)(b - a.first[i]) * kRun;
+  const int n = (int)min((long long)kRun, a.n[i] - at);
+  with_type(a.type[i], [&](auto type) {
+    constexpr int TYPE = decltype(type)::value;
+    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
+    float *w = (float*)a.p[1][i] + at, *v = (float*)a.p[2][i] + at;
+    if (!a.p[3][i])
+      update_run<TYPE, -1>(g, w, v, nullptr, n, s, r);
+    else
+      with_type(a.other[i], [&](auto other) {
+        constexpr int COPY = decltype(other)::value;
+        update_run<TYPE, COPY>(g, w, v, (typename Number<COPY>::T*)a.p[3][i] + at, n, s, r);
+      });
+  });
+}
+
+long long runs(long long n) { return (n + kRun - 1) / kRun; }
+
+// CCT_OK, and how many workgroups the list takes.  Every pointer of a tensor with values must be there and aligned to one.
+int check_list(const cct_tensor_t* list, int count, long long* blocks) {
+  if (count < 0 || (count > 0 && !list)) return CCT_EINVAL;
+  *blocks = 0;
+  for (int i = 0; i < count; ++i) {
+    const cct_tensor_t& t = list[i];
+    if (t.n < 0 || !type_known(t.type) || (t.n > 0 && !t.data) || ((uintptr_t)t.data & (type_bytes(t.type) - 1)))
+      return CCT_EINVAL;
+    if (t.n > (1LL << 44)) return CCT_EUNSUPPORTED;
+    *blocks += runs(t.n);
+  }
+  return *blocks < 0x7fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
+}
+int check_same(const cct_tensor_t* a, const cct_tensor_t* b, int count) {
+  long long blocks;
+  const int rc = check_list(b, count, &blocks);
+  if (rc != CCT_OK) return rc;
+  for (int i = 0; i < count; ++i)
+    if (a[i].n != b[i].n) return CCT_EINVAL;
+  return CCT_OK;
+}
+
+// Tensors [from, to) of the lists as one launch's arguments; returns the first tensor left out.  `forward`: from `from` up,
+// else from `to` down.
+template <class Args, int P>
+int fill(Args* a, const cct_tensor_t* const (&lists)[P], int from, int to, bool forward) {
+  int lo = forward ? from : to, hi = lo, held = 0;
+  auto take = [&](int i) { return lists[0][i].n == 0 || ++held <= Args::kCount; };
+  if (forward)
+    while (hi < to && take(hi)) ++hi;
+  else
+    while (lo > from && take(lo - 1)) --lo;
+  a->count = 0;
+  a->first[0] = 0;
+  for (int i = lo; i < hi; ++i) {
+    if (lists[0][i].n == 0) continue;
+    const int c = a->count++;
+    for (int q = 0; q < P; ++q) a->p[q][c] = lists[q] ? lists[q][i].data : nullptr;
+    a->n[c] = lists[0][i].n;
+    a->type[c] = (unsigned char)lists[0][i].type;
+    a->other[c] = (unsigned char)(lists[P - 1] ? lists[P - 1][i].type : 0);
+    a->first[c + 1] = a->first[c] + (int)runs(a->n[c]);
+  }
+  return forward ? hi : lo;
+}
+template <class Args>
+double list_values(const Args& a, double* g_bytes) {
+  double n = 0.0, by = 0.0;
+  for (int c = 0; c < a.count; ++c) {
+    n += (double)a.n[c];
+    by += (double)a.n[c] * type_bytes(a.type[c]);
+  }
+  *g_bytes = by;
+  return n;
+}
+
+}  // namespace
+}  // namespace cct
+
+using namespace cct;
+
+extern "C" {
+
+int cct_grad_norm_workspace_bytes(const cct_tensor_t* grads, int32_t count, size_t* bytes) {
+  long long blocks;
+  if (!bytes) return CCT_EINVAL;
+  const int rc = check_list(grads, count, &blocks);
+  if (rc != CCT_OK) return rc;
+  *bytes = (size_t)std::max(1LL, blocks) * sizeof(double);
+  return CCT_OK;
+}
+
+int cct_grad_norm(const cct_tensor_t* grads, int32_t count, float max_norm, float* clip, void* workspace,
+                  size_t workspace_bytes, void* hip_stream) {
+  long long blocks;
+  const int rc = check_list(grads, count, &blocks);
+  if (rc != CCT_OK) return rc;
+  if (!clip || ((uintptr_t)clip & 3) || !(max_norm > 0.f)) return CCT_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 255)) return CCT_EINVAL;
+  if (workspace_bytes < (size_t)std::max(1LL, blocks) * sizeof(double)) return CCT_EWORKSPACE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  double* part = (double*)workspace;
+  const cct_tensor_t* const lists[1] = {grads};
+  for (int at = 0; at < count;) {
+    NormArgs a;
+    at = fill(&a, lists, at, count, true);
+    if (a.count == 0) continue;
+    double by;
+    const double n = list_values(a, &by);
+    ProfScope ps("grad_norm_kernel", 2.0 * n, by, st);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(a.first[a.count]), dim3(NT), 0, st, a, part);
+    CCT_CHECK_LAUNCH();
+    part += a.first[a.count];
+  }
+  ProfScope ps("grad_norm_final_kernel", (double)blocks, 8.0 * (double)blocks, st);
+  hipLaunchKernelGGL(grad_norm_final_kernel, dim3(1), dim3(kFinalThreads), 0, st, (const double*)workspace, (int)blocks,
+                     max_norm, clip);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+int cct_grad_scale(const cct_tensor_t* grads, int32_t count, const float* clip, const cct_tensor_t* out,
+                   void* hip_stream) {
+  long long blocks;
+  int rc = check_list(grads, count, &blocks);
+  if (rc == CCT_OK) rc = check_same(grads, out, count);
+  if (rc != CCT_OK) return rc;
+  if (!clip || ((uintptr_t)clip & 3)) return CCT_EINVAL;
+  for (int i = 0; i < count; ++i)
+    if (grads[i].type != out[i].type) return CCT_EINVAL;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const cct_tensor_t* const lists[2] = {grads, out};
+  for (int to = count; to > 0;) {
+    ScaleArgs a;
+    to = fill(&a, lists, 0, to, false);
+    if (a.count == 0) continue;
+    double by;
+    const double n = list_values(a, &by);
+    ProfScope ps("grad_scale_kernel", n, 2.0 * by, st);
+    hipLaunchKernelGGL(grad_scale_kernel, dim3(a.first[a.count]), dim3(NT), 0, st, a, clip);
+    CCT_CHECK_LAUNCH();
+  }
+  return CCT_OK;
+}
+
+int cct_sgd_update(const cct_tensor_t* grads, int32_t count, const float* clip, const cct_tensor_t* weights,
+                   const cct_tensor_t* moments, const cct_tensor_t* copies, float rate, float momentum, float decay,
+                   void* hip_stream) {
+  long long blocks;
+  int rc = check_list(grads, count, &blocks);
+  if (rc == CCT_OK) rc = check_same(grads, weights, count);
+  if (rc == CCT_OK) rc = check_same(grads, moments, count);
+  if (rc == CCT_OK && copies) rc = check_same(grads, copies, count);
+  if (rc != CCT_OK) return rc;
+  if ((uintptr_t)clip & 3) return CCT_EINVAL;
+  if (!std::isfinite(rate) || !std::isfinite(momentum) || !std::isfinite(decay)) return CCT_EINVAL;
+  for (int i = 0; i < count; ++i)
+    if (weights[i].type != CCT_TYPE_F32 || moments[i].type != CCT_TYPE_F32) return CCT_EINVAL;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const cct_tensor_t* const lists[4] = {grads, weights, moments, copies};
+  const StepRule r = {rate, momentum, decay};
+  for (int to = count; to > 0;) {
+    UpdateArgs a;
+    to = fill(&a, lists, 0, to, false);
+    if (a.count == 0) continue;
+    double by;
+    const double n = list_values(a, &by);
+    if (copies)
+      for (int c = 0; c < a.count; ++c) by += (double)a.n[c] * type_bytes(a.other[c]);
+    ProfScope ps("sgd_update_kernel", 7.0 * n, by + 16.0 * n, st);
+    hipLaunchKernelGGL(sgd_update_kernel, dim3(a.first[a.count]), dim3(NT), 0, st, a, clip, r);
+    CCT_CHECK_LAUNCH();
+  }
+  return CCT_OK;
+}
+
+}  // extern "C"
