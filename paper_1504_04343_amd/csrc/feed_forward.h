@@ -6,10 +6,12 @@
 namespace cct {
 
 // One matrix product of a feed-forward operator: sum over segments s and k of A_s(m, k) B_s(n, k), M x N results, and what
-// becomes of them.  An operand's element (row, k) lies at p + row * rs + k * ks elements; one of rs and ks is 1.
+// becomes of them.  An operand's element (row, k) lies at p + row * rs + k * ks elements: one of rs and ks is 1 (`across`: rs),
+// the other one the same in both segments.
 struct FfOperand {
   const void* p;
   long long rs, ks;
+  int across;
 };
 enum FfEpilogue {
   kFfLinear,  // z = sum + bias (kept if z is there), out = act(z) + residual
@@ -30,6 +32,11 @@ struct FfProduct {
   long long ldz, ldz2;
 };
 int launch_ff_product(const FfProduct& p, hipStream_t st);
+// Whether the 16-bit product takes a matrix of `cols` consecutive values and rows `ld` apart in place: 16-byte loads, 256 rows
+// within 32-bit offsets.  Rows that are no multiple of 8 values must be followed by zeros up to one, as copies are.
+inline bool ff_in_place(const void* p, long long ld, long long cols) {
+  return !((uintptr_t)p & 15) && ld % 8 == 0 && cols % 8 == 0 && ld < (1LL << 21);
+}
 
 // dz = dy * act'(z) into rows of ld values (a multiple of 8; zeros behind the N values of a row), and the column sums of the
 // unrounded dz; any of the two may be missing.  z NULL: dz = dy.  `part`: ff_sum_rows(M) * N floats.

@@ -42,33 +42,65 @@ int workspace_ok(const void* workspace, size_t have, long long need) {
   return have >= (size_t)need ? CCT_OK : CCT_EWORKSPACE;
 }
 
-struct LinearBackward {
-  long long dz, part, ld, total;
+// Room for a copy of a matrix whose rows begin at multiples of 16 bytes (16-bit types only: see ff_in_place).
+long long copy_bytes(long long rows, long long cols, int type) {
+  return type == CCT_TYPE_F32 ? 0 : rows * up(cols, 8) * type_bytes(type);
+}
+struct LinearLayout {
+  long long x, w, dz, part, ld, total;
 };
-LinearBackward linear_backward_layout(const cct_linear_desc_t& d) {
+LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   Layout l;
-  LinearBackward b;
+  LinearLayout b;
+  b.x = l.take(copy_bytes(d.M, d.K, d.type));
+  b.w = l.take(copy_bytes(d.N, d.K, d.type));
   b.ld = up(d.N, 8);
-  b.dz = l.take((long long)d.M * b.ld * type_bytes(d.type));
-  b.part = l.take((long long)ff_sum_rows(d.M) * d.N * 4);
+  b.dz = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
+  b.part = l.take(backward ? (long long)ff_sum_rows(d.M) * d.N * 4 : 0);
   b.total = std::max(l.total, 256LL);
   return b;
 }
-struct GatedBackward {
-  long long dg, du, ld, total;
+struct GatedLayout {
+  long long x, wg, wu, dg, du, ld, total;
 };
-GatedBackward gated_backward_layout(const cct_gated_desc_t& d) {
+GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   Layout l;
-  GatedBackward b;
+  GatedLayout b;
+  b.x = l.take(copy_bytes(d.M, d.K, d.type));
+  b.wg = l.take(copy_bytes(d.F, d.K, d.type));
+  b.wu = l.take(copy_bytes(d.F, d.K, d.type));
   b.ld = up(d.F, 8);
-  b.dg = l.take((long long)d.M * b.ld * type_bytes(d.type));
-  b.du = l.take((long long)d.M * b.ld * type_bytes(d.type));
+  b.dg = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
+  b.du = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.total = std::max(l.total, 256LL);
   return b;
 }
 
-FfOperand rows_of(const void* p, long long ld) { return {p, ld, 1}; }
-FfOperand columns_of(const void* p, long long ld) { return {p, 1, ld}; }
+// The matrix itself, or its copy at `to` where the products do not take it in place.
+int operand(const Matrix& m, long long rows, long long cols, int type, void* to, Matrix* use, hipStream_t st) {
+  *use = {m.p, rows <= 1 ? up(cols, 8) : m.ld};
+  if (type == CCT_TYPE_F32 || rows == 0 || ff_in_place(use->p, use->ld, cols)) return CCT_OK;
+  *use = {to, up(cols, 8)};
+  return launch_ff_dz({(int)rows, (int)cols, type, CCT_ACT_NONE, m.p, nullptr, m.ld, 0, to, use->ld, nullptr, nullptr}, st);
+}
+// Two weights that one product takes must have the same strides.
+int weight_pair(const Matrix& g, const Matrix& u, long long rows, long long cols, int type, char* to_g, char* to_u, Matrix* use_g,
+                Matrix* use_u, hipStream_t st) {
+  int rc = operand(g, rows, cols, type, to_g, use_g, st);
+  if (rc == CCT_OK) rc = operand(u, rows, cols, type, to_u, use_u, st);
+  if (rc != CCT_OK || type == CCT_TYPE_F32 || use_g->ld == use_u->ld) return rc;
+  const long long ld = up(cols, 8);
+  auto copy = [&](const Matrix& m, void* to, Matrix* use) {
+    if (use->p == to) return (int)CCT_OK;
+    *use = {to, ld};
+    return launch_ff_dz({(int)rows, (int)cols, type, CCT_ACT_NONE, m.p, nullptr, m.ld, 0, to, ld, nullptr, nullptr}, st);
+  };
+  rc = copy(g, to_g, use_g);
+  return rc == CCT_OK ? copy(u, to_u, use_u) : rc;
+}
+
+FfOperand rows_of(const Matrix& m) { return {m.p, m.ld, 1, 0}; }
+FfOperand columns_of(const Matrix& m) { return {m.p, 1, m.ld, 1}; }
 
 // out (rows x cols) = sum over segments of A_s B_s^T, rounded, nothing else
 FfProduct plain_product(int type, int rows, int cols, int k, void* out, long long ldo) {
@@ -97,7 +129,7 @@ int cct_linear_workspace_bytes(const cct_linear_desc_t* desc, int32_t backward, 
   const cct_linear_desc_t& d = *desc;
   const int rc = dims_ok(d.M, d.N, d.K, d.type, d.activation);
   if (rc != CCT_OK) return rc;
-  *bytes = backward ? (size_t)linear_backward_layout(d).total : 256;
+  *bytes = (size_t)linear_layout(d, backward != 0).total;
   return CCT_OK;
 }
 
@@ -106,7 +138,7 @@ int cct_gated_workspace_bytes(const cct_gated_desc_t* desc, int32_t backward, si
   const cct_gated_desc_t& d = *desc;
   const int rc = dims_ok(d.M, d.F, d.K, d.type, d.activation);
   if (rc != CCT_OK) return rc;
-  *bytes = backward ? (size_t)gated_backward_layout(d).total : 256;
+  *bytes = (size_t)gated_layout(d, backward != 0).total;
   return CCT_OK;
 }
 
@@ -122,18 +154,25 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
       !matrix_ok({y, ldy}, d.M, d.N, d.type) || !vector_ok(bias, d.type) ||
       (residual && !matrix_ok({residual, ldr}, d.M, d.N, d.type)) || (z && !matrix_ok({z, ldz}, d.M, d.N, d.type)))
     return CCT_EINVAL;
-  rc = workspace_ok(workspace, workspace_bytes, 256);
+  const LinearLayout b = linear_layout(d, false);
+  rc = workspace_ok(workspace, workspace_bytes, b.total);
+  if (rc != CCT_OK) return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  char* ws = (char*)workspace;
+  Matrix mx, mw;
+  rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
+  if (rc == CCT_OK) rc = operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, st);
   if (rc != CCT_OK) return rc;
   FfProduct p = plain_product(d.type, d.M, d.N, d.K, y, ldy);
-  p.A[0] = rows_of(x, ldx);
-  p.B[0] = rows_of(w, ldw);
+  p.A[0] = rows_of(mx);
+  p.B[0] = rows_of(mw);
   p.activation = d.activation;
   p.bias = bias;
   p.residual = residual;
   p.ldr = ldr;
   p.z = z;
   p.ldz = ldz;
-  return launch_ff_product(p, (hipStream_t)hip_stream);
+  return launch_ff_product(p, st);
 }
 
 int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -150,31 +189,37 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
                   (dx && !matrix_ok({dx, lddx}, d.M, d.K, d.type))))
     return CCT_EINVAL;
   if ((dw && !matrix_ok({dw, lddw}, d.N, d.K, d.type)) || !vector_ok(dbias, d.type)) return CCT_EINVAL;
-  const LinearBackward b = linear_backward_layout(d);
+  const LinearLayout b = linear_layout(d, true);
   rc = workspace_ok(workspace, workspace_bytes, b.total);
   if (rc != CCT_OK) return rc;
   hipStream_t st = (hipStream_t)hip_stream;
   char* ws = (char*)workspace;
-  const bool copy = act && (dx || dw);
+  // dy itself is dz without an activation, where the products take it in place
+  const bool copy = (dx || dw) && (act || (d.type != CCT_TYPE_F32 && !ff_in_place(dy, d.M <= 1 ? b.ld : lddy, d.N)));
   if (copy || dbias) {
     FfDz q = {d.M, d.N, d.type, d.activation, dy, act ? z : nullptr, lddy, ldz, copy ? ws + b.dz : nullptr, b.ld, dbias,
               (float*)(ws + b.part)};
     rc = launch_ff_dz(q, st);
     if (rc != CCT_OK) return rc;
   }
-  const void* dz = copy ? ws + b.dz : dy;
-  const long long ld = copy ? b.ld : lddy;
+  const Matrix dz = {copy ? ws + b.dz : dy, copy || d.M <= 1 ? b.ld : lddy};
   if (dx && d.M > 0) {
+    Matrix mw;
+    rc = operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, st);
+    if (rc != CCT_OK) return rc;
     FfProduct p = plain_product(d.type, d.M, d.K, d.N, dx, lddx);
-    p.A[0] = rows_of(dz, ld);
-    p.B[0] = columns_of(w, ldw);
+    p.A[0] = rows_of(dz);
+    p.B[0] = columns_of(mw);
     rc = launch_ff_product(p, st);
     if (rc != CCT_OK) return rc;
   }
   if (dw) {
+    Matrix mx;
+    rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
+    if (rc != CCT_OK) return rc;
     FfProduct p = plain_product(d.type, d.N, d.K, d.M, dw, lddw);
-    p.A[0] = columns_of(dz, ld);
-    p.B[0] = columns_of(x, ldx);
+    p.A[0] = columns_of(dz);
+    p.B[0] = columns_of(mx);
     rc = launch_ff_product(p, st);
   }
   return rc;
@@ -192,19 +237,26 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
       !matrix_ok({wu, ldwu}, d.F, d.K, d.type) || !matrix_ok({h, ldh}, d.M, d.F, d.type) || (!g != !u) ||
       (g && (!matrix_ok({g, ldg}, d.M, d.F, d.type) || !matrix_ok({u, ldu}, d.M, d.F, d.type))))
     return CCT_EINVAL;
-  rc = workspace_ok(workspace, workspace_bytes, 256);
+  const GatedLayout b = gated_layout(d, false);
+  rc = workspace_ok(workspace, workspace_bytes, b.total);
+  if (rc != CCT_OK) return rc;
+  hipStream_t st = (hipStream_t)hip_stream;
+  char* ws = (char*)workspace;
+  Matrix mx, mg, mu;
+  rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
+  if (rc == CCT_OK) rc = weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, st);
   if (rc != CCT_OK) return rc;
   FfProduct p = plain_product(d.type, d.M, d.F, d.K, h, ldh);
   p.epilogue = kFfGated;
   p.activation = d.activation;
-  p.A[0] = rows_of(x, ldx);
-  p.B[0] = rows_of(wg, ldwg);
-  p.B[1] = rows_of(wu, ldwu);
+  p.A[0] = rows_of(mx);
+  p.B[0] = rows_of(mg);
+  p.B[1] = rows_of(mu);
   p.z = g;
   p.ldz = ldg;
   p.z2 = u;
   p.ldz2 = ldu;
-  return launch_ff_product(p, (hipStream_t)hip_stream);
+  return launch_ff_product(p, st);
 }
 
 int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
@@ -222,32 +274,38 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
                           !matrix_ok({dx, lddx}, d.M, d.K, d.type)))))
     return CCT_EINVAL;
   if (dwg && (!matrix_ok({dwg, lddwg}, d.F, d.K, d.type) || !matrix_ok({dwu, lddwu}, d.F, d.K, d.type))) return CCT_EINVAL;
-  const GatedBackward b = gated_backward_layout(d);
+  const GatedLayout b = gated_layout(d, true);
   rc = workspace_ok(workspace, workspace_bytes, b.total);
   if (rc != CCT_OK) return rc;
   if (!dx && !dwg) return CCT_OK;
   hipStream_t st = (hipStream_t)hip_stream;
-  void *dg = (char*)workspace + b.dg, *du = (char*)workspace + b.du;
-  rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, dg, du, b.ld}, st);
+  char* ws = (char*)workspace;
+  const Matrix dg = {ws + b.dg, b.ld}, du = {ws + b.du, b.ld};
+  rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, ws + b.dg, ws + b.du, b.ld}, st);
   if (rc != CCT_OK) return rc;
   if (dx && d.M > 0) {
+    Matrix mg, mu;
+    rc = weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, st);
+    if (rc != CCT_OK) return rc;
     FfProduct p = plain_product(d.type, d.M, d.K, d.F, dx, lddx);
     p.segments = 2;
-    p.A[0] = rows_of(dg, b.ld);
-    p.A[1] = rows_of(du, b.ld);
-    p.B[0] = columns_of(wg, ldwg);
-    p.B[1] = columns_of(wu, ldwu);
+    p.A[0] = rows_of(dg);
+    p.A[1] = rows_of(du);
+    p.B[0] = columns_of(mg);
+    p.B[1] = columns_of(mu);
     rc = launch_ff_product(p, st);
     if (rc != CCT_OK) return rc;
   }
-  for (int i = 0; i < 2 && dwg; ++i) {
+  if (!dwg) return CCT_OK;
+  Matrix mx;
+  rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
+  for (int i = 0; i < 2 && rc == CCT_OK; ++i) {
     FfProduct p = plain_product(d.type, d.F, d.K, d.M, i ? dwu : dwg, i ? lddwu : lddwg);
-    p.A[0] = columns_of(i ? du : dg, b.ld);
-    p.B[0] = columns_of(x, ldx);
+    p.A[0] = columns_of(i ? du : dg);
+    p.B[0] = columns_of(mx);
     rc = launch_ff_product(p, st);
-    if (rc != CCT_OK) return rc;
   }
-  return CCT_OK;
+  return rc;
 }
 
 }  // extern "C"

@@ -1,10 +1,11 @@
-// The matrix products of the feed-forward operators with their epilogues, for any type, strides and sizes.
+// The matrix products of the feed-forward operators with their epilogues.
 //
-// A workgroup computes 64 x 64 results, 4 x 4 per thread, from LDS tiles of 16 k in fp32.
+// 16-bit types: ff_tile.h.  fp32: a workgroup computes 64 x 64 results, 4 x 4 per thread, from LDS tiles of 16 k.
 #include <algorithm>
 
 #include "activation.h"
 #include "feed_forward.h"
+#include "ff_tile.h"
 
 namespace cct {
 namespace {
@@ -25,7 +26,7 @@ __global__ __launch_bounds__(NT) void ff_product_kernel(FfProduct p, int tiles_m
       auto stage = [&](float(&to)[BK][BT + 1], const FfOperand& o, int r0, int rows) {
         for (int i = threadIdx.x; i < BT * BK; i += NT) {
           // consecutive threads along the consecutive dimension
-          const int r = o.ks == 1 ? i / BK : i % BT, k = o.ks == 1 ? i % BK : i / BT;
+          const int r = o.across ? i % BT : i / BK, k = o.across ? i / BT : i % BK;
           to[k][r] = r0 + r < rows && k0 + k < p.K ? load1<TYPE>(o.p, (r0 + r) * o.rs + (k0 + k) * o.ks) : 0.f;
         }
       };
@@ -74,6 +75,35 @@ void launch(const FfProduct& p, hipStream_t st) {
     hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_product_kernel<TYPE, false>), dim3(tiles_m * tiles_n), dim3(NT), 0, st, p, tiles_m);
 }
 
+template <int TYPE, int BM, int BN, int WM, int WN, bool AX, bool BX, int EPI>
+int launch_tile(const FfProduct& p, hipStream_t st) {
+  constexpr int lds = 2 * (BM + BN) * kStageK * 2;
+  constexpr auto kernel = ff_tile_kernel<TYPE, BM, BN, WM, WN, AX, BX, EPI>;
+  const int rc = ensure_dynamic_lds<kernel>(lds);
+  if (rc != CCT_OK) return rc;
+  constexpr int cols = EPI == kFfGated ? BN / 2 : BN;
+  const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + cols - 1) / cols;
+  hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n), dim3(WM * WN * 64), lds, st, p, tiles_m, tiles_n);
+  return CCT_OK;
+}
+
+template <int TYPE, int BM, int BN, int WM, int WN>
+int launch_mode(const FfProduct& p, hipStream_t st) {
+  const bool ax = p.A[0].across, bx = p.B[0].across;
+  if (p.epilogue == kFfGated) return launch_tile<TYPE, BM, BN, WM, WN, false, false, kFfGated>(p, st);
+  if (ax) return launch_tile<TYPE, BM, BN, WM, WN, true, true, kFfLinear>(p, st);
+  if (bx) return launch_tile<TYPE, BM, BN, WM, WN, false, true, kFfLinear>(p, st);
+  return launch_tile<TYPE, BM, BN, WM, WN, false, false, kFfLinear>(p, st);
+}
+
+// Tiles of 256 x 256 where they fill the card, else of 128 x 128.
+template <int TYPE>
+int launch_sized(const FfProduct& p, hipStream_t st) {
+  const long long cols = p.epilogue == kFfGated ? 2LL * p.N : p.N;
+  if ((long long)((p.M + 255) / 256) * ((cols + 255) / 256) >= 200) return launch_mode<TYPE, 256, 256, 2, 4>(p, st);
+  return launch_mode<TYPE, 128, 128, 2, 2>(p, st);
+}
+
 }  // namespace
 
 int launch_ff_product(const FfProduct& p, hipStream_t st) {
@@ -82,12 +112,14 @@ int launch_ff_product(const FfProduct& p, hipStream_t st) {
   const double bytes = e * ((double)(p.epilogue == kFfGated ? 1 : p.segments) * p.M * p.K + ops * p.N * p.K +
                             mn * (1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)));
   ProfScope ps("ff_product_kernel", flops, bytes, st);
+  int rc = CCT_OK;
   if (p.type == CCT_TYPE_F32)
     launch<CCT_TYPE_F32>(p, st);
   else if (p.type == CCT_TYPE_BF16)
-    launch<CCT_TYPE_BF16>(p, st);
+    rc = launch_sized<CCT_TYPE_BF16>(p, st);
   else
-    launch<CCT_TYPE_F16>(p, st);
+    rc = launch_sized<CCT_TYPE_F16>(p, st);
+  if (rc != CCT_OK) return rc;
   CCT_CHECK_LAUNCH();
   return CCT_OK;
 }
