@@ -31,7 +31,30 @@ struct FfProduct {
   void *z, *z2;
   long long ldz, ldz2;
 };
-int launch_ff_product(const FfProduct& p, hipStream_t st);
+// `pack` (fp32) and `ws`: room for an operand's terms and for partial sums, as the plans below say.
+int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st);
+// How a 16-bit product is cut (ff_tile.h): its tile, splits of the contraction of so many stages, and the bytes of their
+// partial sums (launch_ff_product's `ws`).
+enum { kTile256, kTile128, kTile64x128, kTile64 };
+constexpr int kFfStage = 64;
+struct FfTilePlan {
+  int tile, splits, stages;
+  long long part_bytes;
+};
+FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments);
+int launch_ff_tile_bf16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
+int launch_ff_tile_f16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
+// fp32 (ff_f32.hip): splits of `len` steps, rows that are packed at a time, and the bytes for them and for the sums.
+struct FfF32Plan {
+  int splits, len, rows;
+  long long pack_bytes, part_bytes;
+};
+FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool along);
+int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st);
+// A forward product (operands along the contraction, at any address) of few rows: up to kFfRowsMost run, up to kFfRows (fp32:
+// kFfRowsF32) are faster so.
+constexpr int kFfRows = 16, kFfRowsF32 = 32, kFfRowsMost = 64;
+int launch_ff_rows(const FfProduct& p, hipStream_t st);
 // Whether the 16-bit product takes a matrix of `cols` consecutive values and rows `ld` apart in place: 16-byte loads, 256 rows
 // within 32-bit offsets.  Rows that are no multiple of 8 values must be followed by zeros up to one, as copies are.
 inline bool ff_in_place(const void* p, long long ld, long long cols) {

@@ -46,8 +46,20 @@ int workspace_ok(const void* workspace, size_t have, long long need) {
 long long copy_bytes(long long rows, long long cols, int type) {
   return type == CCT_TYPE_F32 ? 0 : rows * up(cols, 8) * type_bytes(type);
 }
+// Room for a product's packed operand (fp32) and its partial sums.
+struct Room {
+  long long pack, part;
+};
+Room room(int type, int M, int N, int K, int epilogue, int segments, bool along) {
+  if (M == 0) return {0, 0};
+  if (type != CCT_TYPE_F32) return {0, ff_tile_plan(M, N, K, epilogue, segments).part_bytes};
+  const FfF32Plan plan = ff_f32_plan(M, N, K, epilogue, segments, along);
+  return {plan.pack_bytes, plan.part_bytes};
+}
+Room larger(const Room& a, const Room& b) { return {std::max(a.pack, b.pack), std::max(a.part, b.part)}; }
+
 struct LinearLayout {
-  long long x, w, dz, part, ld, total;
+  long long x, w, dz, sums, pack, part, ld, total;
 };
 LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   Layout l;
@@ -56,12 +68,17 @@ LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   b.w = l.take(copy_bytes(d.N, d.K, d.type));
   b.ld = up(d.N, 8);
   b.dz = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
-  b.part = l.take(backward ? (long long)ff_sum_rows(d.M) * d.N * 4 : 0);
+  b.sums = l.take(backward ? (long long)ff_sum_rows(d.M) * d.N * 4 : 0);
+  // the two gradients are one after the other
+  const Room r = backward ? larger(room(d.type, d.M, d.K, d.N, kFfLinear, 1, false), room(d.type, d.N, d.K, d.M, kFfLinear, 1, false))
+                          : room(d.type, d.M, d.N, d.K, kFfLinear, 1, true);
+  b.pack = l.take(r.pack);
+  b.part = l.take(r.part);
   b.total = std::max(l.total, 256LL);
   return b;
 }
 struct GatedLayout {
-  long long x, wg, wu, dg, du, ld, total;
+  long long x, wg, wu, dg, du, pack, part, ld, total;
 };
 GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   Layout l;
@@ -72,8 +89,19 @@ GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   b.ld = up(d.F, 8);
   b.dg = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.du = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
+  const Room r = backward ? larger(room(d.type, d.M, d.K, d.F, kFfLinear, 2, false), room(d.type, d.F, d.K, d.M, kFfLinear, 1, false))
+                          : room(d.type, d.M, d.F, d.K, kFfGated, 1, true);
+  b.pack = l.take(r.pack);
+  b.part = l.take(r.part);
   b.total = std::max(l.total, 256LL);
   return b;
+}
+
+// Whether a forward product runs on ff_rows.hip.  bf16, 4096 -> 4096: 16 rows 11.7 us there, 12.0 in tiles; 48 rows 22 and 14,
+// but tiles may need a copy of the weight first (three times its bytes).  fp32: 16 rows 22.6 us; 48 rows 41 there, 37 on
+// ff_f32.hip; 64 rows of 4096 -> 16384 183 and 100.
+bool few_rows(int M, int type, bool in_place) {
+  return M <= kFfRows || (M <= (type == CCT_TYPE_F32 ? kFfRowsF32 : kFfRowsMost) && (type == CCT_TYPE_F32 || !in_place));
 }
 
 // The matrix itself, or its copy at `to` where the products do not take it in place.
@@ -159,9 +187,10 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
   if (rc != CCT_OK) return rc;
   hipStream_t st = (hipStream_t)hip_stream;
   char* ws = (char*)workspace;
-  Matrix mx, mw;
-  rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
-  if (rc == CCT_OK) rc = operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, st);
+  const bool few = few_rows(d.M, d.type, ff_in_place(w, d.N <= 1 ? up(d.K, 8) : ldw, d.K));
+  Matrix mx = {x, ldx}, mw = {w, ldw};
+  if (!few) rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
+  if (!few && rc == CCT_OK) rc = operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, st);
   if (rc != CCT_OK) return rc;
   FfProduct p = plain_product(d.type, d.M, d.N, d.K, y, ldy);
   p.A[0] = rows_of(mx);
@@ -172,7 +201,7 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
   p.ldr = ldr;
   p.z = z;
   p.ldz = ldz;
-  return launch_ff_product(p, st);
+  return few ? launch_ff_rows(p, st) : launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
 }
 
 int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -198,7 +227,7 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
   const bool copy = (dx || dw) && (act || (d.type != CCT_TYPE_F32 && !ff_in_place(dy, d.M <= 1 ? b.ld : lddy, d.N)));
   if (copy || dbias) {
     FfDz q = {d.M, d.N, d.type, d.activation, dy, act ? z : nullptr, lddy, ldz, copy ? ws + b.dz : nullptr, b.ld, dbias,
-              (float*)(ws + b.part)};
+              (float*)(ws + b.sums)};
     rc = launch_ff_dz(q, st);
     if (rc != CCT_OK) return rc;
   }
@@ -210,7 +239,7 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
     FfProduct p = plain_product(d.type, d.M, d.K, d.N, dx, lddx);
     p.A[0] = rows_of(dz);
     p.B[0] = columns_of(mw);
-    rc = launch_ff_product(p, st);
+    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
     if (rc != CCT_OK) return rc;
   }
   if (dw) {
@@ -220,7 +249,7 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
     FfProduct p = plain_product(d.type, d.N, d.K, d.M, dw, lddw);
     p.A[0] = columns_of(dz);
     p.B[0] = columns_of(mx);
-    rc = launch_ff_product(p, st);
+    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
   }
   return rc;
 }
@@ -242,9 +271,11 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
   if (rc != CCT_OK) return rc;
   hipStream_t st = (hipStream_t)hip_stream;
   char* ws = (char*)workspace;
-  Matrix mx, mg, mu;
-  rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
-  if (rc == CCT_OK) rc = weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, st);
+  const bool few = few_rows(d.M, d.type, ff_in_place(wg, d.F <= 1 ? up(d.K, 8) : ldwg, d.K) &&
+                                             ff_in_place(wu, d.F <= 1 ? up(d.K, 8) : ldwu, d.K) && ldwg == ldwu);
+  Matrix mx = {x, ldx}, mg = {wg, ldwg}, mu = {wu, ldwu};
+  if (!few) rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
+  if (!few && rc == CCT_OK) rc = weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, st);
   if (rc != CCT_OK) return rc;
   FfProduct p = plain_product(d.type, d.M, d.F, d.K, h, ldh);
   p.epilogue = kFfGated;
@@ -256,7 +287,7 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
   p.ldz = ldg;
   p.z2 = u;
   p.ldz2 = ldu;
-  return launch_ff_product(p, st);
+  return few ? launch_ff_rows(p, st) : launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
 }
 
 int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
@@ -293,7 +324,7 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
     p.A[1] = rows_of(du);
     p.B[0] = columns_of(mg);
     p.B[1] = columns_of(mu);
-    rc = launch_ff_product(p, st);
+    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
     if (rc != CCT_OK) return rc;
   }
   if (!dwg) return CCT_OK;
@@ -303,7 +334,7 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
     FfProduct p = plain_product(d.type, d.F, d.K, d.M, i ? dwu : dwg, i ? lddwu : lddwg);
     p.A[0] = columns_of(i ? du : dg);
     p.B[0] = columns_of(mx);
-    rc = launch_ff_product(p, st);
+    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
   }
   return rc;
 }

@@ -1,0 +1,163 @@
+// The fp32 products of the feed-forward operators, on the bf16 matrix cores as sums of three terms (gemm_split.hip), which is
+// as exact as fp32 instructions and faster.
+//
+// The rows' operand (x of a forward product, dz or its transpose in a backward one) is packed or split in place, the other
+// one is read in place, along or across the contraction.  The contraction may be cut into splits, and two contractions
+// (dx of a gated block) may be summed; then, and where an activation, a residual or z follow, the sums go through the
+// workspace and ff_join_kernel finishes them: 8 to 12 bytes per result against 2 K operations (4096 x 4096 x 4096: 27 of
+// 690 us).
+//
+// Strides that gemm_split cannot address (2^22 values and more) and empty contractions run on ff_general_kernel: 64 x 64
+// results per workgroup, 4 x 4 per thread, from LDS tiles of 16 k.
+#include <algorithm>
+#include <cstring>
+
+#include "ff_tile.h"
+
+namespace cct {
+namespace {
+
+constexpr int NT = 256, BT = 64, BK = 16;
+
+template <bool GATED>
+__global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m) {
+  constexpr int NB = GATED ? 2 : 1;
+  __shared__ float As[BK][BT + 1], Bs[NB][BK][BT + 1];
+  const int tile_n = blockIdx.x / tiles_m, tile_m = blockIdx.x - tile_n * tiles_m;
+  const int m0 = tile_m * BT, n0 = tile_n * BT;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  float acc[NB][4][4] = {};
+  for (int s = 0; s < (GATED ? 1 : p.segments); ++s)
+    for (int k0 = 0; k0 < p.K; k0 += BK) {
+      __syncthreads();
+      auto stage = [&](float(&to)[BK][BT + 1], const FfOperand& o, int r0, int rows) {
+        for (int i = threadIdx.x; i < BT * BK; i += NT) {
+          // consecutive threads along the consecutive dimension
+          const int r = o.across ? i % BT : i / BK, k = o.across ? i / BT : i % BK;
+          to[k][r] = r0 + r < rows && k0 + k < p.K ? ((const float*)o.p)[(r0 + r) * o.rs + (k0 + k) * o.ks] : 0.f;
+        }
+      };
+      stage(As, p.A[s], m0, p.M);
+      stage(Bs[0], p.B[s], n0, p.N);
+      if constexpr (GATED) stage(Bs[1], p.B[1], n0, p.N);
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < BK; ++k)
+#pragma unroll
+        for (int q = 0; q < NB; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[q][i][j] = fmaf(As[k][ty * 4 + i], Bs[q][k][tx * 4 + j], acc[q][i][j]);
+    }
+  const int n = n0 + tx * 4;
+  if (n >= p.N) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (m0 + ty * 4 + i < p.M)
+      finish<CCT_TYPE_F32, GATED ? kFfGated : kFfLinear>(p, m0 + ty * 4 + i, n, acc[0][i], acc[NB - 1][i]);
+}
+
+int launch_general(const FfProduct& p, hipStream_t st) {
+  const int tiles_m = (p.M + BT - 1) / BT;
+  const dim3 grid(tiles_m * ((p.N + BT - 1) / BT));
+  if (p.epilogue == kFfGated)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<true>), grid, dim3(NT), 0, st, p, tiles_m);
+  else
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<false>), grid, dim3(NT), 0, st, p, tiles_m);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+constexpr int kIntMax = 2147483647;
+constexpr long long kMostPack = 1LL << 30;  // bytes; more rows run one part after the other
+constexpr int kLeastSplit = 256;            // steps of the contraction
+
+GemmTN split_problem(int M, int N, int K, int splits) {
+  GemmTN t;
+  std::memset(&t, 0, sizeof(t));
+  t.M = M;
+  t.Mpad = gemm_split_mpad(M);
+  t.Ncols = N;
+  t.Kdim = K;
+  t.Kpad = gemm_split_kpad(K);
+  t.G = splits;
+  t.bmap = t.cmap = ColMap{kIntMax, 0};
+  return t;
+}
+
+}  // namespace
+
+FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool along) {
+  const int planes = epilogue == kFfGated ? 2 : segments;
+  FfF32Plan best = {1, K, M, 0, 0};
+  const long long ld = (N + 3) / 4 * 4;
+  if (M > 0 && K > 0) {
+    double least = 1e30;
+    const long long kpad = gemm_split_kpad(K);
+    best.rows = (int)std::min<long long>(M, std::max(64LL, kMostPack / (6 * kpad) / 64 * 64));
+    for (int sp = 1; sp <= 32 && (sp == 1 || K >= sp * kLeastSplit); sp += sp < 8 ? 1 : 4) {
+      const int len = sp == 1 ? K : gemm_split_kpad((K + sp - 1) / sp), n = (K + len - 1) / len;
+      const double t = gemm_split_seconds(along, true, best.rows, len, N, n) + (n > 1 ? 8.0 * n * best.rows * N / 5.5e12 + 2.5e-6 : 0.0);
+      if (t >= least) continue;
+      least = t;
+      best.splits = n;
+      best.len = len;
+    }
+    best.pack_bytes = 6LL * best.splits * gemm_split_mpad(best.rows) * gemm_split_kpad(best.len);
+  }
+  best.part_bytes = 4LL * best.splits * planes * M * ld;
+  return best;
+}
+
+int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
+  const bool gated = p.epilogue == kFfGated, along = !p.B[0].across;
+  const int products = gated ? 2 : p.segments;
+  const FfF32Plan plan = ff_f32_plan(p.M, p.N, p.K, p.epilogue, p.segments, along);
+  const bool join = plan.splits > 1 || products > 1 || p.residual || p.z || p.activation != CCT_ACT_NONE;
+  const long long ld = join ? (p.N + 3) / 4 * 4 : p.ldo;
+  for (int q = 0; q < products; ++q) {
+    GemmTN t = split_problem(plan.rows, p.N, plan.len, plan.splits);
+    t.b_ks = along ? p.B[q].rs : p.B[q].ks;
+    if (p.K < 1 || !gemm_split_fits(t, along)) return launch_general(p, st);
+  }
+  for (int m0 = 0; m0 < p.M; m0 += plan.rows) {
+    GemmTN t = split_problem(std::min(plan.rows, p.M - m0), p.N, plan.len, plan.splits);
+    for (int q = 0; q < products; ++q) {
+      const FfOperand &A = p.A[gated ? 0 : q], &B = p.B[q];
+      t.B = B.p;
+      t.b_ks = along ? B.rs : B.ks;
+      t.b_gs = plan.len * B.ks;
+      t.b_len = along ? (p.N - 1) * B.rs + p.K : (p.K - 1) * B.ks + p.N;
+      if (q == 0 || !gated) {  // a gated block's products have the same rows
+        const int rc = gemm_split_operand(&t, along, (const float*)A.p + m0 * A.rs, pack, p.K, A.rs, A.ks, plan.len * A.ks, 1, st);
+        if (rc != CCT_OK) return rc;
+      }
+      t.c_ms = ld;
+      if (join) {
+        t.C = ws + ((gated ? q : (long long)q * plan.splits) * p.M + m0) * ld;
+        t.c_gs = (gated ? 2LL : 1LL) * p.M * ld;
+      } else {
+        t.C = (float*)p.out + m0 * ld;
+        t.bias = (const float*)p.bias;
+        t.bias_gs = -1;
+      }
+      const int rc = launch_gemm_split(t, p.K, along, st);
+      if (rc != CCT_OK) return rc;
+    }
+  }
+  if (!join) return CCT_OK;
+  const FfPart part = {ws, (int)ld, plan.splits * (gated ? 1 : products), 0};
+  const dim3 grid((unsigned)((p.M * ld / 4 + 255) / 256));
+  const double mn = (double)p.M * p.N;
+  ProfScope ps("ff_join_kernel", mn * plan.splits * products,
+               4.0 * mn * (plan.splits * products + 1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)), st);
+  if (gated)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<CCT_TYPE_F32, kFfGated>), grid, dim3(256), 0, st, p, part);
+  else
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<CCT_TYPE_F32, kFfLinear>), grid, dim3(256), 0, st, p, part);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+}  // namespace cct

@@ -2,14 +2,15 @@
 //
 // An operand is taken from memory as it lies, with its values consecutive along the contraction (x and a weight in a forward
 // product) or across it (a weight in dx, both in dw).  A stage is 64 steps of the contraction: 128 bytes of every row, or 64
-// rows of the tile's width.  Loads of 16 bytes a lane write LDS directly, without registers, one stage ahead of the one that
-// is multiplied; two stages alternate and the workgroup meets once per stage.
+// rows of the tile's width.  Loads of 16 bytes a lane write LDS directly, without registers, into a ring of stages of which
+// one is multiplied while the others are on their way; the workgroup meets once per stage.
 //
 // LDS, where an operand's 16-byte pieces are permuted so that reads do not conflict (a load cannot place its lanes, but each
 // lane chooses what it loads):
 //   along the contraction: rows of 8 pieces, piece c of row r at c ^ (r & 7).  A matrix instruction's operand is one piece
 //     per lane, 16 rows x 4 pieces.
-//   across it: 64 rows of the tile's width, in windows of 16 values; window v of row k at v ^ (k & 3 | (k >> 1) & 4).  The
+//   across it: 64 rows of the tile's width, in windows of 16 values; window v of row k at v ^ (k & 3 | (k >> 1) & 4)
+//     (64 wide, which has four windows: v ^ (k & 3)).  The
 //     operand is read with the transposing 8-byte LDS load: 16 lanes fetch 4 rows x 16 values and each gets 4 rows of one
 //     column; two of them make a lane's 8 steps.
 //
@@ -28,7 +29,7 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
-constexpr int kStageK = 64;
+constexpr int kStageK = kFfStage;
 
 template <int TYPE>
 __device__ __forceinline__ f32x4 tile_mfma(s16x8 a, s16x8 b, f32x4 c) {
@@ -48,7 +49,7 @@ struct TileOperand {
   unsigned voff[UNITS];                    // a lane's bytes from the tile's first row (and the stage's first step)
   int piece;                               // along: which of a row's 8 pieces a lane loads
 
-  static __device__ __forceinline__ int swizzle(int k) { return (k & 3) | ((k >> 1) & 4); }
+  static __device__ __forceinline__ int swizzle(int k) { return ((k & 3) | ((k >> 1) & 4)) & (ROWS / 16 - 1); }
 
   // rows (along) or columns (across, in whole eights) past `left` load the last again: their results are not stored.
   // PARTS == 2: the second half of the rows is another matrix's (each with `left`).
@@ -69,20 +70,35 @@ struct TileOperand {
       }
     }
   }
-  // steps [k0, k0 + 64) of a contraction of K; `first` and, for the second half of the rows, `second`: the tile's first row
+  // Where the next stage lies: the address of the tile's first row (or, across, the stage's first step), and the bytes from
+  // there to the operand's end, past which loads answer zero.  Rows have room for whole eights, zeros behind a contraction's
+  // end.  PARTS == 2: `second` is where the other matrix's rows begin.
+  struct Cursor {
+    const char *first, *second;
+    long long bytes;
+  };
+  static __device__ __forceinline__ Cursor begin(const char* first, const char* second, long long ld, int left, int k0, int K) {
+    Cursor c;
+    const long long skip = (long long)k0 * (ACROSS ? ld * 2 : 2);
+    c.first = first + skip;
+    c.second = second + skip;
+    c.bytes = (ACROSS ? (long long)(K - 1) * ld + ((left + 7) & ~7) : (long long)(min(left, ROWS) - 1) * ld + ((K + 7) & ~7)) * 2 - skip;
+    return c;
+  }
+  static __device__ __forceinline__ void next(Cursor& c, long long ld) {
+    const long long step = kStageK * (ACROSS ? ld * 2 : 2);
+    c.first += step;
+    c.second += step;
+    c.bytes -= step;
+  }
+  // kl: steps that are left; 0: nothing is loaded, LDS receives zeros
   template <int PARTS>
-  __device__ __forceinline__ void load(unsigned char* lds, int wave, const char* first, const char* second, long long ld, int left,
-                                       int k0, int K) const {
-    const int kl = min(K - k0, kStageK);
-    const long long skip = ACROSS ? (long long)k0 * ld * 2 : (long long)k0 * 2;
-    // rows have room for whole eights, zeros behind a contraction's end
-    const long long bytes = ACROSS ? ((long long)(kl - 1) * ld + ((left + 7) & ~7)) * 2
-                                   : ((long long)(min(left, ROWS) - 1) * ld + ((K - k0 + 7) & ~7)) * 2;
-    const int range = (int)min(bytes, 0x7fffffffLL);
-    const __amdgpu_buffer_rsrc_t r0 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(first + skip), 0, range, 0x00020000);
+  __device__ __forceinline__ void load(unsigned char* lds, int wave, const Cursor& c, int kl) const {
+    const int range = kl <= 0 ? 0 : c.bytes >> 31 ? 0x7fffffff : (int)c.bytes;
+    const __amdgpu_buffer_rsrc_t r0 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(c.first), 0, range, 0x00020000);
     const __amdgpu_buffer_rsrc_t r1 =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>((PARTS == 2 ? second : first) + skip), 0, range, 0x00020000);
-    // along: pieces past the contraction's end ask beyond the range, which answers zero (across: their rows lie beyond it)
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(PARTS == 2 ? c.second : c.first), 0, range, 0x00020000);
+    // along: pieces past the contraction's end ask beyond the range (across: their rows lie beyond it)
     const bool live = ACROSS || piece * 8 < kl;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
@@ -108,65 +124,68 @@ struct TileOperand {
   }
 };
 
-// 4 neighbouring values of one row at any address, those past `left` not there
-template <int TYPE>
-__device__ __forceinline__ void load4(float (&v)[4], const void* p, long long at, int left) {
+// W neighbouring values of one row at any address, those past `left` not there
+template <int TYPE, int W>
+__device__ __forceinline__ void load_some(float (&v)[W], const void* p, long long at, int left) {
   typedef typename Number<TYPE>::T T;
-  typedef T V4 __attribute__((ext_vector_type(4)));
-  typedef V4 U4 __attribute__((aligned(sizeof(T))));
+  typedef T VW __attribute__((ext_vector_type(W)));
+  typedef VW UW __attribute__((aligned(sizeof(T))));
   const T* from = (const T*)p + at;
-  if (left >= 4) {
-    const V4 all = *(const U4*)from;
+  if (left >= W) {
+    const VW all = *(const UW*)from;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)all[e];
+    for (int e = 0; e < W; ++e) v[e] = (float)all[e];
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e < left ? (float)from[e] : 0.f;
+    for (int e = 0; e < W; ++e) v[e] = e < left ? (float)from[e] : 0.f;
   }
 }
-template <int TYPE>
-__device__ __forceinline__ void store4(void* p, long long at, const float (&v)[4], int left) {
+template <int TYPE, int W>
+__device__ __forceinline__ void store_some(void* p, long long at, const float (&v)[W], int left) {
   typedef typename Number<TYPE>::T T;
-  typedef T V4 __attribute__((ext_vector_type(4)));
-  typedef V4 U4 __attribute__((aligned(sizeof(T))));
+  typedef T VW __attribute__((ext_vector_type(W)));
+  typedef VW UW __attribute__((aligned(sizeof(T))));
   T* to = (T*)p + at;
-  if (left >= 4) {
-    V4 all;
+  if (left >= W) {
+    VW all;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) all[e] = (T)v[e];
-    *(U4*)to = all;
+    for (int e = 0; e < W; ++e) all[e] = (T)v[e];
+    *(UW*)to = all;
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < W; ++e)
       if (e < left) to[e] = (T)v[e];
   }
 }
 
-// What becomes of 4 neighbouring sums of row m from column n on (kFfGated: of both products'); `bias`: theirs.
-template <int TYPE, int EPI>
-__device__ __forceinline__ void finish4(const FfProduct& p, int m, int n, float (&v)[4], float (&u)[4], const float (&bias)[4]) {
+// What becomes of W neighbouring sums of row m from column n on (kFfGated: of both products').
+template <int TYPE, int EPI, int W>
+__device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (&v)[W], float (&u)[W]) {
   const int left = p.N - n;
   if constexpr (EPI == kFfGated) {
     if (p.z) {
-      store4<TYPE>(p.z, m * p.ldz + n, v, left);
-      store4<TYPE>(p.z2, m * p.ldz2 + n, u, left);
+      store_some<TYPE>(p.z, m * p.ldz + n, v, left);
+      store_some<TYPE>(p.z2, m * p.ldz2 + n, u, left);
     }
     activate(p.activation, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] *= u[e];
+    for (int e = 0; e < W; ++e) v[e] *= u[e];
   } else {
+    float r[W] = {};
+    if (p.residual) load_some<TYPE>(r, p.residual, m * p.ldr + n, left);
+    if (p.bias) {
+      float b[W];
+      load_some<TYPE>(b, p.bias, n, left);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += bias[e];
-    if (p.z) store4<TYPE>(p.z, m * p.ldz + n, v, left);
-    activate(p.activation, v);
-    if (p.residual) {
-      float r[4];
-      load4<TYPE>(r, p.residual, m * p.ldr + n, left);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += r[e];
+      for (int e = 0; e < W; ++e) v[e] += b[e];
     }
+    if (p.z) store_some<TYPE>(p.z, m * p.ldz + n, v, left);
+    activate(p.activation, v);
+    if (p.residual)
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] += r[e];
   }
-  store4<TYPE>(p.out, m * p.ldo + n, v, left);
+  store_some<TYPE>(p.out, m * p.ldo + n, v, left);
 }
 
 // Which tile a workgroup computes: every XCD (they take workgroups in turn) gets a contiguous run of tiles, which walks over
@@ -179,9 +198,23 @@ __device__ __forceinline__ void tile_of(int idx, int total, int tiles_m, int til
   *tm = strip * 8 + inner - *tn * rows;
 }
 
-// BM x BN results (kFfGated: BM x BN / 2 of each product) with WM x WN waves.
-template <int TYPE, int BM, int BN, int WM, int WN, bool AX, bool BX, int EPI>
-__global__ __launch_bounds__(WM* WN * 64) void ff_tile_kernel(FfProduct p, int tiles_m, int tiles_n) {
+// The sums of one split of the contraction, for ff_join_kernel: M rows of `ld` floats, the second product's behind the first's.
+struct FfPart {
+  float* p;
+  int ld;
+  int splits, stages;  // of one split
+};
+
+// A wave's results on their way out: EROWS rows of PITCH floats in LDS.
+template <int BM, int BN, int WM, int WN>
+struct TileEpilogue {
+  static constexpr int EROWS = BM / WM < 64 ? BM / WM : 64, PITCH = BN / WN + 4;
+  static constexpr int BYTES = WM * WN * EROWS * PITCH * 4;
+};
+
+// BM x BN results (kFfGated: BM x BN / 2 of each product) with WM x WN waves; RING stages in LDS; SPLIT: the sums go to `part`.
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
+__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void ff_tile_kernel(FfProduct p, int tiles_m, int tiles_n, FfPart part) {
   constexpr int NW = WM * WN, RB = BM / WM / 16, CB = BN / WN / 16;
   constexpr int PARTS = EPI == kFfGated ? 2 : 1;
   typedef TileOperand<BM, NW, AX> OpA;
@@ -191,23 +224,43 @@ __global__ __launch_bounds__(WM* WN * 64) void ff_tile_kernel(FfProduct p, int t
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
+  // splits of a tile lie far apart: what runs at a time shares stages of the contraction
+  const int tiles = tiles_m * tiles_n, split = SPLIT ? blockIdx.x / tiles : 0;
   int tm, tn;
-  tile_of(blockIdx.x, tiles_m * tiles_n, tiles_m, tiles_n, &tm, &tn);
+  tile_of(blockIdx.x - split * tiles, tiles, tiles_m, tiles_n, &tm, &tn);
   const int m0 = tm * BM, n0 = tn * (BN / PARTS);
   const int left_m = p.M - m0, left_n = p.N - n0;
 
-  const int per = (p.K + kStageK - 1) / kStageK, stages = per * (EPI == kFfGated ? 1 : p.segments);
+  const int per = max((p.K + kStageK - 1) / kStageK, 1), all = per * (EPI == kFfGated ? 1 : p.segments);
+  const int first = SPLIT ? split * part.stages : 0, stages = SPLIT ? min(part.stages, all - first) : all;
   OpA a;
   OpB b;
   const long long lda = AX ? p.A[0].ks : p.A[0].rs, ldb = BX ? p.B[0].ks : p.B[0].rs;
   a.template init<1>(wave, lane, left_m, lda);
   b.template init<PARTS>(wave, lane, left_n, ldb);
   const long long a_at = (AX ? m0 : m0 * lda) * 2, b_at = (BX ? n0 : n0 * ldb) * 2;
-  auto load = [&](int t) {
-    unsigned char* st = tile_smem + (t & 1) * STAGE;
-    const int s = t >= per ? 1 : 0, k0 = (t - s * per) * kStageK;
-    a.template load<1>(st, wave, (const char*)p.A[s].p + a_at, nullptr, lda, left_m, k0, p.K);
-    b.template load<PARTS>(st + OpA::BYTES, wave, (const char*)p.B[s].p + b_at, (const char*)p.B[1].p + b_at, ldb, left_n, k0, p.K);
+  // the stage that is loaded next; past the last one nothing is, but as many loads are in flight as ever
+  int k_next = first % per * kStageK, to_load = stages;
+  auto cursor_a = [&](int s, int k0) { return OpA::begin((const char*)p.A[s].p + a_at, nullptr, lda, left_m, k0, p.K); };
+  auto cursor_b = [&](int s, int k0) {
+    return OpB::begin((const char*)p.B[s].p + b_at, (const char*)p.B[1].p + b_at, ldb, left_n, k0, p.K);
+  };
+  auto ca = cursor_a(first / per, k_next);
+  auto cb = cursor_b(first / per, k_next);
+  auto load = [&](int slot) {
+    unsigned char* st = tile_smem + slot * STAGE;
+    const int kl = to_load > 0 ? p.K - k_next : 0;
+    a.template load<1>(st, wave, ca, kl);
+    b.template load<PARTS>(st + OpA::BYTES, wave, cb, kl);
+    --to_load;
+    k_next += kStageK;
+    OpA::next(ca, lda);
+    OpB::next(cb, ldb);
+    if (EPI != kFfGated && k_next >= p.K && to_load > 0) {  // the second contraction
+      k_next = 0;
+      ca = cursor_a(1, 0);
+      cb = cursor_b(1, 0);
+    }
   };
   // the weights' rows of block j: half of a wave's are of the second product
   auto row_b = [&](int j) {
@@ -220,49 +273,130 @@ __global__ __launch_bounds__(WM* WN * 64) void ff_tile_kernel(FfProduct p, int t
 #pragma unroll
     for (int i = 0; i < RB; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  if (stages > 0) load(0);
-  for (int t = 0; t < stages; ++t) {
-    // this stage's loads have landed and nobody reads the other buffer any more
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    __syncthreads();
-    if (t + 1 < stages) load(t + 1);
-    const unsigned char *sa = tile_smem + (t & 1) * STAGE, *sb = sa + OpA::BYTES;
+  // Half a stage's operands are read from LDS behind the matrix instructions of the half before.  The workgroup meets between
+  // the halves: then the stage's second half is in registers, so that the next loads take its place, and the next stage has
+  // landed, whose first half is read.
+  s16x8 fa[2][RB], fb[2][CB];
+  auto read = [&](int h, int slot) {
+    const unsigned char *sa = tile_smem + slot * STAGE, *sb = sa + OpA::BYTES;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      s16x8 fa[RB], fb[CB];
+    for (int j = 0; j < CB; ++j) fb[h][j] = OpB::read(sb, lane, row_b(j), h);
 #pragma unroll
-      for (int j = 0; j < CB; ++j) fb[j] = OpB::read(sb, lane, row_b(j), h);
+    for (int i = 0; i < RB; ++i) fa[h][i] = OpA::read(sa, lane, wm * (BM / WM) + i * 16, h);
+  };
+  auto multiply = [&](int h) {
 #pragma unroll
-      for (int i = 0; i < RB; ++i) fa[i] = OpA::read(sa, lane, wm * (BM / WM) + i * 16, h);
+    for (int i = 0; i < RB; ++i)
 #pragma unroll
-      for (int i = 0; i < RB; ++i)
+      for (int j = 0; j < CB; ++j) acc[j][i] = tile_mfma<TYPE>(fb[h][j], fa[h][i], acc[j][i]);
+    // a wave issues in order, and eight waves' reads take LDS as long as the matrix instructions of a half: read by read
+    // between them, not in front of them
+    constexpr int READS = (AX ? 2 : 1) * RB + (BX ? 2 : 1) * CB, EACH = RB * CB / READS;
 #pragma unroll
-        for (int j = 0; j < CB; ++j) acc[j][i] = tile_mfma<TYPE>(fb[j], fa[i], acc[j][i]);
+    for (int q = 0; q < READS; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // all but the last `behind` loads of this wave have landed, its LDS reads too, and everybody's (a meeting and nothing else:
+  // __syncthreads() would wait for all loads)
+  constexpr int L = OpA::UNITS + OpB::UNITS;
+  static_assert((RING - 1) * L < 64, "vmcnt has six bits");
+#define CCT_MEET(behind)                                                               \
+  __builtin_amdgcn_s_waitcnt(0x0070 | ((behind) & 15) | ((behind) >> 4) << 14);        \
+  asm volatile("" ::: "memory");                                                       \
+  __builtin_amdgcn_s_barrier();                                                        \
+  asm volatile("" ::: "memory")
+  for (int q = 0; q < RING; ++q) load(q);
+  CCT_MEET((RING - 1) * L);
+  int slot = 0;
+  read(0, 0);
+  for (int t = 0; t < stages; ++t) {
+    read(1, slot);
+    multiply(0);
+    CCT_MEET((RING - 2) * L);
+    load(slot);
+    slot = slot + 1 == RING ? 0 : slot + 1;
+    read(0, slot);
+    multiply(1);
   }
+#undef CCT_MEET
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // the empty loads write LDS too
 
   constexpr int OUT = CB / PARTS;  // blocks of columns of the result
-  float bias[OUT][4] = {};
-  if (EPI == kFfLinear && p.bias)
+  if constexpr (SPLIT) {
 #pragma unroll
-    for (int j = 0; j < OUT; ++j) load4<TYPE>(bias[j], p.bias, n0 + row_b(j) + (lane >> 4) * 4, p.N - (n0 + row_b(j) + (lane >> 4) * 4));
+    for (int i = 0; i < RB; ++i) {
+      const int m = m0 + wm * (BM / WM) + i * 16 + (lane & 15);
 #pragma unroll
-  for (int i = 0; i < RB; ++i) {
-    const int m = m0 + wm * (BM / WM) + i * 16 + (lane & 15);
-    if (m >= p.M) continue;
-#pragma unroll
-    for (int j = 0; j < OUT; ++j) {
-      const int n = n0 + row_b(j) + (lane >> 4) * 4;
-      if (n >= p.N) continue;
-      float v[4], u[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = acc[j][i][e];
-        u[e] = acc[PARTS == 2 ? j + OUT : j][i][e];
+      for (int j = 0; j < OUT; ++j) {
+        const int n = n0 + row_b(j) + (lane >> 4) * 4;
+        if (m >= p.M || n >= p.N) continue;
+        float* to = part.p + ((long long)split * PARTS * p.M + m) * part.ld + n;
+        *(f32x4*)to = acc[j][i];
+        if constexpr (PARTS == 2) *(f32x4*)(to + (long long)p.M * part.ld) = acc[j + OUT][i];
       }
-      finish4<TYPE, EPI>(p, m, n, v, u, bias[j]);
     }
+    return;
   }
+  // Through LDS, EROWS rows of a wave at a time: a lane then has 8 neighbouring columns, stores are whole rows of the wave's
+  // columns, and the code stands once and not for every block.
+  typedef TileEpilogue<BM, BN, WM, WN> Ep;
+  __syncthreads();
+  float* mine = (float*)tile_smem + wave * (Ep::EROWS * Ep::PITCH);
+#pragma unroll
+  for (int half = 0; half < BM / WM / Ep::EROWS; ++half) {
+    constexpr int IB = Ep::EROWS / 16;
+#pragma unroll
+    for (int i = 0; i < IB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+        *(f32x4*)(mine + (i * 16 + (lane & 15)) * Ep::PITCH + j * 16 + (lane >> 4) * 4) = acc[j][half * IB + i];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int COLS = OUT * 16, PER = COLS / 8;  // lanes of a row
+#pragma unroll 1
+    for (int at = lane; at < Ep::EROWS * PER; at += 64) {
+      const int r = at / PER, c = at % PER * 8;
+      const int m = m0 + wm * (BM / WM) + half * Ep::EROWS + r, n = n0 + wn * COLS + c;
+      if (m >= p.M || n >= p.N) continue;
+      float v[8], u[8];
+      const float* from = mine + r * Ep::PITCH + c;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = from[e];
+        u[e] = PARTS == 2 ? from[COLS + e] : 0.f;
+      }
+      finish<TYPE, EPI>(p, m, n, v, u);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The splits' sums added in order, and finished.  A thread takes 4 columns of a row.
+template <int TYPE, int EPI>
+__global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p, FfPart part) {
+  constexpr int PARTS = EPI == kFfGated ? 2 : 1;
+  const int wide = part.ld / 4;
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int m = (int)(at / wide), n = (int)(at - (long long)m * wide) * 4;
+  if (m >= p.M) return;
+  f32x4 sum[PARTS];
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q) sum[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < part.splits; ++s)
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q)
+      sum[q] += *(const f32x4*)(part.p + (((long long)s * PARTS + q) * p.M + m) * part.ld + n);
+  float v[4], u[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = sum[0][e];
+    u[e] = sum[PARTS - 1][e];
+  }
+  finish<TYPE, EPI>(p, m, n, v, u);
 }
 
 }  // namespace

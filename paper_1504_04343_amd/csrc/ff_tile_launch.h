@@ -1,0 +1,56 @@
+// Launches of ff_tile.h's kernels for one type, as a plan says; a translation unit per type instantiates it.
+#pragma once
+#include "ff_tile.h"
+
+namespace cct {
+namespace {
+
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
+int launch_tile(const FfProduct& p, const FfPart& part, hipStream_t st) {
+  constexpr int ring = RING * (BM + BN) * kStageK * 2, out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
+  constexpr auto kernel = ff_tile_kernel<TYPE, BM, BN, WM, WN, RING, AX, BX, EPI, SPLIT>;
+  const int rc = ensure_dynamic_lds<kernel>(lds);
+  if (rc != CCT_OK) return rc;
+  constexpr int cols = EPI == kFfGated ? BN / 2 : BN;
+  const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + cols - 1) / cols;
+  hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n * part.splits), dim3(WM * WN * 64), lds, st, p, tiles_m, tiles_n, part);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool SPLIT>
+int launch_mode(const FfProduct& p, const FfPart& part, hipStream_t st) {
+  const bool ax = p.A[0].across, bx = p.B[0].across;
+  if (p.epilogue == kFfGated) return launch_tile<TYPE, BM, BN, WM, WN, RING, false, false, kFfGated, SPLIT>(p, part, st);
+  if (ax) return launch_tile<TYPE, BM, BN, WM, WN, RING, true, true, kFfLinear, SPLIT>(p, part, st);
+  if (bx) return launch_tile<TYPE, BM, BN, WM, WN, RING, false, true, kFfLinear, SPLIT>(p, part, st);
+  return launch_tile<TYPE, BM, BN, WM, WN, RING, false, false, kFfLinear, SPLIT>(p, part, st);
+}
+
+template <int TYPE>
+int launch_planned(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st) {
+  const FfPart part = {ws, (p.N + 3) / 4 * 4, plan.splits, plan.stages};
+  if (plan.splits == 1) switch (plan.tile) {
+      case kTile256: return launch_mode<TYPE, 256, 256, 2, 4, 2, false>(p, part, st);
+      case kTile128: return launch_mode<TYPE, 128, 128, 2, 2, 2, false>(p, part, st);
+      case kTile64x128: return launch_mode<TYPE, 64, 128, 2, 2, 3, false>(p, part, st);
+      default: return launch_mode<TYPE, 64, 64, 2, 2, 4, false>(p, part, st);
+    }
+  int rc;
+  switch (plan.tile) {
+    case kTile128: rc = launch_mode<TYPE, 128, 128, 2, 2, 2, true>(p, part, st); break;
+    case kTile64x128: rc = launch_mode<TYPE, 64, 128, 2, 2, 3, true>(p, part, st); break;
+    default: rc = launch_mode<TYPE, 64, 64, 2, 2, 4, true>(p, part, st);
+  }
+  if (rc != CCT_OK) return rc;
+  const dim3 grid((unsigned)(((long long)p.M * part.ld / 4 + 255) / 256));
+  if (p.epilogue == kFfGated)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, kFfGated>), grid, dim3(256), 0, st, p, part);
+  else
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, kFfLinear>), grid, dim3(256), 0, st, p, part);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+}  // namespace
+}  // namespace cct

@@ -669,10 +669,11 @@ int launch_gemm_split(const GemmTN& p0, int Ktotal, bool bt, hipStream_t st) {
   if (p.Mpad != gemm_split_mpad(p.M) || p.Kpad != gemm_split_kpad(p.Kdim)) return CCT_EINVAL;
   if (!gemm_split_fits(p, bt)) return CCT_EUNSUPPORTED;
   p.pair_P = p.pair_cols = 0;
-  // elements of B from p.B on
-  p.b_len = bt                        ? (long long)p.Ncols * p.b_ks
-            : p.bmap.P == 2147483647 ? Ktotal * p.b_ks
-                                     : (long long)(p.Ncols / p.bmap.P) * p.bmap.img_stride;
+  // elements of B from p.B on, unless the caller knows better (rows that are followed by something else)
+  if (!p.b_len)
+    p.b_len = bt                      ? (long long)p.Ncols * p.b_ks
+              : p.bmap.P == 2147483647 ? Ktotal * p.b_ks
+                                       : (long long)(p.Ncols / p.bmap.P) * p.bmap.img_stride;
   if (bt) return launch_columns<kContiguous>(p, Ktotal, st);
   p.pair_cols = gemm_split_pair_columns(p.bmap.P, p.Ncols, &p.pair_P);
   if (p.pair_P) make_fastdiv_parts(p.pair_P, &p.pair_M, &p.pair_sh);

@@ -276,6 +276,73 @@ def test_offsets_beyond_32_bits(B):
         del flat, gx, dx
 
 
+def test_fp32_rows_too_far_apart_for_the_split_product(B):
+    """Rows 2^22 values apart and more, each of x, w and the gradients: the general kernel."""
+    g = torch.Generator().manual_seed(12)
+    M, N, K, ld = 70, 40, 72, (1 << 22) + 5
+    flat = torch.empty((M - 1) * ld + K, device="cuda")
+    far = lambda r, c: flat.as_strided((r, c), (ld, 1))  # noqa: E731
+    x, w, u = ff.rand(g, M, K, torch.float32), ff.rand(g, N, K, torch.float32, 0.1), ff.rand(g, N, K, torch.float32, 0.1)
+    bias, r = ff.rand(g, 1, N, torch.float32).view(N), ff.rand(g, M, N, torch.float32)
+    d = B.make_linear_desc(M, N, K, B.TYPE_F32, B.ACT_GELU)
+    y, z = ff.empty_gpu(M, N, torch.float32), ff.empty_gpu(M, N, torch.float32)
+    far(N, K).copy_(w)
+    B.cct_linear_forward(d, x.cuda(), far(N, K), bias.cuda(), r.cuda(), y, z, B.alloc_linear_workspace(d, B.PASS_FORWARD))
+    want = ff.linear_forward("gelu", x, w, bias, r)
+    ff.check("y", y, want[0])
+    ff.check("z", z, want[1])
+    dy = ff.rand(g, M, N, torch.float32)
+    dx, dw = ff.empty_gpu(M, K, torch.float32), ff.empty_gpu(N, K, torch.float32)
+    ws = B.alloc_linear_workspace(d, B.PASS_BACKWARD)
+    B.cct_linear_backward(d, None, far(N, K), z, dy.cuda(), dx, None, None, ws)
+    far(M, K).copy_(x)
+    B.cct_linear_backward(d, far(M, K), None, z, dy.cuda(), None, dw, None, ws)
+    want = ff.linear_backward("gelu", x, w, z.cpu(), dy)
+    ff.check("dx", dx, want[0])
+    ff.check("dw", dw, want[1])
+    e = B.make_gated_desc(M, N, K, B.TYPE_F32, B.ACT_SILU)
+    far(N, K).copy_(w)
+    h = ff.empty_gpu(M, N, torch.float32)
+    B.cct_gated_forward(e, x.cuda(), far(N, K), u.cuda(), h, None, None, B.alloc_gated_workspace(e, B.PASS_FORWARD))
+    ff.check("h", h, ff.gated_forward("silu", x, w, u)[0])
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_every_tile_and_split(B, type):
+    """Sizes that the plan cuts into tiles of 256, 128, 64 x 128 and 64, with one split and with several."""
+    dt = ff.TYPES[type]
+    for M, N, K in ((3600, 3592, 136), (2050, 520, 72), (1032, 1536, 600), (520, 300, 2056), (72, 136, 8200), (264, 1100, 1032)):
+        print("tiles", type, M, N, K, flush=True)
+        g = torch.Generator().manual_seed(K)
+        x, w, u = ff.rand(g, M, K, dt), ff.rand(g, N, K, dt, K ** -0.5), ff.rand(g, N, K, dt, K ** -0.5)
+        y, z = linear_forward(B, type, "silu", x, w, None, None, True)
+        want = ff.linear_forward("silu", x, w, None, None)
+        ff.check("y", y, want[0])
+        dy, z = ff.rand(g, M, N, dt), z.cpu()
+        for name, t, v in zip(("dx", "dw", "dbias"), linear_backward(B, type, "silu", x, w, z, dy),
+                              ff.linear_backward("silu", x, w, z, dy)):
+            ff.check(name, t, v)
+        h, gg, uu = gated_forward(B, type, "gelu_tanh", x, w, u, True)
+        for name, t, v in zip("hgu", (h, gg, uu), ff.gated_forward("gelu_tanh", x, w, u)):
+            ff.check(name, t, v)
+
+
+def test_weights_of_a_gated_block_with_other_strides(B):
+    """wg and wu in rows of different lengths, as two slices of different tensors."""
+    g = torch.Generator().manual_seed(31)
+    for type in ff.TYPES:
+        for M in (5, 90):
+            dt = ff.TYPES[type]
+            x, wg, wu = ff.rand(g, M, 64, dt), ff.rand(g, 96, 64, dt, 0.1, 8), ff.rand(g, 96, 64, dt, 0.1, 24)
+            h, gg, uu = gated_forward(B, type, "silu", x, wg, wu, True)
+            for name, t, v in zip("hgu", (h, gg, uu), ff.gated_forward("silu", x, wg, wu)):
+                ff.check(name, t, v)
+            dh = ff.rand(g, M, 96, dt)
+            got = gated_backward(B, type, "silu", x, wg, wu, gg.cpu(), uu.cpu(), dh)
+            for name, t, v in zip(("dx", "dwg", "dwu"), got, ff.gated_backward("silu", x, wg, wu, gg.cpu(), uu.cpu(), dh)):
+                ff.check(name, t, v)
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 def test_gradients_against_differences(B, type):
     """<dx, s> and <dw, s> against how the loss changes along a direction s.  The loss is taken in 64 bits from the operator's
