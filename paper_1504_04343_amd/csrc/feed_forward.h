@@ -33,15 +33,18 @@ struct FfProduct {
 };
 // `pack` (fp32) and `ws`: room for an operand's terms and for partial sums, as the plans below say.
 int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st);
-// How a 16-bit product is cut (ff_tile.h): its tile, splits of the contraction of so many stages, and the bytes of their
-// partial sums (launch_ff_product's `ws`).
+// How a 16-bit product is cut (ff_tile.h): its tile, splits of the contraction of so many stages, the bytes of their partial
+// sums (launch_ff_product's `ws`) and an estimate; rows or columns behind which the rest is a launch with a plan of its own.
 enum { kTile256, kTile128, kTile64x128, kTile64 };
 constexpr int kFfStage = 64;
 struct FfTilePlan {
   int tile, splits, stages;
   long long part_bytes;
+  double micros;
+  int cut_rows, cut_cols;
 };
-FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments);
+// `along`: the weights' operand lies along the contraction.
+FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments, bool along);
 int launch_ff_tile_bf16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
 int launch_ff_tile_f16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
 // fp32 (ff_f32.hip): splits of `len` steps, rows that are packed at a time, and the bytes for them and for the sums.
@@ -62,7 +65,7 @@ inline bool ff_in_place(const void* p, long long ld, long long cols) {
 }
 
 // dz = dy * act'(z) into rows of ld values (a multiple of 8; zeros behind the N values of a row), and the column sums of the
-// unrounded dz; any of the two may be missing.  z NULL: dz = dy.  `part`: ff_sum_rows(M) * N floats.
+// unrounded dz; any of the two may be missing.  z NULL: dz = dy.  `part`: ff_sum_rows(M, N) * N floats.
 struct FfDz {
   int M, N, type, activation;
   const void *dy, *z;
@@ -72,7 +75,7 @@ struct FfDz {
   void* dbias;
   float* part;
 };
-int ff_sum_rows(int M);
+int ff_sum_rows(int M, int N);
 int launch_ff_dz(const FfDz& p, hipStream_t st);
 // dg = dh * u * act'(g), du = dh * act(g), both with rows of ld values as dz above.
 struct FfGatedDz {

@@ -52,7 +52,7 @@ struct Room {
 };
 Room room(int type, int M, int N, int K, int epilogue, int segments, bool along) {
   if (M == 0) return {0, 0};
-  if (type != CCT_TYPE_F32) return {0, ff_tile_plan(M, N, K, epilogue, segments).part_bytes};
+  if (type != CCT_TYPE_F32) return {0, ff_tile_plan(M, N, K, epilogue, segments, along).part_bytes};
   const FfF32Plan plan = ff_f32_plan(M, N, K, epilogue, segments, along);
   return {plan.pack_bytes, plan.part_bytes};
 }
@@ -68,7 +68,7 @@ LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   b.w = l.take(copy_bytes(d.N, d.K, d.type));
   b.ld = up(d.N, 8);
   b.dz = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
-  b.sums = l.take(backward ? (long long)ff_sum_rows(d.M) * d.N * 4 : 0);
+  b.sums = l.take(backward ? (long long)ff_sum_rows(d.M, d.N) * d.N * 4 : 0);
   // the two gradients are one after the other
   const Room r = backward ? larger(room(d.type, d.M, d.K, d.N, kFfLinear, 1, false), room(d.type, d.N, d.K, d.M, kFfLinear, 1, false))
                           : room(d.type, d.M, d.N, d.K, kFfLinear, 1, true);

@@ -4,7 +4,8 @@
 // Each input is read once and each output written once; the rounding of dz, dg and du to 16 bits is the matrix cores', which
 // take no more of an operand (2^-9 of a value at most for bf16, the same as the operands themselves were rounded by).
 //
-// A workgroup takes 256 columns x kRows rows, a thread 8 neighbouring columns of every eighth row: its column sums stay in
+// A workgroup takes 256 columns x 64 rows, or 8 where that leaves CUs idle (1531 x 1000: 9.9 -> X us), a thread 8
+// neighbouring columns of every eighth row: its column sums stay in
 // registers, meet in LDS in a fixed order and leave as one row of partial sums per workgroup, which a second kernel adds in
 // order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
 #include <algorithm>
@@ -15,7 +16,7 @@
 namespace cct {
 namespace {
 
-constexpr int NT = 256, kCols = 256, kRows = 64;
+constexpr int NT = 256, kCols = 256;
 
 template <class F>
 void with_type(int type, F f) {
@@ -49,10 +50,10 @@ __device__ __forceinline__ void store_columns(void* p, long long at, const float
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(NT) void ff_dz_kernel(FfDz p) {
+__global__ __launch_bounds__(NT) void ff_dz_kernel(FfDz p, int rows) {
   const int wide = (p.N + kCols - 1) / kCols, down = blockIdx.x / wide, c0 = (blockIdx.x - down * wide) * kCols;
   const int c = c0 + (threadIdx.x & 31) * 8, lane_row = threadIdx.x >> 5;
-  const int r0 = down * kRows, r1 = min(r0 + kRows, p.M);
+  const int r0 = down * rows, r1 = min(r0 + rows, p.M);
   float sum[8] = {};
   if (c < p.N)
     for (int r = r0 + lane_row; r < r1; r += NT / 32) {
@@ -87,26 +88,30 @@ __global__ __launch_bounds__(NT) void ff_dz_kernel(FfDz p) {
   p.part[(long long)down * p.N + col] = s;
 }
 
-// dbias from the rows of partial sums: 64 columns per workgroup, four runs of rows that meet in LDS
+// dbias from the rows of partial sums: 16 columns per workgroup, 64 runs of rows that meet in LDS
+constexpr int kSumRuns = 64;
 template <int TYPE>
-__global__ __launch_bounds__(NT) void ff_bias_sum_kernel(const float* __restrict__ part, int rows, int N, void* dbias) {
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), q = threadIdx.x >> 6;
-  const int per = (rows + 3) / 4, end = min(rows, (q + 1) * per);
+__global__ __launch_bounds__(16 * kSumRuns) void ff_bias_sum_kernel(const float* __restrict__ part, int rows, int N, void* dbias) {
+  const int c = threadIdx.x & 15, col = blockIdx.x * 16 + c, q = threadIdx.x >> 4;
   float s = 0.f;
   if (col < N)
-    for (int r = q * per; r < end; ++r) s += part[(long long)r * N + col];
-  __shared__ float sums[4][64];
-  sums[q][threadIdx.x & 63] = s;
+    for (int r = q; r < rows; r += kSumRuns) s += part[(long long)r * N + col];
+  __shared__ float sums[kSumRuns][17];
+  sums[q][c] = s;
   __syncthreads();
-  if (q == 0 && col < N)
-    store1<TYPE>(dbias, col, (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]));
+#pragma unroll
+  for (int half = kSumRuns / 2; half > 0; half >>= 1) {
+    if (q < half) sums[q][c] += sums[q + half][c];
+    __syncthreads();
+  }
+  if (q == 0 && col < N) store1<TYPE>(dbias, col, sums[0][c]);
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p) {
+__global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows) {
   const int wide = (p.F + kCols - 1) / kCols, down = blockIdx.x / wide;
   const int c = (blockIdx.x - down * wide) * kCols + (threadIdx.x & 31) * 8;
-  const int r0 = down * kRows, r1 = min(r0 + kRows, p.M);
+  const int r0 = down * rows, r1 = min(r0 + rows, p.M);
   if (c >= p.F) return;
   for (int r = r0 + (threadIdx.x >> 5); r < r1; r += NT / 32) {
     float dh[8], g[8], u[8], a[8], d[8];
@@ -126,24 +131,27 @@ __global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p) {
 
 }  // namespace
 
-int ff_sum_rows(int M) { return (M + kRows - 1) / kRows; }
+namespace {
+int rows_of_group(int M, int N) { return (long long)((M + 63) / 64) * ((N + kCols - 1) / kCols) >= 1024 ? 64 : 8; }
+}  // namespace
+int ff_sum_rows(int M, int N) { return (M + rows_of_group(M, N) - 1) / rows_of_group(M, N); }
 
 int launch_ff_dz(const FfDz& p, hipStream_t st) {
-  const int rows = ff_sum_rows(p.M);
+  const int rows = ff_sum_rows(p.M, p.N);
   const double n = (double)p.M * p.N, e = type_bytes(p.type);
   const char* const names[] = {"ff_dz_kernel<f32>", "ff_dz_kernel<bf16>", "ff_dz_kernel<f16>"};
   with_type(p.type, [&](auto type) {
     ProfScope ps(names[p.type], 2.0 * n, e * n * (1 + (p.z != nullptr) + (p.dz != nullptr)), st);
     if (p.M > 0)
       hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_dz_kernel<decltype(type)::value>), dim3((p.N + kCols - 1) / kCols * rows), dim3(NT), 0, st,
-                         p);
+                         p, rows_of_group(p.M, p.N));
   });
   CCT_CHECK_LAUNCH();
   if (!p.dbias) return CCT_OK;
   with_type(p.type, [&](auto type) {
     ProfScope ps("ff_bias_sum_kernel", (double)rows * p.N, 4.0 * rows * p.N, st);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((p.N + 63) / 64), dim3(NT), 0, st,
-                       p.part, rows, p.N, p.dbias);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((p.N + 15) / 16), dim3(16 * kSumRuns), 0,
+                       st, p.part, rows, p.N, p.dbias);
   });
   CCT_CHECK_LAUNCH();
   return CCT_OK;
@@ -155,7 +163,8 @@ int launch_ff_gated_dz(const FfGatedDz& p, hipStream_t st) {
   with_type(p.type, [&](auto type) {
     ProfScope ps("ff_gated_dz_kernel", 6.0 * n, 5.0 * e * n, st);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_gated_dz_kernel<decltype(type)::value>),
-                       dim3((p.F + kCols - 1) / kCols * ff_sum_rows(p.M)), dim3(NT), 0, st, p);
+                       dim3((p.F + kCols - 1) / kCols * ff_sum_rows(p.M, p.F)), dim3(NT), 0, st, p,
+                       rows_of_group(p.M, p.F));
   });
   CCT_CHECK_LAUNCH();
   return CCT_OK;

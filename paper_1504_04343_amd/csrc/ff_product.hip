@@ -7,26 +7,27 @@
 namespace cct {
 namespace {
 
-// Microseconds of a stage (64 steps of the contraction) with one workgroup on a CU and with as many as fit, measured with all
-// 256 CUs busy on products of 1024 to 8192 rows, all three directions (within 8 % of each other).
+// Microseconds of a stage (64 steps of the contraction) with one workgroup on a CU and with as many as fit, forward and with
+// operands across the contraction (whose LDS reads are twice as many), measured on products of 512 to 8192 rows.
 struct TileCost {
   int bm, bn, per_cu;
-  double alone, full;
+  double alone[2], full[2];
 };
-constexpr TileCost kTileCosts[] = {{256, 256, 1, 1.62, 1.62}, {128, 128, 2, 0.65, 1.10}, {64, 128, 2, 0.39, 0.72}, {64, 64, 2, 0.29, 0.54}};
+constexpr TileCost kTileCosts[] = {{256, 256, 1, {1.58, 1.65}, {1.58, 1.70}},
+                                   {128, 128, 2, {0.65, 0.93}, {1.10, 1.08}},
+                                   {64, 128, 2, {0.39, 0.75}, {0.72, 0.83}},
+                                   {64, 64, 2, {0.29, 0.50}, {0.54, 0.60}}};
 constexpr double kJoinMicros = 4.0, kJoinBytesPerMicro = 7.5e6;  // a launch and its gap; partial sums, written and read
 constexpr int kCus = 256, kLeastStages = 4;                       // of a split
-
-}  // namespace
+constexpr double kLaunchMicros = 3.0;
 
 // The tile and the number of splits of the contraction with the least estimate: rounds of workgroups over the card times the
 // stages of one, and what joining the splits costs.  Few large tiles leave CUs idle, small ones read LDS more often per
 // product.  1024 x 4096 x 9216 (forward, bf16): 181 us in tiles of 256 (64 of them), 96 in 128, 82 in 128 and two splits.
-FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments) {
+FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool along) {
   const long long cols = epilogue == kFfGated ? 2LL * N : N;
   const int stages = std::max((K + kFfStage - 1) / kFfStage, 1) * (epilogue == kFfGated ? 1 : segments);
-  FfTilePlan best = {kTile128, 1, stages, 0};
-  double least = 1e30;
+  FfTilePlan best = {kTile128, 1, stages, 0, 1e30, 0, 0};
   for (int tile = kTile256; tile <= kTile64; ++tile) {
     const TileCost& c = kTileCosts[tile];
     const long long tiles = ((M + c.bm - 1LL) / c.bm) * ((cols + c.bn - 1) / c.bn);
@@ -34,28 +35,79 @@ FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments) {
       if (splits > 1 && (tile == kTile256 || stages < splits * kLeastStages || tiles * splits > 4 * kCus)) break;
       const int each = (stages + splits - 1) / splits;
       const long long groups = tiles * splits, slots = (long long)kCus * c.per_cu, rest = groups % slots;
-      double us = (double)(groups / slots) * c.full + (rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full);
-      us *= each;
+      double us = (double)(groups / slots) * c.full[!along] + (rest == 0 ? 0.0 : (rest <= kCus ? c.alone : c.full)[!along]);
+      us = us * each + kLaunchMicros;
       if (splits > 1) us += kJoinMicros + 8.0 * splits * M * cols / kJoinBytesPerMicro;
-      if (us < least) {
-        least = us;
-        best = {tile, (stages + each - 1) / each, each, 0};
-      }
+      if (us < best.micros) best = {tile, (stages + each - 1) / each, each, 0, us, 0, 0};
     }
   }
   best.part_bytes = best.splits > 1 ? 4LL * best.splits * M * (cols + 8) : 0;
   return best;
 }
 
-int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
-  if (p.type == CCT_TYPE_F32) return launch_ff_f32(p, pack, ws, st);
+}  // namespace
+
+// The same, or whole rounds of tiles of 256 and what is left of the columns or rows in a launch of its own: 17 x 16 tiles are
+// two rounds, of which the second one is 16 workgroups (4160 columns of 4096 rows and steps: 187 us in tiles of
+// 128, 133 so).
+FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments, bool along) {
+  FfTilePlan best = whole_plan(M, N, K, epilogue, segments, along);
+  const int wide = epilogue == kFfGated ? 128 : 256;
+  const long long tm = (M + 255LL) / 256, tn = (N + wide - 1LL) / wide, rounds = tm * tn / kCus;
+  if (rounds < 1) return best;
+  const int stages = std::max((K + kFfStage - 1) / kFfStage, 1) * (epilogue == kFfGated ? 1 : segments);
+  const double full = rounds * stages * kTileCosts[kTile256].full[!along] + kLaunchMicros;
+  auto consider = [&](long long rows, long long cols) {  // what the full rounds take
+    if ((rows < M) == (cols < N)) return;
+    const FfTilePlan rest = rows < M ? whole_plan(M - (int)rows, N, K, epilogue, segments, along)
+                                 : whole_plan(M, N - (int)cols, K, epilogue, segments, along);
+    if (full + rest.micros >= best.micros) return;
+    best = {kTile256, 1, stages, rest.part_bytes, full + rest.micros, rows < M ? (int)rows : 0, cols < N ? (int)cols : 0};
+  };
+  if (tm <= rounds * kCus) consider(M, rounds * kCus / tm * wide);
+  if (tn <= rounds * kCus) consider(rounds * kCus / tn * 256, N);
+  return best;
+}
+
+namespace {
+
+// The results from row m and column n on, rows x cols of them.
+FfProduct part_of(FfProduct p, int m, int n, int rows, int cols) {
+  auto at = [&](const void* q, long long ld) { return q ? (void*)((char*)q + (m * ld + n) * 2) : nullptr; };
+  for (int s = 0; s < 2; ++s) {
+    if (p.A[s].p) p.A[s].p = (const char*)p.A[s].p + m * p.A[s].rs * 2;
+    if (p.B[s].p) p.B[s].p = (const char*)p.B[s].p + n * p.B[s].rs * 2;
+  }
+  p.M = rows;
+  p.N = cols;
+  p.bias = p.bias ? (const char*)p.bias + n * 2LL : nullptr;
+  p.residual = at(p.residual, p.ldr);
+  p.out = at(p.out, p.ldo);
+  p.z = at(p.z, p.ldz);
+  p.z2 = at(p.z2, p.ldz2);
+  return p;
+}
+
+int launch_tiles(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st) {
   const double mn = (double)p.M * p.N, ops = p.epilogue == kFfGated ? 2 : p.segments;
   const double bytes = 2.0 * ((double)(p.epilogue == kFfGated ? 1 : p.segments) * p.M * p.K + ops * p.N * p.K +
                               mn * (1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)));
-  const FfTilePlan plan = ff_tile_plan(p.M, p.N, p.K, p.epilogue, p.segments);
   const char* const names[] = {"256x256", "128x128", "64x128", "64x64"};
   ProfScope ps(2.0 * mn * p.K * ops, bytes, st, "ff_tile_kernel<%s, %d splits>", names[plan.tile], plan.splits);
   return p.type == CCT_TYPE_BF16 ? launch_ff_tile_bf16(p, plan, ws, st) : launch_ff_tile_f16(p, plan, ws, st);
+}
+
+}  // namespace
+
+int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
+  if (p.type == CCT_TYPE_F32) return launch_ff_f32(p, pack, ws, st);
+  const FfTilePlan plan = ff_tile_plan(p.M, p.N, p.K, p.epilogue, p.segments, !p.B[0].across);
+  if (!plan.cut_rows && !plan.cut_cols) return launch_tiles(p, plan, ws, st);
+  const int m = plan.cut_rows, n = plan.cut_cols;  // one of them is 0
+  const int rc = launch_tiles(part_of(p, 0, 0, m ? m : p.M, n ? n : p.N), plan, ws, st);
+  if (rc != CCT_OK) return rc;
+  const FfProduct rest = part_of(p, m, n, p.M - m, p.N - n);
+  return launch_tiles(rest, whole_plan(rest.M, rest.N, rest.K, rest.epilogue, rest.segments, !rest.B[0].across), ws, st);
 }
 
 }  // namespace cct

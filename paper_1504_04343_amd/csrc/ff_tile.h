@@ -9,10 +9,15 @@
 // lane chooses what it loads):
 //   along the contraction: rows of 8 pieces, piece c of row r at c ^ (r & 7).  A matrix instruction's operand is one piece
 //     per lane, 16 rows x 4 pieces.
-//   across it: 64 rows of the tile's width, in windows of 16 values; window v of row k at v ^ (k & 3 | (k >> 1) & 4)
+//   across it: rows of the tile's width, in windows of 16 values; window v of row k at v ^ (k & 3 | (k >> 1) & 4)
 //     (64 wide, which has four windows: v ^ (k & 3)).  The
 //     operand is read with the transposing 8-byte LDS load: 16 lanes fetch 4 rows x 16 values and each gets 4 rows of one
 //     column; two of them make a lane's 8 steps.
+//
+// What bounds it (8192 x 8192 x 4096 forward, 405 us): the loads alone take 263 us (16 TB/s out of the L2s), LDS reads and
+// matrix instructions without loads 326, so that a fifth of the loads is not hidden.  Stages of 32 steps in rings of 3 to 5
+// are 450 us whatever their number: half rows of 64 bytes cost more than loads further ahead give.  Four waves of 128 x 128
+// would read a third less LDS and do not hide anything behind each other (557 us).
 //
 // The weights' side is the instruction's first operand: a lane then holds 4 neighbouring columns of one row of the result,
 // stored as 8 bytes.
@@ -29,7 +34,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
-constexpr int kStageK = kFfStage;
+constexpr int SK = kFfStage;  // steps of the contraction per stage
+
 
 template <int TYPE>
 __device__ __forceinline__ f32x4 tile_mfma(s16x8 a, s16x8 b, f32x4 c) {
@@ -42,12 +48,12 @@ __device__ __forceinline__ f32x4 tile_mfma(s16x8 a, s16x8 b, f32x4 c) {
 // One operand of a tile: ROWS rows of it, moved by NW waves.  ACROSS: consecutive across the contraction.
 template <int ROWS, int NW, bool ACROSS>
 struct TileOperand {
-  static constexpr int BYTES = ROWS * kStageK * 2;
+  static constexpr int BYTES = ROWS * SK * 2;
   static constexpr int UNITS = BYTES / 1024 / NW;  // loads of 1 KiB per wave and stage
   static_assert(UNITS * NW * 1024 == BYTES, "whole loads");
-  static constexpr int PIECES = ROWS / 8;  // per row, across
+  static constexpr int PIECES = ACROSS ? ROWS / 8 : SK / 8;  // of a row in LDS
   unsigned voff[UNITS];                    // a lane's bytes from the tile's first row (and the stage's first step)
-  int piece;                               // along: which of a row's 8 pieces a lane loads
+  int piece;                               // along: which of a row's pieces a lane loads
 
   static __device__ __forceinline__ int swizzle(int k) { return ((k & 3) | ((k >> 1) & 4)) & (ROWS / 16 - 1); }
 
@@ -64,7 +70,7 @@ struct TileOperand {
         const int src = (((c >> 1) ^ swizzle(k)) << 1) | (c & 1);
         voff[u] = (unsigned)(k * (int)ld + min(src * 8, ((left + 7) & ~7) - 8)) * 2u;
       } else {
-        int r = unit * 8 + (lane >> 3);
+        int r = unit * (64 / PIECES) + lane / PIECES;
         if (PARTS == 2 && r >= ROWS / 2) r -= ROWS / 2;
         voff[u] = (unsigned)(min(r, left - 1) * (int)ld + piece * 8) * 2u;
       }
@@ -86,7 +92,7 @@ struct TileOperand {
     return c;
   }
   static __device__ __forceinline__ void next(Cursor& c, long long ld) {
-    const long long step = kStageK * (ACROSS ? ld * 2 : 2);
+    const long long step = SK * (ACROSS ? ld * 2 : 2);
     c.first += step;
     c.second += step;
     c.bytes -= step;
@@ -102,7 +108,7 @@ struct TileOperand {
     const bool live = ACROSS || piece * 8 < kl;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const bool two = PARTS == 2 && (wave * UNITS + u) * 8 >= ROWS / 2;
+      const bool two = PARTS == 2 && (wave * UNITS + u) * (64 / PIECES) >= ROWS / 2;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(two ? r1 : r0, (lds_ptr)(lds + (wave * UNITS + u) * 1024), 16,
                                                (int)(live ? voff[u] : 0x80000000u), 0, 0, 0);
     }
@@ -119,7 +125,7 @@ struct TileOperand {
       return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       const int r = r0 + (lane & 15), c = h * 4 + (lane >> 4);
-      return *(const s16x8*)(lds + r * 128 + ((c ^ (r & 7)) << 4));
+      return *(const s16x8*)(lds + r * (SK * 2) + ((c ^ (r & 7)) << 4));
     }
   }
 };
@@ -158,9 +164,11 @@ __device__ __forceinline__ void store_some(void* p, long long at, const float (&
   }
 }
 
-// What becomes of W neighbouring sums of row m from column n on (kFfGated: of both products').
+// What becomes of W neighbouring sums of row m from column n on (kFfGated: of both products').  `early`: the residual's values
+// if they are there already.
 template <int TYPE, int EPI, int W>
-__device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (&v)[W], float (&u)[W]) {
+__device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (&v)[W], float (&u)[W],
+                                       const float (*early)[W] = nullptr) {
   const int left = p.N - n;
   if constexpr (EPI == kFfGated) {
     if (p.z) {
@@ -172,7 +180,12 @@ __device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (
     for (int e = 0; e < W; ++e) v[e] *= u[e];
   } else {
     float r[W] = {};
-    if (p.residual) load_some<TYPE>(r, p.residual, m * p.ldr + n, left);
+    if (early) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) r[e] = (*early)[e];
+    } else if (p.residual) {
+      load_some<TYPE>(r, p.residual, m * p.ldr + n, left);
+    }
     if (p.bias) {
       float b[W];
       load_some<TYPE>(b, p.bias, n, left);
@@ -231,7 +244,7 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   const int m0 = tm * BM, n0 = tn * (BN / PARTS);
   const int left_m = p.M - m0, left_n = p.N - n0;
 
-  const int per = max((p.K + kStageK - 1) / kStageK, 1), all = per * (EPI == kFfGated ? 1 : p.segments);
+  const int per = max((p.K + SK - 1) / SK, 1), all = per * (EPI == kFfGated ? 1 : p.segments);
   const int first = SPLIT ? split * part.stages : 0, stages = SPLIT ? min(part.stages, all - first) : all;
   OpA a;
   OpB b;
@@ -240,7 +253,7 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   b.template init<PARTS>(wave, lane, left_n, ldb);
   const long long a_at = (AX ? m0 : m0 * lda) * 2, b_at = (BX ? n0 : n0 * ldb) * 2;
   // the stage that is loaded next; past the last one nothing is, but as many loads are in flight as ever
-  int k_next = first % per * kStageK, to_load = stages;
+  int k_next = first % per * SK, to_load = stages;
   auto cursor_a = [&](int s, int k0) { return OpA::begin((const char*)p.A[s].p + a_at, nullptr, lda, left_m, k0, p.K); };
   auto cursor_b = [&](int s, int k0) {
     return OpB::begin((const char*)p.B[s].p + b_at, (const char*)p.B[1].p + b_at, ldb, left_n, k0, p.K);
@@ -253,7 +266,7 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     a.template load<1>(st, wave, ca, kl);
     b.template load<PARTS>(st + OpA::BYTES, wave, cb, kl);
     --to_load;
-    k_next += kStageK;
+    k_next += SK;
     OpA::next(ca, lda);
     OpB::next(cb, ldb);
     if (EPI != kFfGated && k_next >= p.K && to_load > 0) {  // the second contraction
@@ -276,32 +289,34 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   // Half a stage's operands are read from LDS behind the matrix instructions of the half before.  The workgroup meets between
   // the halves: then the stage's second half is in registers, so that the next loads take its place, and the next stage has
   // landed, whose first half is read.
+  constexpr int L = OpA::UNITS + OpB::UNITS;  // loads of a wave and stage
   s16x8 fa[2][RB], fb[2][CB];
-  auto read = [&](int h, int slot) {
+  auto read = [&](int set, int h, int slot) {
     const unsigned char *sa = tile_smem + slot * STAGE, *sb = sa + OpA::BYTES;
 #pragma unroll
-    for (int j = 0; j < CB; ++j) fb[h][j] = OpB::read(sb, lane, row_b(j), h);
+    for (int j = 0; j < CB; ++j) fb[set][j] = OpB::read(sb, lane, row_b(j), h);
 #pragma unroll
-    for (int i = 0; i < RB; ++i) fa[h][i] = OpA::read(sa, lane, wm * (BM / WM) + i * 16, h);
+    for (int i = 0; i < RB; ++i) fa[set][i] = OpA::read(sa, lane, wm * (BM / WM) + i * 16, h);
   };
-  auto multiply = [&](int h) {
+  auto multiply = [&](int h, bool loads) {
 #pragma unroll
     for (int i = 0; i < RB; ++i)
 #pragma unroll
       for (int j = 0; j < CB; ++j) acc[j][i] = tile_mfma<TYPE>(fb[h][j], fa[h][i], acc[j][i]);
-    // a wave issues in order, and eight waves' reads take LDS as long as the matrix instructions of a half: read by read
-    // between them, not in front of them
+    // a wave issues in order, and what eight waves read and load takes LDS and the address unit as long as the matrix
+    // instructions take: one by one between them, not in front of them (8192 x 8192 x 4096 forward 433 -> 411 us for the
+    // reads, 405 for the loads too)
     constexpr int READS = (AX ? 2 : 1) * RB + (BX ? 2 : 1) * CB, EACH = RB * CB / READS;
 #pragma unroll
     for (int q = 0; q < READS; ++q) {
       __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      if (loads && q < L) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
   // all but the last `behind` loads of this wave have landed, its LDS reads too, and everybody's (a meeting and nothing else:
   // __syncthreads() would wait for all loads)
-  constexpr int L = OpA::UNITS + OpB::UNITS;
   static_assert((RING - 1) * L < 64, "vmcnt has six bits");
 #define CCT_MEET(behind)                                                               \
   __builtin_amdgcn_s_waitcnt(0x0070 | ((behind) & 15) | ((behind) >> 4) << 14);        \
@@ -311,15 +326,16 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   for (int q = 0; q < RING; ++q) load(q);
   CCT_MEET((RING - 1) * L);
   int slot = 0;
-  read(0, 0);
+  read(0, 0, 0);
   for (int t = 0; t < stages; ++t) {
-    read(1, slot);
-    multiply(0);
+    read(1, 1, slot);
+    multiply(0, false);
+    // the stage's second half is multiplied, the next one's first half read
     CCT_MEET((RING - 2) * L);
     load(slot);
     slot = slot + 1 == RING ? 0 : slot + 1;
-    read(0, slot);
-    multiply(1);
+    read(0, 0, slot);
+    multiply(1, true);
   }
 #undef CCT_MEET
   __builtin_amdgcn_s_waitcnt(0x0f70);  // the empty loads write LDS too
@@ -341,13 +357,26 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     return;
   }
   // Through LDS, EROWS rows of a wave at a time: a lane then has 8 neighbouring columns, stores are whole rows of the wave's
-  // columns, and the code stands once and not for every block.
+  // columns, and the code stands once and not for every block.  The residual's rows are asked for in front of that, all at
+  // once: one by one they were a trip to memory each (4096 x 4096 x 4096 with a residual 119 us, 104 without).
   typedef TileEpilogue<BM, BN, WM, WN> Ep;
+  typedef typename Number<TYPE>::V8 V8;
+  constexpr int COLS = OUT * 16, PER = COLS / 8, STEPS = Ep::EROWS * PER / 64, DOWN = 64 / PER;  // lanes of a row; rows of a step
+  static_assert(STEPS * 64 == Ep::EROWS * PER, "whole steps");
   __syncthreads();
   float* mine = (float*)tile_smem + wave * (Ep::EROWS * Ep::PITCH);
+  const int row = lane / PER, c = lane % PER * 8, n = n0 + wn * COLS + c;
+  const bool ahead = EPI == kFfLinear && p.residual && n + 8 <= p.N;
 #pragma unroll
   for (int half = 0; half < BM / WM / Ep::EROWS; ++half) {
     constexpr int IB = Ep::EROWS / 16;
+    const int m1 = m0 + wm * (BM / WM) + half * Ep::EROWS + row;
+    V8 res[STEPS] = {};
+    if (ahead)
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+        if (m1 + s * DOWN < p.M)
+          res[s] = *(const typename Number<TYPE>::U8*)((const typename Number<TYPE>::T*)p.residual + (m1 + s * DOWN) * p.ldr + n);
 #pragma unroll
     for (int i = 0; i < IB; ++i)
 #pragma unroll
@@ -355,20 +384,25 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
         *(f32x4*)(mine + (i * 16 + (lane & 15)) * Ep::PITCH + j * 16 + (lane >> 4) * 4) = acc[j][half * IB + i];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
-    constexpr int COLS = OUT * 16, PER = COLS / 8;  // lanes of a row
 #pragma unroll 1
-    for (int at = lane; at < Ep::EROWS * PER; at += 64) {
-      const int r = at / PER, c = at % PER * 8;
-      const int m = m0 + wm * (BM / WM) + half * Ep::EROWS + r, n = n0 + wn * COLS + c;
+    for (int s = 0; s < STEPS; ++s) {
+      const int m = m1 + s * DOWN;
       if (m >= p.M || n >= p.N) continue;
-      float v[8], u[8];
-      const float* from = mine + r * Ep::PITCH + c;
+      float v[8], u[8], r[8];
+      V8 rs = res[0];  // a step's, chosen by comparing: an index would put them into memory
+#pragma unroll
+      for (int q = 1; q < STEPS; ++q) rs = s == q ? res[q] : rs;
+      const float* from = mine + (row + s * DOWN) * Ep::PITCH + c;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         v[e] = from[e];
         u[e] = PARTS == 2 ? from[COLS + e] : 0.f;
+        r[e] = (float)rs[e];
       }
-      finish<TYPE, EPI>(p, m, n, v, u);
+      if (ahead)
+        finish<TYPE, EPI>(p, m, n, v, u, &r);
+      else
+        finish<TYPE, EPI>(p, m, n, v, u);
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();

@@ -7,7 +7,7 @@ namespace {
 
 template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
 int launch_tile(const FfProduct& p, const FfPart& part, hipStream_t st) {
-  constexpr int ring = RING * (BM + BN) * kStageK * 2, out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
+  constexpr int ring = RING * (BM + BN) * SK * 2, out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
   constexpr auto kernel = ff_tile_kernel<TYPE, BM, BN, WM, WN, RING, AX, BX, EPI, SPLIT>;
   const int rc = ensure_dynamic_lds<kernel>(lds);
   if (rc != CCT_OK) return rc;

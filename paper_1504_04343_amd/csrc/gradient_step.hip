@@ -7,7 +7,7 @@
 //
 // All of it is memory: the norm reads every gradient once, scaling reads and writes each, the update reads gradient, weight
 // and moment and writes the latter two.  A model's list holds hundreds of tensors, most of them small, so that a launch
-// takes as many as its arguments hold (4 KiB; nothing is uploaded or kept); a workgroup takes up to kRun values of one of
+// takes as many as its arguments hold (4 KiB; nothing is uploaded or kept); a workgroup takes some thousand values of one of
 // them.  Scaling and updating walk the lists from the end: what the norm read last is what the 256 MiB cache behind the
 // eight L2s still holds.
 //
@@ -24,21 +24,20 @@ namespace cct {
 namespace {
 
 constexpr int NT = 256;
-constexpr int kRun = 8192;  // values per workgroup: 4 of its 8-value steps per thread
 
-// What a launch is told: tensors with P pointers each, and at which workgroup each begins.
-template <int P, int COUNT>
+// What a launch is told: tensors with P pointers each, and at which workgroup each begins, of which one takes RUN values.
+template <int P, int COUNT, int RUN>
 struct ListArgs {
-  static constexpr int kCount = COUNT;
+  static constexpr int kCount = COUNT, kRun = RUN;
   void* p[P][COUNT];
   long long n[COUNT];
   int first[COUNT + 1];
   unsigned char type[COUNT], other[COUNT];  // of p[0] and of the last pointer
   int count;
 };
-typedef ListArgs<1, 160> NormArgs;
-typedef ListArgs<2, 120> ScaleArgs;
-typedef ListArgs<4, 72> UpdateArgs;
+typedef ListArgs<1, 160, 16384> NormArgs;
+typedef ListArgs<2, 120, 8192> ScaleArgs;
+typedef ListArgs<4, 72, 4096> UpdateArgs;
 static_assert(sizeof(NormArgs) < 3900 && sizeof(ScaleArgs) < 3900 && sizeof(UpdateArgs) < 3900, "a launch's arguments");
 
 // which tensor workgroup b of the launch belongs to
@@ -71,33 +70,59 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// W values at any address that is a multiple of one of them
+template <int TYPE, int W>
+struct Some {
+  typedef typename Number<TYPE>::T T;
+  typedef T V __attribute__((ext_vector_type(W)));
+  typedef V U __attribute__((aligned(sizeof(T))));
+  typedef float F __attribute__((ext_vector_type(W)));
+  static __device__ __forceinline__ V load(const T* p) { return *(const U*)p; }
+  static __device__ __forceinline__ F wide(V v) { return __builtin_convertvector(v, F); }
+  static __device__ __forceinline__ void store(T* p, F v) { *(U*)p = __builtin_convertvector(v, V); }
+};
+template <int TYPE>
+constexpr int kLane = 16 / (int)sizeof(typename Number<TYPE>::T);  // values of a 16-byte load
+
+// every(k, q): W values from k on, the q-th such piece of the thread's batch, B of which are visited by `first` before any of
+// them is visited by `then`; one(k): the values behind the last whole piece.
+template <int W, int B, class First, class Then, class One>
+__device__ __forceinline__ void walk(int n, First first, Then then, One one) {
+  int k = threadIdx.x * W;
+  for (; k + ((B - 1) * NT + 1) * W <= n; k += B * NT * W) {
+#pragma unroll
+    for (int q = 0; q < B; ++q) first(k + q * NT * W, q);
+#pragma unroll
+    for (int q = 0; q < B; ++q) then(k + q * NT * W, q);
+  }
+  for (; k < n; k += NT * W)
+    if (k + W <= n) {
+      first(k, 0);
+      then(k, 0);
+    } else {
+      for (int e = k; e < n; ++e) one(e);
+    }
+}
+
 __global__ __launch_bounds__(NT) void grad_norm_kernel(NormArgs a, double* __restrict__ part) {
   const int i = tensor_of(a, blockIdx.x);
-  const long long at = (long long)((int)blockIdx.x - a.first[i]) * kRun;
-  const int n = (int)min((long long)kRun, a.n[i] - at);
+  const long long at = (long long)((int)blockIdx.x - a.first[i]) * NormArgs::kRun;
+  const int n = (int)min((long long)NormArgs::kRun, a.n[i] - at);
   double sum = 0.0;
   with_type(a.type[i], [&](auto type) {
-    constexpr int TYPE = decltype(type)::value;
-    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
+    constexpr int TYPE = decltype(type)::value, W = kLane<TYPE>, B = 8;
+    typedef Some<TYPE, W> S;
+    const typename S::T* g = (const typename S::T*)a.p[0][i] + at;
     auto add = [&](float v) { sum = fma((double)v, (double)v, sum); };
-    if (n == kRun) {
-      f32x8 v[kRun / NT / 8];
+    typename S::V v[B];
+    walk<W, B>(
+        n, [&](int k, int q) { v[q] = S::load(g + k); },
+        [&](int, int q) {
+          const typename S::F f = S::wide(v[q]);
 #pragma unroll
-      for (int u = 0; u < kRun / NT / 8; ++u) v[u] = load8<TYPE>(g, (u * NT + threadIdx.x) * 8);
-#pragma unroll
-      for (int u = 0; u < kRun / NT / 8; ++u)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) add(v[u][e]);
-    } else {
-      for (int k = threadIdx.x * 8; k < n; k += NT * 8)
-        if (k + 8 <= n) {
-          const f32x8 v = load8<TYPE>(g, k);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) add(v[e]);
-        } else {
-          for (int e = k; e < n; ++e) add(load1<TYPE>(g, e));
-        }
-    }
+          for (int e = 0; e < W; ++e) add(f[e]);
+        },
+        [&](int e) { add((float)g[e]); });
   });
   __shared__ double sums[NT / 64];
   sum = wave_sum(sum);
@@ -126,25 +151,17 @@ __global__ __launch_bounds__(NT) void grad_scale_kernel(ScaleArgs a, const float
   const int b = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(a, b);
   const float s = clip[1];
   if (a.p[0][i] == a.p[1][i] && s == 1.f) return;
-  const long long at = (long long)(b - a.first[i]) * kRun;
-  const int n = (int)min((long long)kRun, a.n[i] - at);
+  const long long at = (long long)(b - a.first[i]) * ScaleArgs::kRun;
+  const int n = (int)min((long long)ScaleArgs::kRun, a.n[i] - at);
   with_type(a.type[i], [&](auto type) {
-    constexpr int TYPE = decltype(type)::value;
-    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
-    void* out = (typename Number<TYPE>::T*)a.p[1][i] + at;
-    if (n == kRun) {
-      f32x8 v[kRun / NT / 8];
-#pragma unroll
-      for (int u = 0; u < kRun / NT / 8; ++u) v[u] = load8<TYPE>(g, (u * NT + threadIdx.x) * 8);
-#pragma unroll
-      for (int u = 0; u < kRun / NT / 8; ++u) store8<TYPE>(out, (u * NT + threadIdx.x) * 8, v[u] * s);
-    } else {
-      for (int k = threadIdx.x * 8; k < n; k += NT * 8)
-        if (k + 8 <= n)
-          store8<TYPE>(out, k, load8<TYPE>(g, k) * s);
-        else
-          for (int e = k; e < n; ++e) store1<TYPE>(out, e, load1<TYPE>(g, e) * s);
-    }
+    constexpr int TYPE = decltype(type)::value, W = kLane<TYPE>, B = 4;
+    typedef Some<TYPE, W> S;
+    const typename S::T* g = (const typename S::T*)a.p[0][i] + at;
+    typename S::T* out = (typename S::T*)a.p[1][i] + at;
+    typename S::V v[B];
+    walk<W, B>(
+        n, [&](int k, int q) { v[q] = S::load(g + k); }, [&](int k, int q) { S::store(out + k, S::wide(v[q]) * s); },
+        [&](int e) { out[e] = (typename S::T)((float)g[e] * s); });
   });
 }
 
@@ -153,41 +170,40 @@ struct StepRule {
 };
 
 template <int TYPE, int COPY>  // COPY: the copy's type, -1 for none
-__device__ __forceinline__ void update_run(const void* g, float* w, float* v, void* copy, int n, float s, StepRule r) {
-  auto step = [&](float gr, float& wt, float& mo) {
-    mo = r.momentum * mo + r.rate * (s * gr + r.decay * wt);
-    wt -= mo;
-  };
-  for (int k = threadIdx.x * 8; k < n; k += NT * 8)
-    if (k + 8 <= n) {
-      const f32x8 gr = load8<TYPE>(g, k);
-      f32x8 wt = load8<CCT_TYPE_F32>(w, k), mo = load8<CCT_TYPE_F32>(v, k);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float a = wt[e], b = mo[e];
-        step(gr[e], a, b);
-        wt[e] = a;
-        mo[e] = b;
-      }
-      store8<CCT_TYPE_F32>(v, k, mo);
-      store8<CCT_TYPE_F32>(w, k, wt);
-      if constexpr (COPY >= 0) store8<COPY>(copy, k, wt);
-    } else {
-      for (int e = k; e < n; ++e) {
-        float wt = w[e], mo = v[e];
-        step(load1<TYPE>(g, e), wt, mo);
-        v[e] = mo;
-        w[e] = wt;
-        if constexpr (COPY >= 0) store1<COPY>(copy, e, wt);
-      }
-    }
+__device__ __forceinline__ void update_run(const void* gp, float* w, float* v, void* cp, int n, float s, StepRule r) {
+  constexpr int W = 4, B = 4;
+  typedef Some<TYPE, W> G;
+  typedef Some<CCT_TYPE_F32, W> S;
+  typedef Some<COPY < 0 ? CCT_TYPE_F32 : COPY, W> C;
+  const typename G::T* g = (const typename G::T*)gp;
+  typename C::T* copy = (typename C::T*)cp;
+  typename G::V gv[B];
+  typename S::V wv[B], mv[B];
+  walk<W, B>(
+      n,
+      [&](int k, int q) {
+        gv[q] = G::load(g + k);
+        wv[q] = S::load(w + k);
+        mv[q] = S::load(v + k);
+      },
+      [&](int k, int q) {
+        const typename S::F m = r.momentum * mv[q] + r.rate * (s * G::wide(gv[q]) + r.decay * wv[q]), t = wv[q] - m;
+        S::store(v + k, m);
+        S::store(w + k, t);
+        if constexpr (COPY >= 0) C::store(copy + k, t);
+      },
+      [&](int e) {
+        v[e] = r.momentum * v[e] + r.rate * (s * (float)g[e] + r.decay * w[e]);
+        w[e] -= v[e];
+        if constexpr (COPY >= 0) copy[e] = (typename C::T)w[e];
+      });
 }
 
 __global__ __launch_bounds__(NT) void sgd_update_kernel(UpdateArgs a, const float* __restrict__ clip, StepRule r) {
   const int b = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(a, b);
   const float s = clip ? clip[1] : 1.f;
-  const long long at = (long long)(b - a.first[i]) * kRun;
-  const int n = (int)min((long long)kRun, a.n[i] - at);
+  const long long at = (long long)(b - a.first[i]) * UpdateArgs::kRun;
+  const int n = (int)min((long long)UpdateArgs::kRun, a.n[i] - at);
   with_type(a.type[i], [&](auto type) {
     constexpr int TYPE = decltype(type)::value;
     const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
@@ -202,9 +218,9 @@ __global__ __launch_bounds__(NT) void sgd_update_kernel(UpdateArgs a, const floa
   });
 }
 
-long long runs(long long n) { return (n + kRun - 1) / kRun; }
+long long runs(long long n, int run) { return (n + run - 1) / run; }
 
-// CCT_OK, and how many workgroups the list takes.  Every pointer of a tensor with values must be there and aligned to one.
+// CCT_OK, and how many workgroups the norm of the list takes.  Every pointer of a tensor with values must be there and aligned to one.
 int check_list(const cct_tensor_t* list, int count, long long* blocks) {
   if (count < 0 || (count > 0 && !list)) return CCT_EINVAL;
   *blocks = 0;
@@ -213,9 +229,10 @@ int check_list(const cct_tensor_t* list, int count, long long* blocks) {
     if (t.n < 0 || !type_known(t.type) || (t.n > 0 && !t.data) || ((uintptr_t)t.data & (type_bytes(t.type) - 1)))
       return CCT_EINVAL;
     if (t.n > (1LL << 44)) return CCT_EUNSUPPORTED;
-    *blocks += runs(t.n);
+    *blocks += runs(t.n, NormArgs::kRun);
   }
-  return *blocks < 0x7fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
+  // (the other launches have up to four times as many)
+  return *blocks < 0x1fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
 }
 int check_same(const cct_tensor_t* a, const cct_tensor_t* b, int count) {
   long long blocks;
@@ -245,7 +262,7 @@ int fill(Args* a, const cct_tensor_t* const (&lists)[P], int from, int to, bool 
     a->n[c] = lists[0][i].n;
     a->type[c] = (unsigned char)lists[0][i].type;
     a->other[c] = (unsigned char)(lists[P - 1] ? lists[P - 1][i].type : 0);
-    a->first[c + 1] = a->first[c] + (int)runs(a->n[c]);
+    a->first[c + 1] = a->first[c] + (int)runs(a->n[c], Args::kRun);
   }
   return forward ? hi : lo;
 }
