@@ -4,8 +4,13 @@
 // A workgroup takes 16 rows of the weight (gated: of both) and all rows of x, its eight waves every eighth step of the
 // contraction: 64 bytes of each weight row, which go from memory straight into the registers that the matrix cores take (32
 // values of 16 bits per instruction, 4 of fp32 in an order of their own that x follows).  No LDS and no meeting in the loop;
-// two batches of loads are in flight per wave, and x comes from L2 the same way.  The waves' sums meet in LDS in a fixed
+// eight steps' loads are in flight per wave, and x comes from L2 the same way.  The waves' sums meet in LDS in a fixed
 // order.  fp32 runs on v_mfma_f32_16x16x4_f32, which memory outlasts.
+//
+// One row, bf16, weights from memory: 4096 x 4096 7.9 us (4.3 TB/s; 6.8 at the rate of a large copy), 16384 x 4096 25.6 (5.2
+// TB/s), gated 2 x 8192 x 4096 27.0 (5.0).  With two batches of four steps in turn 9.0, 29.1 and 29.8: the compiler waits
+// for all of a batch before it loads the next one into the same registers, so that they are only smaller; with sixteen waves
+// 8.0, 26.8 and 26.8.
 //
 // Any alignment: gfx950 loads 16 bytes at any address.  A last step that is not whole is loaded value by value.
 #include <algorithm>
@@ -18,7 +23,6 @@ namespace cct {
 namespace {
 
 constexpr int kWaves = 8;
-constexpr int kBatch = 4;  // steps per batch of loads
 
 template <int TYPE>
 struct Step {  // 16-bit types
@@ -64,7 +68,7 @@ template <int TYPE, int RM, int EPI>
 __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
-  constexpr int NB = EPI == kFfGated ? 2 : 1;
+  constexpr int NB = EPI == kFfGated ? 2 : 1, BATCH = RM == 4 ? 4 : 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int n0 = blockIdx.x * 16, lo = lane & 15, kq = (lane >> 4) * S::CH;
   long long w_at = (long long)min(n0 + lo, p.N - 1) * p.B[0].rs, u_at = (long long)min(n0 + lo, p.N - 1) * p.B[NB - 1].rs, x_at[RM];
@@ -78,41 +82,34 @@ __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
     for (int i = 0; i < RM; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const int whole = p.K / S::K;  // steps
-  V w[2][kBatch][NB], x[2][kBatch][RM];
+  V w[BATCH][NB], x[BATCH][RM];
   // steps past the last one load it again and multiply zeros
-  auto load = [&](int set, int s0) {
+  auto load = [&](int s0) {
 #pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
+    for (int q = 0; q < BATCH; ++q) {
       const long long k = (long long)min(s0 + q * kWaves, whole - 1) * S::K + kq;
-      w[set][q][0] = S::load(p.B[0].p, w_at + k);
-      if constexpr (NB == 2) w[set][q][1] = S::load(p.B[1].p, u_at + k);
+      w[q][0] = S::load(p.B[0].p, w_at + k);
+      if constexpr (NB == 2) w[q][1] = S::load(p.B[1].p, u_at + k);
 #pragma unroll
-      for (int i = 0; i < RM; ++i) x[set][q][i] = S::load(p.A[0].p, x_at[i] + k);
+      for (int i = 0; i < RM; ++i) x[q][i] = S::load(p.A[0].p, x_at[i] + k);
     }
   };
-  auto multiply = [&](int set, int s0) {
+  auto multiply = [&](int s0) {
     __builtin_amdgcn_sched_barrier(0);  // the loads in front of it are not moved behind
 #pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
+    for (int q = 0; q < BATCH; ++q) {
       const bool live = s0 + q * kWaves < whole;
 #pragma unroll
       for (int i = 0; i < RM; ++i) {
-        const V xv = live ? x[set][q][i] : V{};
+        const V xv = live ? x[q][i] : V{};
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b][i] = S::mfma(live ? w[set][q][b] : V{}, xv, acc[b][i]);
+        for (int b = 0; b < NB; ++b) acc[b][i] = S::mfma(live ? w[q][b] : V{}, xv, acc[b][i]);
       }
     }
   };
-  constexpr int RUN = kBatch * kWaves;
-  if (wave < whole) {
-    load(0, wave);
-    for (int s = wave; s < whole; s += 2 * RUN) {
-      load(1, s + RUN);
-      multiply(0, s);
-      if (s + RUN >= whole) break;
-      load(0, s + 2 * RUN);
-      multiply(1, s + RUN);
-    }
+  for (int s = wave; s < whole; s += BATCH * kWaves) {
+    load(s);
+    multiply(s);
   }
   if (p.K % S::K && whole % kWaves == wave) {
     const int k = whole * S::K + kq, n = max(0, min(S::CH, p.K - k));

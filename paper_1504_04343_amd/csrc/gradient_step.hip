@@ -25,19 +25,23 @@ namespace {
 
 constexpr int NT = 256;
 
-// What a launch is told: tensors with P pointers each, and at which workgroup each begins, of which one takes RUN values.
+// What a launch is told: tensors with P pointers each, at which workgroup each begins, of which one takes RUN values, and how
+// many values its last one takes.  Small, so that few launches do: what a tensor is follows from 6 bytes besides its pointers
+// (400 tensors: two launches for the norm, three for scaling, four for the update; with 64-bit counts 3, 4 and 6, each of
+// which costs 3 to 4 us before it streams).
 template <int P, int COUNT, int RUN>
 struct ListArgs {
   static constexpr int kCount = COUNT, kRun = RUN;
+  static_assert(RUN <= 8192, "13 bits; 12 where there is a second type");
   void* p[P][COUNT];
-  long long n[COUNT];
   int first[COUNT + 1];
-  unsigned char type[COUNT], other[COUNT];  // of p[0] and of the last pointer
+  unsigned short tail[COUNT];  // values of the last workgroup - 1, above three bits (RUN up to 4096: four) that hold p[0]'s
+                               // type and, from bit 2 on, the copy's
   int count;
 };
-typedef ListArgs<1, 160, 16384> NormArgs;
-typedef ListArgs<2, 120, 8192> ScaleArgs;
-typedef ListArgs<4, 72, 4096> UpdateArgs;
+typedef ListArgs<1, 270, 8192> NormArgs;
+typedef ListArgs<2, 172, 8192> ScaleArgs;
+typedef ListArgs<4, 100, 4096> UpdateArgs;
 static_assert(sizeof(NormArgs) < 3900 && sizeof(ScaleArgs) < 3900 && sizeof(UpdateArgs) < 3900, "a launch's arguments");
 
 // which tensor workgroup b of the launch belongs to
@@ -52,6 +56,23 @@ __device__ __forceinline__ int tensor_of(const Args& a, int b) {
       hi = mid - 1;
   }
   return lo;
+}
+
+// A workgroup's part of the list: tensor, its types, the first value and the number of them.
+struct Run {
+  int tensor, type, other, n;
+  long long at;
+};
+template <class Args>
+__device__ __forceinline__ Run run_of(const Args& a, int b) {
+  Run r;
+  r.tensor = tensor_of(a, b);
+  const int k = b - a.first[r.tensor], tail = a.tail[r.tensor];
+  r.type = tail & 3;
+  r.other = tail >> 2 & 3;
+  r.at = (long long)k * Args::kRun;
+  r.n = b + 1 == a.first[r.tensor + 1] ? (Args::kRun > 4096 ? tail >> 3 : tail >> 4) + 1 : Args::kRun;
+  return r;
 }
 
 template <class F>
@@ -105,25 +126,24 @@ __device__ __forceinline__ void walk(int n, First first, Then then, One one) {
 }
 
 __global__ __launch_bounds__(NT) void grad_norm_kernel(NormArgs a, double* __restrict__ part) {
-  const int i = tensor_of(a, blockIdx.x);
-  const long long at = (long long)((int)blockIdx.x - a.first[i]) * NormArgs::kRun;
-  const int n = (int)min((long long)NormArgs::kRun, a.n[i] - at);
-  double sum = 0.0;
-  with_type(a.type[i], [&](auto type) {
-    constexpr int TYPE = decltype(type)::value, W = kLane<TYPE>, B = 8;
+  const Run r = run_of(a, blockIdx.x);
+  double part_sum[4] = {};  // four chains: one waits for itself
+  with_type(r.type, [&](auto type) {
+    constexpr int TYPE = decltype(type)::value, W = kLane<TYPE>, B = 4;
     typedef Some<TYPE, W> S;
-    const typename S::T* g = (const typename S::T*)a.p[0][i] + at;
-    auto add = [&](float v) { sum = fma((double)v, (double)v, sum); };
+    const typename S::T* g = (const typename S::T*)a.p[0][r.tensor] + r.at;
+    auto add = [&](float v, int e) { part_sum[e & 3] = fma((double)v, (double)v, part_sum[e & 3]); };
     typename S::V v[B];
     walk<W, B>(
-        n, [&](int k, int q) { v[q] = S::load(g + k); },
+        r.n, [&](int k, int q) { v[q] = S::load(g + k); },
         [&](int, int q) {
           const typename S::F f = S::wide(v[q]);
 #pragma unroll
-          for (int e = 0; e < W; ++e) add(f[e]);
+          for (int e = 0; e < W; ++e) add(f[e], e);
         },
-        [&](int e) { add((float)g[e]); });
+        [&](int e) { add((float)g[e], 0); });
   });
+  double sum = (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
   __shared__ double sums[NT / 64];
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
@@ -148,19 +168,17 @@ __global__ __launch_bounds__(kFinalThreads) void grad_norm_final_kernel(const do
 }
 
 __global__ __launch_bounds__(NT) void grad_scale_kernel(ScaleArgs a, const float* __restrict__ clip) {
-  const int b = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(a, b);
+  const Run r = run_of(a, (int)(gridDim.x - 1 - blockIdx.x));
   const float s = clip[1];
-  if (a.p[0][i] == a.p[1][i] && s == 1.f) return;
-  const long long at = (long long)(b - a.first[i]) * ScaleArgs::kRun;
-  const int n = (int)min((long long)ScaleArgs::kRun, a.n[i] - at);
-  with_type(a.type[i], [&](auto type) {
+  if (a.p[0][r.tensor] == a.p[1][r.tensor] && s == 1.f) return;
+  with_type(r.type, [&](auto type) {
     constexpr int TYPE = decltype(type)::value, W = kLane<TYPE>, B = 4;
     typedef Some<TYPE, W> S;
-    const typename S::T* g = (const typename S::T*)a.p[0][i] + at;
-    typename S::T* out = (typename S::T*)a.p[1][i] + at;
+    const typename S::T* g = (const typename S::T*)a.p[0][r.tensor] + r.at;
+    typename S::T* out = (typename S::T*)a.p[1][r.tensor] + r.at;
     typename S::V v[B];
     walk<W, B>(
-        n, [&](int k, int q) { v[q] = S::load(g + k); }, [&](int k, int q) { S::store(out + k, S::wide(v[q]) * s); },
+        r.n, [&](int k, int q) { v[q] = S::load(g + k); }, [&](int k, int q) { S::store(out + k, S::wide(v[q]) * s); },
         [&](int e) { out[e] = (typename S::T)((float)g[e] * s); });
   });
 }
@@ -199,21 +217,20 @@ __device__ __forceinline__ void update_run(const void* gp, float* w, float* v, v
       });
 }
 
-__global__ __launch_bounds__(NT) void sgd_update_kernel(UpdateArgs a, const float* __restrict__ clip, StepRule r) {
-  const int b = (int)(gridDim.x - 1 - blockIdx.x), i = tensor_of(a, b);
+__global__ __launch_bounds__(NT) void sgd_update_kernel(UpdateArgs a, const float* __restrict__ clip, StepRule rule) {
+  const Run r = run_of(a, (int)(gridDim.x - 1 - blockIdx.x));
   const float s = clip ? clip[1] : 1.f;
-  const long long at = (long long)(b - a.first[i]) * UpdateArgs::kRun;
-  const int n = (int)min((long long)UpdateArgs::kRun, a.n[i] - at);
-  with_type(a.type[i], [&](auto type) {
+  const int i = r.tensor;
+  with_type(r.type, [&](auto type) {
     constexpr int TYPE = decltype(type)::value;
-    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + at;
-    float *w = (float*)a.p[1][i] + at, *v = (float*)a.p[2][i] + at;
+    const void* g = (const typename Number<TYPE>::T*)a.p[0][i] + r.at;
+    float *w = (float*)a.p[1][i] + r.at, *v = (float*)a.p[2][i] + r.at;
     if (!a.p[3][i])
-      update_run<TYPE, -1>(g, w, v, nullptr, n, s, r);
+      update_run<TYPE, -1>(g, w, v, nullptr, r.n, s, rule);
     else
-      with_type(a.other[i], [&](auto other) {
+      with_type(r.other, [&](auto other) {
         constexpr int COPY = decltype(other)::value;
-        update_run<TYPE, COPY>(g, w, v, (typename Number<COPY>::T*)a.p[3][i] + at, n, s, r);
+        update_run<TYPE, COPY>(g, w, v, (typename Number<COPY>::T*)a.p[3][i] + r.at, r.n, s, rule);
       });
   });
 }
@@ -231,8 +248,8 @@ int check_list(const cct_tensor_t* list, int count, long long* blocks) {
     if (t.n > (1LL << 44)) return CCT_EUNSUPPORTED;
     *blocks += runs(t.n, NormArgs::kRun);
   }
-  // (the other launches have up to four times as many)
-  return *blocks < 0x1fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
+  // (the update has twice as many)
+  return *blocks < 0x3fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
 }
 int check_same(const cct_tensor_t* a, const cct_tensor_t* b, int count) {
   long long blocks;
@@ -244,9 +261,10 @@ int check_same(const cct_tensor_t* a, const cct_tensor_t* b, int count) {
 }
 
 // Tensors [from, to) of the lists as one launch's arguments; returns the first tensor left out.  `forward`: from `from` up,
-// else from `to` down.
+// else from `to` down.  *values, *bytes: of the gradients (and copies).
 template <class Args, int P>
-int fill(Args* a, const cct_tensor_t* const (&lists)[P], int from, int to, bool forward) {
+int fill(Args* a, const cct_tensor_t* const (&lists)[P], int from, int to, bool forward, double* values, double* bytes) {
+  *values = *bytes = 0.0;
   int lo = forward ? from : to, hi = lo, held = 0;
   auto take = [&](int i) { return lists[0][i].n == 0 || ++held <= Args::kCount; };
   if (forward)
@@ -259,22 +277,14 @@ int fill(Args* a, const cct_tensor_t* const (&lists)[P], int from, int to, bool 
     if (lists[0][i].n == 0) continue;
     const int c = a->count++;
     for (int q = 0; q < P; ++q) a->p[q][c] = lists[q] ? lists[q][i].data : nullptr;
-    a->n[c] = lists[0][i].n;
-    a->type[c] = (unsigned char)lists[0][i].type;
-    a->other[c] = (unsigned char)(lists[P - 1] ? lists[P - 1][i].type : 0);
-    a->first[c + 1] = a->first[c] + (int)runs(a->n[c], Args::kRun);
+    const int blocks = (int)runs(lists[0][i].n, Args::kRun), last = (int)(lists[0][i].n - (blocks - 1LL) * Args::kRun) - 1;
+    const int copy = P == 4 && lists[P - 1] ? lists[P - 1][i].type : 0;
+    a->tail[c] = (unsigned short)(last << (Args::kRun > 4096 ? 3 : 4) | copy << 2 | lists[0][i].type);
+    a->first[c + 1] = a->first[c] + blocks;
+    *values += (double)lists[0][i].n;
+    *bytes += (double)lists[0][i].n * (type_bytes(lists[0][i].type) + (P == 4 && lists[P - 1] ? type_bytes(copy) : 0));
   }
   return forward ? hi : lo;
-}
-template <class Args>
-double list_values(const Args& a, double* g_bytes) {
-  double n = 0.0, by = 0.0;
-  for (int c = 0; c < a.count; ++c) {
-    n += (double)a.n[c];
-    by += (double)a.n[c] * type_bytes(a.type[c]);
-  }
-  *g_bytes = by;
-  return n;
 }
 
 }  // namespace
@@ -306,10 +316,9 @@ int cct_grad_norm(const cct_tensor_t* grads, int32_t count, float max_norm, floa
   const cct_tensor_t* const lists[1] = {grads};
   for (int at = 0; at < count;) {
     NormArgs a;
-    at = fill(&a, lists, at, count, true);
+    double n, by;
+    at = fill(&a, lists, at, count, true, &n, &by);
     if (a.count == 0) continue;
-    double by;
-    const double n = list_values(a, &by);
     ProfScope ps("grad_norm_kernel", 2.0 * n, by, st);
     hipLaunchKernelGGL(grad_norm_kernel, dim3(a.first[a.count]), dim3(NT), 0, st, a, part);
     CCT_CHECK_LAUNCH();
@@ -335,10 +344,9 @@ int cct_grad_scale(const cct_tensor_t* grads, int32_t count, const float* clip, 
   const cct_tensor_t* const lists[2] = {grads, out};
   for (int to = count; to > 0;) {
     ScaleArgs a;
-    to = fill(&a, lists, 0, to, false);
+    double n, by;
+    to = fill(&a, lists, 0, to, false, &n, &by);
     if (a.count == 0) continue;
-    double by;
-    const double n = list_values(a, &by);
     ProfScope ps("grad_scale_kernel", n, 2.0 * by, st);
     hipLaunchKernelGGL(grad_scale_kernel, dim3(a.first[a.count]), dim3(NT), 0, st, a, clip);
     CCT_CHECK_LAUNCH();
@@ -364,12 +372,9 @@ int cct_sgd_update(const cct_tensor_t* grads, int32_t count, const float* clip, 
   const StepRule r = {rate, momentum, decay};
   for (int to = count; to > 0;) {
     UpdateArgs a;
-    to = fill(&a, lists, 0, to, false);
+    double n, by;
+    to = fill(&a, lists, 0, to, false, &n, &by);
     if (a.count == 0) continue;
-    double by;
-    const double n = list_values(a, &by);
-    if (copies)
-      for (int c = 0; c < a.count; ++c) by += (double)a.n[c] * type_bytes(a.other[c]);
     ProfScope ps("sgd_update_kernel", 7.0 * n, by + 16.0 * n, st);
     hipLaunchKernelGGL(sgd_update_kernel, dim3(a.first[a.count]), dim3(NT), 0, st, a, clip, r);
     CCT_CHECK_LAUNCH();
