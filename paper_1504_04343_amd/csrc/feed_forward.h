@@ -76,7 +76,12 @@ struct FfDz {
   float* part;
 };
 int ff_sum_rows(int M, int N);
-int launch_ff_dz(const FfDz& p, hipStream_t st);
+// Up to three of them, independent of each other, in one launch (all of one type): dz next to copies of x and w.
+struct FfDzJobs {
+  FfDz job[3];
+  int count;
+};
+int launch_ff_dz(const FfDzJobs& p, hipStream_t st);
 // dg = dh * u * act'(g), du = dh * act(g), both with rows of ld values as dz above.
 struct FfGatedDz {
   int M, F, type, activation;

@@ -31,9 +31,11 @@ bool matrix_ok(const Matrix& m, long long rows, long long cols, int type) {
 }
 bool vector_ok(const void* p, int type) { return !((uintptr_t)p & (type_bytes(type) - 1)); }
 
-// Sizes up to which no product of two of them, a stride and a value's bytes passes 63 bits, and a launch's workgroups 31.
+// Sizes up to which no product of two of them, a stride and a value's bytes passes 63 bits, a size and a tile 31, and a
+// launch's workgroups 31.
 int dims_ok(int32_t M, int32_t N, int32_t K, int32_t type, int32_t activation) {
   if (M < 0 || N < 1 || K < 1 || !type_known(type) || !activation_known(activation)) return CCT_EINVAL;
+  if (std::max(M, std::max(N, K)) > 0x7fffff00) return CCT_EUNSUPPORTED;
   const long long tiles = up(M, 64) / 64 * (up(N, 64) / 64), back = up(std::max(N, K), 64) / 64 * (up(std::max(M, N), 64) / 64);
   return tiles < 0x7fffffffLL && back < 0x7fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
 }
@@ -104,27 +106,23 @@ bool few_rows(int M, int type, bool in_place) {
   return M <= kFfRows || (M <= (type == CCT_TYPE_F32 ? kFfRowsF32 : kFfRowsMost) && (type == CCT_TYPE_F32 || !in_place));
 }
 
-// The matrix itself, or its copy at `to` where the products do not take it in place.
-int operand(const Matrix& m, long long rows, long long cols, int type, void* to, Matrix* use, hipStream_t st) {
-  *use = {m.p, rows <= 1 ? up(cols, 8) : m.ld};
-  if (type == CCT_TYPE_F32 || rows == 0 || ff_in_place(use->p, use->ld, cols)) return CCT_OK;
+void add_copy(const Matrix& m, long long rows, long long cols, int type, void* to, Matrix* use, FfDzJobs* jobs) {
   *use = {to, up(cols, 8)};
-  return launch_ff_dz({(int)rows, (int)cols, type, CCT_ACT_NONE, m.p, nullptr, m.ld, 0, to, use->ld, nullptr, nullptr}, st);
+  jobs->job[jobs->count++] = {(int)rows, (int)cols, type, CCT_ACT_NONE, m.p, nullptr, m.ld, 0, to, use->ld, nullptr, nullptr};
+}
+// The matrix itself, or where its copy at `to` will be, added to the jobs, if the products do not take it in place.
+void operand(const Matrix& m, long long rows, long long cols, int type, void* to, Matrix* use, FfDzJobs* jobs) {
+  *use = {m.p, rows <= 1 ? up(cols, 8) : m.ld};
+  if (type != CCT_TYPE_F32 && rows > 0 && !ff_in_place(use->p, use->ld, cols)) add_copy(m, rows, cols, type, to, use, jobs);
 }
 // Two weights that one product takes must have the same strides.
-int weight_pair(const Matrix& g, const Matrix& u, long long rows, long long cols, int type, char* to_g, char* to_u, Matrix* use_g,
-                Matrix* use_u, hipStream_t st) {
-  int rc = operand(g, rows, cols, type, to_g, use_g, st);
-  if (rc == CCT_OK) rc = operand(u, rows, cols, type, to_u, use_u, st);
-  if (rc != CCT_OK || type == CCT_TYPE_F32 || use_g->ld == use_u->ld) return rc;
-  const long long ld = up(cols, 8);
-  auto copy = [&](const Matrix& m, void* to, Matrix* use) {
-    if (use->p == to) return (int)CCT_OK;
-    *use = {to, ld};
-    return launch_ff_dz({(int)rows, (int)cols, type, CCT_ACT_NONE, m.p, nullptr, m.ld, 0, to, ld, nullptr, nullptr}, st);
-  };
-  rc = copy(g, to_g, use_g);
-  return rc == CCT_OK ? copy(u, to_u, use_u) : rc;
+void weight_pair(const Matrix& g, const Matrix& u, long long rows, long long cols, int type, char* to_g, char* to_u, Matrix* use_g,
+                 Matrix* use_u, FfDzJobs* jobs) {
+  operand(g, rows, cols, type, to_g, use_g, jobs);
+  operand(u, rows, cols, type, to_u, use_u, jobs);
+  if (type == CCT_TYPE_F32 || use_g->ld == use_u->ld) return;
+  if (use_g->p != to_g) add_copy(g, rows, cols, type, to_g, use_g, jobs);
+  if (use_u->p != to_u) add_copy(u, rows, cols, type, to_u, use_u, jobs);
 }
 
 FfOperand rows_of(const Matrix& m) { return {m.p, m.ld, 1, 0}; }
@@ -189,9 +187,13 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
   char* ws = (char*)workspace;
   const bool few = few_rows(d.M, d.type, ff_in_place(w, d.N <= 1 ? up(d.K, 8) : ldw, d.K));
   Matrix mx = {x, ldx}, mw = {w, ldw};
-  if (!few) rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
-  if (!few && rc == CCT_OK) rc = operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, st);
-  if (rc != CCT_OK) return rc;
+  if (!few) {
+    FfDzJobs jobs = {};
+    operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
+    operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, &jobs);
+    rc = launch_ff_dz(jobs, st);
+    if (rc != CCT_OK) return rc;
+  }
   FfProduct p = plain_product(d.type, d.M, d.N, d.K, y, ldy);
   p.A[0] = rows_of(mx);
   p.B[0] = rows_of(mw);
@@ -225,17 +227,17 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
   char* ws = (char*)workspace;
   // dy itself is dz without an activation, where the products take it in place
   const bool copy = (dx || dw) && (act || (d.type != CCT_TYPE_F32 && !ff_in_place(dy, d.M <= 1 ? b.ld : lddy, d.N)));
-  if (copy || dbias) {
-    FfDz q = {d.M, d.N, d.type, d.activation, dy, act ? z : nullptr, lddy, ldz, copy ? ws + b.dz : nullptr, b.ld, dbias,
-              (float*)(ws + b.sums)};
-    rc = launch_ff_dz(q, st);
-    if (rc != CCT_OK) return rc;
-  }
+  FfDzJobs jobs = {};
+  if (copy || dbias)
+    jobs.job[jobs.count++] = {d.M, d.N, d.type, d.activation, dy, act ? z : nullptr, lddy, ldz, copy ? ws + b.dz : nullptr, b.ld,
+                              dbias, (float*)(ws + b.sums)};
+  Matrix mx, mw;
+  if (dx && d.M > 0) operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, &jobs);
+  if (dw) operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
+  rc = launch_ff_dz(jobs, st);
+  if (rc != CCT_OK) return rc;
   const Matrix dz = {copy ? ws + b.dz : dy, copy || d.M <= 1 ? b.ld : lddy};
   if (dx && d.M > 0) {
-    Matrix mw;
-    rc = operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, st);
-    if (rc != CCT_OK) return rc;
     FfProduct p = plain_product(d.type, d.M, d.K, d.N, dx, lddx);
     p.A[0] = rows_of(dz);
     p.B[0] = columns_of(mw);
@@ -243,9 +245,6 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
     if (rc != CCT_OK) return rc;
   }
   if (dw) {
-    Matrix mx;
-    rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
-    if (rc != CCT_OK) return rc;
     FfProduct p = plain_product(d.type, d.N, d.K, d.M, dw, lddw);
     p.A[0] = columns_of(dz);
     p.B[0] = columns_of(mx);
@@ -274,9 +273,13 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
   const bool few = few_rows(d.M, d.type, ff_in_place(wg, d.F <= 1 ? up(d.K, 8) : ldwg, d.K) &&
                                              ff_in_place(wu, d.F <= 1 ? up(d.K, 8) : ldwu, d.K) && ldwg == ldwu);
   Matrix mx = {x, ldx}, mg = {wg, ldwg}, mu = {wu, ldwu};
-  if (!few) rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
-  if (!few && rc == CCT_OK) rc = weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, st);
-  if (rc != CCT_OK) return rc;
+  if (!few) {
+    FfDzJobs jobs = {};
+    operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
+    weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, &jobs);
+    rc = launch_ff_dz(jobs, st);
+    if (rc != CCT_OK) return rc;
+  }
   FfProduct p = plain_product(d.type, d.M, d.F, d.K, h, ldh);
   p.epilogue = kFfGated;
   p.activation = d.activation;
@@ -314,10 +317,13 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
   const Matrix dg = {ws + b.dg, b.ld}, du = {ws + b.du, b.ld};
   rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, ws + b.dg, ws + b.du, b.ld}, st);
   if (rc != CCT_OK) return rc;
+  FfDzJobs jobs = {};
+  Matrix mx, mg, mu;
+  if (dx && d.M > 0) weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, &jobs);
+  if (dwg) operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
+  rc = launch_ff_dz(jobs, st);
+  if (rc != CCT_OK) return rc;
   if (dx && d.M > 0) {
-    Matrix mg, mu;
-    rc = weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, st);
-    if (rc != CCT_OK) return rc;
     FfProduct p = plain_product(d.type, d.M, d.K, d.F, dx, lddx);
     p.segments = 2;
     p.A[0] = rows_of(dg);
@@ -327,10 +333,7 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
     rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
     if (rc != CCT_OK) return rc;
   }
-  if (!dwg) return CCT_OK;
-  Matrix mx;
-  rc = operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, st);
-  for (int i = 0; i < 2 && rc == CCT_OK; ++i) {
+  for (int i = 0; i < 2 && dwg && rc == CCT_OK; ++i) {
     FfProduct p = plain_product(d.type, d.F, d.K, d.M, i ? dwu : dwg, i ? lddwu : lddwg);
     p.A[0] = columns_of(i ? du : dg);
     p.B[0] = columns_of(mx);

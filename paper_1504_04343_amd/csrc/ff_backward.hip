@@ -4,7 +4,7 @@
 // Each input is read once and each output written once; the rounding of dz, dg and du to 16 bits is the matrix cores', which
 // take no more of an operand (2^-9 of a value at most for bf16, the same as the operands themselves were rounded by).
 //
-// A workgroup takes 256 columns x 64 rows, or 8 where that leaves CUs idle (1531 x 1000: 9.9 -> X us), a thread 8
+// A workgroup takes 256 columns x 64 rows, or 8 where that leaves CUs idle (1531 x 1000: 5.3 us, 9.9 before), a thread 8
 // neighbouring columns of every eighth row: its column sums stay in
 // registers, meet in LDS in a fixed order and leave as one row of partial sums per workgroup, which a second kernel adds in
 // order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
@@ -49,9 +49,16 @@ __device__ __forceinline__ void store_columns(void* p, long long at, const float
   store8<TYPE>(p, at, all);
 }
 
+struct DzArgs {
+  FfDz job[3];
+  int first[3], rows[3];  // workgroup that a job begins at, rows of a workgroup
+};
 template <int TYPE>
-__global__ __launch_bounds__(NT) void ff_dz_kernel(FfDz p, int rows) {
-  const int wide = (p.N + kCols - 1) / kCols, down = blockIdx.x / wide, c0 = (blockIdx.x - down * wide) * kCols;
+__global__ __launch_bounds__(NT) void ff_dz_kernel(DzArgs a) {
+  const int which = ((int)blockIdx.x >= a.first[1]) + ((int)blockIdx.x >= a.first[2]), rows = a.rows[which];
+  const FfDz& p = a.job[which];
+  const int group = blockIdx.x - a.first[which], wide = (p.N + kCols - 1) / kCols, down = group / wide;
+  const int c0 = (group - down * wide) * kCols;
   const int c = c0 + (threadIdx.x & 31) * 8, lane_row = threadIdx.x >> 5;
   const int r0 = down * rows, r1 = min(r0 + rows, p.M);
   float sum[8] = {};
@@ -136,24 +143,38 @@ int rows_of_group(int M, int N) { return (long long)((M + 63) / 64) * ((N + kCol
 }  // namespace
 int ff_sum_rows(int M, int N) { return (M + rows_of_group(M, N) - 1) / rows_of_group(M, N); }
 
-int launch_ff_dz(const FfDz& p, hipStream_t st) {
-  const int rows = ff_sum_rows(p.M, p.N);
-  const double n = (double)p.M * p.N, e = type_bytes(p.type);
+int launch_ff_dz(const FfDzJobs& p, hipStream_t st) {
+  if (p.count == 0) return CCT_OK;
+  DzArgs a = {};
+  int groups = 0;
+  double ops = 0.0, bytes = 0.0;
+  for (int i = 0; i < 3; ++i) {
+    a.first[i] = i < p.count ? groups : 0x7fffffff;
+    if (i >= p.count) continue;
+    const FfDz& q = a.job[i] = p.job[i];
+    a.rows[i] = rows_of_group(q.M, q.N);
+    groups += ff_sum_rows(q.M, q.N) * ((q.N + kCols - 1) / kCols);
+    ops += 2.0 * q.M * q.N;
+    bytes += (double)type_bytes(q.type) * q.M * q.N * (1 + (q.z != nullptr) + (q.dz != nullptr));
+  }
   const char* const names[] = {"ff_dz_kernel<f32>", "ff_dz_kernel<bf16>", "ff_dz_kernel<f16>"};
-  with_type(p.type, [&](auto type) {
-    ProfScope ps(names[p.type], 2.0 * n, e * n * (1 + (p.z != nullptr) + (p.dz != nullptr)), st);
-    if (p.M > 0)
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_dz_kernel<decltype(type)::value>), dim3((p.N + kCols - 1) / kCols * rows), dim3(NT), 0, st,
-                         p, rows_of_group(p.M, p.N));
-  });
+  if (groups > 0)
+    with_type(p.job[0].type, [&](auto type) {
+      ProfScope ps(names[p.job[0].type], ops, bytes, st);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_dz_kernel<decltype(type)::value>), dim3(groups), dim3(NT), 0, st, a);
+    });
   CCT_CHECK_LAUNCH();
-  if (!p.dbias) return CCT_OK;
-  with_type(p.type, [&](auto type) {
-    ProfScope ps("ff_bias_sum_kernel", (double)rows * p.N, 4.0 * rows * p.N, st);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((p.N + 15) / 16), dim3(16 * kSumRuns), 0,
-                       st, p.part, rows, p.N, p.dbias);
-  });
-  CCT_CHECK_LAUNCH();
+  for (int i = 0; i < p.count; ++i) {
+    const FfDz& q = p.job[i];
+    if (!q.dbias) continue;
+    const int rows = ff_sum_rows(q.M, q.N);
+    with_type(q.type, [&](auto type) {
+      ProfScope ps("ff_bias_sum_kernel", (double)rows * q.N, 4.0 * rows * q.N, st);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((q.N + 15) / 16), dim3(16 * kSumRuns), 0,
+                         st, q.part, rows, q.N, q.dbias);
+    });
+    CCT_CHECK_LAUNCH();
+  }
   return CCT_OK;
 }
 

@@ -121,8 +121,8 @@ int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
     t.b_ks = along ? p.B[q].rs : p.B[q].ks;
     if (p.K < 1 || !gemm_split_fits(t, along)) return launch_general(p, st);
   }
-  for (int m0 = 0; m0 < p.M; m0 += plan.rows) {
-    GemmTN t = split_problem(std::min(plan.rows, p.M - m0), p.N, plan.len, plan.splits);
+  for (long long m0 = 0; m0 < p.M; m0 += plan.rows) {
+    GemmTN t = split_problem((int)std::min<long long>(plan.rows, p.M - m0), p.N, plan.len, plan.splits);
     for (int q = 0; q < products; ++q) {
       const FfOperand &A = p.A[gated ? 0 : q], &B = p.B[q];
       t.B = B.p;

@@ -19,7 +19,7 @@ constexpr TileCost kTileCosts[] = {{256, 256, 1, {1.58, 1.65}, {1.58, 1.70}},
                                    {64, 64, 2, {0.29, 0.50}, {0.54, 0.60}}};
 constexpr double kJoinMicros = 4.0, kJoinBytesPerMicro = 7.5e6;  // a launch and its gap; partial sums, written and read
 constexpr int kCus = 256, kLeastStages = 4;                       // of a split
-constexpr double kLaunchMicros = 3.0;
+constexpr double kLaunchMicros = 3.0, kBytesPerMicro = 5.0e6;  // operands, from memory
 
 // The tile and the number of splits of the contraction with the least estimate: rounds of workgroups over the card times the
 // stages of one, and what joining the splits costs.  Few large tiles leave CUs idle, small ones read LDS more often per
@@ -27,6 +27,7 @@ constexpr double kLaunchMicros = 3.0;
 FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool along) {
   const long long cols = epilogue == kFfGated ? 2LL * N : N;
   const int stages = std::max((K + kFfStage - 1) / kFfStage, 1) * (epilogue == kFfGated ? 1 : segments);
+  const double bytes = 2.0 * (M + (double)cols) * K * (epilogue == kFfGated ? 1 : segments);
   FfTilePlan best = {kTile128, 1, stages, 0, 1e30, 0, 0};
   for (int tile = kTile256; tile <= kTile64; ++tile) {
     const TileCost& c = kTileCosts[tile];
@@ -36,7 +37,8 @@ FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool alon
       const int each = (stages + splits - 1) / splits;
       const long long groups = tiles * splits, slots = (long long)kCus * c.per_cu, rest = groups % slots;
       double us = (double)(groups / slots) * c.full[!along] + (rest == 0 ? 0.0 : (rest <= kCus ? c.alone : c.full)[!along]);
-      us = us * each + kLaunchMicros;
+      // (fewer workgroups than a third of the CUs' places do not keep memory busy)
+      us = std::max(us * each, bytes / kBytesPerMicro * std::max(1.0, 170.0 / groups)) + kLaunchMicros;
       if (splits > 1) us += kJoinMicros + 8.0 * splits * M * cols / kJoinBytesPerMicro;
       if (us < best.micros) best = {tile, (stages + each - 1) / each, each, 0, us, 0, 0};
     }

@@ -30,10 +30,13 @@ def test_descriptors(B, bad):
 
 
 def test_sizes_beyond_a_launch(B):
-    d = B.make_linear_desc(2 ** 31 - 1, 2 ** 31 - 1, 8, B.TYPE_BF16)
-    with pytest.raises(B.CctError) as e:
-        B.cct_linear_workspace_bytes(d, B.PASS_FORWARD)
-    assert e.value.code == B.EUNSUPPORTED
+    for sizes in ((2 ** 31 - 256, 2 ** 31 - 256, 8), (2 ** 31 - 1, 8, 8), (8, 2 ** 31 - 1, 8), (8, 8, 2 ** 31 - 255)):
+        for make, ask in ((B.make_linear_desc, B.cct_linear_workspace_bytes), (B.make_gated_desc, B.cct_gated_workspace_bytes)):
+            for p in (B.PASS_FORWARD, B.PASS_BACKWARD):
+                with pytest.raises(B.CctError) as e:
+                    ask(make(*sizes, B.TYPE_BF16), p)
+                assert e.value.code == B.EUNSUPPORTED
+    B.cct_linear_workspace_bytes(B.make_linear_desc(2 ** 31 - 256, 8, 8, B.TYPE_F32), B.PASS_FORWARD)
 
 
 def linear(B, d, **k):

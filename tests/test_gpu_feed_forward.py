@@ -223,6 +223,27 @@ def test_fp32_ends_of_the_range(B):
             ff.check("y", y, ff.linear_forward("none", x, w, None, None)[0])
 
 
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_numbers_below_the_normal_ones(B, type):
+    """Operands, and results, that a type holds only as subnormal numbers: products of powers of two, exact."""
+    dt = ff.TYPES[type]
+    low = -132 if type == "bf16" else -23          # subnormal: bf16 below 2^-126, fp16 below 2^-14
+    for M in (2, 90):
+        print("subnormal", type, M, flush=True)
+        x = torch.zeros(M, 16, dtype=torch.float64)
+        x[:, 3] = 2.0 ** low
+        x[:, 4] = 3 * 2.0 ** low
+        w = torch.zeros(24, 16, dtype=torch.float64)
+        w[:, 3], w[:, 4] = 2.0 ** 12, 2.0 ** 12
+        w[1, 3:5], w[2, 3:5], w[3, 3:5] = 1.0, -1.0, 0.5
+        want = (x @ w.t()).to(dt)
+        y, _ = linear_forward(B, type, "none", x.to(dt), w.to(dt), None, None, False)
+        assert torch.equal(y.cpu(), want)
+        dx, dw, _ = linear_backward(B, type, "none", w.to(dt)[:, :16], x.to(dt)[:24], None,
+                                    torch.eye(24, min(M, 24), dtype=dt))
+        assert torch.equal(dx.cpu(), x.to(dt)[:24] if M >= 24 else torch.cat([x.to(dt), torch.zeros(24 - M, 16, dtype=dt)]))
+
+
 @pytest.mark.parametrize("type", list(ff.TYPES))
 def test_empty_batch(B, type):
     dt = ff.TYPES[type]
