@@ -18,6 +18,9 @@ Other modes (tables on stdout, meant to be kept under profiles/):
   --config e2e        one training iteration of CaffeNet (conv, ReLU, pooling, normalisation, fully
                       connected, dropout, softmax loss; no weight update), with the share of time
                       per kind of layer (Sec. 1 and 3.2 of the paper time whole iterations).
+  --config block      whole training steps of a classifier with a gated feed-forward block on CaffeNet's
+                      convolutional features (9216 values): products with their activations and residual,
+                      softmax loss, all gradients, their norm, and the clipped weight update.
 """
 import argparse
 import json
@@ -79,7 +82,7 @@ def parse():
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=20)
     ap.add_argument("--warmup", type=int, default=5)
-    ap.add_argument("--config", choices=["caffenet", "sweep", "batching", "e2e"], default="caffenet")
+    ap.add_argument("--config", choices=["caffenet", "sweep", "batching", "e2e", "block"], default="caffenet")
     ap.add_argument("--batch", type=int, default=None)
     ap.add_argument("--precision", choices=["f32", "bf16"], default="f32")
     ap.add_argument("--lowering", type=int, default=0, help="0 = auto (default), 1..4 = force")
@@ -584,6 +587,101 @@ def run_e2e(args, B, synth, torch):
                       "conv_share_of_time": round(share.get("conv", 0.0) / total, 4)}))
 
 
+class Block:
+    """A classifier on M feature vectors: r = relu(x w1^T + b1), h = silu(r wg^T) * (r wu^T), y = h w2^T + r,
+    scores = y w3^T + b3, softmax loss; trained by the clipped momentum rule.  fp32: the whole of it.  bf16: every product
+    on 16-bit tensors, fp32 weights behind them, and an upstream gradient of y given instead of scores and loss (which
+    the library takes in fp32)."""
+
+    def __init__(self, B, torch, M, K, D, F, classes, bf16, seed=0):
+        self.B, self.bf16 = B, bf16
+        dt, ty = (torch.bfloat16, B.TYPE_BF16) if bf16 else (torch.float32, B.TYPE_F32)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rand = lambda *s, std=1.0: torch.randn(s, generator=g, device="cuda") * std  # noqa: E731
+        empty = lambda *s: torch.empty(s, dtype=dt, device="cuda")                    # noqa: E731
+        self.x = rand(M, K).relu_().to(dt)
+        self.weights = [rand(D, K, std=(2.0 / K) ** 0.5), rand(D, std=0.01), rand(F, D, std=D ** -0.5),
+                        rand(F, D, std=D ** -0.5), rand(D, F, std=F ** -0.5)]
+        if not bf16:
+            self.weights += [rand(classes, D, std=D ** -0.5), rand(classes, std=0.01)]
+        self.moments = [torch.zeros_like(w) for w in self.weights]
+        self.w = [w.to(dt) for w in self.weights] if bf16 else self.weights      # what the products read
+        self.grads = [torch.empty_like(w) for w in self.w]
+        self.r, self.z1, self.h, self.gg, self.uu, self.y = empty(M, D), empty(M, D), empty(M, F), empty(M, F), empty(M, F), empty(M, D)
+        self.dy, self.dh, self.dr = empty(M, D), empty(M, F), empty(M, D)
+        self.d1 = B.make_linear_desc(M, D, K, ty, B.ACT_RELU)
+        self.dg = B.make_gated_desc(M, F, D, ty, B.ACT_SILU)
+        self.d2 = B.make_linear_desc(M, D, F, ty)
+        self.d3 = B.make_linear_desc(M, classes, D, ty)
+        descs = [(B.cct_linear_workspace_bytes, d) for d in (self.d1, self.d2, self.d3)] + [(B.cct_gated_workspace_bytes, self.dg)]
+        self.ws = torch.empty(max(ask(d, p) for ask, d in descs for p in (B.PASS_FORWARD, B.PASS_BACKWARD)), dtype=torch.uint8,
+                              device="cuda")
+        self.lists = [B.make_tensor_list(t) for t in (self.grads, self.weights, self.moments)]
+        self.copies = B.make_tensor_list(self.w) if bf16 else None
+        self.clip, self.norm_ws = torch.empty(2, device="cuda"), B.alloc_norm_workspace(self.lists[0])
+        if bf16:
+            self.dy.copy_(rand(M, D, std=1.0 / M))
+        else:
+            self.label = torch.randint(0, classes, (M,), generator=g, device="cuda", dtype=torch.int32)
+            self.scores, self.prob, self.ds = empty(M, classes), empty(M, classes), empty(M, classes)
+            self.image_loss, self.loss = empty(M), torch.empty(1, device="cuda")
+        ops = M * K * D + 3 * M * D * F + (0 if bf16 else M * D * classes)
+        self.flops = 6 * ops - 2 * M * K * D                                       # x has no gradient
+        self.parameters = sum(w.numel() for w in self.weights)
+
+    def forward(self):
+        B, w = self.B, self.w
+        B.cct_linear_forward(self.d1, self.x, w[0], w[1], None, self.r, self.z1, self.ws)
+        B.cct_gated_forward(self.dg, self.r, w[2], w[3], self.h, self.gg, self.uu, self.ws)
+        B.cct_linear_forward(self.d2, self.h, w[4], None, self.r, self.y, None, self.ws)
+        if not self.bf16:
+            B.cct_linear_forward(self.d3, self.y, w[5], w[6], None, self.scores, None, self.ws)
+            B.cct_softmax_loss_forward(self.scores, self.label, self.prob, self.image_loss, self.loss)
+
+    def backward(self):
+        B, w, g = self.B, self.w, self.grads
+        if not self.bf16:
+            B.cct_softmax_loss_backward(self.prob, self.label, self.ds)
+            B.cct_linear_backward(self.d3, self.y, w[5], None, self.ds, self.dy, g[5], g[6], self.ws)
+        B.cct_linear_backward(self.d2, self.h, w[4], None, self.dy, self.dh, g[4], None, self.ws)
+        B.cct_gated_backward(self.dg, self.r, w[2], w[3], self.gg, self.uu, self.dh, self.dr, g[2], g[3], self.ws)
+        self.dr.add_(self.dy)     # the residual's gradient is dy itself
+        B.cct_linear_backward(self.d1, self.x, None, self.z1, self.dr, None, g[0], g[1], self.ws)
+
+    def step(self, rate=0.01, momentum=0.9, decay=0.0005, max_norm=1.0):
+        B = self.B
+        self.forward()
+        self.backward()
+        B.cct_grad_norm(self.lists[0], max_norm, self.clip, self.norm_ws)
+        B.cct_sgd_update(self.lists[0], self.clip, self.lists[1], self.lists[2], self.copies, rate, momentum, decay)
+
+
+def run_block(args, B, synth, torch):
+    """Training steps of a classifier with a gated feed-forward block (class Block): 9216 features -> 4096, a gated block of
+    8192, 1000 classes."""
+    M = args.batch or 1024
+    bf16 = args.precision == "bf16"
+    block = Block(B, torch, M, 9216, 4096, 8192, 1000, bf16)
+    block.forward()
+    first = None if bf16 else float(block.loss)
+    elapsed, per_step = time_steps(block.step, args.steps, args.warmup)
+    ms = elapsed / args.steps * 1e3
+    block.forward()
+    last = None if bf16 else float(block.loss)
+    print("# training step of a gated feed-forward block, %d rows, %s: %.3f ms, %.0f TFLOP/s, gradient norm %.3g%s" % (
+        M, args.precision, ms, block.flops / ms / 1e9, float(block.clip[0]),
+        "" if bf16 else ", loss %.3f -> %.3f" % (first, last)), file=sys.stderr)
+    if args.per_kernel:
+        for e in sorted(profiled(B, block.step, 2), key=lambda e: -e["total_ms"]):
+            msk = e["total_ms"] / e["launches"]
+            print("# %-44s launches/step %5.1f  avg %8.4f ms  %8.2f TFLOP/s  %8.1f GB/s" % (
+                e["name"], e["launches"] / 2, msk, e["flops"] / e["launches"] / msk / 1e9,
+                e["bytes"] / e["launches"] / msk / 1e6), file=sys.stderr)
+    print(json.dumps({"config": "block", "batch": M, "precision": args.precision, "parameters": block.parameters,
+                      "ms_per_step": round(ms, 4), "tflops": round(block.flops / 1e9 / ms, 1), "loss_first": first,
+                      "loss_last": last, "step_time_spread": spread(per_step)}))
+
+
 def main():
     args = parse()
     if args.gpus != 1:
@@ -613,6 +711,8 @@ def main():
         run_batching(args, B, synth, torch)
     elif args.config == "e2e":
         run_e2e(args, B, synth, torch)
+    elif args.config == "block":
+        run_block(args, B, synth, torch)
     else:
         run_caffenet(args, B, synth, torch)
 
