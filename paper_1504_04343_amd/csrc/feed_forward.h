@@ -6,23 +6,24 @@
 namespace cct {
 
 // One matrix product of a feed-forward operator: sum over segments s and k of A_s(m, k) B_s(n, k), M x N results, and what
-// becomes of them.  An operand's element (row, k) lies at p + row * rs + k * ks elements: one of rs and ks is 1 (`across`: rs),
-// the other one the same in both segments.
+// becomes of them.
 struct FfOperand {
   const void* p;
-  long long rs, ks;
-  int across;
+  long long ld;  // elements between rows in memory
 };
+// An operand's element (row, k) lies at p + row * ff_row + k * ff_step elements: along the contraction or across it.
+inline long long ff_row(const FfOperand& o, bool across) { return across ? 1 : o.ld; }
+inline long long ff_step(const FfOperand& o, bool across) { return across ? o.ld : 1; }
 enum FfEpilogue {
   kFfLinear,  // z = sum + bias (kept if z is there), out = act(z) + residual
   kFfGated    // two products of the same A: g and u (kept if z and z2 are there), out = act(g) * u
 };
+// What a kernel needs first stands first: a launch's arguments come from memory, and every 64 bytes of them that it waits for
+// take about 0.5 us (one row of 4096 x 4096, 8 us: 0.6 more with a fifth such line).
 struct FfProduct {
   int M, N, K;
-  int type;
-  int segments;        // 1 or 2: contractions that are summed; kFfGated: B[0] and B[1] are the two products'
-  FfOperand A[2], B[2];
-  int epilogue, activation;
+  int activation;
+  FfOperand B[2], A[2];  // kFfGated: B[0] and B[1] are the two products'
   const void* bias;
   const void* residual;
   long long ldr;
@@ -30,6 +31,10 @@ struct FfProduct {
   long long ldo;
   void *z, *z2;
   long long ldz, ldz2;
+  int type;
+  int segments;  // 1 or 2: contractions that are summed
+  int epilogue;
+  bool a_across, b_across;  // in both segments, whose strides are the same
 };
 // `pack` (fp32) and `ws`: room for an operand's terms and for partial sums, as the plans below say.
 int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st);
@@ -57,7 +62,9 @@ int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st);
 // A forward product (operands along the contraction, at any address) of few rows: up to kFfRowsMost run, up to kFfRows (fp32:
 // kFfRowsF32) are faster so.
 constexpr int kFfRows = 16, kFfRowsF32 = 32, kFfRowsMost = 64;
-int launch_ff_rows(const FfProduct& p, hipStream_t st);
+// `ws`: ff_rows_part_bytes.
+long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue);
+int launch_ff_rows(const FfProduct& p, float* ws, hipStream_t st);
 // Whether the 16-bit product takes a matrix of `cols` consecutive values and rows `ld` apart in place: 16-byte loads, 256 rows
 // within 32-bit offsets.  Rows that are no multiple of 8 values must be followed by zeros up to one, as copies are.
 inline bool ff_in_place(const void* p, long long ld, long long cols) {

@@ -20,10 +20,7 @@ struct Layout {
   }
 };
 
-struct Matrix {
-  const void* p;
-  long long ld;
-};
+typedef FfOperand Matrix;
 // A tensor of rows x cols of a type: there, aligned to a value, rows that do not overlap.
 bool matrix_ok(const Matrix& m, long long rows, long long cols, int type) {
   if (!m.p || ((uintptr_t)m.p & (type_bytes(type) - 1)) || m.ld < 0) return false;
@@ -58,6 +55,11 @@ Room room(int type, int M, int N, int K, int epilogue, int segments, bool along)
   const FfF32Plan plan = ff_f32_plan(M, N, K, epilogue, segments, along);
   return {plan.pack_bytes, plan.part_bytes};
 }
+// ... of a forward product, whichever kernel takes it
+Room forward_room(int type, int M, int N, int K, int epilogue) {
+  const Room r = room(type, M, N, K, epilogue, 1, true);
+  return {r.pack, std::max(r.part, ff_rows_part_bytes(M, N, K, type, epilogue))};
+}
 Room larger(const Room& a, const Room& b) { return {std::max(a.pack, b.pack), std::max(a.part, b.part)}; }
 
 struct LinearLayout {
@@ -73,7 +75,7 @@ LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   b.sums = l.take(backward ? (long long)ff_sum_rows(d.M, d.N) * d.N * 4 : 0);
   // the two gradients are one after the other
   const Room r = backward ? larger(room(d.type, d.M, d.K, d.N, kFfLinear, 1, false), room(d.type, d.N, d.K, d.M, kFfLinear, 1, false))
-                          : room(d.type, d.M, d.N, d.K, kFfLinear, 1, true);
+                          : forward_room(d.type, d.M, d.N, d.K, kFfLinear);
   b.pack = l.take(r.pack);
   b.part = l.take(r.part);
   b.total = std::max(l.total, 256LL);
@@ -92,7 +94,7 @@ GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   b.dg = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.du = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   const Room r = backward ? larger(room(d.type, d.M, d.K, d.F, kFfLinear, 2, false), room(d.type, d.F, d.K, d.M, kFfLinear, 1, false))
-                          : room(d.type, d.M, d.F, d.K, kFfGated, 1, true);
+                          : forward_room(d.type, d.M, d.F, d.K, kFfGated);
   b.pack = l.take(r.pack);
   b.part = l.take(r.part);
   b.total = std::max(l.total, 256LL);
@@ -125,16 +127,16 @@ void weight_pair(const Matrix& g, const Matrix& u, long long rows, long long col
   if (use_u->p != to_u) add_copy(u, rows, cols, type, to_u, use_u, jobs);
 }
 
-FfOperand rows_of(const Matrix& m) { return {m.p, m.ld, 1, 0}; }
-FfOperand columns_of(const Matrix& m) { return {m.p, 1, m.ld, 1}; }
 
 // out (rows x cols) = sum over segments of A_s B_s^T, rounded, nothing else
-FfProduct plain_product(int type, int rows, int cols, int k, void* out, long long ldo) {
+FfProduct plain_product(int type, int rows, int cols, int k, bool a_across, bool b_across, void* out, long long ldo) {
   FfProduct p = {};
   p.M = rows;
   p.N = cols;
   p.K = k;
   p.type = type;
+  p.a_across = a_across;
+  p.b_across = b_across;
   p.segments = 1;
   p.epilogue = kFfLinear;
   p.activation = CCT_ACT_NONE;
@@ -194,16 +196,16 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
     rc = launch_ff_dz(jobs, st);
     if (rc != CCT_OK) return rc;
   }
-  FfProduct p = plain_product(d.type, d.M, d.N, d.K, y, ldy);
-  p.A[0] = rows_of(mx);
-  p.B[0] = rows_of(mw);
+  FfProduct p = plain_product(d.type, d.M, d.N, d.K, false, false, y, ldy);
+  p.A[0] = mx;
+  p.B[0] = mw;
   p.activation = d.activation;
   p.bias = bias;
   p.residual = residual;
   p.ldr = ldr;
   p.z = z;
   p.ldz = ldz;
-  return few ? launch_ff_rows(p, st) : launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
+  return few ? launch_ff_rows(p, (float*)(ws + b.part), st) : launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
 }
 
 int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -238,16 +240,16 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
   if (rc != CCT_OK) return rc;
   const Matrix dz = {copy ? ws + b.dz : dy, copy || d.M <= 1 ? b.ld : lddy};
   if (dx && d.M > 0) {
-    FfProduct p = plain_product(d.type, d.M, d.K, d.N, dx, lddx);
-    p.A[0] = rows_of(dz);
-    p.B[0] = columns_of(mw);
+    FfProduct p = plain_product(d.type, d.M, d.K, d.N, false, true, dx, lddx);
+    p.A[0] = dz;
+    p.B[0] = mw;
     rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
     if (rc != CCT_OK) return rc;
   }
   if (dw) {
-    FfProduct p = plain_product(d.type, d.N, d.K, d.M, dw, lddw);
-    p.A[0] = columns_of(dz);
-    p.B[0] = columns_of(mx);
+    FfProduct p = plain_product(d.type, d.N, d.K, d.M, true, true, dw, lddw);
+    p.A[0] = dz;
+    p.B[0] = mx;
     rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
   }
   return rc;
@@ -280,17 +282,17 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
     rc = launch_ff_dz(jobs, st);
     if (rc != CCT_OK) return rc;
   }
-  FfProduct p = plain_product(d.type, d.M, d.F, d.K, h, ldh);
+  FfProduct p = plain_product(d.type, d.M, d.F, d.K, false, false, h, ldh);
   p.epilogue = kFfGated;
   p.activation = d.activation;
-  p.A[0] = rows_of(mx);
-  p.B[0] = rows_of(mg);
-  p.B[1] = rows_of(mu);
+  p.A[0] = mx;
+  p.B[0] = mg;
+  p.B[1] = mu;
   p.z = g;
   p.ldz = ldg;
   p.z2 = u;
   p.ldz2 = ldu;
-  return few ? launch_ff_rows(p, st) : launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
+  return few ? launch_ff_rows(p, (float*)(ws + b.part), st) : launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
 }
 
 int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
@@ -324,19 +326,19 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
   rc = launch_ff_dz(jobs, st);
   if (rc != CCT_OK) return rc;
   if (dx && d.M > 0) {
-    FfProduct p = plain_product(d.type, d.M, d.K, d.F, dx, lddx);
+    FfProduct p = plain_product(d.type, d.M, d.K, d.F, false, true, dx, lddx);
     p.segments = 2;
-    p.A[0] = rows_of(dg);
-    p.A[1] = rows_of(du);
-    p.B[0] = columns_of(mg);
-    p.B[1] = columns_of(mu);
+    p.A[0] = dg;
+    p.A[1] = du;
+    p.B[0] = mg;
+    p.B[1] = mu;
     rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
     if (rc != CCT_OK) return rc;
   }
   for (int i = 0; i < 2 && dwg && rc == CCT_OK; ++i) {
-    FfProduct p = plain_product(d.type, d.F, d.K, d.M, i ? dwu : dwg, i ? lddwu : lddwg);
-    p.A[0] = columns_of(i ? du : dg);
-    p.B[0] = columns_of(mx);
+    FfProduct p = plain_product(d.type, d.F, d.K, d.M, true, true, i ? dwu : dwg, i ? lddwu : lddwg);
+    p.A[0] = i ? du : dg;
+    p.B[0] = mx;
     rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
   }
   return rc;

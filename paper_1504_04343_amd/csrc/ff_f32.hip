@@ -30,16 +30,17 @@ __global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m
   for (int s = 0; s < (GATED ? 1 : p.segments); ++s)
     for (int k0 = 0; k0 < p.K; k0 += BK) {
       __syncthreads();
-      auto stage = [&](float(&to)[BK][BT + 1], const FfOperand& o, int r0, int rows) {
+      auto stage = [&](float(&to)[BK][BT + 1], const FfOperand& o, bool across, int r0, int rows) {
         for (int i = threadIdx.x; i < BT * BK; i += NT) {
           // consecutive threads along the consecutive dimension
-          const int r = o.across ? i % BT : i / BK, k = o.across ? i / BT : i % BK;
-          to[k][r] = r0 + r < rows && k0 + k < p.K ? ((const float*)o.p)[(r0 + r) * o.rs + (k0 + k) * o.ks] : 0.f;
+          const int r = across ? i % BT : i / BK, k = across ? i / BT : i % BK;
+          const long long at = across ? (r0 + r) + (k0 + k) * o.ld : (r0 + r) * o.ld + (k0 + k);
+          to[k][r] = r0 + r < rows && k0 + k < p.K ? ((const float*)o.p)[at] : 0.f;
         }
       };
-      stage(As, p.A[s], m0, p.M);
-      stage(Bs[0], p.B[s], n0, p.N);
-      if constexpr (GATED) stage(Bs[1], p.B[1], n0, p.N);
+      stage(As, p.A[s], p.a_across, m0, p.M);
+      stage(Bs[0], p.B[s], p.b_across, n0, p.N);
+      if constexpr (GATED) stage(Bs[1], p.B[1], p.b_across, n0, p.N);
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < BK; ++k)
@@ -111,14 +112,14 @@ FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool alon
 }
 
 int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
-  const bool gated = p.epilogue == kFfGated, along = !p.B[0].across;
+  const bool gated = p.epilogue == kFfGated, along = !p.b_across;
   const int products = gated ? 2 : p.segments;
   const FfF32Plan plan = ff_f32_plan(p.M, p.N, p.K, p.epilogue, p.segments, along);
   const bool join = plan.splits > 1 || products > 1 || p.residual || p.z || p.activation != CCT_ACT_NONE;
   const long long ld = join ? (p.N + 3) / 4 * 4 : p.ldo;
   for (int q = 0; q < products; ++q) {
     GemmTN t = split_problem(plan.rows, p.N, plan.len, plan.splits);
-    t.b_ks = along ? p.B[q].rs : p.B[q].ks;
+    t.b_ks = p.B[q].ld;
     if (p.K < 1 || !gemm_split_fits(t, along)) return launch_general(p, st);
   }
   for (long long m0 = 0; m0 < p.M; m0 += plan.rows) {
@@ -126,11 +127,12 @@ int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
     for (int q = 0; q < products; ++q) {
       const FfOperand &A = p.A[gated ? 0 : q], &B = p.B[q];
       t.B = B.p;
-      t.b_ks = along ? B.rs : B.ks;
-      t.b_gs = plan.len * B.ks;
-      t.b_len = along ? (p.N - 1) * B.rs + p.K : (p.K - 1) * B.ks + p.N;
+      t.b_ks = B.ld;
+      t.b_gs = plan.len * ff_step(B, !along);
+      t.b_len = along ? (p.N - 1) * B.ld + p.K : (p.K - 1) * B.ld + p.N;
       if (q == 0 || !gated) {  // a gated block's products have the same rows
-        const int rc = gemm_split_operand(&t, along, (const float*)A.p + m0 * A.rs, pack, p.K, A.rs, A.ks, plan.len * A.ks, 1, st);
+        const long long row = ff_row(A, p.a_across), step = ff_step(A, p.a_across);
+        const int rc = gemm_split_operand(&t, along, (const float*)A.p + m0 * row, pack, p.K, row, step, plan.len * step, 1, st);
         if (rc != CCT_OK) return rc;
       }
       t.c_ms = ld;

@@ -77,8 +77,8 @@ namespace {
 FfProduct part_of(FfProduct p, int m, int n, int rows, int cols) {
   auto at = [&](const void* q, long long ld) { return q ? (void*)((char*)q + (m * ld + n) * 2) : nullptr; };
   for (int s = 0; s < 2; ++s) {
-    if (p.A[s].p) p.A[s].p = (const char*)p.A[s].p + m * p.A[s].rs * 2;
-    if (p.B[s].p) p.B[s].p = (const char*)p.B[s].p + n * p.B[s].rs * 2;
+    if (p.A[s].p) p.A[s].p = (const char*)p.A[s].p + m * ff_row(p.A[s], p.a_across) * 2;
+    if (p.B[s].p) p.B[s].p = (const char*)p.B[s].p + n * ff_row(p.B[s], p.b_across) * 2;
   }
   p.M = rows;
   p.N = cols;
@@ -103,13 +103,13 @@ int launch_tiles(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStrea
 
 int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
   if (p.type == CCT_TYPE_F32) return launch_ff_f32(p, pack, ws, st);
-  const FfTilePlan plan = ff_tile_plan(p.M, p.N, p.K, p.epilogue, p.segments, !p.B[0].across);
+  const FfTilePlan plan = ff_tile_plan(p.M, p.N, p.K, p.epilogue, p.segments, !p.b_across);
   if (!plan.cut_rows && !plan.cut_cols) return launch_tiles(p, plan, ws, st);
   const int m = plan.cut_rows, n = plan.cut_cols;  // one of them is 0
   const int rc = launch_tiles(part_of(p, 0, 0, m ? m : p.M, n ? n : p.N), plan, ws, st);
   if (rc != CCT_OK) return rc;
   const FfProduct rest = part_of(p, m, n, p.M - m, p.N - n);
-  return launch_tiles(rest, whole_plan(rest.M, rest.N, rest.K, rest.epilogue, rest.segments, !rest.B[0].across), ws, st);
+  return launch_tiles(rest, whole_plan(rest.M, rest.N, rest.K, rest.epilogue, rest.segments, !rest.b_across), ws, st);
 }
 
 }  // namespace cct

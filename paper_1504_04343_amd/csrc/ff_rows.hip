@@ -1,8 +1,8 @@
 // Forward products of few rows (serving: one token, or a batch of sequences with one each): the weights are read once and
 // nothing else matters.
 //
-// A workgroup takes 16 rows of the weight (gated: of both) and all rows of x, its eight waves every eighth step of the
-// contraction: 64 bytes of each weight row, which go from memory straight into the registers that the matrix cores take (32
+// A workgroup takes 16 rows of the weight (gated: of both) and all rows of x, its waves (eight; fp32 with up to 16 rows
+// sixteen) one step of the contraction after the other: 64 bytes of each weight row, which go from memory straight into the registers that the matrix cores take (32
 // values of 16 bits per instruction, 4 of fp32 in an order of their own that x follows).  No LDS and no meeting in the loop;
 // eight steps' loads are in flight per wave, and x comes from L2 the same way.  The waves' sums meet in LDS in a fixed
 // order.  fp32 runs on v_mfma_f32_16x16x4_f32, which memory outlasts.
@@ -10,7 +10,10 @@
 // One row, bf16, weights from memory: 4096 x 4096 7.9 us (4.3 TB/s; 6.8 at the rate of a large copy), 16384 x 4096 25.6 (5.2
 // TB/s), gated 2 x 8192 x 4096 27.0 (5.0).  With two batches of four steps in turn 9.0, 29.1 and 29.8: the compiler waits
 // for all of a batch before it loads the next one into the same registers, so that they are only smaller; with sixteen waves
-// 8.0, 26.8 and 26.8.
+// 8.0, 26.8 and 26.8.  fp32, eight and sixteen waves: 18.7 and 16.6, 56.7 and 52.0, 62.5 and 56.5 (4096 x 16384).
+//
+// Few columns of long rows leave most CUs idle: the contraction is then cut into splits, whose sums ff_join_kernel adds (64
+// outputs of 16384 inputs, bf16: 19.3 us on four CUs, 9.8 in eight splits).
 //
 // Any alignment: gfx950 loads 16 bytes at any address.  A last step that is not whole is loaded value by value.
 #include <algorithm>
@@ -21,8 +24,6 @@
 
 namespace cct {
 namespace {
-
-constexpr int kWaves = 8;
 
 template <int TYPE>
 struct Step {  // 16-bit types
@@ -64,16 +65,21 @@ struct Step<CCT_TYPE_F32> {
 };
 
 // RM: blocks of 16 rows of x
-template <int TYPE, int RM, int EPI>
-__global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
+template <int TYPE, int RM>
+constexpr int kWaves = TYPE == CCT_TYPE_F32 && RM == 1 ? 16 : 8;
+
+// SPLIT: the contraction is cut (a form of its own: what tells it how is a cache line of arguments more, 0.6 of 8 us)
+template <int TYPE, int RM, int EPI, bool SPLIT>
+__global__ __launch_bounds__((kWaves<TYPE, RM> * 64)) void ff_rows_kernel(FfProduct p, FfPart part) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
   constexpr int NB = EPI == kFfGated ? 2 : 1, BATCH = RM == 4 ? 4 : 8;
+  constexpr int NW = kWaves<TYPE, RM>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int n0 = blockIdx.x * 16, lo = lane & 15, kq = (lane >> 4) * S::CH;
-  long long w_at = (long long)min(n0 + lo, p.N - 1) * p.B[0].rs, u_at = (long long)min(n0 + lo, p.N - 1) * p.B[NB - 1].rs, x_at[RM];
+  const int split = SPLIT ? blockIdx.y : 0, n0 = blockIdx.x * 16, lo = lane & 15, kq = (lane >> 4) * S::CH;
+  long long w_at = (long long)min(n0 + lo, p.N - 1) * p.B[0].ld, u_at = (long long)min(n0 + lo, p.N - 1) * p.B[NB - 1].ld, x_at[RM];
 #pragma unroll
-  for (int i = 0; i < RM; ++i) x_at[i] = (long long)min(i * 16 + lo, p.M - 1) * p.A[0].rs;
+  for (int i = 0; i < RM; ++i) x_at[i] = (long long)min(i * 16 + lo, p.M - 1) * p.A[0].ld;
 
   f32x4 acc[NB][RM];
 #pragma unroll
@@ -81,13 +87,13 @@ __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
 #pragma unroll
     for (int i = 0; i < RM; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int whole = p.K / S::K;  // steps
+  const int all = p.K / S::K, first = SPLIT ? split * part.stages : 0, whole = SPLIT ? min(all, first + part.stages) : all;  // steps
   V w[BATCH][NB], x[BATCH][RM];
   // steps past the last one load it again and multiply zeros
   auto load = [&](int s0) {
 #pragma unroll
     for (int q = 0; q < BATCH; ++q) {
-      const long long k = (long long)min(s0 + q * kWaves, whole - 1) * S::K + kq;
+      const long long k = (long long)min(s0 + q * NW, whole - 1) * S::K + kq;
       w[q][0] = S::load(p.B[0].p, w_at + k);
       if constexpr (NB == 2) w[q][1] = S::load(p.B[1].p, u_at + k);
 #pragma unroll
@@ -98,7 +104,7 @@ __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
     __builtin_amdgcn_sched_barrier(0);  // the loads in front of it are not moved behind
 #pragma unroll
     for (int q = 0; q < BATCH; ++q) {
-      const bool live = s0 + q * kWaves < whole;
+      const bool live = s0 + q * NW < whole;
 #pragma unroll
       for (int i = 0; i < RM; ++i) {
         const V xv = live ? x[q][i] : V{};
@@ -107,12 +113,12 @@ __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
       }
     }
   };
-  for (int s = wave; s < whole; s += BATCH * kWaves) {
+  for (int s = first + wave; s < whole; s += BATCH * NW) {
     load(s);
     multiply(s);
   }
-  if (p.K % S::K && whole % kWaves == wave) {
-    const int k = whole * S::K + kq, n = max(0, min(S::CH, p.K - k));
+  if (p.K % S::K && (!SPLIT || split == part.splits - 1) && all % NW == wave) {
+    const int k = all * S::K + kq, n = max(0, min(S::CH, p.K - k));
     V wv[NB];
     wv[0] = S::part(p.B[0].p, w_at + k, n);
     if constexpr (NB == 2) wv[1] = S::part(p.B[1].p, u_at + k, n);
@@ -124,22 +130,27 @@ __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
     }
   }
 
-  __shared__ f32x4 sums[kWaves][NB * RM][64];
+  __shared__ f32x4 sums[NW][NB * RM][64];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < RM; ++i) sums[wave][b * RM + i][lane] = acc[b][i];
   __syncthreads();
-  for (int i = wave; i < RM; i += kWaves) {
+  for (int i = wave; i < RM; i += NW) {
     f32x4 s[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       s[b] = sums[0][b * RM + i][lane];
 #pragma unroll
-      for (int q = 1; q < kWaves; ++q) s[b] += sums[q][b * RM + i][lane];
+      for (int q = 1; q < NW; ++q) s[b] += sums[q][b * RM + i][lane];
     }
     const int m = i * 16 + lo, n = n0 + (lane >> 4) * 4;
     if (m >= p.M || n >= p.N) continue;
+    if constexpr (SPLIT) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) *(f32x4*)(part.p + (((long long)split * NB + b) * p.M + m) * part.ld + n) = s[b];
+      continue;
+    }
     float v[4], u[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -150,37 +161,60 @@ __global__ __launch_bounds__(kWaves * 64) void ff_rows_kernel(FfProduct p) {
   }
 }
 
+int rows_splits(int N, int K, int type) {
+  const int groups = (N + 15) / 16, least = type == CCT_TYPE_F32 ? 1024 : 2048;  // steps of a split
+  return groups > 64 || K < 4 * least ? 1 : std::min(128 / groups, K / least);
+}
+
 template <int TYPE, int EPI>
-void launch(const FfProduct& p, hipStream_t st) {
-  const dim3 grid((p.N + 15) / 16), block(kWaves * 64);
+void launch(const FfProduct& p, float* ws, hipStream_t st) {
+  const int groups = (p.N + 15) / 16, steps = std::max(p.K / Step<TYPE>::K, 1);
+  FfPart part = {ws, (p.N + 3) / 4 * 4, rows_splits(p.N, p.K, TYPE), 0};
+  part.stages = (steps + part.splits - 1) / part.splits;
+  part.splits = (steps + part.stages - 1) / part.stages;
+  auto run = [&](auto rm) {
+    constexpr int RM = decltype(rm)::value;
+    const dim3 grid(groups, part.splits), block(kWaves<TYPE, RM> * 64);
+    if (part.splits > 1)
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, RM, EPI, true>), grid, block, 0, st, p, part);
+    else
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, RM, EPI, false>), grid, block, 0, st, p, part);
+  };
   if (p.M <= 16)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, 1, EPI>), grid, block, 0, st, p);
-  else if (p.M <= 32)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, 2, EPI>), grid, block, 0, st, p);
+    run(std::integral_constant<int, 1>());
+  else if (p.M <= 32 || TYPE == CCT_TYPE_F32)
+    run(std::integral_constant<int, 2>());
   else
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, 4, EPI>), grid, block, 0, st, p);
+    run(std::integral_constant<int, TYPE == CCT_TYPE_F32 ? 2 : 4>());
+  if (part.splits > 1)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, EPI>), dim3((p.M * part.ld / 4 + 255) / 256), dim3(256), 0, st, p, part);
 }
 template <int TYPE>
-void launch(const FfProduct& p, hipStream_t st) {
+void launch(const FfProduct& p, float* ws, hipStream_t st) {
   if (p.epilogue == kFfGated)
-    launch<TYPE, kFfGated>(p, st);
+    launch<TYPE, kFfGated>(p, ws, st);
   else
-    launch<TYPE, kFfLinear>(p, st);
+    launch<TYPE, kFfLinear>(p, ws, st);
 }
 
 }  // namespace
 
-int launch_ff_rows(const FfProduct& p, hipStream_t st) {
+long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue) {
+  const int splits = M <= kFfRowsMost ? rows_splits(N, K, type) : 1;
+  return splits == 1 ? 0 : 4LL * splits * (epilogue == kFfGated ? 2 : 1) * M * ((N + 3) / 4 * 4);
+}
+
+int launch_ff_rows(const FfProduct& p, float* ws, hipStream_t st) {
   const double e = type_bytes(p.type), mn = (double)p.M * p.N, ops = p.epilogue == kFfGated ? 2 : 1;
   const double bytes = e * ((double)p.M * p.K + ops * p.N * p.K +
                             mn * (1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)));
   ProfScope ps("ff_rows_kernel", 2.0 * mn * p.K * ops, bytes, st);
   if (p.type == CCT_TYPE_F32)
-    launch<CCT_TYPE_F32>(p, st);
+    launch<CCT_TYPE_F32>(p, ws, st);
   else if (p.type == CCT_TYPE_BF16)
-    launch<CCT_TYPE_BF16>(p, st);
+    launch<CCT_TYPE_BF16>(p, ws, st);
   else
-    launch<CCT_TYPE_F16>(p, st);
+    launch<CCT_TYPE_F16>(p, ws, st);
   CCT_CHECK_LAUNCH();
   return CCT_OK;
 }

@@ -248,7 +248,7 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   const int first = SPLIT ? split * part.stages : 0, stages = SPLIT ? min(part.stages, all - first) : all;
   OpA a;
   OpB b;
-  const long long lda = AX ? p.A[0].ks : p.A[0].rs, ldb = BX ? p.B[0].ks : p.B[0].rs;
+  const long long lda = p.A[0].ld, ldb = p.B[0].ld;
   a.template init<1>(wave, lane, left_m, lda);
   b.template init<PARTS>(wave, lane, left_n, ldb);
   const long long a_at = (AX ? m0 : m0 * lda) * 2, b_at = (BX ? n0 : n0 * ldb) * 2;

@@ -20,7 +20,7 @@ int launch_tile(const FfProduct& p, const FfPart& part, hipStream_t st) {
 
 template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool SPLIT>
 int launch_mode(const FfProduct& p, const FfPart& part, hipStream_t st) {
-  const bool ax = p.A[0].across, bx = p.B[0].across;
+  const bool ax = p.a_across, bx = p.b_across;
   if (p.epilogue == kFfGated) return launch_tile<TYPE, BM, BN, WM, WN, RING, false, false, kFfGated, SPLIT>(p, part, st);
   if (ax) return launch_tile<TYPE, BM, BN, WM, WN, RING, true, true, kFfLinear, SPLIT>(p, part, st);
   if (bx) return launch_tile<TYPE, BM, BN, WM, WN, RING, false, true, kFfLinear, SPLIT>(p, part, st);

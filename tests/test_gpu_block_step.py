@@ -31,7 +31,7 @@ def reference(weights, moments, x, label, max_norm, rate, momentum, decay):
     norm = torch.sqrt(sum((g ** 2).sum() for g in grads))
     s = min(1.0, max_norm / float(norm))
     moments = [momentum * m + rate * (s * g + decay * t.detach()) for m, g, t in zip(moments, grads, w)]
-    return float(loss), float(norm), [t.detach() - m for t, m in zip(w, moments)], moments
+    return float(loss.detach()), float(norm), [t.detach() - m for t, m in zip(w, moments)], moments
 
 
 def close(name, got, want):

@@ -328,6 +328,24 @@ def test_fp32_rows_too_far_apart_for_the_split_product(B):
     ff.check("h", h, ff.gated_forward("silu", x, w, u)[0])
 
 
+@pytest.mark.parametrize("type", list(ff.TYPES))
+def test_few_rows_and_columns_of_long_rows(B, type):
+    """The contraction of a forward product of few rows in splits, whole and not, at any address."""
+    dt = ff.TYPES[type]
+    for M, N, K, pad in ((1, 10, 8192, 0), (3, 33, 9001, 1), (16, 72, 20000, 0), (30, 100, 12288, 3), (50, 40, 8200, 5)):
+        print("splits", type, M, N, K, flush=True)
+        g = torch.Generator().manual_seed(N)
+        x, w, u = (ff.rand(g, r, K, dt, s, pad) for r, s in ((M, 1.0), (N, K ** -0.5), (N, K ** -0.5)))
+        bias, r = ff.rand(g, 1, N, dt).view(N), ff.rand(g, M, N, dt)
+        y, z = linear_forward(B, type, "gelu", x, w, bias, r, True)
+        want = ff.linear_forward("gelu", x, w, bias, r)
+        ff.check("y", y, want[0])
+        ff.check("z", z, want[1])
+        h, gg, uu = gated_forward(B, type, "silu", x, w, u, True)
+        for name, t, v in zip("hgu", (h, gg, uu), ff.gated_forward("silu", x, w, u)):
+            ff.check(name, t, v)
+
+
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_every_tile_and_split(B, type):
     """Sizes that the plan cuts into tiles of 256, 128, 64 x 128 and 64, with one split and with several."""
