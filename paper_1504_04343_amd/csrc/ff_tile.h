@@ -10,17 +10,17 @@
 //   along the contraction: rows of 8 pieces, piece c of row r at c ^ (r & 7).  A matrix instruction's operand is one piece
 //     per lane, 16 rows x 4 pieces.
 //   across it: rows of the tile's width, in windows of 16 values; window v of row k at v ^ (k & 3 | (k >> 1) & 4)
-//     (64 wide, which has four windows: v ^ (k & 3)).  The
-//     operand is read with the transposing 8-byte LDS load: 16 lanes fetch 4 rows x 16 values and each gets 4 rows of one
-//     column; two of them make a lane's 8 steps.
+//     (64 wide, which has four windows: v ^ (k & 3)).  The operand is read with the transposing 8-byte LDS load: 16 lanes
+//     fetch 4 rows x 16 values and each gets 4 rows of one column; two of them make a lane's 8 steps.
 //
-// What bounds it (8192 x 8192 x 4096 forward, 405 us): the loads alone take 263 us (16 TB/s out of the L2s), LDS reads and
-// matrix instructions without loads 326, so that a fifth of the loads is not hidden.  Stages of 32 steps in rings of 3 to 5
-// are 450 us whatever their number: half rows of 64 bytes cost more than loads further ahead give.  Four waves of 128 x 128
-// would read a third less LDS and do not hide anything behind each other (557 us).
+// What bounds the tiles of 256 (8192 x 8192 x 4096 forward: 405 to 425 us by card, 1290 to 1360 TFLOP/s): LDS reads and matrix
+// instructions without the loads take 326 us, loads and LDS reads without the matrix instructions 263.  Half of what they
+// take more together is the clock that the card holds (zeros as operands: 4096 x 4096 x 4096 in 89 us, 102 with normals).
+// Latency it is not: 64 steps at a time with a third stage for one operand, lines asked for two stages ahead and 32 steps at
+// a time in rings of 3 to 5 (428, 440, 450 us) gain nothing; nor LDS (four waves of 128 x 128, which read a third less, hide
+// nothing behind each other: 561).
 //
-// The weights' side is the instruction's first operand: a lane then holds 4 neighbouring columns of one row of the result,
-// stored as 8 bytes.
+// The weights' side is the instruction's first operand: a lane then holds 4 neighbouring columns of one row of the result.
 #pragma once
 #include "activation.h"
 #include "feed_forward.h"
@@ -35,7 +35,6 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
 constexpr int SK = kFfStage;  // steps of the contraction per stage
-
 
 template <int TYPE>
 __device__ __forceinline__ f32x4 tile_mfma(s16x8 a, s16x8 b, f32x4 c) {
@@ -306,7 +305,7 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     // a wave issues in order, and what eight waves read and load takes LDS and the address unit as long as the matrix
     // instructions take: one by one between them, not in front of them (8192 x 8192 x 4096 forward 433 -> 411 us for the
     // reads, 405 for the loads too)
-    constexpr int READS = (AX ? 2 : 1) * RB + (BX ? 2 : 1) * CB, EACH = RB * CB / READS;
+    constexpr int READS = (AX ? 2 : 1) * RB + (BX ? 2 : 1) * CB, EACH = RB * CB > READS ? RB * CB / READS : 1;
 #pragma unroll
     for (int q = 0; q < READS; ++q) {
       __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
