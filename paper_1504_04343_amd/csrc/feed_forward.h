@@ -40,7 +40,7 @@ struct FfProduct {
 int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st);
 // How a 16-bit product is cut (ff_tile.h): its tile, splits of the contraction of so many stages, the bytes of their partial
 // sums (launch_ff_product's `ws`) and an estimate; rows or columns behind which the rest is a launch with a plan of its own.
-enum { kTile256, kTile128, kTile64x128, kTile64 };
+enum { kTile256, kTile192 /* 192 x 256 */, kTile128, kTile64x128, kTile64 };
 constexpr int kFfStage = 64;
 struct FfTilePlan {
   int tile, splits, stages;

@@ -14,6 +14,7 @@ struct TileCost {
   double alone[2], full[2];
 };
 constexpr TileCost kTileCosts[] = {{256, 256, 1, {1.58, 1.65}, {1.58, 1.70}},
+                                   {192, 256, 1, {1.24, 1.30}, {1.24, 1.34}},
                                    {128, 128, 2, {0.65, 0.93}, {1.10, 1.08}},
                                    {64, 128, 2, {0.39, 0.75}, {0.72, 0.83}},
                                    {64, 64, 2, {0.29, 0.50}, {0.54, 0.60}}};
@@ -33,7 +34,7 @@ FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool alon
     const TileCost& c = kTileCosts[tile];
     const long long tiles = ((M + c.bm - 1LL) / c.bm) * ((cols + c.bn - 1) / c.bn);
     for (int splits = 1; splits <= 32; splits *= 2) {
-      if (splits > 1 && (tile == kTile256 || stages < splits * kLeastStages || tiles * splits > 4 * kCus)) break;
+      if (splits > 1 && (tile <= kTile192 || stages < splits * kLeastStages || tiles * splits > 4 * kCus)) break;
       const int each = (stages + splits - 1) / splits;
       const long long groups = tiles * splits, slots = (long long)kCus * c.per_cu, rest = groups % slots;
       double us = (double)(groups / slots) * c.full[!along] + (rest == 0 ? 0.0 : (rest <= kCus ? c.alone : c.full)[!along]);
@@ -94,7 +95,7 @@ int launch_tiles(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStrea
   const double mn = (double)p.M * p.N, ops = p.epilogue == kFfGated ? 2 : p.segments;
   const double bytes = 2.0 * ((double)(p.epilogue == kFfGated ? 1 : p.segments) * p.M * p.K + ops * p.N * p.K +
                               mn * (1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)));
-  const char* const names[] = {"256x256", "128x128", "64x128", "64x64"};
+  const char* const names[] = {"256x256", "192x256", "128x128", "64x128", "64x64"};
   ProfScope ps(2.0 * mn * p.K * ops, bytes, st, "ff_tile_kernel<%s, %d splits>", names[plan.tile], plan.splits);
   return p.type == CCT_TYPE_BF16 ? launch_ff_tile_bf16(p, plan, ws, st) : launch_ff_tile_f16(p, plan, ws, st);
 }

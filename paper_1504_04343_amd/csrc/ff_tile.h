@@ -10,7 +10,7 @@
 //   along the contraction: rows of 8 pieces, piece c of row r at c ^ (r & 7).  A matrix instruction's operand is one piece
 //     per lane, 16 rows x 4 pieces.
 //   across it: rows of the tile's width, in windows of 16 values; window v of row k at v ^ (k & 3 | (k >> 1) & 4)
-//     (64 wide, which has four windows: v ^ (k & 3)).  The operand is read with the transposing 8-byte LDS load: 16 lanes
+//     (64 and 192 wide, whose windows come in fours: v ^ (k & 3)).  The operand is read with the transposing 8-byte LDS load: 16 lanes
 //     fetch 4 rows x 16 values and each gets 4 rows of one column; two of them make a lane's 8 steps.
 //
 // What bounds the tiles of 256 (8192 x 8192 x 4096 forward: 405 to 425 us by card, 1290 to 1360 TFLOP/s): LDS reads and matrix
@@ -54,7 +54,7 @@ struct TileOperand {
   unsigned voff[UNITS];                    // a lane's bytes from the tile's first row (and the stage's first step)
   int piece;                               // along: which of a row's pieces a lane loads
 
-  static __device__ __forceinline__ int swizzle(int k) { return ((k & 3) | ((k >> 1) & 4)) & (ROWS / 16 - 1); }
+  static __device__ __forceinline__ int swizzle(int k) { return (k & 3) | (ROWS % 128 ? 0 : (k >> 1) & 4); }
 
   // rows (along) or columns (across, in whole eights) past `left` load the last again: their results are not stored.
   // PARTS == 2: the second half of the rows is another matrix's (each with `left`).
@@ -220,7 +220,8 @@ struct FfPart {
 // A wave's results on their way out: EROWS rows of PITCH floats in LDS.
 template <int BM, int BN, int WM, int WN>
 struct TileEpilogue {
-  static constexpr int EROWS = BM / WM < 64 ? BM / WM : 64, PITCH = BN / WN + 4;
+  static constexpr int EROWS = BM / WM % 64 == 0 ? 64 : BM / WM % 48 == 0 ? 48 : 32, PITCH = BN / WN + 4;
+  static_assert(BM / WM % EROWS == 0, "whole passes");
   static constexpr int BYTES = WM * WN * EROWS * PITCH * 4;
 };
 

@@ -32,6 +32,7 @@ int launch_planned(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStr
   const FfPart part = {ws, (p.N + 3) / 4 * 4, plan.splits, plan.stages};
   if (plan.splits == 1) switch (plan.tile) {
       case kTile256: return launch_mode<TYPE, 256, 256, 2, 4, 2, false>(p, part, st);
+      case kTile192: return launch_mode<TYPE, 192, 256, 2, 4, 2, false>(p, part, st);
       case kTile128: return launch_mode<TYPE, 128, 128, 2, 2, 2, false>(p, part, st);
       case kTile64x128: return launch_mode<TYPE, 64, 128, 2, 2, 3, false>(p, part, st);
       default: return launch_mode<TYPE, 64, 64, 2, 2, 4, false>(p, part, st);

@@ -348,9 +348,11 @@ def test_few_rows_and_columns_of_long_rows(B, type):
 
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_every_tile_and_split(B, type):
-    """Sizes that the plan cuts into tiles of 256, 128, 64 x 128 and 64, with one split and with several."""
+    """Sizes that the plan cuts into tiles of 256, 192 x 256, 128, 64 x 128 and 64, each direction, with one split and with
+    several, and with a remainder in a launch of its own."""
     dt = ff.TYPES[type]
-    for M, N, K in ((3600, 3592, 136), (2050, 520, 72), (1032, 1536, 600), (520, 300, 2056), (72, 136, 8200), (264, 1100, 1032)):
+    for M, N, K in ((3600, 3592, 136), (3600, 136, 3592), (136, 3600, 3592), (2500, 4096, 136), (2500, 136, 4096),
+                    (136, 2500, 4096), (4104, 4104, 200), (4104, 200, 4104), (200, 4104, 4104), (2050, 520, 72), (1032, 1536, 600), (520, 300, 2056), (72, 136, 8200), (264, 1100, 1032)):
         print("tiles", type, M, N, K, flush=True)
         g = torch.Generator().manual_seed(K)
         x, w, u = ff.rand(g, M, K, dt), ff.rand(g, N, K, dt, K ** -0.5), ff.rand(g, N, K, dt, K ** -0.5)
