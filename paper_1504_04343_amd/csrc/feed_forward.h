@@ -70,6 +70,8 @@ int launch_ff_rows(const FfProduct& p, float* ws, hipStream_t st);
 inline bool ff_in_place(const void* p, long long ld, long long cols) {
   return !((uintptr_t)p & 15) && ld % 8 == 0 && cols % 8 == 0 && ld < (1LL << 21);
 }
+// Whether the rows of a matrix of 16-bit values begin at multiples of four bytes.
+inline bool ff_words(const FfOperand& m) { return !((uintptr_t)m.p & 3) && m.ld % 2 == 0; }
 
 // dz = dy * act'(z) into rows of ld values (a multiple of 8; zeros behind the N values of a row), and the column sums of the
 // unrounded dz; any of the two may be missing.  z NULL: dz = dy.  `part`: ff_sum_rows(M, N) * N floats.

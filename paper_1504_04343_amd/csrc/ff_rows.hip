@@ -15,7 +15,10 @@
 // Few columns of long rows leave most CUs idle: the contraction is then cut into splits, whose sums ff_join_kernel adds (64
 // outputs of 16384 inputs, bf16: 19.3 us on four CUs, 9.8 in eight splits).
 //
-// Any alignment: gfx950 loads 16 bytes at any address.  A last step that is not whole is loaded value by value.
+// Any alignment: gfx950 loads 16 bytes at any address, at multiples of four as fast as at multiples of sixteen while memory is
+// the bound.  16-bit rows that begin between them (up to 16 rows of x; with more the caller has such weights copied) are loaded
+// from the words below and shifted: 4096 x 4096, bf16, rows 4097 apart, 1 / 16 rows of x: 16.1 / 19.4 us, loaded as they lie
+// 16.0 / 26.7, with a copy first 23 / 29.  A last step that is not whole is loaded value by value.
 #include <algorithm>
 
 #include "activation.h"
@@ -32,6 +35,18 @@ struct Step {  // 16-bit types
   static __device__ __forceinline__ V load(const void* p, long long at) {
     typedef s16x8 U __attribute__((aligned(2)));
     return *(const U*)((const short*)p + at);
+  }
+  // Eight values at any even address, from the four words that hold the first seven and the eighth by itself.  The first word's
+  // lower half may lie in front of the value, in the same four bytes and so in the same page.
+  static __device__ __forceinline__ V load_odd(const void* p, long long at) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    typedef i32x4 U __attribute__((aligned(4)));
+    const unsigned long long a = (unsigned long long)((const short*)p + at);
+    const i32x4 d = *(const U*)(a & ~3ull);
+    const int last = ((const unsigned short*)p)[at + 7], by = a & 2 ? 16 : 0;
+    const i32x4 v = {(int)__builtin_amdgcn_alignbit(d[1], d[0], by), (int)__builtin_amdgcn_alignbit(d[2], d[1], by),
+                     (int)__builtin_amdgcn_alignbit(d[3], d[2], by), by ? (int)__builtin_amdgcn_alignbit(last, d[3], 16) : d[3]};
+    return __builtin_bit_cast(V, v);
   }
   static __device__ __forceinline__ V part(const void* p, long long at, int n) {
     V v = {};
@@ -69,7 +84,7 @@ template <int TYPE, int RM>
 constexpr int kWaves = TYPE == CCT_TYPE_F32 && RM == 1 ? 16 : 8;
 
 // SPLIT: the contraction is cut (a form of its own: what tells it how is a cache line of arguments more, 0.6 of 8 us)
-template <int TYPE, int RM, int EPI, bool SPLIT>
+template <int TYPE, int RM, int EPI, bool SPLIT, bool ODD>
 __global__ __launch_bounds__((kWaves<TYPE, RM> * 64)) void ff_rows_kernel(FfProduct p, FfPart part) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
@@ -89,15 +104,21 @@ __global__ __launch_bounds__((kWaves<TYPE, RM> * 64)) void ff_rows_kernel(FfProd
 
   const int all = p.K / S::K, first = SPLIT ? split * part.stages : 0, whole = SPLIT ? min(all, first + part.stages) : all;  // steps
   V w[BATCH][NB], x[BATCH][RM];
+  auto fetch = [](const void* from, long long at) {
+    if constexpr (ODD)
+      return S::load_odd(from, at);
+    else
+      return S::load(from, at);
+  };
   // steps past the last one load it again and multiply zeros
   auto load = [&](int s0) {
 #pragma unroll
     for (int q = 0; q < BATCH; ++q) {
       const long long k = (long long)min(s0 + q * NW, whole - 1) * S::K + kq;
-      w[q][0] = S::load(p.B[0].p, w_at + k);
-      if constexpr (NB == 2) w[q][1] = S::load(p.B[1].p, u_at + k);
+      w[q][0] = fetch(p.B[0].p, w_at + k);
+      if constexpr (NB == 2) w[q][1] = fetch(p.B[1].p, u_at + k);
 #pragma unroll
-      for (int i = 0; i < RM; ++i) x[q][i] = S::load(p.A[0].p, x_at[i] + k);
+      for (int i = 0; i < RM; ++i) x[q][i] = fetch(p.A[0].p, x_at[i] + k);
     }
   };
   auto multiply = [&](int s0) {
@@ -172,20 +193,25 @@ void launch(const FfProduct& p, float* ws, hipStream_t st) {
   FfPart part = {ws, (p.N + 3) / 4 * 4, rows_splits(p.N, p.K, TYPE), 0};
   part.stages = (steps + part.splits - 1) / part.splits;
   part.splits = (steps + part.stages - 1) / part.stages;
-  auto run = [&](auto rm) {
+  auto run = [&](auto rm, auto odd) {
     constexpr int RM = decltype(rm)::value;
+    constexpr bool ODD = decltype(odd)::value;
     const dim3 grid(groups, part.splits), block(kWaves<TYPE, RM> * 64);
     if (part.splits > 1)
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, RM, EPI, true>), grid, block, 0, st, p, part);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, RM, EPI, true, ODD>), grid, block, 0, st, p, part);
     else
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, RM, EPI, false>), grid, block, 0, st, p, part);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_rows_kernel<TYPE, RM, EPI, false, ODD>), grid, block, 0, st, p, part);
   };
-  if (p.M <= 16)
-    run(std::integral_constant<int, 1>());
-  else if (p.M <= 32 || TYPE == CCT_TYPE_F32)
-    run(std::integral_constant<int, 2>());
+  constexpr bool F32 = TYPE == CCT_TYPE_F32;
+  const bool words = F32 || (ff_words(p.A[0]) && ff_words(p.B[0]) && (EPI != kFfGated || ff_words(p.B[1])));
+  if (p.M <= 16 && words)
+    run(std::integral_constant<int, 1>(), std::false_type());
+  else if (p.M <= 16)
+    run(std::integral_constant<int, 1>(), std::integral_constant<bool, !F32>());
+  else if (p.M <= 32 || F32)
+    run(std::integral_constant<int, 2>(), std::false_type());
   else
-    run(std::integral_constant<int, TYPE == CCT_TYPE_F32 ? 2 : 4>());
+    run(std::integral_constant<int, F32 ? 2 : 4>(), std::false_type());
   if (part.splits > 1)
     hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, EPI>), dim3((p.M * part.ld / 4 + 255) / 256), dim3(256), 0, st, p, part);
 }

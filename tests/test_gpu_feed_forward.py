@@ -346,6 +346,38 @@ def test_few_rows_and_columns_of_long_rows(B, type):
             ff.check(name, t, v)
 
 
+@pytest.mark.parametrize("type", list(ff.TYPES))
+def test_few_rows_at_odd_addresses(B, type):
+    """Rows of 16-bit values that begin between multiples of four bytes, all of them or every other one, in x, in the weights
+    or in one weight only; NaN in front of each row, which the loads may touch."""
+    dt = ff.TYPES[type]
+    for M, N, K, pad, off in ((1, 33, 96, 1, 1), (3, 100, 515, 2, 1), (16, 40, 8224, 1, 0), (17, 50, 130, 3, 1),
+                              (32, 20, 264, 1, 3), (64, 72, 520, 2, 1), (60, 90, 1024, 1, 0)):
+        print("odd", type, M, N, K, pad, off, flush=True)
+        g = torch.Generator().manual_seed(K)
+
+        def rows(r, std, pad, off):
+            v = ff.rand(g, r, K, dt, std)
+            flat = torch.full((off + r * (K + pad),), float("nan"), dtype=dt, device="cuda")
+            t = flat[off:].view(r, K + pad)[:, :K]
+            t.copy_(v)
+            return v, t
+
+        for odd_x, odd_w, odd_u in ((1, 1, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1)):
+            (x, xg), (w, wg), (u, ug) = (rows(r, s, pad if o else 8, off if o else 0)
+                                         for r, s, o in ((M, 1.0, odd_x), (N, K ** -0.5, odd_w), (N, K ** -0.5, odd_u)))
+            y, z = ff.empty_gpu(M, N, dt), ff.empty_gpu(M, N, dt)
+            d = B.make_linear_desc(M, N, K, getattr(B, "TYPE_" + type.upper()), B.ACT_GELU)
+            B.cct_linear_forward(d, xg, wg, None, None, y, z, B.alloc_linear_workspace(d, B.PASS_FORWARD))
+            for name, t, v in zip("yz", (y, z), ff.linear_forward("gelu", x, w, None, None)):
+                ff.check(name, t, v)
+            h, gg, uu = (ff.empty_gpu(M, N, dt) for _ in range(3))
+            e = B.make_gated_desc(M, N, K, getattr(B, "TYPE_" + type.upper()), B.ACT_SILU)
+            B.cct_gated_forward(e, xg, wg, ug, h, gg, uu, B.alloc_gated_workspace(e, B.PASS_FORWARD))
+            for name, t, v in zip("hgu", (h, gg, uu), ff.gated_forward("silu", x, w, u)):
+                ff.check(name, t, v)
+
+
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_every_tile_and_split(B, type):
     """Sizes that the plan cuts into tiles of 256, 192 x 256, 128, 64 x 128 and 64, each direction, with one split and with
