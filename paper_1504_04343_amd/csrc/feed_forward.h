@@ -90,7 +90,15 @@ struct FfDzJobs {
   FfDz job[3];
   int count;
 };
-int launch_ff_dz(const FfDzJobs& p, hipStream_t st);
+// What is left of a sum of columns, if dbias is there: rows of partial sums.
+struct FfBiasSum {
+  const float* part;
+  void* dbias;
+  int rows, N, type;
+};
+// Only the first job may have a dbias, which *left finishes: launch_ff_bias_sum or launch_ff_products.
+int launch_ff_dz(const FfDzJobs& p, FfBiasSum* left, hipStream_t st);
+int launch_ff_bias_sum(const FfBiasSum& p, hipStream_t st);
 // dg = dh * u * act'(g), du = dh * act(g), both with rows of ld values as dz above.
 struct FfGatedDz {
   int M, F, type, activation;
@@ -99,6 +107,14 @@ struct FfGatedDz {
   void *dg, *du;
   long long ld;
 };
-int launch_ff_gated_dz(const FfGatedDz& p, hipStream_t st);
+// With copies (no dbias) in the same launch.
+int launch_ff_gated_dz(const FfGatedDz& p, const FfDzJobs& copies, hipStream_t st);
+// Up to kFfTogether products whose B lies across the contraction, nothing added, none of which needs another's results, and
+// a sum of columns: one launch for all, or one after the other.  Those without `out` are not wanted; they are there because
+// the choice is made for all, so that a result's last bits do not depend on what else is asked for.
+constexpr int kFfTogether = 3;
+int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char* pack, float* ws, hipStream_t st);
+int launch_ff_together_bf16(const FfProduct* p, int count, const FfBiasSum& sum, int tile, hipStream_t st);
+int launch_ff_together_f16(const FfProduct* p, int count, const FfBiasSum& sum, int tile, hipStream_t st);
 
 }  // namespace cct

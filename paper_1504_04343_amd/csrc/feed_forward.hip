@@ -195,7 +195,8 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
     FfDzJobs jobs = {};
     operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
     operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, &jobs);
-    rc = launch_ff_dz(jobs, st);
+    FfBiasSum none;
+    rc = launch_ff_dz(jobs, &none, st);
     if (rc != CCT_OK) return rc;
   }
   FfProduct p = plain_product(d.type, d.M, d.N, d.K, false, false, y, ldy);
@@ -235,26 +236,24 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
   if (copy || dbias)
     jobs.job[jobs.count++] = {d.M, d.N, d.type, d.activation, dy, act ? z : nullptr, lddy, ldz, copy ? ws + b.dz : nullptr, b.ld,
                               dbias, (float*)(ws + b.sums)};
-  Matrix mx, mw;
+  Matrix mx = {}, mw = {};
   if (dx && d.M > 0) operand({w, ldw}, d.N, d.K, d.type, ws + b.w, &mw, &jobs);
   if (dw) operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
-  rc = launch_ff_dz(jobs, st);
+  FfBiasSum sum;
+  rc = launch_ff_dz(jobs, &sum, st);
   if (rc != CCT_OK) return rc;
   const Matrix dz = {copy ? ws + b.dz : dy, copy || d.M <= 1 ? b.ld : lddy};
-  if (dx && d.M > 0) {
-    FfProduct p = plain_product(d.type, d.M, d.K, d.N, false, true, dx, lddx);
-    p.A[0] = dz;
-    p.B[0] = mw;
-    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
-    if (rc != CCT_OK) return rc;
+  FfProduct p[2];
+  int count = 0;
+  if (d.M > 0) {
+    p[count] = plain_product(d.type, d.M, d.K, d.N, false, true, dx, lddx);
+    p[count].A[0] = dz;
+    p[count++].B[0] = mw;
   }
-  if (dw) {
-    FfProduct p = plain_product(d.type, d.N, d.K, d.M, true, true, dw, lddw);
-    p.A[0] = dz;
-    p.B[0] = mx;
-    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
-  }
-  return rc;
+  p[count] = plain_product(d.type, d.N, d.K, d.M, true, true, dw, lddw);
+  p[count].A[0] = dz;
+  p[count++].B[0] = mx;
+  return launch_ff_products(p, count, sum, ws + b.pack, (float*)(ws + b.part), st);
 }
 
 int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
@@ -282,7 +281,8 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
     FfDzJobs jobs = {};
     operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
     weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, &jobs);
-    rc = launch_ff_dz(jobs, st);
+    FfBiasSum none;
+    rc = launch_ff_dz(jobs, &none, st);
     if (rc != CCT_OK) return rc;
   }
   FfProduct p = plain_product(d.type, d.M, d.F, d.K, false, false, h, ldh);
@@ -320,31 +320,28 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
   hipStream_t st = (hipStream_t)hip_stream;
   char* ws = (char*)workspace;
   const Matrix dg = {ws + b.dg, b.ld}, du = {ws + b.du, b.ld};
-  rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, ws + b.dg, ws + b.du, b.ld}, st);
-  if (rc != CCT_OK) return rc;
   FfDzJobs jobs = {};
-  Matrix mx, mg, mu;
+  Matrix mx = {}, mg = {}, mu = {};
   if (dx && d.M > 0) weight_pair({wg, ldwg}, {wu, ldwu}, d.F, d.K, d.type, ws + b.wg, ws + b.wu, &mg, &mu, &jobs);
   if (dwg) operand({x, ldx}, d.M, d.K, d.type, ws + b.x, &mx, &jobs);
-  rc = launch_ff_dz(jobs, st);
+  rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, ws + b.dg, ws + b.du, b.ld}, jobs, st);
   if (rc != CCT_OK) return rc;
-  if (dx && d.M > 0) {
-    FfProduct p = plain_product(d.type, d.M, d.K, d.F, false, true, dx, lddx);
-    p.segments = 2;
-    p.A[0] = dg;
-    p.A[1] = du;
-    p.B[0] = mg;
-    p.B[1] = mu;
-    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
-    if (rc != CCT_OK) return rc;
+  FfProduct p[3];
+  int count = 0;
+  if (d.M > 0) {
+    p[count] = plain_product(d.type, d.M, d.K, d.F, false, true, dx, lddx);
+    p[count].segments = 2;
+    p[count].A[0] = dg;
+    p[count].A[1] = du;
+    p[count].B[0] = mg;
+    p[count++].B[1] = mu;
   }
-  for (int i = 0; i < 2 && dwg && rc == CCT_OK; ++i) {
-    FfProduct p = plain_product(d.type, d.F, d.K, d.M, true, true, i ? dwu : dwg, i ? lddwu : lddwg);
-    p.A[0] = i ? du : dg;
-    p.B[0] = mx;
-    rc = launch_ff_product(p, ws + b.pack, (float*)(ws + b.part), st);
+  for (int i = 0; i < 2; ++i) {
+    p[count] = plain_product(d.type, d.F, d.K, d.M, true, true, i ? dwu : dwg, i ? lddwu : lddwg);
+    p[count].A[0] = i ? du : dg;
+    p[count++].B[0] = mx;
   }
-  return rc;
+  return launch_ff_products(p, count, {}, ws + b.pack, (float*)(ws + b.part), st);
 }
 
 }  // extern "C"

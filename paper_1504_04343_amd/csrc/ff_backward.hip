@@ -6,12 +6,12 @@
 //
 // A workgroup takes 256 columns x 64 rows, or 8 where that leaves CUs idle (1531 x 1000: 5.3 us, 9.9 before), a thread 8
 // neighbouring columns of every eighth row: its column sums stay in
-// registers, meet in LDS in a fixed order and leave as one row of partial sums per workgroup, which a second kernel adds in
+// registers, meet in LDS in a fixed order and leave as one row of partial sums per workgroup, which ff_bias_sum.h adds in
 // order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
 #include <algorithm>
 
 #include "activation.h"
-#include "feed_forward.h"
+#include "ff_bias_sum.h"
 
 namespace cct {
 namespace {
@@ -54,10 +54,10 @@ struct DzArgs {
   int first[3], rows[3];  // workgroup that a job begins at, rows of a workgroup
 };
 template <int TYPE>
-__global__ __launch_bounds__(NT) void ff_dz_kernel(DzArgs a) {
-  const int which = ((int)blockIdx.x >= a.first[1]) + ((int)blockIdx.x >= a.first[2]), rows = a.rows[which];
+__device__ __forceinline__ void do_dz(const DzArgs& a, int block) {
+  const int which = (block >= a.first[1]) + (block >= a.first[2]), rows = a.rows[which];
   const FfDz& p = a.job[which];
-  const int group = blockIdx.x - a.first[which], wide = (p.N + kCols - 1) / kCols, down = group / wide;
+  const int group = block - a.first[which], wide = (p.N + kCols - 1) / kCols, down = group / wide;
   const int c0 = (group - down * wide) * kCols;
   const int c = c0 + (threadIdx.x & 31) * 8, lane_row = threadIdx.x >> 5;
   const int r0 = down * rows, r1 = min(r0 + rows, p.M);
@@ -92,30 +92,26 @@ __global__ __launch_bounds__(NT) void ff_dz_kernel(DzArgs a) {
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < NT / 32; ++k) s += sums[k][threadIdx.x];
-  p.part[(long long)down * p.N + col] = s;
+  if (p.M <= rows)
+    store1<TYPE>(p.dbias, col, s);
+  else
+    p.part[(long long)down * p.N + col] = s;
+}
+template <int TYPE>
+__global__ __launch_bounds__(NT) void ff_dz_kernel(DzArgs a) {
+  do_dz<TYPE>(a, blockIdx.x);
 }
 
-// dbias from the rows of partial sums: 16 columns per workgroup, 64 runs of rows that meet in LDS
-constexpr int kSumRuns = 64;
+constexpr int kSumThreads = kBiasColumns * kBiasRuns;
 template <int TYPE>
-__global__ __launch_bounds__(16 * kSumRuns) void ff_bias_sum_kernel(const float* __restrict__ part, int rows, int N, void* dbias) {
-  const int c = threadIdx.x & 15, col = blockIdx.x * 16 + c, q = threadIdx.x >> 4;
-  float s = 0.f;
-  if (col < N)
-    for (int r = q; r < rows; r += kSumRuns) s += part[(long long)r * N + col];
-  __shared__ float sums[kSumRuns][17];
-  sums[q][c] = s;
-  __syncthreads();
-#pragma unroll
-  for (int half = kSumRuns / 2; half > 0; half >>= 1) {
-    if (q < half) sums[q][c] += sums[q + half][c];
-    __syncthreads();
-  }
-  if (q == 0 && col < N) store1<TYPE>(dbias, col, sums[0][c]);
+__global__ __launch_bounds__(kSumThreads) void ff_bias_sum_kernel(FfBiasSum p) {
+  __shared__ float sums[kBiasRuns][kBiasColumns + 1];
+  sum_bias<TYPE, kSumThreads>(p, blockIdx.x, sums);
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows) {
+__global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows, int groups, DzArgs copies) {
+  if ((int)blockIdx.x >= groups) return do_dz<TYPE>(copies, blockIdx.x - groups);
   const int wide = (p.F + kCols - 1) / kCols, down = blockIdx.x / wide;
   const int c = (blockIdx.x - down * wide) * kCols + (threadIdx.x & 31) * 8;
   const int r0 = down * rows, r1 = min(r0 + rows, p.M);
@@ -140,52 +136,65 @@ __global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows) 
 
 namespace {
 int rows_of_group(int M, int N) { return (long long)((M + 63) / 64) * ((N + kCols - 1) / kCols) >= 1024 ? 64 : 8; }
+// Column sums of up to 32 rows need no second launch if a workgroup takes them all (4 rows per thread).
+int rows_of_group(const FfDz& p) { return p.dbias && p.M <= 32 ? 32 : rows_of_group(p.M, p.N); }
+
+// What a launch's workgroups need to know of the jobs, and how many they are.
+int place(const FfDzJobs& p, DzArgs* a, double* ops, double* bytes) {
+  int groups = 0;
+  for (int i = 0; i < 3; ++i) {
+    a->first[i] = i < p.count ? groups : 0x7fffffff;
+    if (i >= p.count) continue;
+    const FfDz& q = a->job[i] = p.job[i];
+    a->rows[i] = rows_of_group(q);
+    groups += (q.M + a->rows[i] - 1) / a->rows[i] * ((q.N + kCols - 1) / kCols);
+    *ops += 2.0 * q.M * q.N;
+    *bytes += (double)type_bytes(q.type) * q.M * q.N * (1 + (q.z != nullptr) + (q.dz != nullptr));
+  }
+  return groups;
+}
 }  // namespace
 int ff_sum_rows(int M, int N) { return (M + rows_of_group(M, N) - 1) / rows_of_group(M, N); }
 
-int launch_ff_dz(const FfDzJobs& p, hipStream_t st) {
+int launch_ff_dz(const FfDzJobs& p, FfBiasSum* left, hipStream_t st) {
+  *left = {};
   if (p.count == 0) return CCT_OK;
   DzArgs a = {};
-  int groups = 0;
   double ops = 0.0, bytes = 0.0;
-  for (int i = 0; i < 3; ++i) {
-    a.first[i] = i < p.count ? groups : 0x7fffffff;
-    if (i >= p.count) continue;
-    const FfDz& q = a.job[i] = p.job[i];
-    a.rows[i] = rows_of_group(q.M, q.N);
-    groups += ff_sum_rows(q.M, q.N) * ((q.N + kCols - 1) / kCols);
-    ops += 2.0 * q.M * q.N;
-    bytes += (double)type_bytes(q.type) * q.M * q.N * (1 + (q.z != nullptr) + (q.dz != nullptr));
-  }
+  const int groups = place(p, &a, &ops, &bytes);
+  const FfDz& q = p.job[0];
+  if (q.dbias && (q.M == 0 || q.M > a.rows[0])) *left = {q.part, q.dbias, ff_sum_rows(q.M, q.N), q.N, q.type};
+  if (groups == 0) return CCT_OK;
   const char* const names[] = {"ff_dz_kernel<f32>", "ff_dz_kernel<bf16>", "ff_dz_kernel<f16>"};
-  if (groups > 0)
-    with_type(p.job[0].type, [&](auto type) {
-      ProfScope ps(names[p.job[0].type], ops, bytes, st);
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_dz_kernel<decltype(type)::value>), dim3(groups), dim3(NT), 0, st, a);
-    });
+  with_type(q.type, [&](auto type) {
+    ProfScope ps(names[q.type], ops, bytes, st);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_dz_kernel<decltype(type)::value>), dim3(groups), dim3(NT), 0, st, a);
+  });
   CCT_CHECK_LAUNCH();
-  for (int i = 0; i < p.count; ++i) {
-    const FfDz& q = p.job[i];
-    if (!q.dbias) continue;
-    const int rows = ff_sum_rows(q.M, q.N);
-    with_type(q.type, [&](auto type) {
-      ProfScope ps("ff_bias_sum_kernel", (double)rows * q.N, 4.0 * rows * q.N, st);
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((q.N + 15) / 16), dim3(16 * kSumRuns), 0,
-                         st, q.part, rows, q.N, q.dbias);
-    });
-    CCT_CHECK_LAUNCH();
-  }
   return CCT_OK;
 }
 
-int launch_ff_gated_dz(const FfGatedDz& p, hipStream_t st) {
-  if (p.M == 0) return CCT_OK;
-  const double n = (double)p.M * p.F, e = type_bytes(p.type);
+int launch_ff_bias_sum(const FfBiasSum& p, hipStream_t st) {
+  if (!p.dbias) return CCT_OK;
   with_type(p.type, [&](auto type) {
-    ProfScope ps("ff_gated_dz_kernel", 6.0 * n, 5.0 * e * n, st);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_gated_dz_kernel<decltype(type)::value>),
-                       dim3((p.F + kCols - 1) / kCols * ff_sum_rows(p.M, p.F)), dim3(NT), 0, st, p,
-                       rows_of_group(p.M, p.F));
+    ProfScope ps("ff_bias_sum_kernel", (double)p.rows * p.N, 4.0 * p.rows * p.N, st);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((p.N + kBiasColumns - 1) / kBiasColumns),
+                       dim3(kSumThreads), 0, st, p);
+  });
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+
+int launch_ff_gated_dz(const FfGatedDz& p, const FfDzJobs& copies, hipStream_t st) {
+  if (p.M == 0) return CCT_OK;  // and nothing to copy: x has no rows, and dx, which takes the weights, has none
+  DzArgs a = {};
+  const double n = (double)p.M * p.F, e = type_bytes(p.type);
+  double ops = 6.0 * n, bytes = 5.0 * e * n;
+  const int groups = (p.F + kCols - 1) / kCols * ff_sum_rows(p.M, p.F), more = place(copies, &a, &ops, &bytes);
+  with_type(p.type, [&](auto type) {
+    ProfScope ps("ff_gated_dz_kernel", ops, bytes, st);
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_gated_dz_kernel<decltype(type)::value>), dim3(groups + more), dim3(NT), 0, st, p,
+                       rows_of_group(p.M, p.F), groups, a);
   });
   CCT_CHECK_LAUNCH();
   return CCT_OK;

@@ -91,12 +91,35 @@ FfProduct part_of(FfProduct p, int m, int n, int rows, int cols) {
   return p;
 }
 
+const char* const kTileNames[] = {"256x256", "192x256", "128x128", "64x128", "64x64"};
+
+int stages_of(const FfProduct& p) { return std::max((p.K + kFfStage - 1) / kFfStage, 1) * p.segments; }
+double operand_bytes(const FfProduct& p) { return 2.0 * p.segments * p.K * ((double)p.M + p.N); }
+
+// An estimate for products in one launch of such tiles: the workgroups' stages (three more for what stands around the
+// contraction) over the places on the card and a quarter of a short one's behind that, or the longest one's.
+double together_micros(const FfProduct* p, int count, const TileCost& c) {
+  double groups = 0, work = 0, bytes = 0;
+  int longest = 0, shortest = 0x7fffffff;
+  for (int i = 0; i < count; ++i) {
+    const double tiles = (double)((p[i].M + c.bm - 1) / c.bm) * ((p[i].N + c.bn - 1) / c.bn);
+    groups += tiles;
+    work += tiles * (stages_of(p[i]) + 3);
+    longest = std::max(longest, stages_of(p[i]));
+    shortest = std::min(shortest, stages_of(p[i]));
+    bytes += operand_bytes(p[i]);
+  }
+  if (groups > 0x7fffffff / 2) return 1e30;
+  const double slots = (double)kCus * c.per_cu;
+  const double us = groups <= kCus ? longest * c.alone[1] : std::max<double>(longest, work / slots + 0.25 * shortest) * c.full[1];
+  return std::max(us, bytes / kBytesPerMicro * std::max(1.0, 170.0 / groups)) + kLaunchMicros;
+}
+
 int launch_tiles(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st) {
   const double mn = (double)p.M * p.N, ops = p.epilogue == kFfGated ? 2 : p.segments;
   const double bytes = 2.0 * ((double)(p.epilogue == kFfGated ? 1 : p.segments) * p.M * p.K + ops * p.N * p.K +
                               mn * (1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)));
-  const char* const names[] = {"256x256", "192x256", "128x128", "64x128", "64x64"};
-  ProfScope ps(2.0 * mn * p.K * ops, bytes, st, "ff_tile_kernel<%s, %d splits>", names[plan.tile], plan.splits);
+  ProfScope ps(2.0 * mn * p.K * ops, bytes, st, "ff_tile_kernel<%s, %d splits>", kTileNames[plan.tile], plan.splits);
   return p.type == CCT_TYPE_BF16 ? launch_ff_tile_bf16(p, plan, ws, st) : launch_ff_tile_f16(p, plan, ws, st);
 }
 
@@ -111,6 +134,38 @@ int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st)
   if (rc != CCT_OK) return rc;
   const FfProduct rest = part_of(p, m, n, p.M - m, p.N - n);
   return launch_tiles(rest, whole_plan(rest.M, rest.N, rest.K, rest.epilogue, rest.segments, !rest.b_across), ws, st);
+}
+
+int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char* pack, float* ws, hipStream_t st) {
+  int tile = -1;
+  if (count > 1 && p[0].type != CCT_TYPE_F32) {
+    double least = 0;
+    for (int i = 0; i < count; ++i) least += ff_tile_plan(p[i].M, p[i].N, p[i].K, p[i].epilogue, p[i].segments, false).micros;
+    for (int t = kTile128; t <= kTile64; ++t) {
+      const double us = together_micros(p, count, kTileCosts[t]);
+      if (us < least) {
+        least = us;
+        tile = t;
+      }
+    }
+  }
+  FfProduct wanted[kFfTogether];
+  const int n = (int)(std::copy_if(p, p + count, wanted, [](const FfProduct& q) { return q.out != nullptr; }) - wanted);
+  if (tile < 0 || n == 0) {
+    int rc = launch_ff_bias_sum(sum, st);
+    for (int i = 0; i < n && rc == CCT_OK; ++i) rc = launch_ff_product(wanted[i], pack, ws, st);
+    return rc;
+  }
+  // the longest contractions first
+  std::stable_sort(wanted, wanted + n, [](const FfProduct& a, const FfProduct& b) { return stages_of(a) > stages_of(b); });
+  double flops = 0, bytes = 0;
+  for (int i = 0; i < n; ++i) {
+    flops += 2.0 * wanted[i].M * wanted[i].N * wanted[i].K * wanted[i].segments;
+    bytes += operand_bytes(wanted[i]) + 2.0 * wanted[i].M * wanted[i].N;
+  }
+  ProfScope ps(flops, bytes, st, "ff_tile_kernel_together<%s, %d products>", kTileNames[tile], n);
+  return p[0].type == CCT_TYPE_BF16 ? launch_ff_together_bf16(wanted, n, sum, tile, st)
+                                    : launch_ff_together_f16(wanted, n, sum, tile, st);
 }
 
 }  // namespace cct

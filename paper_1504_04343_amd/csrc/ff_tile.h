@@ -23,7 +23,7 @@
 // The weights' side is the instruction's first operand: a lane then holds 4 neighbouring columns of one row of the result.
 #pragma once
 #include "activation.h"
-#include "feed_forward.h"
+#include "ff_bias_sum.h"
 #include "gemm_common.h"
 
 namespace cct {
@@ -227,7 +227,7 @@ struct TileEpilogue {
 
 // BM x BN results (kFfGated: BM x BN / 2 of each product) with WM x WN waves; RING stages in LDS; SPLIT: the sums go to `part`.
 template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
-__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void ff_tile_kernel(FfProduct p, int tiles_m, int tiles_n, FfPart part) {
+__device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, int tiles_n, const FfPart& part, int index) {
   constexpr int NW = WM * WN, RB = BM / WM / 16, CB = BN / WN / 16;
   constexpr int PARTS = EPI == kFfGated ? 2 : 1;
   typedef TileOperand<BM, NW, AX> OpA;
@@ -238,9 +238,9 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
   // splits of a tile lie far apart: what runs at a time shares stages of the contraction
-  const int tiles = tiles_m * tiles_n, split = SPLIT ? blockIdx.x / tiles : 0;
+  const int tiles = tiles_m * tiles_n, split = SPLIT ? index / tiles : 0;
   int tm, tn;
-  tile_of(blockIdx.x - split * tiles, tiles, tiles_m, tiles_n, &tm, &tn);
+  tile_of(index - split * tiles, tiles, tiles_m, tiles_n, &tm, &tn);
   const int m0 = tm * BM, n0 = tn * (BN / PARTS);
   const int left_m = p.M - m0, left_n = p.N - n0;
 
@@ -407,6 +407,37 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
+__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void ff_tile_kernel(FfProduct p, int tiles_m, int tiles_n, FfPart part) {
+  compute_tile<TYPE, BM, BN, WM, WN, RING, AX, BX, EPI, SPLIT>(p, tiles_m, tiles_n, part, blockIdx.x);
+}
+
+// The products of a backward pass, which do not wait for one another, in one launch: the first workgroups finish a sum of
+// columns, those from first[i] on are p[i]'s.  Alone each leaves CUs idle at its end, or all along; a launch more is 5 us where
+// the host is the bound.  bf16, backward, one after the other and so: linear 1024 x 1024 x 1024 25.2 -> 18.1 us, 2048 x 2048 x
+// 2048 68 -> 53; gated 512 x 512 x 512 27.6 -> 17.1, 2048 x 2048 x 2048 123 -> 93; fp16 linear 1531 x 1000 x 2049 61.7 -> 44.2.
+struct FfTogether {
+  int count, first[kFfTogether], tiles_m[kFfTogether], tiles_n[kFfTogether];
+  FfProduct p[kFfTogether];
+  FfBiasSum sum;
+};
+template <int TYPE, int BM, int BN, int WM, int WN, int RING>
+__global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void ff_tile_kernel_together(FfTogether a) {
+  if ((int)blockIdx.x < a.first[0]) {
+    __shared__ float sums[WM * WN * 64 / kBiasColumns][kBiasColumns + 1];
+    return sum_bias<TYPE, WM * WN * 64>(a.sum, blockIdx.x, sums);
+  }
+  int i = 0;
+#pragma unroll
+  for (int q = 1; q < kFfTogether; ++q) i += q < a.count && (int)blockIdx.x >= a.first[q];
+  const int index = blockIdx.x - a.first[i];
+  const FfPart none = {};
+  if (a.p[i].a_across)
+    compute_tile<TYPE, BM, BN, WM, WN, RING, true, true, kFfLinear, false>(a.p[i], a.tiles_m[i], a.tiles_n[i], none, index);
+  else
+    compute_tile<TYPE, BM, BN, WM, WN, RING, false, true, kFfLinear, false>(a.p[i], a.tiles_m[i], a.tiles_n[i], none, index);
 }
 
 // The splits' sums added in order, and finished.  A thread takes 4 columns of a row.

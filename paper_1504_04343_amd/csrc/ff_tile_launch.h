@@ -53,5 +53,35 @@ int launch_planned(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStr
   return CCT_OK;
 }
 
+template <int TYPE, int BM, int BN, int WM, int WN, int RING>
+int launch_together(const FfProduct* p, int count, const FfBiasSum& sum, hipStream_t st) {
+  constexpr int ring = RING * (BM + BN) * SK * 2, out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
+  constexpr auto kernel = ff_tile_kernel_together<TYPE, BM, BN, WM, WN, RING>;
+  const int rc = ensure_dynamic_lds<kernel>(lds);
+  if (rc != CCT_OK) return rc;
+  FfTogether a = {};
+  a.count = count;
+  a.sum = sum;
+  int groups = sum.dbias ? (sum.N + kBiasColumns - 1) / kBiasColumns : 0;
+  for (int i = 0; i < count; ++i) {
+    a.p[i] = p[i];
+    a.first[i] = groups;
+    a.tiles_m[i] = (p[i].M + BM - 1) / BM;
+    a.tiles_n[i] = (p[i].N + BN - 1) / BN;
+    groups += a.tiles_m[i] * a.tiles_n[i];
+  }
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(WM * WN * 64), lds, st, a);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
+}
+template <int TYPE>
+int launch_together(const FfProduct* p, int count, const FfBiasSum& sum, int tile, hipStream_t st) {
+  switch (tile) {
+    case kTile128: return launch_together<TYPE, 128, 128, 2, 2, 2>(p, count, sum, st);
+    case kTile64x128: return launch_together<TYPE, 64, 128, 2, 2, 3>(p, count, sum, st);
+    default: return launch_together<TYPE, 64, 64, 2, 2, 4>(p, count, sum, st);
+  }
+}
+
 }  // namespace
 }  // namespace cct

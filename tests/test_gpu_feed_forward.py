@@ -379,6 +379,29 @@ def test_few_rows_at_odd_addresses(B, type):
 
 
 @pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_backward_products_in_one_launch(B, type):
+    """Sizes whose products share a launch, in tiles of 64, 64 x 128 and 128, ragged, with the sum of columns beside them (by
+    one workgroup of rows, by several) and without; every result alone and in pairs has the same bits."""
+    dt = ff.TYPES[type]
+    for M, N, K, pad, off in ((20, 100, 300, 0, 0), (33, 72, 136, 1, 1), (500, 300, 500, 5, 0), (1030, 1023, 1030, 0, 0),
+                              (1531, 1000, 2049, 3, 0), (2000, 1500, 700, 0, 0)):
+        print("together", type, M, N, K, flush=True)
+        g = torch.Generator().manual_seed(M)
+        x, w, u = (ff.rand(g, r, K, dt, s, pad, off) for r, s in ((M, 1.0), (N, K ** -0.5), (N, K ** -0.5)))
+        z, dy, uu = (ff.rand(g, M, N, dt, 1.0, pad, off) for _ in range(3))
+        names = ("dx", "dw", "dbias")
+        got = linear_backward(B, type, "gelu", x, w, z, dy, pad)
+        for name, t, v in zip(names, got, ff.linear_backward("gelu", x, w, z, dy)):
+            ff.check(name, t, v)
+        for want in (("dx", "dw"), ("dx", "dbias"), ("dw", "dbias"), ("dx",), ("dw",), ("dbias",)):
+            some = linear_backward(B, type, "gelu", x, w, z, dy, pad, want)
+            assert all(torch.equal(some[i], got[i]) for i in range(3) if names[i] in want), want
+        for name, t, v in zip(("dx", "dwg", "dwu"), gated_backward(B, type, "silu", x, w, u, z, uu, dy, pad),
+                              ff.gated_backward("silu", x, w, u, z, uu, dy)):
+            ff.check(name, t, v)
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_every_tile_and_split(B, type):
     """Sizes that the plan cuts into tiles of 256, 192 x 256, 128, 64 x 128 and 64, each direction, with one split and with
     several, and with a remainder in a launch of its own."""
