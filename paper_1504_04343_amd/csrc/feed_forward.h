@@ -114,7 +114,15 @@ int launch_ff_gated_dz(const FfGatedDz& p, const FfDzJobs& copies, hipStream_t s
 // the choice is made for all, so that a result's last bits do not depend on what else is asked for.
 constexpr int kFfTogether = 3;
 int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char* pack, float* ws, hipStream_t st);
-int launch_ff_together_bf16(const FfProduct* p, int count, const FfBiasSum& sum, int tile, hipStream_t st);
-int launch_ff_together_f16(const FfProduct* p, int count, const FfBiasSum& sum, int tile, hipStream_t st);
+// That choice (16-bit types), which follows from sizes alone: tile < 0 if one after the other; splits, stages of one, and where
+// in `ws` each product's partial sums lie.
+struct FfTogetherPlan {
+  int tile, splits[kFfTogether], stages[kFfTogether];
+  long long at[kFfTogether], part_bytes;
+  double micros;
+};
+FfTogetherPlan ff_together_plan(const FfProduct* p, int count);
+int launch_ff_together_bf16(const FfProduct* p, int count, const FfBiasSum& sum, const FfTogetherPlan& plan, char* ws, hipStream_t st);
+int launch_ff_together_f16(const FfProduct* p, int count, const FfBiasSum& sum, const FfTogetherPlan& plan, char* ws, hipStream_t st);
 
 }  // namespace cct

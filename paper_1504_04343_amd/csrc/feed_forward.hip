@@ -62,6 +62,48 @@ Room forward_room(int type, int M, int N, int K, int epilogue) {
 }
 Room larger(const Room& a, const Room& b) { return {std::max(a.pack, b.pack), std::max(a.part, b.part)}; }
 
+// out (rows x cols) = sum over segments of A_s B_s^T, rounded, nothing else
+FfProduct plain_product(int type, int rows, int cols, int k, bool a_across, bool b_across, void* out, long long ldo) {
+  FfProduct p = {};
+  p.M = rows;
+  p.N = cols;
+  p.K = k;
+  p.type = type;
+  p.a_across = a_across;
+  p.b_across = b_across;
+  p.segments = 1;
+  p.epilogue = kFfLinear;
+  p.activation = CCT_ACT_NONE;
+  p.out = out;
+  p.ldo = ldo;
+  return p;
+}
+
+// The products of a backward pass, with their results' places and nothing else yet; their number.
+int linear_gradients(const cct_linear_desc_t& d, void* dx, long long lddx, void* dw, long long lddw, FfProduct* p) {
+  int count = 0;
+  if (d.M > 0) p[count++] = plain_product(d.type, d.M, d.K, d.N, false, true, dx, lddx);
+  p[count++] = plain_product(d.type, d.N, d.K, d.M, true, true, dw, lddw);
+  return count;
+}
+int gated_gradients(const cct_gated_desc_t& d, void* dx, long long lddx, void* dwg, long long lddwg, void* dwu, long long lddwu,
+                    FfProduct* p) {
+  int count = 0;
+  if (d.M > 0) {
+    p[count] = plain_product(d.type, d.M, d.K, d.F, false, true, dx, lddx);
+    p[count++].segments = 2;
+  }
+  p[count++] = plain_product(d.type, d.F, d.K, d.M, true, true, dwg, lddwg);
+  p[count++] = plain_product(d.type, d.F, d.K, d.M, true, true, dwu, lddwu);
+  return count;
+}
+// Room for them in one launch, or one after the other.
+Room backward_room(const FfProduct* p, int count) {
+  Room r = {0, p[0].type == CCT_TYPE_F32 ? 0 : ff_together_plan(p, count).part_bytes};
+  for (int i = 0; i < count; ++i) r = larger(r, room(p[i].type, p[i].M, p[i].N, p[i].K, kFfLinear, p[i].segments, false));
+  return r;
+}
+
 struct LinearLayout {
   long long x, w, dz, sums, pack, part, ld, total;
 };
@@ -73,9 +115,8 @@ LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   b.ld = up(d.N, 8);
   b.dz = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.sums = l.take(backward ? (long long)ff_sum_rows(d.M, d.N) * d.N * 4 : 0);
-  // the two gradients are one after the other
-  const Room r = backward ? larger(room(d.type, d.M, d.K, d.N, kFfLinear, 1, false), room(d.type, d.N, d.K, d.M, kFfLinear, 1, false))
-                          : forward_room(d.type, d.M, d.N, d.K, kFfLinear);
+  FfProduct p[2];
+  const Room r = backward ? backward_room(p, linear_gradients(d, nullptr, 0, nullptr, 0, p)) : forward_room(d.type, d.M, d.N, d.K, kFfLinear);
   b.pack = l.take(r.pack);
   b.part = l.take(r.part);
   b.total = std::max(l.total, 256LL);
@@ -93,7 +134,8 @@ GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   b.ld = up(d.F, 8);
   b.dg = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.du = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
-  const Room r = backward ? larger(room(d.type, d.M, d.K, d.F, kFfLinear, 2, false), room(d.type, d.F, d.K, d.M, kFfLinear, 1, false))
+  FfProduct p[3];
+  const Room r = backward ? backward_room(p, gated_gradients(d, nullptr, 0, nullptr, 0, nullptr, 0, p))
                           : forward_room(d.type, d.M, d.F, d.K, kFfGated);
   b.pack = l.take(r.pack);
   b.part = l.take(r.part);
@@ -127,24 +169,6 @@ void weight_pair(const Matrix& g, const Matrix& u, long long rows, long long col
   if (type == CCT_TYPE_F32 || use_g->ld == use_u->ld) return;
   if (use_g->p != to_g) add_copy(g, rows, cols, type, to_g, use_g, jobs);
   if (use_u->p != to_u) add_copy(u, rows, cols, type, to_u, use_u, jobs);
-}
-
-
-// out (rows x cols) = sum over segments of A_s B_s^T, rounded, nothing else
-FfProduct plain_product(int type, int rows, int cols, int k, bool a_across, bool b_across, void* out, long long ldo) {
-  FfProduct p = {};
-  p.M = rows;
-  p.N = cols;
-  p.K = k;
-  p.type = type;
-  p.a_across = a_across;
-  p.b_across = b_across;
-  p.segments = 1;
-  p.epilogue = kFfLinear;
-  p.activation = CCT_ACT_NONE;
-  p.out = out;
-  p.ldo = ldo;
-  return p;
 }
 
 }  // namespace
@@ -244,15 +268,11 @@ int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ld
   if (rc != CCT_OK) return rc;
   const Matrix dz = {copy ? ws + b.dz : dy, copy || d.M <= 1 ? b.ld : lddy};
   FfProduct p[2];
-  int count = 0;
-  if (d.M > 0) {
-    p[count] = plain_product(d.type, d.M, d.K, d.N, false, true, dx, lddx);
-    p[count].A[0] = dz;
-    p[count++].B[0] = mw;
+  const int count = linear_gradients(d, dx, lddx, dw, lddw, p);
+  for (int i = 0; i < count; ++i) {
+    p[i].A[0] = dz;
+    p[i].B[0] = i == count - 1 ? mx : mw;
   }
-  p[count] = plain_product(d.type, d.N, d.K, d.M, true, true, dw, lddw);
-  p[count].A[0] = dz;
-  p[count++].B[0] = mx;
   return launch_ff_products(p, count, sum, ws + b.pack, (float*)(ws + b.part), st);
 }
 
@@ -327,19 +347,16 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
   rc = launch_ff_gated_dz({d.M, d.F, d.type, d.activation, dh, g, u, lddh, ldg, ldu, ws + b.dg, ws + b.du, b.ld}, jobs, st);
   if (rc != CCT_OK) return rc;
   FfProduct p[3];
-  int count = 0;
+  const int count = gated_gradients(d, dx, lddx, dwg, lddwg, dwu, lddwu, p);
   if (d.M > 0) {
-    p[count] = plain_product(d.type, d.M, d.K, d.F, false, true, dx, lddx);
-    p[count].segments = 2;
-    p[count].A[0] = dg;
-    p[count].A[1] = du;
-    p[count].B[0] = mg;
-    p[count++].B[1] = mu;
+    p[0].A[0] = dg;
+    p[0].A[1] = du;
+    p[0].B[0] = mg;
+    p[0].B[1] = mu;
   }
-  for (int i = 0; i < 2; ++i) {
-    p[count] = plain_product(d.type, d.F, d.K, d.M, true, true, i ? dwu : dwg, i ? lddwu : lddwg);
-    p[count].A[0] = i ? du : dg;
-    p[count++].B[0] = mx;
+  for (int i = count - 2; i < count; ++i) {
+    p[i].A[0] = i == count - 2 ? dg : du;
+    p[i].B[0] = mx;
   }
   return launch_ff_products(p, count, {}, ws + b.pack, (float*)(ws + b.part), st);
 }

@@ -93,28 +93,6 @@ FfProduct part_of(FfProduct p, int m, int n, int rows, int cols) {
 
 const char* const kTileNames[] = {"256x256", "192x256", "128x128", "64x128", "64x64"};
 
-int stages_of(const FfProduct& p) { return std::max((p.K + kFfStage - 1) / kFfStage, 1) * p.segments; }
-double operand_bytes(const FfProduct& p) { return 2.0 * p.segments * p.K * ((double)p.M + p.N); }
-
-// An estimate for products in one launch of such tiles: the workgroups' stages (three more for what stands around the
-// contraction) over the places on the card and a quarter of a short one's behind that, or the longest one's.
-double together_micros(const FfProduct* p, int count, const TileCost& c) {
-  double groups = 0, work = 0, bytes = 0;
-  int longest = 0, shortest = 0x7fffffff;
-  for (int i = 0; i < count; ++i) {
-    const double tiles = (double)((p[i].M + c.bm - 1) / c.bm) * ((p[i].N + c.bn - 1) / c.bn);
-    groups += tiles;
-    work += tiles * (stages_of(p[i]) + 3);
-    longest = std::max(longest, stages_of(p[i]));
-    shortest = std::min(shortest, stages_of(p[i]));
-    bytes += operand_bytes(p[i]);
-  }
-  if (groups > 0x7fffffff / 2) return 1e30;
-  const double slots = (double)kCus * c.per_cu;
-  const double us = groups <= kCus ? longest * c.alone[1] : std::max<double>(longest, work / slots + 0.25 * shortest) * c.full[1];
-  return std::max(us, bytes / kBytesPerMicro * std::max(1.0, 170.0 / groups)) + kLaunchMicros;
-}
-
 int launch_tiles(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st) {
   const double mn = (double)p.M * p.N, ops = p.epilogue == kFfGated ? 2 : p.segments;
   const double bytes = 2.0 * ((double)(p.epilogue == kFfGated ? 1 : p.segments) * p.M * p.K + ops * p.N * p.K +
@@ -136,36 +114,85 @@ int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st)
   return launch_tiles(rest, whole_plan(rest.M, rest.N, rest.K, rest.epilogue, rest.segments, !rest.b_across), ws, st);
 }
 
-int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char* pack, float* ws, hipStream_t st) {
-  int tile = -1;
-  if (count > 1 && p[0].type != CCT_TYPE_F32) {
-    double least = 0;
-    for (int i = 0; i < count; ++i) least += ff_tile_plan(p[i].M, p[i].N, p[i].K, p[i].epilogue, p[i].segments, false).micros;
-    for (int t = kTile128; t <= kTile64; ++t) {
-      const double us = together_micros(p, count, kTileCosts[t]);
-      if (us < least) {
-        least = us;
-        tile = t;
+namespace {
+int stages_of(const FfProduct& p) { return std::max((p.K + kFfStage - 1) / kFfStage, 1) * p.segments; }
+double operand_bytes(const FfProduct& p) { return 2.0 * p.segments * p.K * ((double)p.M + p.N); }
+}  // namespace
+
+// The tile, and the stages that a workgroup has at most, with the least estimate: the workgroups' stages (three more for what
+// stands around the contraction) over the places on the card and a quarter of a short one's behind that, or the longest one's,
+// and what joining costs.  4096 rows, gated 256 -> 1024,
+// backward: 43 us so, 59 without splits.
+FfTogetherPlan ff_together_plan(const FfProduct* p, int count) {
+  FfTogetherPlan best = {};
+  best.tile = -1;
+  if (count < 2) return best;
+  for (int i = 0; i < count; ++i) best.micros += ff_tile_plan(p[i].M, p[i].N, p[i].K, p[i].epilogue, p[i].segments, false).micros;
+  for (int tile = kTile128; tile <= kTile64; ++tile) {
+    const TileCost& c = kTileCosts[tile];
+    for (int most = kLeastStages; most <= 512; most *= 2) {
+      FfTogetherPlan plan = {};
+      double groups = 0, work = 0, bytes = 0, joined = 0;
+      int longest = 0, shortest = 0x7fffffff;
+      for (int i = 0; i < count; ++i) {
+        const int all = stages_of(p[i]);
+        const int splits = std::min(32, std::max(1, (all + most - 1) / most)), each = (all + splits - 1) / splits;
+        plan.splits[i] = (all + each - 1) / each;
+        plan.stages[i] = each;
+        plan.at[i] = plan.part_bytes;
+        if (plan.splits[i] > 1) {
+          const double values = (double)p[i].M * ((p[i].N + 3) / 4 * 4) * plan.splits[i];
+          plan.part_bytes += ((long long)values * 4 + 255) / 256 * 256;
+          joined += 8.0 * values;
+        }
+        const double tiles = (double)((p[i].M + c.bm - 1) / c.bm) * ((p[i].N + c.bn - 1) / c.bn) * plan.splits[i];
+        groups += tiles;
+        work += tiles * (each + 3);
+        longest = std::max(longest, each);
+        shortest = std::min(shortest, each);
+        bytes += operand_bytes(p[i]);
       }
+      if (groups > 1 << 30) break;
+      const double slots = (double)kCus * c.per_cu;
+      const double us = groups <= kCus ? longest * c.alone[1] : std::max<double>(longest, work / slots + 0.25 * shortest) * c.full[1];
+      plan.tile = tile;
+      plan.micros = std::max(us, bytes / kBytesPerMicro * std::max(1.0, 170.0 / groups)) + kLaunchMicros;
+      if (joined > 0) plan.micros += kJoinMicros + joined / kJoinBytesPerMicro;
+      if (plan.micros < best.micros) best = plan;
+      if (joined == 0) break;  // more stages split nothing either
     }
   }
-  FfProduct wanted[kFfTogether];
-  const int n = (int)(std::copy_if(p, p + count, wanted, [](const FfProduct& q) { return q.out != nullptr; }) - wanted);
-  if (tile < 0 || n == 0) {
+  return best;
+}
+
+int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char* pack, float* ws, hipStream_t st) {
+  FfTogetherPlan plan = {};
+  plan.tile = -1;
+  if (p[0].type != CCT_TYPE_F32) plan = ff_together_plan(p, count);
+  int order[kFfTogether], n = 0;
+  for (int i = 0; i < count; ++i)
+    if (p[i].out) order[n++] = i;
+  if (plan.tile < 0 || n == 0) {
     int rc = launch_ff_bias_sum(sum, st);
-    for (int i = 0; i < n && rc == CCT_OK; ++i) rc = launch_ff_product(wanted[i], pack, ws, st);
+    for (int i = 0; i < n && rc == CCT_OK; ++i) rc = launch_ff_product(p[order[i]], pack, ws, st);
     return rc;
   }
-  // the longest contractions first
-  std::stable_sort(wanted, wanted + n, [](const FfProduct& a, const FfProduct& b) { return stages_of(a) > stages_of(b); });
+  // the longest first
+  std::stable_sort(order, order + n, [&](int a, int b) { return plan.stages[a] > plan.stages[b]; });
+  FfProduct wanted[kFfTogether];
+  FfTogetherPlan theirs = plan;
   double flops = 0, bytes = 0;
   for (int i = 0; i < n; ++i) {
-    flops += 2.0 * wanted[i].M * wanted[i].N * wanted[i].K * wanted[i].segments;
-    bytes += operand_bytes(wanted[i]) + 2.0 * wanted[i].M * wanted[i].N;
+    const FfProduct& q = wanted[i] = p[order[i]];
+    theirs.splits[i] = plan.splits[order[i]];
+    theirs.stages[i] = plan.stages[order[i]];
+    theirs.at[i] = plan.at[order[i]];
+    flops += 2.0 * q.M * q.N * q.K * q.segments;
+    bytes += operand_bytes(q) + 2.0 * q.M * q.N;
   }
-  ProfScope ps(flops, bytes, st, "ff_tile_kernel_together<%s, %d products>", kTileNames[tile], n);
-  return p[0].type == CCT_TYPE_BF16 ? launch_ff_together_bf16(wanted, n, sum, tile, st)
-                                    : launch_ff_together_f16(wanted, n, sum, tile, st);
+  ProfScope ps(flops, bytes, st, "ff_tile_kernel_together<%s, %d products>", kTileNames[plan.tile], n);
+  return p[0].type == CCT_TYPE_BF16 ? launch_ff_together_bf16(wanted, n, sum, theirs, (char*)ws, st)
+                                    : launch_ff_together_f16(wanted, n, sum, theirs, (char*)ws, st);
 }
 
 }  // namespace cct

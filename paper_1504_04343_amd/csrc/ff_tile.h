@@ -225,8 +225,10 @@ struct TileEpilogue {
   static constexpr int BYTES = WM * WN * EROWS * PITCH * 4;
 };
 
-// BM x BN results (kFfGated: BM x BN / 2 of each product) with WM x WN waves; RING stages in LDS; SPLIT: the sums go to `part`.
-template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
+// BM x BN results (kFfGated: BM x BN / 2 of each product) with WM x WN waves; RING stages in LDS; SPLIT: the sums go to `part`,
+// always or if it says so.
+enum { kWhole, kSplit, kEither };
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, int SPLIT>
 __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, int tiles_n, const FfPart& part, int index) {
   constexpr int NW = WM * WN, RB = BM / WM / 16, CB = BN / WN / 16;
   constexpr int PARTS = EPI == kFfGated ? 2 : 1;
@@ -341,7 +343,7 @@ __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, in
   __builtin_amdgcn_s_waitcnt(0x0f70);  // the empty loads write LDS too
 
   constexpr int OUT = CB / PARTS;  // blocks of columns of the result
-  if constexpr (SPLIT) {
+  if (SPLIT == kSplit || (SPLIT == kEither && part.splits > 1)) {
 #pragma unroll
     for (int i = 0; i < RB; ++i) {
       const int m = m0 + wm * (BM / WM) + i * 16 + (lane & 15);
@@ -409,7 +411,7 @@ __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, in
   }
 }
 
-template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, bool SPLIT>
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, int SPLIT>
 __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void ff_tile_kernel(FfProduct p, int tiles_m, int tiles_n, FfPart part) {
   compute_tile<TYPE, BM, BN, WM, WN, RING, AX, BX, EPI, SPLIT>(p, tiles_m, tiles_n, part, blockIdx.x);
 }
@@ -418,8 +420,10 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
 // columns, those from first[i] on are p[i]'s.  Alone each leaves CUs idle at its end, or all along; a launch more is 5 us where
 // the host is the bound.  bf16, backward, one after the other and so: linear 1024 x 1024 x 1024 25.2 -> 18.1 us, 2048 x 2048 x
 // 2048 68 -> 53; gated 512 x 512 x 512 27.6 -> 17.1, 2048 x 2048 x 2048 123 -> 93; fp16 linear 1531 x 1000 x 2049 61.7 -> 44.2.
+// Contractions in splits, which one ff_join_kernel_together adds: gated 60 x 1301 x 64 27.7 -> 19.5, 1024 x 4096 x 1024 87 -> 70.
 struct FfTogether {
   int count, first[kFfTogether], tiles_m[kFfTogether], tiles_n[kFfTogether];
+  FfPart part[kFfTogether];
   FfProduct p[kFfTogether];
   FfBiasSum sum;
 };
@@ -433,19 +437,18 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
   for (int q = 1; q < kFfTogether; ++q) i += q < a.count && (int)blockIdx.x >= a.first[q];
   const int index = blockIdx.x - a.first[i];
-  const FfPart none = {};
   if (a.p[i].a_across)
-    compute_tile<TYPE, BM, BN, WM, WN, RING, true, true, kFfLinear, false>(a.p[i], a.tiles_m[i], a.tiles_n[i], none, index);
+    compute_tile<TYPE, BM, BN, WM, WN, RING, true, true, kFfLinear, kEither>(a.p[i], a.tiles_m[i], a.tiles_n[i], a.part[i], index);
   else
-    compute_tile<TYPE, BM, BN, WM, WN, RING, false, true, kFfLinear, false>(a.p[i], a.tiles_m[i], a.tiles_n[i], none, index);
+    compute_tile<TYPE, BM, BN, WM, WN, RING, false, true, kFfLinear, kEither>(a.p[i], a.tiles_m[i], a.tiles_n[i], a.part[i], index);
 }
 
 // The splits' sums added in order, and finished.  A thread takes 4 columns of a row.
 template <int TYPE, int EPI>
-__global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p, FfPart part) {
+__device__ __forceinline__ void join(const FfProduct& p, const FfPart& part, int block) {
   constexpr int PARTS = EPI == kFfGated ? 2 : 1;
   const int wide = part.ld / 4;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long at = (long long)block * 256 + threadIdx.x;
   const int m = (int)(at / wide), n = (int)(at - (long long)m * wide) * 4;
   if (m >= p.M) return;
   f32x4 sum[PARTS];
@@ -462,6 +465,18 @@ __global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p, FfPart part) 
     u[e] = sum[PARTS - 1][e];
   }
   finish<TYPE, EPI>(p, m, n, v, u);
+}
+template <int TYPE, int EPI>
+__global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p, FfPart part) {
+  join<TYPE, EPI>(p, part, blockIdx.x);
+}
+// Those of several products: workgroups from first[i] on are p[i]'s.
+template <int TYPE>
+__global__ __launch_bounds__(256) void ff_join_kernel_together(FfTogether a) {
+  int i = 0;
+#pragma unroll
+  for (int q = 1; q < kFfTogether; ++q) i += q < a.count && (int)blockIdx.x >= a.first[q];
+  join<TYPE, kFfLinear>(a.p[i], a.part[i], blockIdx.x - a.first[i]);
 }
 
 }  // namespace

@@ -54,33 +54,47 @@ int launch_planned(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStr
 }
 
 template <int TYPE, int BM, int BN, int WM, int WN, int RING>
-int launch_together(const FfProduct* p, int count, const FfBiasSum& sum, hipStream_t st) {
+int launch_together(FfTogether a, hipStream_t st) {
   constexpr int ring = RING * (BM + BN) * SK * 2, out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
   constexpr auto kernel = ff_tile_kernel_together<TYPE, BM, BN, WM, WN, RING>;
   const int rc = ensure_dynamic_lds<kernel>(lds);
   if (rc != CCT_OK) return rc;
-  FfTogether a = {};
-  a.count = count;
-  a.sum = sum;
-  int groups = sum.dbias ? (sum.N + kBiasColumns - 1) / kBiasColumns : 0;
-  for (int i = 0; i < count; ++i) {
-    a.p[i] = p[i];
+  int groups = a.sum.dbias ? (a.sum.N + kBiasColumns - 1) / kBiasColumns : 0;
+  for (int i = 0; i < a.count; ++i) {
     a.first[i] = groups;
-    a.tiles_m[i] = (p[i].M + BM - 1) / BM;
-    a.tiles_n[i] = (p[i].N + BN - 1) / BN;
-    groups += a.tiles_m[i] * a.tiles_n[i];
+    a.tiles_m[i] = (a.p[i].M + BM - 1) / BM;
+    a.tiles_n[i] = (a.p[i].N + BN - 1) / BN;
+    groups += a.tiles_m[i] * a.tiles_n[i] * a.part[i].splits;
   }
   hipLaunchKernelGGL(kernel, dim3(groups), dim3(WM * WN * 64), lds, st, a);
   CCT_CHECK_LAUNCH();
   return CCT_OK;
 }
 template <int TYPE>
-int launch_together(const FfProduct* p, int count, const FfBiasSum& sum, int tile, hipStream_t st) {
-  switch (tile) {
-    case kTile128: return launch_together<TYPE, 128, 128, 2, 2, 2>(p, count, sum, st);
-    case kTile64x128: return launch_together<TYPE, 64, 128, 2, 2, 3>(p, count, sum, st);
-    default: return launch_together<TYPE, 64, 64, 2, 2, 4>(p, count, sum, st);
+int launch_together(const FfProduct* p, int count, const FfBiasSum& sum, const FfTogetherPlan& plan, char* ws, hipStream_t st) {
+  FfTogether a = {}, joined = {};
+  a.count = count;
+  a.sum = sum;
+  int groups = 0;
+  for (int i = 0; i < count; ++i) {
+    a.p[i] = p[i];
+    a.part[i] = {(float*)(ws + plan.at[i]), (p[i].N + 3) / 4 * 4, plan.splits[i], plan.stages[i]};
+    if (plan.splits[i] == 1) continue;
+    joined.p[joined.count] = p[i];
+    joined.part[joined.count] = a.part[i];
+    joined.first[joined.count++] = groups;
+    groups += (int)(((long long)p[i].M * a.part[i].ld / 4 + 255) / 256);
   }
+  int rc;
+  switch (plan.tile) {
+    case kTile128: rc = launch_together<TYPE, 128, 128, 2, 2, 2>(a, st); break;
+    case kTile64x128: rc = launch_together<TYPE, 64, 128, 2, 2, 3>(a, st); break;
+    default: rc = launch_together<TYPE, 64, 64, 2, 2, 4>(a, st);
+  }
+  if (rc != CCT_OK || groups == 0) return rc;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel_together<TYPE>), dim3(groups), dim3(256), 0, st, joined);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
 }
 
 }  // namespace

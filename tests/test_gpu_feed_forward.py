@@ -381,10 +381,12 @@ def test_few_rows_at_odd_addresses(B, type):
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 def test_backward_products_in_one_launch(B, type):
     """Sizes whose products share a launch, in tiles of 64, 64 x 128 and 128, ragged, with the sum of columns beside them (by
-    one workgroup of rows, by several) and without; every result alone and in pairs has the same bits."""
+    one workgroup of rows, by several) and without, whole and in splits; every result alone and in pairs has the same bits."""
     dt = ff.TYPES[type]
     for M, N, K, pad, off in ((20, 100, 300, 0, 0), (33, 72, 136, 1, 1), (500, 300, 500, 5, 0), (1030, 1023, 1030, 0, 0),
-                              (1531, 1000, 2049, 3, 0), (2000, 1500, 700, 0, 0)):
+                              (1531, 1000, 2049, 3, 0), (2000, 1500, 700, 0, 0),
+                              # long contractions of few results, cut into splits: dx, dw, all
+                              (60, 1301, 64, 0, 0), (1, 1565, 32, 8, 0), (2799, 10, 406, 1, 1), (700, 650, 40, 0, 0)):
         print("together", type, M, N, K, flush=True)
         g = torch.Generator().manual_seed(M)
         x, w, u = (ff.rand(g, r, K, dt, s, pad, off) for r, s in ((M, 1.0), (N, K ** -0.5), (N, K ** -0.5)))
