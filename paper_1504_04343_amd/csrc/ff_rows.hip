@@ -2,9 +2,9 @@
 // nothing else matters.
 //
 // A workgroup takes 16 rows of the weight (gated: of both) and all rows of x, its waves (eight; fp32 with up to 16 rows
-// sixteen) one step of the contraction after the other: 64 bytes of each weight row, which go from memory straight into the registers that the matrix cores take (32
-// values of 16 bits per instruction, 4 of fp32 in an order of their own that x follows).  No LDS and no meeting in the loop;
-// eight steps' loads are in flight per wave, and x comes from L2 the same way.  The waves' sums meet in LDS in a fixed
+// sixteen) one step of the contraction after the other: 64 bytes of each weight row, which go from memory straight into the
+// registers that the matrix cores take (32 values of 16 bits per instruction, 4 of fp32 in an order of their own that x
+// follows).  No LDS and no meeting in the loop; eight steps' loads are in flight per wave, and x comes from L2 the same way.  The waves' sums meet in LDS in a fixed
 // order.  fp32 runs on v_mfma_f32_16x16x4_f32, which memory outlasts.
 //
 // One row, bf16, weights from memory: 4096 x 4096 7.9 us (4.3 TB/s; 6.8 at the rate of a large copy), 16384 x 4096 25.6 (5.2
