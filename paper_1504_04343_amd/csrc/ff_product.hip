@@ -20,6 +20,9 @@ constexpr TileCost kTileCosts[] = {{256, 256, 1, {1.58, 1.65}, {1.58, 1.70}},
                                    {64, 64, 2, {0.29, 0.50}, {0.54, 0.60}}};
 constexpr double kJoinMicros = 4.0, kJoinBytesPerMicro = 7.5e6;  // a launch and its gap; partial sums, written and read
 constexpr int kCus = 256, kLeastStages = 4;                       // of a split
+// What stands around a contraction, in stages: two tell tiles of short contractions of backward products apart (linear 4000 x
+// 200 x 9000 91 -> 82 us, 77 x 14144 x 9696 226 -> 211; one and three 82 and 227, 82 and 211), forward ones gain nothing.
+constexpr int kAround = 2;
 constexpr double kLaunchMicros = 3.0, kBytesPerMicro = 5.0e6;  // operands, from memory
 
 // The tile and the number of splits of the contraction with the least estimate: rounds of workgroups over the card times the
@@ -39,7 +42,7 @@ FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool alon
       const long long groups = tiles * splits, slots = (long long)kCus * c.per_cu, rest = groups % slots;
       double us = (double)(groups / slots) * c.full[!along] + (rest == 0 ? 0.0 : (rest <= kCus ? c.alone : c.full)[!along]);
       // (fewer workgroups than a third of the CUs' places do not keep memory busy)
-      us = std::max(us * each, bytes / kBytesPerMicro * std::max(1.0, 170.0 / groups)) + kLaunchMicros;
+      us = std::max(us * (each + (along ? 0 : kAround)), bytes / kBytesPerMicro * std::max(1.0, 170.0 / groups)) + kLaunchMicros;
       if (splits > 1) us += kJoinMicros + 8.0 * splits * M * cols / kJoinBytesPerMicro;
       if (us < best.micros) best = {tile, (stages + each - 1) / each, each, 0, us, 0, 0};
     }
