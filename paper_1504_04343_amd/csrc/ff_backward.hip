@@ -2,12 +2,12 @@
 //   linear  dz = dy act'(z), and dbias = column sums of dz;
 //   gated   dg = dh u act'(g), du = dh act(g).
 // Each input is read once and each output written once; the rounding of dz, dg and du to 16 bits is the matrix cores', which
-// take no more of an operand (2^-9 of a value at most for bf16, the same as the operands themselves were rounded by).
+// take no more of an operand (bf16 at most 2^-8 of a value, fp16 2^-11, as the operands themselves were rounded by; a gradient
+// then has sqrt(2) times the error that its own rounding makes).
 //
 // A workgroup takes 256 columns x 64 rows, or 8 where that leaves CUs idle (1531 x 1000: 5.3 us, 9.9 before), a thread 8
-// neighbouring columns of every eighth row: its column sums stay in
-// registers, meet in LDS in a fixed order and leave as one row of partial sums per workgroup, which ff_bias_sum.h adds in
-// order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
+// neighbouring columns of every eighth row: its column sums stay in registers, meet in LDS in a fixed order and leave as one
+// row of partial sums per workgroup, which ff_bias_sum.h adds in order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
 #include <algorithm>
 
 #include "activation.h"

@@ -465,7 +465,7 @@ def test_gradients_against_differences(B, type):
         for got, s, diff in ((dx, sx, loss(x + h * sx, w) - loss(x - h * sx, w)),
                              (dw, sw, loss(x, w + h * sw) - loss(x, w - h * sw))):
             terms = got.cpu().double() * s.double()
-            # bf16: z, dz and the result are rounded by 2^-9 each, errors of either sign over the terms
+            # bf16: z, dz and the result are off by 2^-8 each at most, errors of either sign over the terms
             tol = (2.0 ** -7 if type == "bf16" else 2.0 ** -12) * float(terms.norm()) * 8
             assert abs(diff / (2 * h) - float(terms.sum())) <= tol
 
