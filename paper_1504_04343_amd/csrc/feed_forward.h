@@ -40,7 +40,7 @@ struct FfProduct {
 int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st);
 // How a 16-bit product is cut (ff_tile.h): its tile, splits of the contraction of so many stages, the bytes of their partial
 // sums (launch_ff_product's `ws`) and an estimate; rows or columns behind which the rest is a launch with a plan of its own.
-enum { kTile256, kTile192 /* 192 x 256 */, kTile128, kTile64x128, kTile64 };
+enum { kTile256, kTile192 /* 192 x 256 */, kTile128, kTile64x128, kTile64, kNoTile /* ff_general_kernel */ };
 constexpr int kFfStage = 64;
 struct FfTilePlan {
   int tile, splits, stages;
@@ -48,8 +48,8 @@ struct FfTilePlan {
   double micros;
   int cut_rows, cut_cols;
 };
-// `along`: the weights' operand lies along the contraction.
-FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments, bool along);
+// From the product's sizes and how its operands lie; pointers and strides are not looked at.
+FfTilePlan ff_tile_plan(const FfProduct& p);
 int launch_ff_tile_bf16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
 int launch_ff_tile_f16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
 // fp32 (ff_f32.hip): splits of `len` steps, rows that are packed at a time, and the bytes for them and for the sums.
@@ -57,8 +57,16 @@ struct FfF32Plan {
   int splits, len, rows;
   long long pack_bytes, part_bytes;
 };
+// `along`: the weights' operand lies along the contraction.
 FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool along);
 int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st);
+// Products that neither takes (ff_general.hip), which may be cut into splits of so many steps of 16.
+struct FfGeneralPlan {
+  int splits, steps;
+  long long part_bytes;
+};
+FfGeneralPlan ff_general_plan(const FfProduct& p);
+int launch_ff_general(const FfProduct& p, const FfGeneralPlan& plan, float* ws, hipStream_t st);
 // A forward product (operands along the contraction, at any address) of few rows: up to kFfRowsMost run, up to kFfRows (fp32:
 // kFfRowsF32) are faster so.
 constexpr int kFfRows = 16, kFfRowsF32 = 32, kFfRowsMost = 64;
@@ -66,7 +74,7 @@ constexpr int kFfRows = 16, kFfRowsF32 = 32, kFfRowsMost = 64;
 long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue);
 int launch_ff_rows(const FfProduct& p, float* ws, hipStream_t st);
 // Whether the 16-bit product takes a matrix of `cols` consecutive values and rows `ld` apart in place: 16-byte loads, 256 rows
-// within 32-bit offsets.  Rows that are no multiple of 8 values must be followed by zeros up to one, as copies are.
+// within 32-bit offsets (a copy's rows are as long as they are: ff_tile_plan chooses a tile that reaches them).  Rows that are no multiple of 8 values must be followed by zeros up to one, as copies are.
 inline bool ff_in_place(const void* p, long long ld, long long cols) {
   return !((uintptr_t)p & 15) && ld % 8 == 0 && cols % 8 == 0 && ld < (1LL << 21);
 }

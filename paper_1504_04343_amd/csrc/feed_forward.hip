@@ -49,16 +49,11 @@ long long copy_bytes(long long rows, long long cols, int type) {
 struct Room {
   long long pack, part;
 };
-Room room(int type, int M, int N, int K, int epilogue, int segments, bool along) {
-  if (M == 0) return {0, 0};
-  if (type != CCT_TYPE_F32) return {0, ff_tile_plan(M, N, K, epilogue, segments, along).part_bytes};
-  const FfF32Plan plan = ff_f32_plan(M, N, K, epilogue, segments, along);
+Room room(const FfProduct& p) {
+  if (p.M == 0) return {0, 0};
+  if (p.type != CCT_TYPE_F32) return {0, ff_tile_plan(p).part_bytes};
+  const FfF32Plan plan = ff_f32_plan(p.M, p.N, p.K, p.epilogue, p.segments, !p.b_across);
   return {plan.pack_bytes, plan.part_bytes};
-}
-// ... of a forward product, whichever kernel takes it
-Room forward_room(int type, int M, int N, int K, int epilogue) {
-  const Room r = room(type, M, N, K, epilogue, 1, true);
-  return {r.pack, std::max(r.part, ff_rows_part_bytes(M, N, K, type, epilogue))};
 }
 Room larger(const Room& a, const Room& b) { return {std::max(a.pack, b.pack), std::max(a.part, b.part)}; }
 
@@ -77,6 +72,13 @@ FfProduct plain_product(int type, int rows, int cols, int k, bool a_across, bool
   p.out = out;
   p.ldo = ldo;
   return p;
+}
+// Room for a forward product, whichever kernel takes it.
+Room forward_room(int type, int M, int N, int K, FfEpilogue epilogue) {
+  FfProduct p = plain_product(type, M, N, K, false, false, nullptr, 0);
+  p.epilogue = epilogue;
+  const Room r = room(p);
+  return {r.pack, std::max(r.part, ff_rows_part_bytes(M, N, K, type, epilogue))};
 }
 
 // The products of a backward pass, with their results' places and nothing else yet; their number.
@@ -100,7 +102,7 @@ int gated_gradients(const cct_gated_desc_t& d, void* dx, long long lddx, void* d
 // Room for them in one launch, or one after the other.
 Room backward_room(const FfProduct* p, int count) {
   Room r = {0, p[0].type == CCT_TYPE_F32 ? 0 : ff_together_plan(p, count).part_bytes};
-  for (int i = 0; i < count; ++i) r = larger(r, room(p[i].type, p[i].M, p[i].N, p[i].K, kFfLinear, p[i].segments, false));
+  for (int i = 0; i < count; ++i) r = larger(r, room(p[i]));
   return r;
 }
 

@@ -7,8 +7,7 @@
 // workspace and ff_join_kernel finishes them: 8 to 12 bytes per result against 2 K operations (4096 x 4096 x 4096: 27 of
 // 690 us).
 //
-// Strides that gemm_split cannot address (2^22 values and more) and empty contractions run on ff_general_kernel: 64 x 64
-// results per workgroup, 4 x 4 per thread, from LDS tiles of 16 k.
+// Strides that gemm_split cannot address (2^22 values and more) and empty contractions run on ff_general_kernel.
 #include <algorithm>
 #include <cstring>
 
@@ -16,59 +15,6 @@
 
 namespace cct {
 namespace {
-
-constexpr int NT = 256, BT = 64, BK = 16;
-
-template <bool GATED>
-__global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m) {
-  constexpr int NB = GATED ? 2 : 1;
-  __shared__ float As[BK][BT + 1], Bs[NB][BK][BT + 1];
-  const int tile_n = blockIdx.x / tiles_m, tile_m = blockIdx.x - tile_n * tiles_m;
-  const int m0 = tile_m * BT, n0 = tile_n * BT;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[NB][4][4] = {};
-  for (int s = 0; s < (GATED ? 1 : p.segments); ++s)
-    for (int k0 = 0; k0 < p.K; k0 += BK) {
-      __syncthreads();
-      auto stage = [&](float(&to)[BK][BT + 1], const FfOperand& o, bool across, int r0, int rows) {
-        for (int i = threadIdx.x; i < BT * BK; i += NT) {
-          // consecutive threads along the consecutive dimension
-          const int r = across ? i % BT : i / BK, k = across ? i / BT : i % BK;
-          const long long at = across ? (r0 + r) + (k0 + k) * o.ld : (r0 + r) * o.ld + (k0 + k);
-          to[k][r] = r0 + r < rows && k0 + k < p.K ? ((const float*)o.p)[at] : 0.f;
-        }
-      };
-      stage(As, p.A[s], p.a_across, m0, p.M);
-      stage(Bs[0], p.B[s], p.b_across, n0, p.N);
-      if constexpr (GATED) stage(Bs[1], p.B[1], p.b_across, n0, p.N);
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < BK; ++k)
-#pragma unroll
-        for (int q = 0; q < NB; ++q)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[q][i][j] = fmaf(As[k][ty * 4 + i], Bs[q][k][tx * 4 + j], acc[q][i][j]);
-    }
-  const int n = n0 + tx * 4;
-  if (n >= p.N) return;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (m0 + ty * 4 + i < p.M)
-      finish<CCT_TYPE_F32, GATED ? kFfGated : kFfLinear>(p, m0 + ty * 4 + i, n, acc[0][i], acc[NB - 1][i]);
-}
-
-int launch_general(const FfProduct& p, hipStream_t st) {
-  const int tiles_m = (p.M + BT - 1) / BT;
-  const dim3 grid(tiles_m * ((p.N + BT - 1) / BT));
-  if (p.epilogue == kFfGated)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<true>), grid, dim3(NT), 0, st, p, tiles_m);
-  else
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<false>), grid, dim3(NT), 0, st, p, tiles_m);
-  CCT_CHECK_LAUNCH();
-  return CCT_OK;
-}
 
 constexpr int kIntMax = 2147483647;
 constexpr long long kMostPack = 1LL << 30;  // bytes; more rows run one part after the other
@@ -120,7 +66,7 @@ int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
   for (int q = 0; q < products; ++q) {
     GemmTN t = split_problem(plan.rows, p.N, plan.len, plan.splits);
     t.b_ks = p.B[q].ld;
-    if (p.K < 1 || !gemm_split_fits(t, along)) return launch_general(p, st);
+    if (p.K < 1 || !gemm_split_fits(t, along)) return launch_ff_general(p, {1, 0, 0}, nullptr, st);
   }
   for (long long m0 = 0; m0 < p.M; m0 += plan.rows) {
     GemmTN t = split_problem((int)std::min<long long>(plan.rows, p.M - m0), p.N, plan.len, plan.splits);

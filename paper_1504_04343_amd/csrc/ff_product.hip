@@ -25,16 +25,34 @@ constexpr int kCus = 256, kLeastStages = 4;                       // of a split
 constexpr int kAround = 2;
 constexpr double kLaunchMicros = 3.0, kBytesPerMicro = 5.0e6;  // operands, from memory
 
+// Whether a tile's loads reach the operands.  A lane's offset from its tile's first row, or from its stage's first step, is 32
+// bits, and what lies 2^31 bytes behind that is taken for what lies behind the operand.  Matrices in place always are reached
+// (ff_in_place); rows of a copy, and of dz, are as far apart as they are long, so that 128 rows of 2^24 steps are not.
+bool reaches(const FfProduct& p, const TileCost& c) {
+  constexpr long long most = 1LL << 30;  // 16-bit values
+  auto operand = [&](bool across, int rows, int tile) {
+    const long long ld = ((across ? rows : p.K) + 7LL) / 8 * 8;
+    if (!across) return (std::min(rows, tile) - 1) * ld + kFfStage <= most;
+    // steps past the contraction's end may lie anywhere beyond it, if they do not come round to its beginning
+    return (std::min(p.K, kFfStage) - 1) * ld + tile <= most && (kFfStage - 1) * ld + tile < 2 * most;
+  };
+  return operand(p.a_across, p.M, c.bm) && operand(p.b_across, p.N, p.epilogue == kFfGated ? c.bn / 2 : c.bn);
+}
+
 // The tile and the number of splits of the contraction with the least estimate: rounds of workgroups over the card times the
 // stages of one, and what joining the splits costs.  Few large tiles leave CUs idle, small ones read LDS more often per
 // product.  1024 x 4096 x 9216 (forward, bf16): 181 us in tiles of 256 (64 of them), 96 in 128, 82 in 128 and two splits.
-FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool along) {
-  const long long cols = epilogue == kFfGated ? 2LL * N : N;
-  const int stages = std::max((K + kFfStage - 1) / kFfStage, 1) * (epilogue == kFfGated ? 1 : segments);
-  const double bytes = 2.0 * (M + (double)cols) * K * (epilogue == kFfGated ? 1 : segments);
-  FfTilePlan best = {kTile128, 1, stages, 0, 1e30, 0, 0};
+// For M x N of the product's results.
+FfTilePlan whole_plan(const FfProduct& p, int M, int N) {
+  const bool along = !p.b_across;
+  const int segments = p.epilogue == kFfGated ? 1 : p.segments;
+  const long long cols = p.epilogue == kFfGated ? 2LL * N : N;
+  const int stages = std::max((p.K + kFfStage - 1) / kFfStage, 1) * segments;
+  const double bytes = 2.0 * (M + (double)cols) * p.K * segments;
+  FfTilePlan best = {kNoTile, 1, stages, 0, 1e30, 0, 0};
   for (int tile = kTile256; tile <= kTile64; ++tile) {
     const TileCost& c = kTileCosts[tile];
+    if (!reaches(p, c)) continue;
     const long long tiles = ((M + c.bm - 1LL) / c.bm) * ((cols + c.bn - 1) / c.bn);
     for (int splits = 1; splits <= 32; splits *= 2) {
       if (splits > 1 && (tile <= kTile192 || stages < splits * kLeastStages || tiles * splits > 4 * kCus)) break;
@@ -47,7 +65,8 @@ FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool alon
       if (us < best.micros) best = {tile, (stages + each - 1) / each, each, 0, us, 0, 0};
     }
   }
-  best.part_bytes = best.splits > 1 ? 4LL * best.splits * M * (cols + 8) : 0;
+  if (best.tile == kNoTile) best.part_bytes = ff_general_plan(p).part_bytes;
+  else if (best.splits > 1) best.part_bytes = 4LL * best.splits * M * (cols + 8);
   return best;
 }
 
@@ -56,17 +75,17 @@ FfTilePlan whole_plan(int M, int N, int K, int epilogue, int segments, bool alon
 // The same, or whole rounds of tiles of 256 and what is left of the columns or rows in a launch of its own: 17 x 16 tiles are
 // two rounds, of which the second one is 16 workgroups (4160 columns of 4096 rows and steps: 187 us in tiles of
 // 128, 133 so).
-FfTilePlan ff_tile_plan(int M, int N, int K, int epilogue, int segments, bool along) {
-  FfTilePlan best = whole_plan(M, N, K, epilogue, segments, along);
-  const int wide = epilogue == kFfGated ? 128 : 256;
+FfTilePlan ff_tile_plan(const FfProduct& p) {
+  const int M = p.M, N = p.N;
+  FfTilePlan best = whole_plan(p, M, N);
+  const int wide = p.epilogue == kFfGated ? 128 : 256;
   const long long tm = (M + 255LL) / 256, tn = (N + wide - 1LL) / wide, rounds = tm * tn / kCus;
-  if (rounds < 1) return best;
-  const int stages = std::max((K + kFfStage - 1) / kFfStage, 1) * (epilogue == kFfGated ? 1 : segments);
-  const double full = rounds * stages * kTileCosts[kTile256].full[!along] + kLaunchMicros;
+  if (rounds < 1 || !reaches(p, kTileCosts[kTile256])) return best;
+  const int stages = std::max((p.K + kFfStage - 1) / kFfStage, 1) * (p.epilogue == kFfGated ? 1 : p.segments);
+  const double full = rounds * stages * kTileCosts[kTile256].full[p.b_across] + kLaunchMicros;
   auto consider = [&](long long rows, long long cols) {  // what the full rounds take
     if ((rows < M) == (cols < N)) return;
-    const FfTilePlan rest = rows < M ? whole_plan(M - (int)rows, N, K, epilogue, segments, along)
-                                 : whole_plan(M, N - (int)cols, K, epilogue, segments, along);
+    const FfTilePlan rest = rows < M ? whole_plan(p, M - (int)rows, N) : whole_plan(p, M, N - (int)cols);
     if (full + rest.micros >= best.micros) return;
     best = {kTile256, 1, stages, rest.part_bytes, full + rest.micros, rows < M ? (int)rows : 0, cols < N ? (int)cols : 0};
   };
@@ -108,13 +127,14 @@ int launch_tiles(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStrea
 
 int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
   if (p.type == CCT_TYPE_F32) return launch_ff_f32(p, pack, ws, st);
-  const FfTilePlan plan = ff_tile_plan(p.M, p.N, p.K, p.epilogue, p.segments, !p.b_across);
+  const FfTilePlan plan = ff_tile_plan(p);
+  if (plan.tile == kNoTile) return launch_ff_general(p, ff_general_plan(p), ws, st);
   if (!plan.cut_rows && !plan.cut_cols) return launch_tiles(p, plan, ws, st);
   const int m = plan.cut_rows, n = plan.cut_cols;  // one of them is 0
   const int rc = launch_tiles(part_of(p, 0, 0, m ? m : p.M, n ? n : p.N), plan, ws, st);
   if (rc != CCT_OK) return rc;
   const FfProduct rest = part_of(p, m, n, p.M - m, p.N - n);
-  return launch_tiles(rest, whole_plan(rest.M, rest.N, rest.K, rest.epilogue, rest.segments, !rest.b_across), ws, st);
+  return launch_tiles(rest, whole_plan(p, rest.M, rest.N), ws, st);
 }
 
 namespace {
@@ -130,9 +150,10 @@ FfTogetherPlan ff_together_plan(const FfProduct* p, int count) {
   FfTogetherPlan best = {};
   best.tile = -1;
   if (count < 2) return best;
-  for (int i = 0; i < count; ++i) best.micros += ff_tile_plan(p[i].M, p[i].N, p[i].K, p[i].epilogue, p[i].segments, false).micros;
+  for (int i = 0; i < count; ++i) best.micros += ff_tile_plan(p[i]).micros;
   for (int tile = kTile128; tile <= kTile64; ++tile) {
     const TileCost& c = kTileCosts[tile];
+    if (!std::all_of(p, p + count, [&](const FfProduct& q) { return reaches(q, c); })) continue;
     for (int most = kLeastStages; most <= 512; most *= 2) {
       FfTogetherPlan plan = {};
       double groups = 0, work = 0, bytes = 0, joined = 0;

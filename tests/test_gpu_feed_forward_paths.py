@@ -1,0 +1,112 @@
+"""Which kernels the products of feed-forward blocks run on, and that every one of them is right: whole numbers, whose sums are
+exact in fp32 in any order, so that a step of a contraction that is lost, repeated or taken from another row shows in the
+results' bits.  The reference is a product in 64 bits of the same numbers; the names are those of the profile."""
+import pytest
+import torch
+
+import feed_forward_util as ff
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    assert torch.cuda.is_available()
+    from paper_1504_04343_amd import binding
+    yield binding
+    torch.cuda.empty_cache()
+
+
+def consts(B, type):
+    return dict(f32=B.TYPE_F32, bf16=B.TYPE_BF16, f16=B.TYPE_F16)[type], ff.TYPES[type]
+
+
+def numbers(g, rows, cols, dt, most=1, pad=0):
+    """Whole numbers from -most to most, rows cols + pad apart."""
+    flat = torch.empty(rows, cols + pad, dtype=dt, device="cuda")
+    for r in range(0, rows, max(1, (1 << 28) // (cols + pad))):     # in parts: whole int64 tensors would not fit
+        part = flat[r:r + max(1, (1 << 28) // (cols + pad))]
+        part.copy_(torch.randint(-most, most + 1, part.shape, generator=g, device="cuda", dtype=torch.int8))
+    return flat[:, :cols]
+
+
+def product(a, b, step=1 << 20):
+    """a b^T in 64 bits, `step` steps of the contraction at a time."""
+    out = torch.zeros(a.shape[0], b.shape[0], dtype=torch.float64, device="cuda")
+    for k in range(0, a.shape[1], step):
+        out += a[:, k:k + step].double() @ b[:, k:k + step].double().t()
+    assert out.numel() == 0 or float(out.abs().max()) < 2 ** 24
+    return out
+
+
+def empty(rows, cols, dt, pad=0):
+    return ff.empty_gpu(rows, cols, dt, pad)
+
+
+def profiled(B, call):
+    """The names of what a call launches, in order of their first launch."""
+    torch.cuda.synchronize()
+    B.cct_profile_enable(True)
+    try:
+        call()
+        torch.cuda.synchronize()
+    finally:
+        B.cct_profile_enable(False)
+    return [e["name"] for e in B.cct_profile_read(64) for _ in range(e["launches"])]
+
+
+def same(name, got, want):
+    """Bit for bit the value rounded once to the type."""
+    want = want.to(got.dtype)
+    if not torch.equal(got, want):
+        bad = got != want
+        at = tuple(int(i) for i in bad.nonzero()[0])
+        raise AssertionError("%s: %d of %d differ; the first at %s: %g, expected %g" % (
+            name, int(bad.sum()), got.numel(), at, float(got[at]), float(want[at])))
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("N,K,kernel", [(130, 1 << 24, "ff_tile_kernel<64x64"), (70, (1 << 24) + (1 << 19), "ff_general_kernel")])
+def test_rows_longer_than_a_tile_reaches(B, type, N, K, kernel):
+    """A tile's loads have 32 bits for its rows: 128 rows of 2^24 values are beyond them, 64 of somewhat more too."""
+    t, dt = consts(B, type)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x, w = numbers(g, N, K, dt), numbers(g, N, K, dt)
+    bias = numbers(g, 1, N, dt).view(N)
+    d = B.make_linear_desc(N, N, K, t, B.ACT_RELU)
+    y, z = empty(N, N, dt), empty(N, N, dt)
+    ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+    assert any(n.startswith(kernel) for n in profiled(B, lambda: B.cct_linear_forward(d, x, w, bias, None, y, z, ws)))
+    del ws
+    want = product(x, w) + bias.double()
+    same("z", z, want)
+    same("y", y, want.clamp(min=0))
+    e = B.make_gated_desc(N, N // 2, K, t, B.ACT_RELU)
+    h, gg, uu = (empty(N, N // 2, dt) for _ in range(3))
+    B.cct_gated_forward(e, x, w[:N // 2], w[N // 2:N // 2 * 2], h, gg, uu, B.alloc_gated_workspace(e, B.PASS_FORWARD))
+    both = product(x, w)
+    same("g", gg, both[:, :N // 2])
+    same("u", uu, both[:, N // 2:N // 2 * 2])
+    # act(g) * u of the fp32 sums may need more than 24 bits: rounded to fp32 first, then to the type
+    same("h", h, (both[:, :N // 2].clamp(min=0) * both[:, N // 2:N // 2 * 2]).float())
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_gradients_of_rows_longer_than_a_tile_reaches(B, type):
+    """Weights and inputs of such rows across the contraction, 64 steps of which are a stage."""
+    t, dt = consts(B, type)
+    M, N, K = 70, 66, (1 << 24) + (1 << 19)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, w, dy, z = numbers(g, M, K, dt), numbers(g, N, K, dt), numbers(g, M, N, dt), numbers(g, M, N, dt)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    dx, dw = empty(M, K, dt), empty(N, K, dt)
+    db = torch.full((N,), float("nan"), dtype=dt, device="cuda")
+    ws = B.alloc_linear_workspace(d, B.PASS_BACKWARD)
+    names = profiled(B, lambda: B.cct_linear_backward(d, x, w, z, dy, dx, dw, db, ws))
+    assert names.count("ff_general_kernel") == 2, names
+    dy.mul_(z > 0)
+    same("dbias", db, dy.double().sum(0))
+    for k in range(0, K, 1 << 21):
+        part = slice(k, k + (1 << 21))
+        same("dx", dx[:, part], product(dy, w[:, part].t()))
+        same("dw", dw[:, part], product(dy.t(), x[:, part].t()))
