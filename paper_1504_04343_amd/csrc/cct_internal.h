@@ -330,6 +330,9 @@ int ensure_dynamic_lds(int bytes) {
   return CCT_OK;
 }
 
+// What HIP takes at most along one dimension of a launch's grid: workgroups times their threads.
+constexpr long long kMostThreads = 0xffffffffLL;
+
 #define CCT_CHECK_LAUNCH()                       \
   do {                                           \
     hipError_t e__ = hipGetLastError();          \

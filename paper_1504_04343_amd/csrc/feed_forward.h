@@ -70,6 +70,7 @@ int launch_ff_general(const FfProduct& p, const FfGeneralPlan& plan, float* ws, 
 // A forward product (operands along the contraction, at any address) of few rows: up to kFfRowsMost run, up to kFfRows (fp32:
 // kFfRowsF32) are faster so.
 constexpr int kFfRows = 16, kFfRowsF32 = 32, kFfRowsMost = 64;
+bool ff_rows_fits(int N, int type);  // whether a launch takes so many columns
 // `ws`: ff_rows_part_bytes.
 long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue);
 int launch_ff_rows(const FfProduct& p, float* ws, hipStream_t st);

@@ -149,7 +149,8 @@ GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
 // but tiles may need a copy of the weight first (three times its bytes): 64 rows 17 to 21 and 30.  Rows that begin between
 // multiples of four bytes take 44 there, so that more than 16 are copied: 62 rows of 10881 -> 2880 166 us there, 43 so.
 // fp32: 16 rows 22.6 us; 48 rows 41 there, 37 on ff_f32.hip; 64 rows of 4096 -> 16384 183 and 100.
-bool few_rows(int M, int type, bool in_place, bool words) {
+bool few_rows(int M, int N, int type, bool in_place, bool words) {
+  if (!ff_rows_fits(N, type)) return false;
   if (type == CCT_TYPE_F32) return M <= kFfRowsF32;
   return M <= kFfRows || (M <= kFfRowsMost && words && !in_place);
 }
@@ -215,7 +216,7 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
   if (rc != CCT_OK) return rc;
   hipStream_t st = (hipStream_t)hip_stream;
   char* ws = (char*)workspace;
-  const bool few = few_rows(d.M, d.type, ff_in_place(w, d.N <= 1 ? up(d.K, 8) : ldw, d.K),
+  const bool few = few_rows(d.M, d.N, d.type, ff_in_place(w, d.N <= 1 ? up(d.K, 8) : ldw, d.K),
                             ff_words({x, ldx}) && ff_words({w, ldw}));
   Matrix mx = {x, ldx}, mw = {w, ldw};
   if (!few) {
@@ -298,7 +299,7 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
   char* ws = (char*)workspace;
   const bool in_place = ff_in_place(wg, d.F <= 1 ? up(d.K, 8) : ldwg, d.K) && ff_in_place(wu, d.F <= 1 ? up(d.K, 8) : ldwu, d.K) &&
                         ldwg == ldwu;
-  const bool few = few_rows(d.M, d.type, in_place, ff_words({x, ldx}) && ff_words({wg, ldwg}) && ff_words({wu, ldwu}));
+  const bool few = few_rows(d.M, d.F, d.type, in_place, ff_words({x, ldx}) && ff_words({wg, ldwg}) && ff_words({wu, ldwu}));
   Matrix mx = {x, ldx}, mg = {wg, ldwg}, mu = {wu, ldwu};
   if (!few) {
     FfDzJobs jobs = {};

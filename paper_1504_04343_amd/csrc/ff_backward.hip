@@ -104,9 +104,9 @@ __global__ __launch_bounds__(NT) void ff_dz_kernel(DzArgs a) {
 
 constexpr int kSumThreads = kBiasColumns * kBiasRuns;
 template <int TYPE>
-__global__ __launch_bounds__(kSumThreads) void ff_bias_sum_kernel(FfBiasSum p) {
+__global__ __launch_bounds__(kSumThreads) void ff_bias_sum_kernel(FfBiasSum p, int first) {
   __shared__ float sums[kBiasRuns][kBiasColumns + 1];
-  sum_bias<TYPE, kSumThreads>(p, blockIdx.x, sums);
+  sum_bias<TYPE, kSumThreads>(p, first + blockIdx.x, sums);
 }
 
 template <int TYPE>
@@ -135,7 +135,15 @@ __global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows, 
 }  // namespace
 
 namespace {
-int rows_of_group(int M, int N) { return (long long)((M + 63) / 64) * ((N + kCols - 1) / kCols) >= 1024 ? 64 : 8; }
+// Up to four matrices share a launch: of each at most 2^21 workgroups, or one for every 256 columns (2^23), which together
+// are less than 2^24.
+int rows_of_group(int M, int N) {
+  const long long wide = (N + kCols - 1) / kCols;
+  if ((M + 63) / 64 * wide < 1024) return 8;
+  int rows = 64;
+  while (rows < M && (M + rows - 1LL) / rows * wide > 1 << 21) rows *= 2;
+  return rows;
+}
 // Column sums of up to 32 rows need no second launch if a workgroup takes them all (4 rows per thread).
 int rows_of_group(const FfDz& p) { return p.dbias && p.M <= 32 ? 32 : rows_of_group(p.M, p.N); }
 
@@ -147,14 +155,14 @@ int place(const FfDzJobs& p, DzArgs* a, double* ops, double* bytes) {
     if (i >= p.count) continue;
     const FfDz& q = a->job[i] = p.job[i];
     a->rows[i] = rows_of_group(q);
-    groups += (q.M + a->rows[i] - 1) / a->rows[i] * ((q.N + kCols - 1) / kCols);
+    groups += (int)((q.M + a->rows[i] - 1LL) / a->rows[i]) * ((q.N + kCols - 1) / kCols);
     *ops += 2.0 * q.M * q.N;
     *bytes += (double)type_bytes(q.type) * q.M * q.N * (1 + (q.z != nullptr) + (q.dz != nullptr));
   }
   return groups;
 }
 }  // namespace
-int ff_sum_rows(int M, int N) { return (M + rows_of_group(M, N) - 1) / rows_of_group(M, N); }
+int ff_sum_rows(int M, int N) { return (int)((M + rows_of_group(M, N) - 1LL) / rows_of_group(M, N)); }
 
 int launch_ff_dz(const FfDzJobs& p, FfBiasSum* left, hipStream_t st) {
   *left = {};
@@ -178,8 +186,10 @@ int launch_ff_bias_sum(const FfBiasSum& p, hipStream_t st) {
   if (!p.dbias) return CCT_OK;
   with_type(p.type, [&](auto type) {
     ProfScope ps("ff_bias_sum_kernel", (double)p.rows * p.N, 4.0 * p.rows * p.N, st);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3((p.N + kBiasColumns - 1) / kBiasColumns),
-                       dim3(kSumThreads), 0, st, p);
+    const int groups = (p.N + kBiasColumns - 1) / kBiasColumns, most = (int)(kMostThreads / kSumThreads);
+    for (int first = 0; first < groups; first += most)
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3(std::min(most, groups - first)),
+                         dim3(kSumThreads), 0, st, p, first);
   });
   CCT_CHECK_LAUNCH();
   return CCT_OK;

@@ -6,7 +6,7 @@
 
 namespace cct {
 
-constexpr int kBiasColumns = 16, kBiasRuns = 64;
+constexpr int kBiasColumns = 16, kBiasRuns = 64, kBiasMost = 1 << 20;  // workgroups next to products
 
 template <int TYPE, int THREADS>
 __device__ __forceinline__ void sum_bias(const FfBiasSum& p, int group, float (*sums)[kBiasColumns + 1]) {

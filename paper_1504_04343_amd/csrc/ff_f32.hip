@@ -43,6 +43,9 @@ FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool alon
     double least = 1e30;
     const long long kpad = gemm_split_kpad(K);
     best.rows = (int)std::min<long long>(M, std::max(64LL, kMostPack / (6 * kpad) / 64 * 64));
+    // in tiles of 32 x 128 at the least, one launch
+    while (best.rows > 32 && (best.rows + 31LL) / 32 * ((N + 127LL) / 128) * 256 > kMostThreads)
+      best.rows = std::max(32, best.rows / 2 / 64 * 64);
     for (int sp = 1; sp <= 32 && (sp == 1 || K >= sp * kLeastSplit); sp += sp < 8 ? 1 : 4) {
       const int len = sp == 1 ? K : gemm_split_kpad((K + sp - 1) / sp), n = (K + len - 1) / len;
       const double t = gemm_split_seconds(along, true, best.rows, len, N, n) + (n > 1 ? 8.0 * n * best.rows * N / 5.5e12 + 2.5e-6 : 0.0);
@@ -96,14 +99,13 @@ int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
   }
   if (!join) return CCT_OK;
   const FfPart part = {ws, (int)ld, plan.splits * (gated ? 1 : products), 0};
-  const dim3 grid((unsigned)((p.M * ld / 4 + 255) / 256));
   const double mn = (double)p.M * p.N;
   ProfScope ps("ff_join_kernel", mn * plan.splits * products,
                4.0 * mn * (plan.splits * products + 1 + (p.residual != nullptr) + (p.z != nullptr) + (p.z2 != nullptr)), st);
   if (gated)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<CCT_TYPE_F32, kFfGated>), grid, dim3(256), 0, st, p, part);
+    launch_join<CCT_TYPE_F32, kFfGated>(p, part, st);
   else
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<CCT_TYPE_F32, kFfLinear>), grid, dim3(256), 0, st, p, part);
+    launch_join<CCT_TYPE_F32, kFfLinear>(p, part, st);
   CCT_CHECK_LAUNCH();
   return CCT_OK;
 }

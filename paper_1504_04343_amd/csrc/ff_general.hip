@@ -14,10 +14,10 @@ namespace {
 constexpr int NT = 256, BT = 64, BK = 16;
 
 template <int TYPE, bool GATED>
-__global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m, FfPart part) {
+__global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m, int first, FfPart part) {
   constexpr int NB = GATED ? 2 : 1;
   __shared__ float As[BK][BT + 1], Bs[NB][BK][BT + 1];
-  const int tile_n = blockIdx.x / tiles_m, tile_m = blockIdx.x - tile_n * tiles_m, split = blockIdx.y;
+  const int tile = first + blockIdx.x, tile_n = tile / tiles_m, tile_m = tile - tile_n * tiles_m, split = blockIdx.y;
   const int m0 = tile_m * BT, n0 = tile_n * BT;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   float acc[NB][4][4] = {};
@@ -65,12 +65,11 @@ __global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m
 
 template <int TYPE, int EPI>
 void launch(const FfProduct& p, const FfPart& part, hipStream_t st) {
-  const int tiles_m = (p.M + BT - 1) / BT;
-  const dim3 grid(tiles_m * ((p.N + BT - 1) / BT), part.splits);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<TYPE, EPI == kFfGated>), grid, dim3(NT), 0, st, p, tiles_m, part);
-  if (part.splits > 1)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, EPI>), dim3((unsigned)(((long long)p.M * part.ld / 4 + 255) / 256)),
-                       dim3(256), 0, st, p, part);
+  const int tiles_m = (p.M + BT - 1) / BT, tiles = tiles_m * ((p.N + BT - 1) / BT), most = (int)(kMostThreads / NT);
+  for (int first = 0; first < tiles; first += most)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<TYPE, EPI == kFfGated>), dim3(std::min(most, tiles - first), part.splits),
+                       dim3(NT), 0, st, p, tiles_m, first, part);
+  if (part.splits > 1) launch_join<TYPE, EPI>(p, part, st);
 }
 template <int TYPE>
 void launch(const FfProduct& p, const FfPart& part, hipStream_t st) {

@@ -2,7 +2,7 @@
 // ff_f32.hip).
 #include <algorithm>
 
-#include "feed_forward.h"
+#include "ff_bias_sum.h"
 
 namespace cct {
 namespace {
@@ -10,14 +10,14 @@ namespace {
 // Microseconds of a stage (64 steps of the contraction) with one workgroup on a CU and with as many as fit, forward and with
 // operands across the contraction (whose LDS reads are twice as many), measured on products of 512 to 8192 rows.
 struct TileCost {
-  int bm, bn, per_cu;
+  int bm, bn, per_cu, threads;
   double alone[2], full[2];
 };
-constexpr TileCost kTileCosts[] = {{256, 256, 1, {1.58, 1.65}, {1.58, 1.70}},
-                                   {192, 256, 1, {1.24, 1.30}, {1.24, 1.34}},
-                                   {128, 128, 2, {0.65, 0.93}, {1.10, 1.08}},
-                                   {64, 128, 2, {0.39, 0.75}, {0.72, 0.83}},
-                                   {64, 64, 2, {0.29, 0.50}, {0.54, 0.60}}};
+constexpr TileCost kTileCosts[] = {{256, 256, 1, 512, {1.58, 1.65}, {1.58, 1.70}},
+                                   {192, 256, 1, 512, {1.24, 1.30}, {1.24, 1.34}},
+                                   {128, 128, 2, 256, {0.65, 0.93}, {1.10, 1.08}},
+                                   {64, 128, 2, 256, {0.39, 0.75}, {0.72, 0.83}},
+                                   {64, 64, 2, 256, {0.29, 0.50}, {0.54, 0.60}}};
 constexpr double kJoinMicros = 4.0, kJoinBytesPerMicro = 7.5e6;  // a launch and its gap; partial sums, written and read
 constexpr int kCus = 256, kLeastStages = 4;                       // of a split
 // What stands around a contraction, in stages: two tell tiles of short contractions of backward products apart (linear 4000 x
@@ -54,6 +54,7 @@ FfTilePlan whole_plan(const FfProduct& p, int M, int N) {
     const TileCost& c = kTileCosts[tile];
     if (!reaches(p, c)) continue;
     const long long tiles = ((M + c.bm - 1LL) / c.bm) * ((cols + c.bn - 1) / c.bn);
+    if (tiles * c.threads > kMostThreads) continue;  // more than 2^30 rows of few columns in tiles of 64
     for (int splits = 1; splits <= 32; splits *= 2) {
       if (splits > 1 && (tile <= kTile192 || stages < splits * kLeastStages || tiles * splits > 4 * kCus)) break;
       const int each = (stages + splits - 1) / splits;
@@ -80,7 +81,7 @@ FfTilePlan ff_tile_plan(const FfProduct& p) {
   FfTilePlan best = whole_plan(p, M, N);
   const int wide = p.epilogue == kFfGated ? 128 : 256;
   const long long tm = (M + 255LL) / 256, tn = (N + wide - 1LL) / wide, rounds = tm * tn / kCus;
-  if (rounds < 1 || !reaches(p, kTileCosts[kTile256])) return best;
+  if (rounds < 1 || !reaches(p, kTileCosts[kTile256]) || tm * tn * kTileCosts[kTile256].threads > kMostThreads) return best;
   const int stages = std::max((p.K + kFfStage - 1) / kFfStage, 1) * (p.epilogue == kFfGated ? 1 : p.segments);
   const double full = rounds * stages * kTileCosts[kTile256].full[p.b_across] + kLaunchMicros;
   auto consider = [&](long long rows, long long cols) {  // what the full rounds take
@@ -156,7 +157,7 @@ FfTogetherPlan ff_together_plan(const FfProduct* p, int count) {
     if (!std::all_of(p, p + count, [&](const FfProduct& q) { return reaches(q, c); })) continue;
     for (int most = kLeastStages; most <= 512; most *= 2) {
       FfTogetherPlan plan = {};
-      double groups = 0, work = 0, bytes = 0, joined = 0;
+      double groups = 0, work = 0, bytes = 0, joined = 0, joining = 0;  // `joining`: threads
       int longest = 0, shortest = 0x7fffffff;
       for (int i = 0; i < count; ++i) {
         const int all = stages_of(p[i]);
@@ -168,6 +169,7 @@ FfTogetherPlan ff_together_plan(const FfProduct* p, int count) {
           const double values = (double)p[i].M * ((p[i].N + 3) / 4 * 4) * plan.splits[i];
           plan.part_bytes += ((long long)values * 4 + 255) / 256 * 256;
           joined += 8.0 * values;
+          joining += values / plan.splits[i] / 4 + 256;
         }
         const double tiles = (double)((p[i].M + c.bm - 1) / c.bm) * ((p[i].N + c.bn - 1) / c.bn) * plan.splits[i];
         groups += tiles;
@@ -176,7 +178,7 @@ FfTogetherPlan ff_together_plan(const FfProduct* p, int count) {
         shortest = std::min(shortest, each);
         bytes += operand_bytes(p[i]);
       }
-      if (groups > 1 << 30) break;
+      if ((groups + kBiasMost) * c.threads > kMostThreads || joining > kMostThreads) continue;
       const double slots = (double)kCus * c.per_cu;
       const double us = groups <= kCus ? longest * c.alone[1] : std::max<double>(longest, work / slots + 0.25 * shortest) * c.full[1];
       plan.tile = tile;
@@ -196,8 +198,11 @@ int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char
   int order[kFfTogether], n = 0;
   for (int i = 0; i < count; ++i)
     if (p[i].out) order[n++] = i;
+  const bool apart = plan.tile < 0 || n == 0 || sum.N > kBiasMost * kBiasColumns;  // the sum of columns, the same bits
+  int rc = apart ? launch_ff_bias_sum(sum, st) : CCT_OK;
+  if (rc != CCT_OK) return rc;
+  const FfBiasSum beside = apart ? FfBiasSum{} : sum;
   if (plan.tile < 0 || n == 0) {
-    int rc = launch_ff_bias_sum(sum, st);
     for (int i = 0; i < n && rc == CCT_OK; ++i) rc = launch_ff_product(p[order[i]], pack, ws, st);
     return rc;
   }
@@ -215,8 +220,8 @@ int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char
     bytes += operand_bytes(q) + 2.0 * q.M * q.N;
   }
   ProfScope ps(flops, bytes, st, "ff_tile_kernel_together<%s, %d products>", kTileNames[plan.tile], n);
-  return p[0].type == CCT_TYPE_BF16 ? launch_ff_together_bf16(wanted, n, sum, theirs, (char*)ws, st)
-                                    : launch_ff_together_f16(wanted, n, sum, theirs, (char*)ws, st);
+  return p[0].type == CCT_TYPE_BF16 ? launch_ff_together_bf16(wanted, n, beside, theirs, (char*)ws, st)
+                                    : launch_ff_together_f16(wanted, n, beside, theirs, (char*)ws, st);
 }
 
 }  // namespace cct

@@ -213,7 +213,7 @@ void launch(const FfProduct& p, float* ws, hipStream_t st) {
   else
     run(std::integral_constant<int, F32 ? 2 : 4>(), std::false_type());
   if (part.splits > 1)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, EPI>), dim3((p.M * part.ld / 4 + 255) / 256), dim3(256), 0, st, p, part);
+    launch_join<TYPE, EPI>(p, part, st);
 }
 template <int TYPE>
 void launch(const FfProduct& p, float* ws, hipStream_t st) {
@@ -224,6 +224,8 @@ void launch(const FfProduct& p, float* ws, hipStream_t st) {
 }
 
 }  // namespace
+
+bool ff_rows_fits(int N, int type) { return (N + 15LL) / 16 * (type == CCT_TYPE_F32 ? 1024 : 512) <= kMostThreads; }
 
 long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue) {
   const int splits = M <= kFfRowsMost ? rows_splits(N, K, type) : 1;

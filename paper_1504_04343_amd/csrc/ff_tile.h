@@ -467,8 +467,15 @@ __device__ __forceinline__ void join(const FfProduct& p, const FfPart& part, int
   finish<TYPE, EPI>(p, m, n, v, u);
 }
 template <int TYPE, int EPI>
-__global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p, FfPart part) {
-  join<TYPE, EPI>(p, part, blockIdx.x);
+__global__ __launch_bounds__(256) void ff_join_kernel(FfProduct p, FfPart part, int first) {
+  join<TYPE, EPI>(p, part, first + blockIdx.x);
+}
+template <int TYPE, int EPI>
+void launch_join(const FfProduct& p, const FfPart& part, hipStream_t st) {
+  const long long groups = ((long long)p.M * part.ld / 4 + 255) / 256, most = kMostThreads / 256;
+  for (long long first = 0; first < groups; first += most)
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, EPI>), dim3((unsigned)(groups - first < most ? groups - first : most)),
+                       dim3(256), 0, st, p, part, (int)first);
 }
 // Those of several products: workgroups from first[i] on are p[i]'s.
 template <int TYPE>

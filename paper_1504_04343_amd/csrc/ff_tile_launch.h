@@ -44,11 +44,10 @@ int launch_planned(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStr
     default: rc = launch_mode<TYPE, 64, 64, 2, 2, 4, true>(p, part, st);
   }
   if (rc != CCT_OK) return rc;
-  const dim3 grid((unsigned)(((long long)p.M * part.ld / 4 + 255) / 256));
   if (p.epilogue == kFfGated)
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, kFfGated>), grid, dim3(256), 0, st, p, part);
+    launch_join<TYPE, kFfGated>(p, part, st);
   else
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_join_kernel<TYPE, kFfLinear>), grid, dim3(256), 0, st, p, part);
+    launch_join<TYPE, kFfLinear>(p, part, st);
   CCT_CHECK_LAUNCH();
   return CCT_OK;
 }

@@ -585,7 +585,7 @@ template <int RB, BForm BF, AForm AF, int ALONE = 0>
 int launch_variant(const GemmTN& p, int Ktotal, hipStream_t st) {
   const int tiles_m = (p.M + 16 * RB - 1) / (16 * RB), tiles_n = ((BF == kPairs ? p.pair_cols : p.Ncols) + BN - 1) / BN;
   const long long blocks = (long long)tiles_m * tiles_n;
-  if (blocks <= 0 || blocks >= 2147483647LL || p.G < 1 || p.G > 65535) return CCT_EUNSUPPORTED;
+  if (blocks <= 0 || blocks * NT > kMostThreads || p.G < 1 || p.G > 65535) return CCT_EUNSUPPORTED;
   const double mk = (double)p.M * p.Kdim * p.G, kn = (double)p.Kdim * p.Ncols * p.G;
   ProfScope ps(2.0 * p.M * kn, (AF == kPacked ? 6.0 : 4.0) * mk + 4.0 * kn + 4.0 * (double)p.M * p.Ncols * p.G, st,
                "gemm_split<%d, %s>", 16 * RB, BF == kContiguous ? "k-contiguous" : "in place");
@@ -615,7 +615,7 @@ int launch_pack_rows_split(const float* src, void* pack, int G, int M, int Mpad,
                            long long sm, long long sk, long long sg, hipStream_t st, int taps) {
   const RowsPack d{G, M, Mpad, Kpad, Kdim, Ktotal, sm, sk, sg, taps};
   const long long total = (long long)Kpad / 8 * Mpad * G, blocks = (total + 255) / 256;
-  if (blocks <= 0 || blocks >= 2147483647LL) return CCT_EUNSUPPORTED;
+  if (blocks <= 0 || blocks * 256 > kMostThreads) return CCT_EUNSUPPORTED;
   ProfScope ps("pack_rows_split_kernel", 0.0, 4.0 * M * (double)Ktotal + 48.0 * total, st);
   hipLaunchKernelGGL(pack_rows_split_kernel, dim3((unsigned)blocks), dim3(256), 0, st, src,
                      reinterpret_cast<unsigned short*>(pack), d);

@@ -39,6 +39,16 @@ def product(a, b, step=1 << 20):
     return out
 
 
+def column_product(a, b):
+    """a^T b in 64 bits for long columns, 2^14 of their values at a time."""
+    n = a.shape[0] >> 14 << 14
+    out = a[n:].double().t() @ b[n:].double()
+    if n:
+        tall = [t[:n].double().view(-1, 1 << 14, t.shape[1]) for t in (a, b)]
+        out += torch.bmm(tall[0].transpose(1, 2).contiguous(), tall[1]).sum(0)
+    return out
+
+
 def empty(rows, cols, dt, pad=0):
     return ff.empty_gpu(rows, cols, dt, pad)
 
@@ -110,3 +120,56 @@ def test_gradients_of_rows_longer_than_a_tile_reaches(B, type):
         part = slice(k, k + (1 << 21))
         same("dx", dx[:, part], product(dy, w[:, part].t()))
         same("dw", dw[:, part], product(dy.t(), x[:, part].t()))
+
+
+def test_more_rows_than_threads_of_a_launch(B):
+    """2^30 rows of 8 values: in tiles of 64, or 64 rows to a workgroup of dz, more than the 2^32 threads that a launch takes."""
+    t, dt = consts(B, "bf16")
+    M, N, K = (1 << 30) + 100, 8, 8
+    if torch.cuda.mem_get_info()[0] < 150e9:
+        pytest.skip("needs 150 GB")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w = numbers(g, M, K, dt), numbers(g, N, K, dt)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    y, z = (torch.empty(M, N, dtype=dt, device="cuda") for _ in range(2))
+    ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+    B.cct_linear_forward(d, x, w, None, None, y, z, ws)
+    del ws
+    parts = [slice(m, min(m + (1 << 26), M)) for m in range(0, M, 1 << 26)]
+    for p in parts:
+        want = product(x[p], w)
+        same("z", z[p], want)
+        same("y", y[p], want.clamp_(min=0))
+    del want
+    dy, dx, dw = y, torch.empty(M, K, dtype=dt, device="cuda"), empty(N, K, dt)
+    for p in parts:
+        dy[p].copy_(torch.randint(-1, 2, dy[p].shape, generator=g, device="cuda", dtype=torch.int8))
+    db = torch.full((N,), float("nan"), dtype=dt, device="cuda")
+    ws = B.alloc_linear_workspace(d, B.PASS_BACKWARD)
+    B.cct_linear_backward(d, x, w, z, dy, dx, dw, db, ws)
+    del ws
+    want_w, want_b = torch.zeros(N, K, dtype=torch.float64, device="cuda"), torch.zeros(N, dtype=torch.float64, device="cuda")
+    for p in parts:
+        dz = dy[p].mul_(z[p] > 0)
+        same("dx", dx[p], product(dz, w.t()))
+        want_w += column_product(dz, x[p])
+        want_b += dz.double().sum(0)
+    same("dw", dw, want_w)
+    same("dbias", db, want_b)
+
+
+def test_more_joined_results_than_threads_of_a_launch(B):
+    """fp32 results with an activation go through the workspace: 2^34 of them, four to a thread."""
+    M, N, K = (1 << 22) + 40, 4096, 4
+    if torch.cuda.mem_get_info()[0] < 160e9:
+        pytest.skip("needs 160 GB")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, w = numbers(g, M, K, torch.float32, 3), numbers(g, N, K, torch.float32, 3)
+    d = B.make_linear_desc(M, N, K, B.TYPE_F32, B.ACT_RELU)
+    y = torch.empty(M, N, device="cuda")
+    ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+    B.cct_linear_forward(d, x, w, None, None, y, None, ws)
+    for m in range(0, M, 1 << 17):
+        p = slice(m, min(m + (1 << 17), M))
+        want = x[p] @ w.t()          # exact in any precision that holds 36
+        same("y", y[p], want.clamp_(min=0))
