@@ -335,7 +335,8 @@ typedef enum {
 } cct_activation_t;
 
 /* Host structs.  `type` holds a cct_type_t, `activation` a cct_activation_t.  M >= 0, the others >= 1; M == 0 is an
- * empty batch: nothing is read, gradients of weights are zero. */
+ * empty batch: nothing is read, gradients of weights are zero.  CCT_EUNSUPPORTED: a size above 2^31 - 256, a matrix of more
+ * than 2^38 bytes. */
 typedef struct {
   int32_t M, N, K; /* x: M x K, w: N x K, y: M x N */
   int32_t type, activation;

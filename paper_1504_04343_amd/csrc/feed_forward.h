@@ -52,21 +52,22 @@ struct FfTilePlan {
 FfTilePlan ff_tile_plan(const FfProduct& p);
 int launch_ff_tile_bf16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
 int launch_ff_tile_f16(const FfProduct& p, const FfTilePlan& plan, float* ws, hipStream_t st);
-// fp32 (ff_f32.hip): splits of `len` steps, rows that are packed at a time, and the bytes for them and for the sums.
-struct FfF32Plan {
-  int splits, len, rows;
-  long long pack_bytes, part_bytes;
-};
-// `along`: the weights' operand lies along the contraction.
-FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool along);
-int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st);
-// Products that neither takes (ff_general.hip), which may be cut into splits of so many steps of 16.
+// Products that neither those nor the fp32 ones take (ff_general.hip), in splits of so many steps of 16.
 struct FfGeneralPlan {
   int splits, steps;
   long long part_bytes;
 };
 FfGeneralPlan ff_general_plan(const FfProduct& p);
 int launch_ff_general(const FfProduct& p, const FfGeneralPlan& plan, float* ws, hipStream_t st);
+// fp32 (ff_f32.hip): splits of `len` steps, rows that are packed at a time, and the bytes for them and for the sums; how the
+// general kernel runs where it has to.
+struct FfF32Plan {
+  int splits, len, rows;
+  long long pack_bytes, part_bytes;
+  FfGeneralPlan general;
+};
+FfF32Plan ff_f32_plan(const FfProduct& p);
+int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st);
 // A forward product (operands along the contraction, at any address) of few rows: up to kFfRowsMost run, up to kFfRows (fp32:
 // kFfRowsF32) are faster so.
 constexpr int kFfRows = 16, kFfRowsF32 = 32, kFfRowsMost = 64;

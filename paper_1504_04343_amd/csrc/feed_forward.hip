@@ -28,13 +28,13 @@ bool matrix_ok(const Matrix& m, long long rows, long long cols, int type) {
 }
 bool vector_ok(const void* p, int type) { return !((uintptr_t)p & (type_bytes(type) - 1)); }
 
-// Sizes up to which no product of two of them, a stride and a value's bytes passes 63 bits, a size and a tile 31, and a
-// launch's workgroups 31.
+// Sizes up to which no product of two of them, a stride and a value's bytes passes 63 bits and a size and a tile 31, and each
+// matrix is no larger than 2^38 bytes, which no card holds: the kernels' launches count on that.
 int dims_ok(int32_t M, int32_t N, int32_t K, int32_t type, int32_t activation) {
   if (M < 0 || N < 1 || K < 1 || !type_known(type) || !activation_known(activation)) return CCT_EINVAL;
   if (std::max(M, std::max(N, K)) > 0x7fffff00) return CCT_EUNSUPPORTED;
-  const long long tiles = up(M, 64) / 64 * (up(N, 64) / 64), back = up(std::max(N, K), 64) / 64 * (up(std::max(M, N), 64) / 64);
-  return tiles < 0x7fffffffLL && back < 0x7fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
+  const long long most = (1LL << 38) / type_bytes(type);
+  return std::max((long long)M * N, std::max((long long)M * K, (long long)N * K)) <= most ? CCT_OK : CCT_EUNSUPPORTED;
 }
 int workspace_ok(const void* workspace, size_t have, long long need) {
   if (!workspace || ((uintptr_t)workspace & 255)) return CCT_EINVAL;
@@ -52,7 +52,7 @@ struct Room {
 Room room(const FfProduct& p) {
   if (p.M == 0) return {0, 0};
   if (p.type != CCT_TYPE_F32) return {0, ff_tile_plan(p).part_bytes};
-  const FfF32Plan plan = ff_f32_plan(p.M, p.N, p.K, p.epilogue, p.segments, !p.b_across);
+  const FfF32Plan plan = ff_f32_plan(p);
   return {plan.pack_bytes, plan.part_bytes};
 }
 Room larger(const Room& a, const Room& b) { return {std::max(a.pack, b.pack), std::max(a.part, b.part)}; }

@@ -33,11 +33,18 @@ GemmTN split_problem(int M, int N, int K, int splits) {
   return t;
 }
 
+bool fits(const FfF32Plan& plan, int N, long long ldb, bool along) {
+  GemmTN t = split_problem(plan.rows, N, plan.len, plan.splits);
+  t.b_ks = ldb;
+  return gemm_split_fits(t, along);
+}
+
 }  // namespace
 
-FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool along) {
-  const int planes = epilogue == kFfGated ? 2 : segments;
-  FfF32Plan best = {1, K, M, 0, 0};
+FfF32Plan ff_f32_plan(const FfProduct& p) {
+  const int M = p.M, N = p.N, K = p.K, planes = p.epilogue == kFfGated ? 2 : p.segments;
+  const bool along = !p.b_across;
+  FfF32Plan best = {1, K, M, 0, 0, {1, 0, 0}};
   const long long ld = (N + 3) / 4 * 4;
   if (M > 0 && K > 0) {
     double least = 1e30;
@@ -57,20 +64,23 @@ FfF32Plan ff_f32_plan(int M, int N, int K, int epilogue, int segments, bool alon
     best.pack_bytes = 6LL * best.splits * gemm_split_mpad(best.rows) * gemm_split_kpad(best.len);
   }
   best.part_bytes = 4LL * best.splits * planes * M * ld;
+  // rows so long that the split product does not address them wherever they lie
+  if (M > 0 && K > 0 && !fits(best, N, along ? K : N, along)) {
+    best.general = ff_general_plan(p);
+    best.pack_bytes = 0;
+    best.part_bytes = best.general.part_bytes;
+  }
   return best;
 }
 
 int launch_ff_f32(const FfProduct& p, char* pack, float* ws, hipStream_t st) {
   const bool gated = p.epilogue == kFfGated, along = !p.b_across;
   const int products = gated ? 2 : p.segments;
-  const FfF32Plan plan = ff_f32_plan(p.M, p.N, p.K, p.epilogue, p.segments, along);
+  const FfF32Plan plan = ff_f32_plan(p);
   const bool join = plan.splits > 1 || products > 1 || p.residual || p.z || p.activation != CCT_ACT_NONE;
   const long long ld = join ? (p.N + 3) / 4 * 4 : p.ldo;
-  for (int q = 0; q < products; ++q) {
-    GemmTN t = split_problem(plan.rows, p.N, plan.len, plan.splits);
-    t.b_ks = p.B[q].ld;
-    if (p.K < 1 || !gemm_split_fits(t, along)) return launch_ff_general(p, {1, 0, 0}, nullptr, st);
-  }
+  for (int q = 0; q < products; ++q)
+    if (p.K < 1 || !fits(plan, p.N, p.B[q].ld, along)) return launch_ff_general(p, plan.general, ws, st);
   for (long long m0 = 0; m0 < p.M; m0 += plan.rows) {
     GemmTN t = split_problem((int)std::min<long long>(plan.rows, p.M - m0), p.N, plan.len, plan.splits);
     for (int q = 0; q < products; ++q) {

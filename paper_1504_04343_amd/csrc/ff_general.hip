@@ -81,7 +81,7 @@ void launch(const FfProduct& p, const FfPart& part, hipStream_t st) {
 
 }  // namespace
 
-// Four workgroups per CU of at least 256 steps of 16 k.
+// Up to four workgroups per CU, of at least 256 steps of 16 k each.
 FfGeneralPlan ff_general_plan(const FfProduct& p) {
   const long long tiles = ((p.M + BT - 1LL) / BT) * ((p.N + BT - 1LL) / BT), products = p.epilogue == kFfGated ? 2 : 1;
   const long long steps = (p.K + BK - 1LL) / BK * (p.epilogue == kFfGated ? 1 : p.segments);

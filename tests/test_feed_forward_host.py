@@ -136,3 +136,26 @@ def test_the_binding_looks_at_tensors(B):
         B.make_tensor_list([cpu])
     with pytest.raises(B.CctError):
         B.cct_linear_forward(B.make_linear_desc(4, 8, 16, 9), cpu, cpu, None, None, cpu, None, cpu)
+
+
+def test_sizes_of_matrices_that_fit_a_card(B):
+    """What is refused is a matrix that no card holds, not two sizes that no matrix has."""
+    def ask(M, N, K, type):
+        out = set()
+        for make, f in ((B.make_linear_desc, B.cct_linear_workspace_bytes), (B.make_gated_desc, B.cct_gated_workspace_bytes)):
+            for p in (B.PASS_FORWARD, B.PASS_BACKWARD):
+                try:
+                    assert f(make(M, N, K, type), p) > 0
+                    out.add(B.OK)
+                except B.CctError as e:
+                    out.add(e.code)
+        assert len(out) == 1
+        return out.pop()
+    for type in (B.TYPE_F32, B.TYPE_BF16, B.TYPE_F16):
+        for sizes in ((8, 3000000, 8), (8, 8, 3000000), (1, 2 ** 31 - 256, 8), (2 ** 31 - 256, 1, 1), (1, 1, 2 ** 31 - 256),
+                      (1 << 24, 64, 1 << 12)):
+            assert ask(*sizes, type) == B.OK, sizes
+        for sizes in ((1 << 20, 1 << 20, 8), (8, 1 << 20, 1 << 20), (1 << 20, 8, 1 << 20)):
+            assert ask(*sizes, type) == B.EUNSUPPORTED, sizes
+    assert ask(1 << 19, 1 << 18, 8, B.TYPE_BF16) == B.OK
+    assert ask(1 << 19, 1 << 18, 8, B.TYPE_F32) == B.EUNSUPPORTED

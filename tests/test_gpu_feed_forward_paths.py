@@ -13,7 +13,13 @@ pytestmark = pytest.mark.gpu
 def B():
     assert torch.cuda.is_available()
     from paper_1504_04343_amd import binding
-    yield binding
+    return binding
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    """Tensors of tens of gigabytes are given back, not kept for the next test."""
+    yield
     torch.cuda.empty_cache()
 
 
@@ -173,3 +179,124 @@ def test_more_joined_results_than_threads_of_a_launch(B):
         p = slice(m, min(m + (1 << 17), M))
         want = x[p] @ w.t()          # exact in any precision that holds 36
         same("y", y[p], want.clamp_(min=0))
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_gradients_of_more_outputs_than_a_tile_reaches(B, type):
+    """17 million outputs: dz's rows, along the contraction of dx and across that of dw."""
+    t, dt = consts(B, type)
+    M, N, K = 70, (1 << 24) + (1 << 21), 16
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, w, dy, z = numbers(g, M, K, dt), numbers(g, N, K, dt), numbers(g, M, N, dt), numbers(g, M, N, dt)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    dx, dw = empty(M, K, dt), empty(N, K, dt)
+    db = torch.full((N,), float("nan"), dtype=dt, device="cuda")
+    ws = B.alloc_linear_workspace(d, B.PASS_BACKWARD)
+    assert "ff_general_kernel" in profiled(B, lambda: B.cct_linear_backward(d, x, w, z, dy, dx, dw, db, ws))
+    dy.mul_(z > 0)
+    same("dx", dx, product(dy, w.t()))
+    for n in range(0, N, 1 << 21):
+        cols = dy[:, n:n + (1 << 21)]
+        same("dw", dw[n:n + (1 << 21)], product(cols.t(), x.t()))
+        same("dbias", db[n:n + (1 << 21)], cols.double().sum(0))
+
+
+@pytest.mark.parametrize("type", list(ff.TYPES))
+def test_three_million_outputs(B, type):
+    """More outputs than their square allows, of few inputs."""
+    t, dt = consts(B, type)
+    M, N, K = 8, 3000000, 8
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, w, bias, dy = numbers(g, M, K, dt), numbers(g, N, K, dt), numbers(g, 1, N, dt).view(N), numbers(g, M, N, dt)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    y, z, dx, dw = empty(M, N, dt), empty(M, N, dt), empty(M, K, dt), empty(N, K, dt)
+    db = torch.full((N,), float("nan"), dtype=dt, device="cuda")
+    B.cct_linear_forward(d, x, w, bias, None, y, z, B.alloc_linear_workspace(d, B.PASS_FORWARD))
+    want = product(x, w) + bias.double()
+    same("z", z, want)
+    same("y", y, want.clamp(min=0))
+    B.cct_linear_backward(d, x, w, z, dy, dx, dw, db, B.alloc_linear_workspace(d, B.PASS_BACKWARD))
+    dy.mul_(z > 0)
+    same("dx", dx, product(dy, w.t()))
+    same("dw", dw, product(dy.t(), x.t()))
+    same("dbias", db, dy.double().sum(0))
+    e = B.make_gated_desc(M, N, K, t, B.ACT_RELU)
+    dx, dwg, dwu, h, gg, uu = empty(M, K, dt), empty(N, K, dt), empty(N, K, dt), empty(M, N, dt), empty(M, N, dt), empty(M, N, dt)
+    wu = numbers(g, N, K, dt)
+    B.cct_gated_forward(e, x, w, wu, h, gg, uu, B.alloc_gated_workspace(e, B.PASS_FORWARD))
+    want_g, want_u = product(x, w), product(x, wu)
+    same("g", gg, want_g)
+    same("u", uu, want_u)
+    same("h", h, want_g.clamp(min=0) * want_u)
+    B.cct_gated_backward(e, x, w, wu, gg, uu, dy, dx, dwg, dwu, B.alloc_gated_workspace(e, B.PASS_BACKWARD))
+    dg, du = dy.double() * want_u * (want_g > 0), dy.double() * want_g.clamp(min=0)
+    same("dx", dx, product(dg, w.t()) + product(du, wu.t()))
+    same("dwg", dwg, product(dg.t(), x.t()))
+    same("dwu", dwu, product(du.t(), x.t()))
+
+
+@pytest.mark.parametrize("type,N", [("f32", (1 << 26) + 80), ("bf16", (1 << 27) + 80)])
+def test_few_rows_of_more_outputs_than_threads_of_a_launch(B, type, N):
+    """16 outputs to a workgroup of the kernel for few rows would be 2^32 threads."""
+    t, dt = consts(B, type)
+    M, K = 2, 8
+    g = torch.Generator(device="cuda").manual_seed(10)
+    x, w = numbers(g, M, K, dt), numbers(g, N, K, dt)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    y = empty(M, N, dt)
+    ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+    assert "ff_rows_kernel" not in profiled(B, lambda: B.cct_linear_forward(d, x, w, None, None, y, None, ws))
+    for n in range(0, N, 1 << 24):
+        same("y", y[:, n:n + (1 << 24)], product(x, w[n:n + (1 << 24)]).clamp(min=0))
+    small = B.make_linear_desc(M, 4096, K, t, B.ACT_RELU)
+    assert "ff_rows_kernel" in profiled(B, lambda: B.cct_linear_forward(small, x, w[:4096], None, None, empty(M, 4096, dt), None, ws))
+
+
+def test_column_sums_of_more_outputs_than_threads_of_a_launch(B):
+    """The sum of columns takes 16 of them and 1024 threads to a workgroup, in two launches."""
+    t, dt = consts(B, "bf16")
+    M, N, K = 70, (1 << 26) + 80, 8      # more rows than one workgroup of dz takes
+    if torch.cuda.mem_get_info()[0] < 60e9:
+        pytest.skip("needs 60 GB")
+    g = torch.Generator(device="cuda").manual_seed(11)
+    x, w, dy, z = numbers(g, M, K, dt), numbers(g, N, K, dt), numbers(g, M, N, dt), numbers(g, M, N, dt)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    dx, dw = empty(M, K, dt), empty(N, K, dt)
+    db = torch.full((N,), float("nan"), dtype=dt, device="cuda")
+    ws = B.alloc_linear_workspace(d, B.PASS_BACKWARD)
+    B.cct_linear_backward(d, x, w, z, dy, dx, dw, db, ws)
+    dy.mul_(z > 0)
+    same("dx", dx, product(dy, w.t()))
+    for n in range(0, N, 1 << 22):
+        cols = dy[:, n:n + (1 << 22)]
+        same("dw", dw[n:n + (1 << 22)], product(cols.t(), x.t()))
+        same("dbias", db[n:n + (1 << 22)], cols.double().sum(0))
+
+
+def test_fp32_rows_longer_than_the_split_product_addresses(B):
+    """Weights of 2^22 values a row and more run on the general kernel, in splits of the contraction."""
+    M, N, K = 40, 48, (1 << 22) + 8
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x, w, u = (numbers(g, r, K, torch.float32) for r in (M, N, N))
+    d = B.make_linear_desc(M, N, K, B.TYPE_F32, B.ACT_RELU)
+    y, z = empty(M, N, torch.float32), empty(M, N, torch.float32)
+    ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+    ws.fill_(0xff)
+    assert profiled(B, lambda: B.cct_linear_forward(d, x, w, None, None, y, z, ws)) == ["ff_general_kernel"]
+    want = product(x, w)
+    same("z", z, want)
+    same("y", y, want.clamp(min=0))
+    e = B.make_gated_desc(M, N, K, B.TYPE_F32, B.ACT_RELU)
+    h, gg, uu = (empty(M, N, torch.float32) for _ in range(3))
+    ws = B.alloc_gated_workspace(e, B.PASS_FORWARD)
+    ws.fill_(0xff)
+    B.cct_gated_forward(e, x, w, u, h, gg, uu, ws)
+    same("g", gg, want)
+    same("u", uu, product(x, u))
+    same("h", h, (want.clamp(min=0) * product(x, u)).float())
+    dz = numbers(g, M, N, torch.float32)
+    dx, dw = empty(M, K, torch.float32), empty(N, K, torch.float32)
+    l = B.make_linear_desc(M, N, K, B.TYPE_F32)
+    B.cct_linear_backward(l, x, w, None, dz, dx, dw, None, B.alloc_linear_workspace(l, B.PASS_BACKWARD))
+    same("dx", dx, product(dz, w.t()))
+    same("dw", dw, product(dz.t(), x.t()))
