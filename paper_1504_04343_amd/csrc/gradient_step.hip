@@ -240,36 +240,42 @@ __global__ __launch_bounds__(NT) void sgd_update_kernel(UpdateArgs a, const floa
 
 long long runs(long long n, int run) { return (n + run - 1) / run; }
 
-// CCT_OK, and how many workgroups the norm of the list takes.  Every pointer of a tensor with values must be there and aligned to one.
-int check_list(const cct_tensor_t* list, int count, long long* blocks) {
+constexpr long long kMostRuns = kMostThreads / NT;  // of a launch
+
+// CCT_OK, and how many workgroups the list takes at `run` values each; a tensor's must fit one launch (2^37 values, 2^36 for
+// the update: no card holds more).  Every pointer of a tensor with values must be there and aligned to one.
+int check_list(const cct_tensor_t* list, int count, int run, long long* blocks) {
   if (count < 0 || (count > 0 && !list)) return CCT_EINVAL;
   *blocks = 0;
   for (int i = 0; i < count; ++i) {
     const cct_tensor_t& t = list[i];
     if (t.n < 0 || !type_known(t.type) || (t.n > 0 && !t.data) || ((uintptr_t)t.data & (type_bytes(t.type) - 1)))
       return CCT_EINVAL;
-    if (t.n > (1LL << 44)) return CCT_EUNSUPPORTED;
-    *blocks += runs(t.n, NormArgs::kRun);
+    if (t.n > kMostRuns * run) return CCT_EUNSUPPORTED;
+    *blocks += runs(t.n, run);
   }
-  // (the update has twice as many)
-  return *blocks < 0x3fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
+  return *blocks < 0x7fffffffLL ? CCT_OK : CCT_EUNSUPPORTED;
 }
-int check_same(const cct_tensor_t* a, const cct_tensor_t* b, int count) {
+int check_same(const cct_tensor_t* a, const cct_tensor_t* b, int count, int run) {
   long long blocks;
-  const int rc = check_list(b, count, &blocks);
+  const int rc = check_list(b, count, run, &blocks);
   if (rc != CCT_OK) return rc;
   for (int i = 0; i < count; ++i)
     if (a[i].n != b[i].n) return CCT_EINVAL;
   return CCT_OK;
 }
 
-// Tensors [from, to) of the lists as one launch's arguments; returns the first tensor left out.  `forward`: from `from` up,
-// else from `to` down.  *values, *bytes: of the gradients (and copies).
+// Tensors [from, to) of the lists as one launch's arguments, as many as it takes; returns the first tensor left out.
+// `forward`: from `from` up, else from `to` down.  *values, *bytes: of the gradients (and copies).
 template <class Args, int P>
 int fill(Args* a, const cct_tensor_t* const (&lists)[P], int from, int to, bool forward, double* values, double* bytes) {
   *values = *bytes = 0.0;
   int lo = forward ? from : to, hi = lo, held = 0;
-  auto take = [&](int i) { return lists[0][i].n == 0 || ++held <= Args::kCount; };
+  long long blocks_held = 0;
+  auto take = [&](int i) {
+    blocks_held += runs(lists[0][i].n, Args::kRun);
+    return lists[0][i].n == 0 || (++held <= Args::kCount && blocks_held <= kMostRuns);
+  };
   if (forward)
     while (hi < to && take(hi)) ++hi;
   else
@@ -300,7 +306,7 @@ extern "C" {
 int cct_grad_norm_workspace_bytes(const cct_tensor_t* grads, int32_t count, size_t* bytes) {
   long long blocks;
   if (!bytes) return CCT_EINVAL;
-  const int rc = check_list(grads, count, &blocks);
+  const int rc = check_list(grads, count, NormArgs::kRun, &blocks);
   if (rc != CCT_OK) return rc;
   *bytes = (size_t)std::max(1LL, blocks) * sizeof(double);
   return CCT_OK;
@@ -309,7 +315,7 @@ int cct_grad_norm_workspace_bytes(const cct_tensor_t* grads, int32_t count, size
 int cct_grad_norm(const cct_tensor_t* grads, int32_t count, float max_norm, float* clip, void* workspace,
                   size_t workspace_bytes, void* hip_stream) {
   long long blocks;
-  const int rc = check_list(grads, count, &blocks);
+  const int rc = check_list(grads, count, NormArgs::kRun, &blocks);
   if (rc != CCT_OK) return rc;
   if (!clip || ((uintptr_t)clip & 3) || !(max_norm > 0.f)) return CCT_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 255)) return CCT_EINVAL;
@@ -337,8 +343,8 @@ int cct_grad_norm(const cct_tensor_t* grads, int32_t count, float max_norm, floa
 int cct_grad_scale(const cct_tensor_t* grads, int32_t count, const float* clip, const cct_tensor_t* out,
                    void* hip_stream) {
   long long blocks;
-  int rc = check_list(grads, count, &blocks);
-  if (rc == CCT_OK) rc = check_same(grads, out, count);
+  int rc = check_list(grads, count, ScaleArgs::kRun, &blocks);
+  if (rc == CCT_OK) rc = check_same(grads, out, count, ScaleArgs::kRun);
   if (rc != CCT_OK) return rc;
   if (!clip || ((uintptr_t)clip & 3)) return CCT_EINVAL;
   for (int i = 0; i < count; ++i)
@@ -361,10 +367,10 @@ int cct_sgd_update(const cct_tensor_t* grads, int32_t count, const float* clip, 
                    const cct_tensor_t* moments, const cct_tensor_t* copies, float rate, float momentum, float decay,
                    void* hip_stream) {
   long long blocks;
-  int rc = check_list(grads, count, &blocks);
-  if (rc == CCT_OK) rc = check_same(grads, weights, count);
-  if (rc == CCT_OK) rc = check_same(grads, moments, count);
-  if (rc == CCT_OK && copies) rc = check_same(grads, copies, count);
+  int rc = check_list(grads, count, UpdateArgs::kRun, &blocks);
+  if (rc == CCT_OK) rc = check_same(grads, weights, count, UpdateArgs::kRun);
+  if (rc == CCT_OK) rc = check_same(grads, moments, count, UpdateArgs::kRun);
+  if (rc == CCT_OK && copies) rc = check_same(grads, copies, count, UpdateArgs::kRun);
   if (rc != CCT_OK) return rc;
   if ((uintptr_t)clip & 3) return CCT_EINVAL;
   if (!std::isfinite(rate) || !std::isfinite(momentum) || !std::isfinite(decay)) return CCT_EINVAL;

@@ -159,3 +159,20 @@ def test_sizes_of_matrices_that_fit_a_card(B):
             assert ask(*sizes, type) == B.EUNSUPPORTED, sizes
     assert ask(1 << 19, 1 << 18, 8, B.TYPE_BF16) == B.OK
     assert ask(1 << 19, 1 << 18, 8, B.TYPE_F32) == B.EUNSUPPORTED
+
+
+def test_tensors_beyond_a_launch(B):
+    """A launch takes 2^24 - 1 workgroups of 8192 values (the update: 4096); more in one tensor are refused, in several not."""
+    lib, n = B._lib, ctypes.c_size_t()
+
+    def lst(*sizes, type=1):
+        return (B.Tensor * len(sizes))(*(B.Tensor(P, s, type, 0) for s in sizes))
+    most = ((1 << 24) - 1) * 8192
+    assert lib.cct_grad_norm_workspace_bytes(lst(most), 1, ctypes.byref(n)) == B.OK and n.value == 8 * ((1 << 24) - 1)
+    assert lib.cct_grad_norm_workspace_bytes(lst(most, most), 2, ctypes.byref(n)) == B.OK
+    for more in (most + 1, 1 << 40):
+        assert lib.cct_grad_norm_workspace_bytes(lst(5, more), 2, ctypes.byref(n)) == B.EUNSUPPORTED
+        assert lib.cct_grad_norm(lst(5, more), 2, 1.0, P, P, 1 << 60, None) == B.EUNSUPPORTED
+        assert lib.cct_grad_scale(lst(5, more), 2, P, lst(5, more), None) == B.EUNSUPPORTED
+    w = lst(most // 2 + 1, type=0)
+    assert lib.cct_sgd_update(lst(most // 2 + 1), 1, P, w, w, None, 0.1, 0.9, 0.0, None) == B.EUNSUPPORTED

@@ -155,3 +155,22 @@ def test_same_bits_every_time_and_from_a_graph(B):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(clip, wc) and all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_a_list_of_more_workgroups_than_a_launch_takes(B):
+    """2^37 values and more in one list, which is one tensor 17 times over: two launches."""
+    if torch.cuda.mem_get_info()[0] < 40e9:
+        pytest.skip("needs 40 GB")
+    flat = torch.zeros(1 << 33, dtype=torch.bfloat16, device="cuda")
+    flat[::1 << 23] = 2.0
+    flat[-1] = 5.0
+    lst = B.make_tensor_list([flat] * 17)
+    clip = torch.full((2,), float("nan"), device="cuda")
+    B.cct_grad_norm(lst, 1e6, clip, B.alloc_norm_workspace(lst))
+    want = (17 * (1024 * 4.0 + 25.0)) ** 0.5
+    norm, scale = clip.tolist()
+    assert abs(norm - want) <= 2.0 ** -23 * want and scale == 1.0
+    B.cct_grad_scale(lst, clip, lst)                # scale 1 in place: nothing is written
+    assert float(flat[-1]) == 5.0 and float(flat[1 << 23]) == 2.0
+    del flat, lst
+    torch.cuda.empty_cache()
