@@ -5,15 +5,26 @@
 namespace cct {
 namespace {
 
-// 1 / (1 + exp(-z)); both ends are exact (exp overflows to infinity, its reciprocal is 0)
-__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + expf(-z)); }
+// 1 / (1 + exp(-a)) as the product q c.  Below a = -87 it is no normal number, and from -88.7 on exp(-a) overflows, while what
+// it is multiplied by keeps the products normal: far down q is exp(a + 32) (the sum is exact, and 1 + exp(a) is 1) and c is
+// exp(-32), which is multiplied by last; elsewhere c is 1.
+struct Logistic {
+  float q, c;
+};
+__device__ __forceinline__ Logistic logistic(float a) {
+  const bool far = a < -64.f;
+  const float e = expf(far ? a + 32.f : -a);
+  return {far ? e : 1.f / (1.f + e), far ? 1.26641655e-14f : 1.f};
+}
 
 constexpr float kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhC = 0.79788456080286536f, kTanhD = 0.044715f;
 
-// act(z) for several values: one uniform branch for all of them
+// act(z) = z c for several values: one uniform branch for all of them
 template <int N>
-__device__ __forceinline__ void activate(int act, float (&z)[N]) {
+__device__ __forceinline__ void activate(int act, float (&z)[N], float (&c)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) c[e] = 1.f;
   switch (act) {
     case CCT_ACT_RELU:
 #pragma unroll
@@ -21,7 +32,11 @@ __device__ __forceinline__ void activate(int act, float (&z)[N]) {
       break;
     case CCT_ACT_SILU:
 #pragma unroll
-      for (int e = 0; e < N; ++e) z[e] *= logistic(z[e]);
+      for (int e = 0; e < N; ++e) {
+        const Logistic s = logistic(z[e]);
+        z[e] *= s.q;
+        c[e] = s.c;
+      }
       break;
     case CCT_ACT_GELU:  // erfc, not 1 + erf: the left tail keeps its digits
 #pragma unroll
@@ -29,15 +44,21 @@ __device__ __forceinline__ void activate(int act, float (&z)[N]) {
       break;
     case CCT_ACT_GELU_TANH:  // (1 + tanh(a)) / 2 is the logistic function of 2 a
 #pragma unroll
-      for (int e = 0; e < N; ++e) z[e] *= logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z[e] * z[e]));
+      for (int e = 0; e < N; ++e) {
+        const Logistic s = logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z[e] * z[e]));
+        z[e] *= s.q;
+        c[e] = s.c;
+      }
       break;
     default: break;
   }
 }
 
-// act(z) and act'(z)
+// act(z) = a c and act'(z) = d c
 template <int N>
-__device__ __forceinline__ void activate_both(int act, const float (&z)[N], float (&a)[N], float (&d)[N]) {
+__device__ __forceinline__ void activate_both(int act, const float (&z)[N], float (&a)[N], float (&d)[N], float (&c)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) c[e] = 1.f;
   switch (act) {
     case CCT_ACT_RELU:
 #pragma unroll
@@ -49,9 +70,10 @@ __device__ __forceinline__ void activate_both(int act, const float (&z)[N], floa
     case CCT_ACT_SILU:
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float s = logistic(z[e]);
-        a[e] = z[e] * s;
-        d[e] = s * (1.f + z[e] * (1.f - s));
+        const Logistic s = logistic(z[e]);
+        a[e] = z[e] * s.q;
+        d[e] = s.q * (1.f + z[e] * (1.f - s.q * s.c));
+        c[e] = s.c;
       }
       break;
     case CCT_ACT_GELU:
@@ -65,10 +87,12 @@ __device__ __forceinline__ void activate_both(int act, const float (&z)[N], floa
     case CCT_ACT_GELU_TANH:
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float z2 = z[e] * z[e], s = logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z2));
-        const float slope = 2.f * s * (1.f - s);  // 0 where z2 overflows: no infinity times 0
-        a[e] = z[e] * s;
-        d[e] = s + (slope == 0.f ? 0.f : z[e] * slope * (kTanhC * (1.f + 3.f * kTanhD * z2)));
+        const float z2 = z[e] * z[e];
+        const Logistic s = logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z2));
+        const float slope = 2.f * s.q * (1.f - s.q * s.c);  // 0 where z2 overflows: no infinity times 0
+        a[e] = z[e] * s.q;
+        d[e] = s.q + (slope == 0.f ? 0.f : z[e] * slope * (kTanhC * (1.f + 3.f * kTanhD * z2)));
+        c[e] = s.c;
       }
       break;
     default:
