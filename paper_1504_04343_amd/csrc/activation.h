@@ -20,68 +20,64 @@ __device__ __forceinline__ Logistic logistic(float a) {
 constexpr float kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTanhC = 0.79788456080286536f, kTanhD = 0.044715f;
 
-// act(z) = z c for several values: one uniform branch for all of them
-template <int N>
-__device__ __forceinline__ void activate(int act, float (&z)[N], float (&c)[N]) {
-#pragma unroll
-  for (int e = 0; e < N; ++e) c[e] = 1.f;
+// act(z) for several values, or act(z) u: one uniform branch for all of them
+template <bool GATE, int N>
+__device__ __forceinline__ void activate(int act, float (&z)[N], const float (&u)[N]) {
+  auto gate = [&](float v, int e) { return GATE ? v * u[e] : v; };
   switch (act) {
     case CCT_ACT_RELU:
 #pragma unroll
-      for (int e = 0; e < N; ++e) z[e] = z[e] < 0.f ? 0.f : z[e];  // NaN stays
+      for (int e = 0; e < N; ++e) z[e] = gate(z[e] < 0.f ? 0.f : z[e], e);  // NaN stays
       break;
     case CCT_ACT_SILU:
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const Logistic s = logistic(z[e]);
-        z[e] *= s.q;
-        c[e] = s.c;
+        z[e] = gate(z[e] * s.q, e) * s.c;
       }
       break;
     case CCT_ACT_GELU:  // erfc, not 1 + erf: the left tail keeps its digits
 #pragma unroll
-      for (int e = 0; e < N; ++e) z[e] *= 0.5f * erfcf(-kSqrtHalf * z[e]);
+      for (int e = 0; e < N; ++e) z[e] = gate(z[e] * (0.5f * erfcf(-kSqrtHalf * z[e])), e);
       break;
     case CCT_ACT_GELU_TANH:  // (1 + tanh(a)) / 2 is the logistic function of 2 a
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const Logistic s = logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z[e] * z[e]));
-        z[e] *= s.q;
-        c[e] = s.c;
+        z[e] = gate(z[e] * s.q, e) * s.c;
       }
       break;
-    default: break;
+    default:
+#pragma unroll
+      for (int e = 0; e < N; ++e) z[e] = gate(z[e], e);
   }
 }
 
-// act(z) = a c and act'(z) = d c
-template <int N>
-__device__ __forceinline__ void activate_both(int act, const float (&z)[N], float (&a)[N], float (&d)[N], float (&c)[N]) {
-#pragma unroll
-  for (int e = 0; e < N; ++e) c[e] = 1.f;
+// v act'(z), and w act(z) if BOTH
+template <bool BOTH, int N>
+__device__ __forceinline__ void activate_back(int act, const float (&z)[N], float (&v)[N], float (&w)[N]) {
   switch (act) {
     case CCT_ACT_RELU:
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        a[e] = z[e] < 0.f ? 0.f : z[e];
-        d[e] = z[e] > 0.f ? 1.f : 0.f;
+        v[e] *= z[e] > 0.f ? 1.f : 0.f;
+        if (BOTH) w[e] *= z[e] < 0.f ? 0.f : z[e];
       }
       break;
     case CCT_ACT_SILU:
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const Logistic s = logistic(z[e]);
-        a[e] = z[e] * s.q;
-        d[e] = s.q * (1.f + z[e] * (1.f - s.q * s.c));
-        c[e] = s.c;
+        v[e] = v[e] * (s.q * (1.f + z[e] * (1.f - s.q * s.c))) * s.c;
+        if (BOTH) w[e] = w[e] * (z[e] * s.q) * s.c;
       }
       break;
     case CCT_ACT_GELU:
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float phi = 0.5f * erfcf(-kSqrtHalf * z[e]);
-        a[e] = z[e] * phi;
-        d[e] = phi + z[e] * (kInvSqrt2Pi * expf(-0.5f * z[e] * z[e]));
+        v[e] *= phi + z[e] * (kInvSqrt2Pi * expf(-0.5f * z[e] * z[e]));
+        if (BOTH) w[e] *= z[e] * phi;
       }
       break;
     case CCT_ACT_GELU_TANH:
@@ -90,17 +86,14 @@ __device__ __forceinline__ void activate_both(int act, const float (&z)[N], floa
         const float z2 = z[e] * z[e];
         const Logistic s = logistic(2.f * kTanhC * (z[e] + kTanhD * z[e] * z2));
         const float slope = 2.f * s.q * (1.f - s.q * s.c);  // 0 where z2 overflows: no infinity times 0
-        a[e] = z[e] * s.q;
-        d[e] = s.q + (slope == 0.f ? 0.f : z[e] * slope * (kTanhC * (1.f + 3.f * kTanhD * z2)));
-        c[e] = s.c;
+        v[e] = v[e] * (s.q + (slope == 0.f ? 0.f : z[e] * slope * (kTanhC * (1.f + 3.f * kTanhD * z2)))) * s.c;
+        if (BOTH) w[e] = w[e] * (z[e] * s.q) * s.c;
       }
       break;
     default:
+      if (BOTH)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        a[e] = z[e];
-        d[e] = 1.f;
-      }
+        for (int e = 0; e < N; ++e) w[e] *= z[e];
   }
 }
 

@@ -67,11 +67,9 @@ __device__ __forceinline__ void do_dz(const DzArgs& a, int block) {
       float v[8];
       load_columns<TYPE>(v, p.dy, r * p.lddy, c, p.N);
       if (p.z) {
-        float z[8], a[8], d[8], f[8];
+        float z[8];
         load_columns<TYPE>(z, p.z, r * p.ldz, c, p.N);
-        activate_both(p.activation, z, a, d, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = v[e] * d[e] * f[e];
+        activate_back<false>(p.activation, z, v, v);
       }
       if (p.dz) {
 #pragma unroll
@@ -117,18 +115,18 @@ __global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows, 
   const int r0 = down * rows, r1 = min(r0 + rows, p.M);
   if (c >= p.F) return;
   for (int r = r0 + (threadIdx.x >> 5); r < r1; r += NT / 32) {
-    float dh[8], g[8], u[8], a[8], d[8], f[8];
+    float dh[8], g[8], u[8];
     load_columns<TYPE>(dh, p.dh, r * p.lddh, c, p.F);
     load_columns<TYPE>(g, p.g, r * p.ldg, c, p.F);
     load_columns<TYPE>(u, p.u, r * p.ldu, c, p.F);
-    activate_both(p.activation, g, a, d, f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      d[e] = c + e < p.F ? dh[e] * u[e] * d[e] * f[e] : 0.f;
-      a[e] = c + e < p.F ? dh[e] * a[e] * f[e] : 0.f;
-    }
-    store_columns<TYPE>(p.dg, r * p.ld + c, d);
-    store_columns<TYPE>(p.du, r * p.ld + c, a);
+    for (int e = 0; e < 8; ++e) u[e] *= dh[e];
+    activate_back<true>(p.activation, g, u, dh);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e >= p.F) u[e] = dh[e] = 0.f;
+    store_columns<TYPE>(p.dg, r * p.ld + c, u);
+    store_columns<TYPE>(p.du, r * p.ld + c, dh);
   }
 }
 

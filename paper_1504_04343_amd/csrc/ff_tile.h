@@ -169,15 +169,12 @@ template <int TYPE, int EPI, int W>
 __device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (&v)[W], float (&u)[W],
                                        const float (*early)[W] = nullptr) {
   const int left = p.N - n;
-  float c[W];
   if constexpr (EPI == kFfGated) {
     if (p.z) {
       store_some<TYPE>(p.z, m * p.ldz + n, v, left);
       store_some<TYPE>(p.z2, m * p.ldz2 + n, u, left);
     }
-    activate(p.activation, v, c);
-#pragma unroll
-    for (int e = 0; e < W; ++e) v[e] = v[e] * u[e] * c[e];
+    activate<true>(p.activation, v, u);
   } else {
     float r[W] = {};
     if (early) {
@@ -193,9 +190,7 @@ __device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (
       for (int e = 0; e < W; ++e) v[e] += b[e];
     }
     if (p.z) store_some<TYPE>(p.z, m * p.ldz + n, v, left);
-    activate(p.activation, v, c);
-#pragma unroll
-    for (int e = 0; e < W; ++e) v[e] *= c[e];
+    activate<false>(p.activation, v, u);
     if (p.residual)
 #pragma unroll
       for (int e = 0; e < W; ++e) v[e] += r[e];
