@@ -73,8 +73,13 @@ FfProduct plain_product(int type, int rows, int cols, int k, bool a_across, bool
   p.ldo = ldo;
   return p;
 }
+// Whether a forward product runs on ff_rows.hip wherever its operands lie (see few_rows): they are not copied then.
+bool always_rows(int M, int N, int type) {
+  return ff_rows_fits(N, type) && M <= (type == CCT_TYPE_F32 ? kFfRowsF32 : kFfRows);
+}
 // Room for a forward product, whichever kernel takes it.
 Room forward_room(int type, int M, int N, int K, FfEpilogue epilogue) {
+  if (always_rows(M, N, type)) return {0, ff_rows_part_bytes(M, N, K, type, epilogue)};
   FfProduct p = plain_product(type, M, N, K, false, false, nullptr, 0);
   p.epilogue = epilogue;
   const Room r = room(p);
@@ -112,8 +117,9 @@ struct LinearLayout {
 LinearLayout linear_layout(const cct_linear_desc_t& d, bool backward) {
   Layout l;
   LinearLayout b;
-  b.x = l.take(copy_bytes(d.M, d.K, d.type));
-  b.w = l.take(copy_bytes(d.N, d.K, d.type));
+  const bool copies = backward || !always_rows(d.M, d.N, d.type);
+  b.x = l.take(copies ? copy_bytes(d.M, d.K, d.type) : 0);
+  b.w = l.take(copies ? copy_bytes(d.N, d.K, d.type) : 0);
   b.ld = up(d.N, 8);
   b.dz = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.sums = l.take(backward ? (long long)ff_sum_rows(d.M, d.N) * d.N * 4 : 0);
@@ -130,9 +136,10 @@ struct GatedLayout {
 GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   Layout l;
   GatedLayout b;
-  b.x = l.take(copy_bytes(d.M, d.K, d.type));
-  b.wg = l.take(copy_bytes(d.F, d.K, d.type));
-  b.wu = l.take(copy_bytes(d.F, d.K, d.type));
+  const bool copies = backward || !always_rows(d.M, d.F, d.type);
+  b.x = l.take(copies ? copy_bytes(d.M, d.K, d.type) : 0);
+  b.wg = l.take(copies ? copy_bytes(d.F, d.K, d.type) : 0);
+  b.wu = l.take(copies ? copy_bytes(d.F, d.K, d.type) : 0);
   b.ld = up(d.F, 8);
   b.dg = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
   b.du = l.take(backward ? (long long)d.M * b.ld * type_bytes(d.type) : 0);
@@ -150,9 +157,7 @@ GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
 // multiples of four bytes take 44 there, so that more than 16 are copied: 62 rows of 10881 -> 2880 166 us there, 43 so.
 // fp32: 16 rows 22.6 us; 48 rows 41 there, 37 on ff_f32.hip; 64 rows of 4096 -> 16384 183 and 100.
 bool few_rows(int M, int N, int type, bool in_place, bool words) {
-  if (!ff_rows_fits(N, type)) return false;
-  if (type == CCT_TYPE_F32) return M <= kFfRowsF32;
-  return M <= kFfRows || (M <= kFfRowsMost && words && !in_place);
+  return always_rows(M, N, type) || (type != CCT_TYPE_F32 && ff_rows_fits(N, type) && M <= kFfRowsMost && words && !in_place);
 }
 
 void add_copy(const Matrix& m, long long rows, long long cols, int type, void* to, Matrix* use, FfDzJobs* jobs) {

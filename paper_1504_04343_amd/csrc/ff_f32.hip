@@ -63,7 +63,8 @@ FfF32Plan ff_f32_plan(const FfProduct& p) {
     }
     best.pack_bytes = 6LL * best.splits * gemm_split_mpad(best.rows) * gemm_split_kpad(best.len);
   }
-  best.part_bytes = 4LL * best.splits * planes * M * ld;
+  // a gradient of one contraction that is not cut is stored as it is; behind a forward product anything may follow
+  best.part_bytes = p.b_across && planes * best.splits == 1 ? 0 : 4LL * best.splits * planes * M * ld;
   // rows so long that the split product does not address them wherever they lie
   if (M > 0 && K > 0 && !fits(best, N, along ? K : N, along)) {
     best.general = ff_general_plan(p);

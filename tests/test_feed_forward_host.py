@@ -176,3 +176,23 @@ def test_tensors_beyond_a_launch(B):
         assert lib.cct_grad_scale(lst(5, more), 2, P, lst(5, more), None) == B.EUNSUPPORTED
     w = lst(most // 2 + 1, type=0)
     assert lib.cct_sgd_update(lst(most // 2 + 1), 1, P, w, w, None, 0.1, 0.9, 0.0, None) == B.EUNSUPPORTED
+
+
+def test_workspace_is_what_a_call_may_need(B):
+    """A forward pass of up to 16 rows (fp32: 32) copies nothing, whatever its operands' addresses; an fp32 gradient whose
+    contraction is not cut is stored without partial sums."""
+    def linear(M, N, K, type, p):
+        return B.cct_linear_workspace_bytes(B.make_linear_desc(M, N, K, type, B.ACT_RELU), p)
+
+    def gated(M, N, K, type, p):
+        return B.cct_gated_workspace_bytes(B.make_gated_desc(M, N, K, type), p)
+    for type, most in ((B.TYPE_BF16, 16), (B.TYPE_F16, 16), (B.TYPE_F32, 32)):
+        for M in (1, most):
+            assert linear(M, 4096, 4096, type, B.PASS_FORWARD) == 256
+            assert gated(M, 8192, 4096, type, B.PASS_FORWARD) == 256
+    assert linear(17, 4096, 4096, B.TYPE_BF16, B.PASS_FORWARD) >= (17 + 4096) * 4096 * 2   # copies
+    # partial sums of few columns of long rows
+    assert linear(16, 64, 9216, B.TYPE_BF16, B.PASS_FORWARD) > 256
+    # dz, its column sums (one row of 64), a packed operand of three terms
+    n = 8192 * 8192
+    assert 0 <= linear(8192, 8192, 8192, B.TYPE_F32, B.PASS_BACKWARD) - (4 * n + 4 * n // 64 + 6 * n) < 1024
