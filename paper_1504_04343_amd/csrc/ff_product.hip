@@ -219,7 +219,8 @@ int launch_ff_products(const FfProduct* p, int count, const FfBiasSum& sum, char
     flops += 2.0 * q.M * q.N * q.K * q.segments;
     bytes += operand_bytes(q) + 2.0 * q.M * q.N;
   }
-  ProfScope ps(flops, bytes, st, "ff_tile_kernel_together<%s, %d products>", kTileNames[plan.tile], n);
+  ProfScope ps(flops, bytes, st, "ff_tile_kernel_together<%s, %d products, %d splits>", kTileNames[plan.tile], n,
+               *std::max_element(theirs.splits, theirs.splits + n));
   return p[0].type == CCT_TYPE_BF16 ? launch_ff_together_bf16(wanted, n, beside, theirs, (char*)ws, st)
                                     : launch_ff_together_f16(wanted, n, beside, theirs, (char*)ws, st);
 }

@@ -300,3 +300,260 @@ def test_fp32_rows_longer_than_the_split_product_addresses(B):
     B.cct_linear_backward(l, x, w, None, dz, dx, dw, None, B.alloc_linear_workspace(l, B.PASS_BACKWARD))
     same("dx", dx, product(dz, w.t()))
     same("dw", dw, product(dz.t(), x.t()))
+
+
+# What is computed; the tile; whether the contraction is split; what of the results is left for a launch of its own; M, N, K in
+# multiples of 8, whose operands are taken in place, and otherwise, copied.
+ALONE = [
+    ("linear", "256x256", False, None, (8121, 1312, 144), (8121, 1305, 141)),
+    ("linear", "256x256", False, "columns", (3082, 5144, 264), (3082, 5139, 259)),
+    ("linear", "256x256", False, "rows", (5470, 2952, 264), (7223, 2207, 261)),
+    ("linear", "192x256", False, None, (3349, 2328, 136), (2307, 3345, 139)),
+    ("linear", "128x128", True, None, (328, 648, 3360), (328, 647, 3357)),
+    ("linear", "128x128", False, None, (1677, 1176, 136), (1685, 1157, 141)),
+    ("linear", "64x128", True, None, (264, 392, 2016), (399, 257, 2001)),
+    ("linear", "64x128", False, None, (1220, 784, 136), (1220, 769, 143)),
+    ("linear", "64x64", True, None, (136, 136, 1224), (136, 137, 1217)),
+    ("linear", "64x64", False, None, (137, 136, 144), (136, 139, 139)),
+    ("gated", "256x256", False, None, (580, 8288, 144), (580, 8283, 137)),
+    ("gated", "256x256", False, "columns", (2949, 2696, 264), (2949, 2693, 263)),
+    ("gated", "256x256", False, "rows", (2331, 3424, 272), (2818, 2857, 257)),
+    ("gated", "192x256", False, None, (385, 8200, 144), (385, 8197, 143)),
+    ("gated", "128x128", True, None, (258, 400, 3360), (258, 399, 3357)),
+    ("gated", "128x128", False, None, (833, 1176, 136), (769, 1251, 139)),
+    ("gated", "64x128", True, None, (139, 328, 2008), (258, 195, 2001)),
+    ("gated", "64x128", False, None, (774, 616, 136), (644, 737, 137)),
+    ("gated", "64x64", True, None, (136, 136, 1224), (136, 137, 1217)),
+    ("gated", "64x64", False, None, (137, 136, 144), (136, 139, 139)),
+    ("dx", "256x256", False, None, (1613, 144, 8888), (1613, 139, 8883)),
+    ("dx", "256x256", False, "columns", (3723, 152, 5328), (3723, 147, 5321)),
+    ("dx", "256x256", False, "rows", (8667, 400, 2000), (8666, 385, 1935)),
+    ("dx", "192x256", False, None, (1737, 272, 6168), (1735, 265, 6177)),
+    ("dx", "128x128", True, None, (403, 6008, 1960), (403, 6005, 1953)),
+    ("dx", "128x128", False, None, (784, 776, 8592), (784, 775, 8587)),
+    ("dx", "64x128", True, None, (139, 6296, 2440), (139, 6291, 2437)),
+    ("dx", "64x128", False, None, (398, 4912, 8984), (398, 4909, 8979)),
+    ("dx", "64x64", True, None, (174, 6264, 5408), (174, 6257, 5401)),
+    ("dx", "64x64", False, None, (272, 1760, 6024), (272, 1755, 6019)),
+    ("dw", "256x256", False, None, (141, 1608, 8840), (141, 1605, 8839)),
+    ("dw", "256x256", False, "columns", (145, 3744, 5272), (152, 3713, 5255)),
+    ("dw", "256x256", False, "rows", (410, 8688, 1968), (410, 8681, 1963)),
+    ("dw", "192x256", False, None, (272, 1760, 6024), (272, 1755, 6019)),
+    ("dw", "128x128", True, None, (5958, 400, 1928), (5995, 395, 1923)),
+    ("dw", "128x128", False, None, (784, 776, 8592), (784, 775, 8587)),
+    ("dw", "64x128", True, None, (6292, 144, 2456), (6292, 139, 2449)),
+    ("dw", "64x128", False, None, (5511, 408, 8968), (5511, 401, 8967)),
+    ("dw", "64x64", True, None, (6179, 176, 5440), (6214, 183, 5417)),
+    ("dw", "64x64", False, None, (1737, 272, 6168), (1735, 265, 6177)),
+    ("gated dx", "256x256", False, None, (1348, 776, 8928), (1348, 773, 8925)),
+    ("gated dx", "256x256", False, "columns", (1794, 840, 8232), (1794, 833, 8229)),
+    ("gated dx", "256x256", False, "rows", (1834, 792, 8824), (1813, 841, 8549)),
+    ("gated dx", "192x256", False, None, (1026, 776, 8928), (1026, 775, 8923)),
+    ("gated dx", "128x128", True, None, (387, 5696, 1928), (387, 5695, 1929)),
+    ("gated dx", "128x128", False, None, (925, 920, 8032), (925, 917, 8027)),
+    ("gated dx", "64x128", True, None, (138, 2960, 5352), (136, 3013, 5271)),
+    ("gated dx", "64x128", False, None, (398, 4912, 8984), (398, 4909, 8979)),
+    ("gated dx", "64x64", True, None, (20, 4112, 6408), (20, 4113, 6405)),
+    ("gated dw", "256x256", False, None, (136, 4168, 3776), (136, 4161, 3773)),
+    ("gated dw", "256x256", False, "columns", (408, 8992, 1960), (408, 8985, 1955)),
+    ("gated dw", "256x256", False, "rows", (151, 5072, 3976), (151, 5065, 3975)),
+    ("gated dw", "192x256", False, None, (387, 5696, 1928), (387, 5695, 1929)),
+    ("gated dw", "128x128", True, None, (5349, 1776, 2216), (5349, 1769, 2213)),
+    ("gated dw", "128x128", False, None, (925, 920, 8032), (925, 917, 8027)),
+    ("gated dw", "64x128", True, None, (8987, 16, 8992), (8987, 15, 8987)),
+]
+# The backward pass of; the tile that its products share; whether dx's contraction is split, and the weights'; sizes as above.
+TOGETHER = [
+    ("linear", "128x128", (False, False), (144, 136, 5416), (144, 137, 5409)),
+    ("linear", "128x128", (False, True), (5470, 144, 136), (5472, 139, 137)),
+    ("linear", "128x128", (True, False), (137, 5512, 144), (137, 5505, 139)),
+    ("linear", "128x128", (True, True), (1805, 520, 136), (1805, 515, 137)),
+    ("linear", "64x128", (False, False), (136, 144, 2752), (136, 137, 2753)),
+    ("linear", "64x128", (False, True), (4313, 144, 136), (4286, 137, 137)),
+    ("linear", "64x128", (True, False), (138, 4312, 136), (141, 4161, 137)),
+    ("linear", "64x128", (True, True), (265, 2288, 136), (258, 2261, 139)),
+    ("linear", "64x64", (False, False), (137, 136, 144), (136, 139, 139)),
+    ("linear", "64x64", (False, True), (775, 144, 144), (777, 137, 137)),
+    ("linear", "64x64", (True, False), (137, 792, 144), (137, 789, 139)),
+    ("linear", "64x64", (True, True), (266, 816, 136), (771, 257, 141)),
+    ("gated", "128x128", (False, False), (197, 136, 4880), (197, 137, 4877)),
+    ("gated", "128x128", (False, True), (7391, 144, 136), (6981, 143, 137)),
+    ("gated", "128x128", (True, False), (141, 2768, 136), (138, 2717, 137)),
+    ("gated", "128x128", (True, True), (1540, 264, 144), (1548, 261, 143)),
+    ("gated", "64x128", (False, False), (136, 144, 3464), (136, 141, 3463)),
+    ("gated", "64x128", (False, True), (1547, 136, 456), (1093, 137, 643)),
+    ("gated", "64x128", (True, False), (137, 2056, 144), (137, 2055, 139)),
+    ("gated", "64x128", (True, True), (259, 1104, 136), (259, 1101, 137)),
+    ("gated", "64x64", (False, False), (137, 136, 144), (136, 139, 139)),
+    ("gated", "64x64", (False, True), (1096, 136, 200), (1097, 137, 193)),
+    ("gated", "64x64", (True, False), (136, 392, 144), (136, 387, 143)),
+    ("gated", "64x64", (True, True), (265, 392, 136), (265, 387, 137)),
+]
+
+
+def forms(rows):
+    """Each with its sizes in multiples of 8, in rows that are further apart, in bf16, and with the others in fp16."""
+    return [pytest.param(*r[:-2], r[-2 + i], t, 8 * (1 - i), id="-".join(str(v).replace(" ", "_") for v in (*r[:-2], t)))
+            for r in rows for i, t in enumerate(("bf16", "f16"))]
+
+
+def check_launches(names, tile, split, cut, products=1):
+    tiles = [n for n in names if n.startswith("ff_tile_kernel")]
+    assert len(tiles) == products * (2 if cut else 1), names
+    first = [n for n in tiles if n.startswith("ff_tile_kernel<%s, " % tile)]
+    assert first and (", 1 splits>" in first[0]) == (not split), names
+
+
+def forward_case(B, kind, tile, split, cut, sizes, type, pad):
+    t, dt = consts(B, type)
+    M, N, K = sizes
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    x, w = numbers(g, M, K, dt, 1, pad), numbers(g, N, K, dt, 1, pad)
+    if kind == "linear":
+        bias, r = numbers(g, 1, N, dt, 5).view(N), numbers(g, M, N, dt, 5, 3)
+        d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+        y, z = empty(M, N, dt, 3), empty(M, N, dt, 3)
+        ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+        ws.fill_(0xff)
+        check_launches(profiled(B, lambda: B.cct_linear_forward(d, x, w, bias, r, y, z, ws)), tile, split, cut)
+        want = product(x, w) + bias.double()
+        same("z", z, want)
+        same("y", y, want.clamp(min=0) + r.double())
+        assert ff.untouched(y, N) and ff.untouched(z, N)
+        return
+    wu = numbers(g, N, K, dt, 1, pad)
+    e = B.make_gated_desc(M, N, K, t, B.ACT_RELU)
+    h, gg, uu = (empty(M, N, dt, 3) for _ in range(3))
+    ws = B.alloc_gated_workspace(e, B.PASS_FORWARD)
+    ws.fill_(0xff)
+    check_launches(profiled(B, lambda: B.cct_gated_forward(e, x, w, wu, h, gg, uu, ws)), tile, split, cut)
+    want_g, want_u = product(x, w), product(x, wu)
+    same("g", gg, want_g)
+    same("u", uu, want_u)
+    same("h", h, want_g.clamp(min=0) * want_u)
+    assert all(ff.untouched(v, N) for v in (h, gg, uu))
+
+
+class Backward:
+    """The backward pass of a linear layer or a gated block with ReLU, z (g, u) and dy of -1, 0 and 1: dz, dg and du are
+    whole numbers too."""
+
+    def __init__(self, B, gated, sizes, type, pad):
+        self.B, self.gated = B, gated
+        t, dt = consts(B, type)
+        M, N, K = self.sizes = sizes
+        g = torch.Generator(device="cuda").manual_seed(M + N + K)
+        self.dt = dt
+        self.x = numbers(g, M, K, dt, 1, pad)
+        self.w = [numbers(g, N, K, dt, 1, pad) for _ in range(1 + gated)]
+        self.z = [numbers(g, M, N, dt, 1, pad) for _ in range(1 + gated)]
+        self.dy = numbers(g, M, N, dt, 1, pad)
+        self.d = (B.make_gated_desc if gated else B.make_linear_desc)(M, N, K, t, B.ACT_RELU)
+        self.ws = (B.alloc_gated_workspace if gated else B.alloc_linear_workspace)(self.d, B.PASS_BACKWARD)
+
+    def run(self, dx=True, dw=True, db=True):
+        """Results, and the names of the launches."""
+        M, N, K = self.sizes
+        self.ws.fill_(0xff)
+        dx = empty(M, K, self.dt, 3) if dx else None
+        dw = [empty(N, K, self.dt, 3) for _ in self.w] if dw else [None] * len(self.w)
+        if self.gated:
+            names = profiled(self.B, lambda: self.B.cct_gated_backward(self.d, self.x, *self.w, *self.z, self.dy, dx, *dw, self.ws))
+            return [dx, *dw], names
+        db = torch.full((N,), float("nan"), dtype=self.dt, device="cuda") if db else None
+        names = profiled(self.B, lambda: self.B.cct_linear_backward(self.d, self.x, self.w[0], self.z[0], self.dy, dx, dw[0], db, self.ws))
+        return [dx, *dw, db], names
+
+    def check(self, got):
+        K, dy = self.sizes[2], self.dy.double()
+        g = self.z[0].double()
+        if self.gated:
+            dz = [dy * self.z[1].double() * (g > 0), dy * g.clamp(min=0)]
+        else:
+            dz = [dy * (g > 0)]
+        for name, t, v in zip(("dx", "dw", "du"), got, [sum(product(a, w.t()) for a, w in zip(dz, self.w))] +
+                              [product(a.t(), self.x.t()) for a in dz]):
+            same(name, t, v)
+            assert ff.untouched(t, K)
+        if not self.gated:
+            same("dbias", got[2], dz[0].sum(0))
+
+
+@pytest.mark.parametrize("what,tile,split,cut,sizes,type,pad", forms([r for r in ALONE if r[0] in ("linear", "gated")]))
+def test_forward_tiles(B, what, tile, split, cut, sizes, type, pad):
+    forward_case(B, what, tile, split, cut, sizes, type, pad)
+
+
+@pytest.mark.parametrize("what,tile,split,cut,sizes,type,pad", forms([r for r in ALONE if r[0] not in ("linear", "gated")]))
+def test_backward_tiles(B, what, tile, split, cut, sizes, type, pad):
+    """Products in launches of their own; each gradient alone has the same bits."""
+    b = Backward(B, what.startswith("gated"), sizes, type, pad)
+    got, names = b.run()
+    assert not any(n.startswith("ff_tile_kernel_together") for n in names), names
+    b.check(got)
+    dx, names_x = b.run(True, False, False)
+    dw, names_w = b.run(False, True, False)
+    assert torch.equal(dx[0], got[0]) and all(torch.equal(v, u) for v, u in zip(dw[1:1 + len(b.w)], got[1:]))
+    if what.endswith("dx"):
+        check_launches(names_x, tile, split, cut)
+    else:
+        check_launches(names_w, tile, split, cut, len(b.w))
+
+
+@pytest.mark.parametrize("what,tile,splits,sizes,type,pad", forms(TOGETHER))
+def test_backward_products_that_share_a_launch(B, what, tile, splits, sizes, type, pad):
+    b = Backward(B, what == "gated", sizes, type, pad)
+    got, names = b.run()
+    shared = "ff_tile_kernel_together<%s, %d products" % (tile, 1 + len(b.w))
+    assert [n for n in names if n.startswith("ff_tile_kernel")][0].startswith(shared), names
+    b.check(got)
+    for i, want in enumerate(((True, False, False), (False, True, False))):
+        some, names = b.run(*want)
+        assert all(torch.equal(u, v) for u, v in zip(some, got) if u is not None)
+        mine = [n for n in names if n.startswith("ff_tile_kernel_together<" + tile)]
+        assert len(mine) == 1 and (", 1 splits>" in mine[0]) == (not splits[i]), names
+
+
+def test_every_plan_has_a_case():
+    """Of the tiles and splits that ff_product.hip chooses from, with what is left over of the large ones."""
+    plans = {(t, s, None) for t in ("128x128", "64x128", "64x64") for s in (False, True)}
+    plans |= {("256x256", False, c) for c in (None, "rows", "columns")} | {("192x256", False, None)}
+    have = {}
+    for what, tile, split, cut, *_ in ALONE:
+        have.setdefault(what, set()).add((tile, split, cut))
+    for what in ("linear", "gated", "dx", "dw"):
+        assert have[what] == plans, what
+    assert len(TOGETHER) == 24
+
+
+@pytest.mark.parametrize("type", list(ff.TYPES))
+@pytest.mark.parametrize("M", [1, 16, 17, 32, 33, 64])
+def test_few_rows_of_ragged_contractions(B, type, M):
+    """No step lost or repeated at the ends of steps, waves and splits, in rows at any address."""
+    t, dt = consts(B, type)
+    rows = 0
+    for N in (10, 72, 1100):
+        for K in (1, 31, 33, 255, 1025, 8193, 20005):
+            for pad in (0, 1, 2, 8 - K % 8):
+                g = torch.Generator(device="cuda").manual_seed(K)
+                x, w, u = numbers(g, M, K, dt, 1, pad), numbers(g, N, K, dt, 1, pad), numbers(g, N, K, dt, 1, pad)
+                bias, r = numbers(g, 1, N, dt, 5).view(N), numbers(g, M, N, dt, 5)
+                d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+                y, z = empty(M, N, dt, 1), empty(M, N, dt, 1)
+                ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+                ws.fill_(0xff)
+                rows += "ff_rows_kernel" in profiled(B, lambda: B.cct_linear_forward(d, x, w, bias, r, y, z, ws))
+                want = product(x, w) + bias.double()
+                same("z", z, want)
+                same("y", y, want.clamp(min=0) + r.double())
+                e = B.make_gated_desc(M, N, K, t, B.ACT_RELU)
+                h, gg, uu = (empty(M, N, dt, 1) for _ in range(3))
+                ws = B.alloc_gated_workspace(e, B.PASS_FORWARD)
+                ws.fill_(0xff)
+                B.cct_gated_forward(e, x, w, u, h, gg, uu, ws)
+                want_g, want_u = product(x, w), product(x, u)
+                same("g", gg, want_g)
+                same("u", uu, want_u)
+                same("h", h, want_g.clamp(min=0) * want_u)
+    cases = 3 * 7 * 4
+    assert rows == (cases if M <= (32 if type == "f32" else 16) else 0) or (type != "f32" and 0 < rows < cases)
