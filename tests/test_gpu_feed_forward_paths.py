@@ -557,3 +557,55 @@ def test_few_rows_of_ragged_contractions(B, type, M):
                 same("h", h, want_g.clamp(min=0) * want_u)
     cases = 3 * 7 * 4
     assert rows == (cases if M <= (32 if type == "f32" else 16) else 0) or (type != "f32" and 0 < rows < cases)
+
+
+def split_launches(names):
+    """How many fp32 products ran, and whether partial sums were joined."""
+    return sum(n.startswith("gemm_split") for n in names), "ff_join_kernel" in names
+
+
+def test_fp32_products_in_several_parts_of_rows(B):
+    """The packed operand of more than 19392 rows of 9216 values is more than 2^30 bytes: one part after the other, the last one
+    smaller, stored directly, with an activation, in splits, and of a gated block."""
+    dt = torch.float32
+    M, N, K = 19600, 4096, 9216
+    g = torch.Generator(device="cuda").manual_seed(13)
+    x, w, bias, r = numbers(g, M, K, dt), numbers(g, N, K, dt), numbers(g, 1, N, dt, 5).view(N), numbers(g, M, N, dt, 5, 3)
+    want = product(x, w)
+    plain, act = (B.make_linear_desc(M, N, K, B.TYPE_F32, a) for a in (B.ACT_NONE, B.ACT_RELU))
+    ws = B.alloc_linear_workspace(act, B.PASS_FORWARD)
+    ws.fill_(0xff)
+    y, z = empty(M, N, dt, 3), empty(M, N, dt, 3)
+    assert split_launches(profiled(B, lambda: B.cct_linear_forward(plain, x, w, bias, None, y, None, ws))) == (2, False)
+    same("y", y, want + bias.double())
+    ws.fill_(0xff)
+    assert split_launches(profiled(B, lambda: B.cct_linear_forward(act, x, w, bias, r, y, z, ws))) == (2, True)
+    same("z", z, want + bias.double())
+    same("y", y, (want + bias.double()).clamp(min=0) + r.double())
+    few = B.make_linear_desc(M, 72, K, B.TYPE_F32)                       # the contraction in splits
+    y = empty(M, 72, dt)
+    ws.fill_(0xff)
+    assert split_launches(profiled(B, lambda: B.cct_linear_forward(few, x, w[:72], None, None, y, None, ws))) == (2, True)
+    same("y", y, want[:, :72])
+    del ws, y, z, r
+    F = 264
+    e = B.make_gated_desc(M, F, K, B.TYPE_F32, B.ACT_RELU)
+    h, gg, uu = (empty(M, F, dt, 3) for _ in range(3))
+    ws = B.alloc_gated_workspace(e, B.PASS_FORWARD)
+    ws.fill_(0xff)
+    assert split_launches(profiled(B, lambda: B.cct_gated_forward(e, x, w[:F], w[F:2 * F], h, gg, uu, ws))) == (4, True)
+    same("g", gg, want[:, :F])
+    same("u", uu, want[:, F:2 * F])
+    same("h", h, want[:, :F].clamp(min=0) * want[:, F:2 * F])
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("K,splits", [(264, True), (2048, False)])
+def test_fp32_gradients_in_several_parts_of_rows(B, gated, K, splits):
+    """dx of 19600 rows and 9216 outputs, and dw of 9216 rows and a contraction of 19600 steps."""
+    b = Backward(B, gated, (19600, 9216, K), "f32", 0)
+    got, names = b.run()
+    assert split_launches(names) == (8 if gated else 4, splits or gated), names
+    b.check(got)
+    dx, names = b.run(True, False, False)
+    assert split_launches(names)[0] == (4 if gated else 2) and torch.equal(dx[0], got[0])
