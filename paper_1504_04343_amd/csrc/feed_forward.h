@@ -5,6 +5,9 @@
 
 namespace cct {
 
+// How many pieces of `of` make n >= 0.  Unsigned: sizes go up to 2^31 - 256, and pieces are as large.
+__host__ __device__ inline int pieces(int n, int of) { return (int)(((unsigned)n + (unsigned)of - 1u) / (unsigned)of); }
+
 // One matrix product of a feed-forward operator: sum over segments s and k of A_s(m, k) B_s(n, k), M x N results, and what
 // becomes of them.
 struct FfOperand {

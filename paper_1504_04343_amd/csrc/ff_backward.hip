@@ -57,10 +57,10 @@ template <int TYPE>
 __device__ __forceinline__ void do_dz(const DzArgs& a, int block) {
   const int which = (block >= a.first[1]) + (block >= a.first[2]), rows = a.rows[which];
   const FfDz& p = a.job[which];
-  const int group = block - a.first[which], wide = (p.N + kCols - 1) / kCols, down = group / wide;
+  const int group = block - a.first[which], wide = pieces(p.N, kCols), down = group / wide;
   const int c0 = (group - down * wide) * kCols;
   const int c = c0 + (threadIdx.x & 31) * 8, lane_row = threadIdx.x >> 5;
-  const int r0 = down * rows, r1 = min(r0 + rows, p.M);
+  const int r0 = down * rows, r1 = rows < p.M - r0 ? r0 + rows : p.M;
   float sum[8] = {};
   if (c < p.N)
     for (int r = r0 + lane_row; r < r1; r += NT / 32) {
@@ -110,9 +110,9 @@ __global__ __launch_bounds__(kSumThreads) void ff_bias_sum_kernel(FfBiasSum p, i
 template <int TYPE>
 __global__ __launch_bounds__(NT) void ff_gated_dz_kernel(FfGatedDz p, int rows, int groups, DzArgs copies) {
   if ((int)blockIdx.x >= groups) return do_dz<TYPE>(copies, blockIdx.x - groups);
-  const int wide = (p.F + kCols - 1) / kCols, down = blockIdx.x / wide;
+  const int wide = pieces(p.F, kCols), down = blockIdx.x / wide;
   const int c = (blockIdx.x - down * wide) * kCols + (threadIdx.x & 31) * 8;
-  const int r0 = down * rows, r1 = min(r0 + rows, p.M);
+  const int r0 = down * rows, r1 = rows < p.M - r0 ? r0 + rows : p.M;
   if (c >= p.F) return;
   for (int r = r0 + (threadIdx.x >> 5); r < r1; r += NT / 32) {
     float dh[8], g[8], u[8];
@@ -136,10 +136,10 @@ namespace {
 // Up to four matrices share a launch: of each at most 2^21 workgroups, or one for every 256 columns (2^23), which together
 // are less than 2^24.
 int rows_of_group(int M, int N) {
-  const long long wide = (N + kCols - 1) / kCols;
-  if ((M + 63) / 64 * wide < 1024) return 8;
+  const long long wide = pieces(N, kCols);
+  if (pieces(M, 64) * wide < 1024) return 8;
   int rows = 64;
-  while (rows < M && (M + rows - 1LL) / rows * wide > 1 << 21) rows *= 2;
+  while (rows < M && pieces(M, rows) * wide > 1 << 21) rows *= 2;
   return rows;
 }
 // Column sums of up to 32 rows need no second launch if a workgroup takes them all (4 rows per thread).
@@ -153,14 +153,14 @@ int place(const FfDzJobs& p, DzArgs* a, double* ops, double* bytes) {
     if (i >= p.count) continue;
     const FfDz& q = a->job[i] = p.job[i];
     a->rows[i] = rows_of_group(q);
-    groups += (int)((q.M + a->rows[i] - 1LL) / a->rows[i]) * ((q.N + kCols - 1) / kCols);
+    groups += pieces(q.M, a->rows[i]) * pieces(q.N, kCols);
     *ops += 2.0 * q.M * q.N;
     *bytes += (double)type_bytes(q.type) * q.M * q.N * (1 + (q.z != nullptr) + (q.dz != nullptr));
   }
   return groups;
 }
 }  // namespace
-int ff_sum_rows(int M, int N) { return (int)((M + rows_of_group(M, N) - 1LL) / rows_of_group(M, N)); }
+int ff_sum_rows(int M, int N) { return pieces(M, rows_of_group(M, N)); }
 
 int launch_ff_dz(const FfDzJobs& p, FfBiasSum* left, hipStream_t st) {
   *left = {};
@@ -184,7 +184,7 @@ int launch_ff_bias_sum(const FfBiasSum& p, hipStream_t st) {
   if (!p.dbias) return CCT_OK;
   with_type(p.type, [&](auto type) {
     ProfScope ps("ff_bias_sum_kernel", (double)p.rows * p.N, 4.0 * p.rows * p.N, st);
-    const int groups = (p.N + kBiasColumns - 1) / kBiasColumns, most = (int)(kMostThreads / kSumThreads);
+    const int groups = pieces(p.N, kBiasColumns), most = (int)(kMostThreads / kSumThreads);
     for (int first = 0; first < groups; first += most)
       hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_bias_sum_kernel<decltype(type)::value>), dim3(std::min(most, groups - first)),
                          dim3(kSumThreads), 0, st, p, first);
@@ -198,7 +198,7 @@ int launch_ff_gated_dz(const FfGatedDz& p, const FfDzJobs& copies, hipStream_t s
   DzArgs a = {};
   const double n = (double)p.M * p.F, e = type_bytes(p.type);
   double ops = 6.0 * n, bytes = 5.0 * e * n;
-  const int groups = (p.F + kCols - 1) / kCols * ff_sum_rows(p.M, p.F), more = place(copies, &a, &ops, &bytes);
+  const int groups = pieces(p.F, kCols) * ff_sum_rows(p.M, p.F), more = place(copies, &a, &ops, &bytes);
   with_type(p.type, [&](auto type) {
     ProfScope ps("ff_gated_dz_kernel", ops, bytes, st);
     hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_gated_dz_kernel<decltype(type)::value>), dim3(groups + more), dim3(NT), 0, st, p,

@@ -54,7 +54,7 @@ FfF32Plan ff_f32_plan(const FfProduct& p) {
     while (best.rows > 32 && (best.rows + 31LL) / 32 * ((N + 127LL) / 128) * 256 > kMostThreads)
       best.rows = std::max(32, best.rows / 2 / 64 * 64);
     for (int sp = 1; sp <= 32 && (sp == 1 || K >= sp * kLeastSplit); sp += sp < 8 ? 1 : 4) {
-      const int len = sp == 1 ? K : gemm_split_kpad((K + sp - 1) / sp), n = (K + len - 1) / len;
+      const int len = sp == 1 ? K : gemm_split_kpad((K + sp - 1) / sp), n = pieces(K, len);
       const double t = gemm_split_seconds(along, true, best.rows, len, N, n) + (n > 1 ? 8.0 * n * best.rows * N / 5.5e12 + 2.5e-6 : 0.0);
       if (t >= least) continue;
       least = t;

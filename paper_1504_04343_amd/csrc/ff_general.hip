@@ -21,7 +21,7 @@ __global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m
   const int m0 = tile_m * BT, n0 = tile_n * BT;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   float acc[NB][4][4] = {};
-  const int per = (p.K + BK - 1) / BK, all = per * (GATED ? 1 : p.segments);
+  const int per = pieces(p.K, BK), all = per * (GATED ? 1 : p.segments);
   const int end = part.splits > 1 ? min((split + 1) * part.stages, all) : all;
   for (int t = part.splits > 1 ? split * part.stages : 0; t < end; ++t) {
     const int s = t >= per, k0 = (t - s * per) * BK;
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(NT) void ff_general_kernel(FfProduct p, int tiles_m
 
 template <int TYPE, int EPI>
 void launch(const FfProduct& p, const FfPart& part, hipStream_t st) {
-  const int tiles_m = (p.M + BT - 1) / BT, tiles = tiles_m * ((p.N + BT - 1) / BT), most = (int)(kMostThreads / NT);
+  const int tiles_m = pieces(p.M, BT), tiles = tiles_m * pieces(p.N, BT), most = (int)(kMostThreads / NT);
   for (int first = 0; first < tiles; first += most)
     hipLaunchKernelGGL(HIP_KERNEL_NAME(ff_general_kernel<TYPE, EPI == kFfGated>), dim3(std::min(most, tiles - first), part.splits),
                        dim3(NT), 0, st, p, tiles_m, first, part);
@@ -83,8 +83,8 @@ void launch(const FfProduct& p, const FfPart& part, hipStream_t st) {
 
 // Up to four workgroups per CU, of at least 256 steps of 16 k each.
 FfGeneralPlan ff_general_plan(const FfProduct& p) {
-  const long long tiles = ((p.M + BT - 1LL) / BT) * ((p.N + BT - 1LL) / BT), products = p.epilogue == kFfGated ? 2 : 1;
-  const long long steps = (p.K + BK - 1LL) / BK * (p.epilogue == kFfGated ? 1 : p.segments);
+  const long long tiles = (long long)pieces(p.M, BT) * pieces(p.N, BT), products = p.epilogue == kFfGated ? 2 : 1;
+  const long long steps = (long long)pieces(p.K, BK) * (p.epilogue == kFfGated ? 1 : p.segments);
   const int splits = (int)std::max(1LL, std::min(1024 / tiles, steps / 256));
   FfGeneralPlan plan;
   plan.steps = (int)((steps + splits - 1) / splits);

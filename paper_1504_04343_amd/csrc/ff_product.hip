@@ -47,13 +47,13 @@ FfTilePlan whole_plan(const FfProduct& p, int M, int N) {
   const bool along = !p.b_across;
   const int segments = p.epilogue == kFfGated ? 1 : p.segments;
   const long long cols = p.epilogue == kFfGated ? 2LL * N : N;
-  const int stages = std::max((p.K + kFfStage - 1) / kFfStage, 1) * segments;
+  const int stages = std::max(pieces(p.K, kFfStage), 1) * segments;
   const double bytes = 2.0 * (M + (double)cols) * p.K * segments;
   FfTilePlan best = {kNoTile, 1, stages, 0, 1e30, 0, 0};
   for (int tile = kTile256; tile <= kTile64; ++tile) {
     const TileCost& c = kTileCosts[tile];
     if (!reaches(p, c)) continue;
-    const long long tiles = ((M + c.bm - 1LL) / c.bm) * ((cols + c.bn - 1) / c.bn);
+    const long long tiles = pieces(M, c.bm) * ((cols + c.bn - 1) / c.bn);
     if (tiles * c.threads > kMostThreads) continue;  // more than 2^30 rows of few columns in tiles of 64
     for (int splits = 1; splits <= 32; splits *= 2) {
       if (splits > 1 && (tile <= kTile192 || stages < splits * kLeastStages || tiles * splits > 4 * kCus)) break;
@@ -80,9 +80,9 @@ FfTilePlan ff_tile_plan(const FfProduct& p) {
   const int M = p.M, N = p.N;
   FfTilePlan best = whole_plan(p, M, N);
   const int wide = p.epilogue == kFfGated ? 128 : 256;
-  const long long tm = (M + 255LL) / 256, tn = (N + wide - 1LL) / wide, rounds = tm * tn / kCus;
+  const long long tm = pieces(M, 256), tn = pieces(N, wide), rounds = tm * tn / kCus;
   if (rounds < 1 || !reaches(p, kTileCosts[kTile256]) || tm * tn * kTileCosts[kTile256].threads > kMostThreads) return best;
-  const int stages = std::max((p.K + kFfStage - 1) / kFfStage, 1) * (p.epilogue == kFfGated ? 1 : p.segments);
+  const int stages = std::max(pieces(p.K, kFfStage), 1) * (p.epilogue == kFfGated ? 1 : p.segments);
   const double full = rounds * stages * kTileCosts[kTile256].full[p.b_across] + kLaunchMicros;
   auto consider = [&](long long rows, long long cols) {  // what the full rounds take
     if ((rows < M) == (cols < N)) return;
@@ -139,7 +139,7 @@ int launch_ff_product(const FfProduct& p, char* pack, float* ws, hipStream_t st)
 }
 
 namespace {
-int stages_of(const FfProduct& p) { return std::max((p.K + kFfStage - 1) / kFfStage, 1) * p.segments; }
+int stages_of(const FfProduct& p) { return std::max(pieces(p.K, kFfStage), 1) * p.segments; }
 double operand_bytes(const FfProduct& p) { return 2.0 * p.segments * p.K * ((double)p.M + p.N); }
 }  // namespace
 
@@ -171,7 +171,7 @@ FfTogetherPlan ff_together_plan(const FfProduct* p, int count) {
           joined += 8.0 * values;
           joining += values / plan.splits[i] / 4 + 256;
         }
-        const double tiles = (double)((p[i].M + c.bm - 1) / c.bm) * ((p[i].N + c.bn - 1) / c.bn) * plan.splits[i];
+        const double tiles = (double)pieces(p[i].M, c.bm) * pieces(p[i].N, c.bn) * plan.splits[i];
         groups += tiles;
         work += tiles * (each + 3);
         longest = std::max(longest, each);

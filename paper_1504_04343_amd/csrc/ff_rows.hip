@@ -183,13 +183,13 @@ __global__ __launch_bounds__((kWaves<TYPE, RM> * 64)) void ff_rows_kernel(FfProd
 }
 
 int rows_splits(int N, int K, int type) {
-  const int groups = (N + 15) / 16, least = type == CCT_TYPE_F32 ? 1024 : 2048;  // steps of a split
+  const int groups = pieces(N, 16), least = type == CCT_TYPE_F32 ? 1024 : 2048;  // steps of a split
   return groups > 64 || K < 4 * least ? 1 : std::min(128 / groups, K / least);
 }
 
 template <int TYPE, int EPI>
 void launch(const FfProduct& p, float* ws, hipStream_t st) {
-  const int groups = (p.N + 15) / 16, steps = std::max(p.K / Step<TYPE>::K, 1);
+  const int groups = pieces(p.N, 16), steps = std::max(p.K / Step<TYPE>::K, 1);
   FfPart part = {ws, (p.N + 3) / 4 * 4, rows_splits(p.N, p.K, TYPE), 0};
   part.stages = (steps + part.splits - 1) / part.splits;
   part.splits = (steps + part.stages - 1) / part.stages;
@@ -225,7 +225,7 @@ void launch(const FfProduct& p, float* ws, hipStream_t st) {
 
 }  // namespace
 
-bool ff_rows_fits(int N, int type) { return (N + 15LL) / 16 * (type == CCT_TYPE_F32 ? 1024 : 512) <= kMostThreads; }
+bool ff_rows_fits(int N, int type) { return (long long)pieces(N, 16) * (type == CCT_TYPE_F32 ? 1024 : 512) <= kMostThreads; }
 
 long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue) {
   const int splits = M <= kFfRowsMost ? rows_splits(N, K, type) : 1;

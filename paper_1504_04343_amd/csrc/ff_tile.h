@@ -244,7 +244,7 @@ __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, in
   const int m0 = tm * BM, n0 = tn * (BN / PARTS);
   const int left_m = p.M - m0, left_n = p.N - n0;
 
-  const int per = max((p.K + SK - 1) / SK, 1), all = per * (EPI == kFfGated ? 1 : p.segments);
+  const int per = max(pieces(p.K, SK), 1), all = per * (EPI == kFfGated ? 1 : p.segments);
   const int first = SPLIT ? split * part.stages : 0, stages = SPLIT ? min(part.stages, all - first) : all;
   OpA a;
   OpB b;
@@ -253,7 +253,8 @@ __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, in
   b.template init<PARTS>(wave, lane, left_n, ldb);
   const long long a_at = (AX ? m0 : m0 * lda) * 2, b_at = (BX ? n0 : n0 * ldb) * 2;
   // the stage that is loaded next; past the last one nothing is, but as many loads are in flight as ever
-  int k_next = first % per * SK, to_load = stages;
+  unsigned k_next = first % per * SK;  // goes a ring past K, up to 2^31
+  int to_load = stages;
   auto cursor_a = [&](int s, int k0) { return OpA::begin((const char*)p.A[s].p + a_at, nullptr, lda, left_m, k0, p.K); };
   auto cursor_b = [&](int s, int k0) {
     return OpB::begin((const char*)p.B[s].p + b_at, (const char*)p.B[1].p + b_at, ldb, left_n, k0, p.K);
@@ -262,14 +263,14 @@ __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, in
   auto cb = cursor_b(first / per, k_next);
   auto load = [&](int slot) {
     unsigned char* st = tile_smem + slot * STAGE;
-    const int kl = to_load > 0 ? p.K - k_next : 0;
+    const int kl = to_load > 0 ? (int)(p.K - k_next) : 0;
     a.template load<1>(st, wave, ca, kl);
     b.template load<PARTS>(st + OpA::BYTES, wave, cb, kl);
     --to_load;
     k_next += SK;
     OpA::next(ca, lda);
     OpB::next(cb, ldb);
-    if (EPI != kFfGated && k_next >= p.K && to_load > 0) {  // the second contraction
+    if (EPI != kFfGated && k_next >= (unsigned)p.K && to_load > 0) {  // the second contraction
       k_next = 0;
       ca = cursor_a(1, 0);
       cb = cursor_b(1, 0);

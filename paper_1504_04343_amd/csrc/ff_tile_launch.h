@@ -12,7 +12,7 @@ int launch_tile(const FfProduct& p, const FfPart& part, hipStream_t st) {
   const int rc = ensure_dynamic_lds<kernel>(lds);
   if (rc != CCT_OK) return rc;
   constexpr int cols = EPI == kFfGated ? BN / 2 : BN;
-  const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + cols - 1) / cols;
+  const int tiles_m = pieces(p.M, BM), tiles_n = pieces(p.N, cols);
   hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n * part.splits), dim3(WM * WN * 64), lds, st, p, tiles_m, tiles_n, part);
   CCT_CHECK_LAUNCH();
   return CCT_OK;
@@ -58,11 +58,11 @@ int launch_together(FfTogether a, hipStream_t st) {
   constexpr auto kernel = ff_tile_kernel_together<TYPE, BM, BN, WM, WN, RING>;
   const int rc = ensure_dynamic_lds<kernel>(lds);
   if (rc != CCT_OK) return rc;
-  int groups = a.sum.dbias ? (a.sum.N + kBiasColumns - 1) / kBiasColumns : 0;
+  int groups = a.sum.dbias ? pieces(a.sum.N, kBiasColumns) : 0;
   for (int i = 0; i < a.count; ++i) {
     a.first[i] = groups;
-    a.tiles_m[i] = (a.p[i].M + BM - 1) / BM;
-    a.tiles_n[i] = (a.p[i].N + BN - 1) / BN;
+    a.tiles_m[i] = pieces(a.p[i].M, BM);
+    a.tiles_n[i] = pieces(a.p[i].N, BN);
     groups += a.tiles_m[i] * a.tiles_n[i] * a.part[i].splits;
   }
   hipLaunchKernelGGL(kernel, dim3(groups), dim3(WM * WN * 64), lds, st, a);

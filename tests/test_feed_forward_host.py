@@ -196,3 +196,23 @@ def test_workspace_is_what_a_call_may_need(B):
     # dz, its column sums (one row of 64), a packed operand of three terms
     n = 8192 * 8192
     assert 0 <= linear(8192, 8192, 8192, B.TYPE_F32, B.PASS_BACKWARD) - (4 * n + 4 * n // 64 + 6 * n) < 1024
+
+
+def test_workspace_of_the_largest_sizes(B):
+    """Counts of workgroups and of rows of partial sums next to 2^31: negative ones made the workspace smaller."""
+    for type, size in ((B.TYPE_F32, 4), (B.TYPE_BF16, 2)):
+        for n in ((1 << 30) - 8, (1 << 30) + 104, (1 << 31) - 2048, (1 << 31) - 1024, (1 << 31) - 512, (1 << 31) - 256):
+            for i in range(3):
+                dims = [n if k == i else 1 for k in range(3)]
+                for p in (B.PASS_FORWARD, B.PASS_BACKWARD):
+                    assert B.cct_gated_workspace_bytes(B.make_gated_desc(*dims, type), p) >= 256
+                # dz in rows of 8 values
+                assert B.cct_linear_workspace_bytes(B.make_linear_desc(*dims, type), B.PASS_BACKWARD) >= \
+                    dims[0] * -(-dims[1] // 8) * 8 * size, dims
+            rows = 64                   # of a workgroup of dz, which leaves one of column sums; of these at most 2^21
+            while -(-n // rows) > 1 << 21:
+                rows *= 2
+            # dz, the sums, and x's copy in such rows or 2^30 bytes of dz as three terms of 32 steps, 64 rows at a time
+            least = n * 8 * size + -(-n // rows) * 4 + (n * 8 * size if size == 2 else (1 << 30) // 192 // 64 * 64 * 192)
+            total = B.cct_linear_workspace_bytes(B.make_linear_desc(n, 1, 1, type), B.PASS_BACKWARD)
+            assert least <= total < least + (1 << 16), (n, type, total, least)

@@ -609,3 +609,91 @@ def test_fp32_gradients_in_several_parts_of_rows(B, gated, K, splits):
     b.check(got)
     dx, names = b.run(True, False, False)
     assert split_launches(names)[0] == (4 if gated else 2) and torch.equal(dx[0], got[0])
+
+
+@pytest.mark.parametrize("type", list(ff.TYPES))
+@pytest.mark.parametrize("which", range(3), ids=["rows", "outputs", "inputs"])
+def test_sizes_at_the_limit(B, type, which):
+    """2^31 - 256 rows, outputs or inputs, of one value each."""
+    t, dt = consts(B, type)
+    if torch.cuda.mem_get_info()[0] < 150e9:
+        pytest.skip("needs 150 GB")
+    M, N, K = [(1 << 31) - 256 if i == which else 1 for i in range(3)]
+    g = torch.Generator(device="cuda").manual_seed(which)
+
+    def values(r, c):
+        return numbers(g, 1, r * c, dt).view(r, c) if r > 1 else numbers(g, r, c, dt)
+    x, w = values(M, K), values(N, K)
+    d = B.make_linear_desc(M, N, K, t, B.ACT_RELU)
+    y, z = (torch.full((M, N), float("nan"), dtype=dt, device="cuda") for _ in range(2))
+    ws = B.alloc_linear_workspace(d, B.PASS_FORWARD)
+    print("forward", type, M, N, K, flush=True)
+    B.cct_linear_forward(d, x, w, None, None, y, z, ws)
+    torch.cuda.synchronize()
+    del ws
+    # with one input, z is x w whatever the shape; with one row and output, a sum
+    step = 1 << 26
+    flat = [v.reshape(-1) for v in (x, w, y, z)]
+
+    def part(v, p):
+        return v[p] if v.numel() > 1 else v
+    spans = [slice(i, min(i + step, (1 << 31) - 256)) for i in range(0, (1 << 31) - 256, step)]
+    if which == 2:
+        want = sum(float((flat[0][p].double() * flat[1][p].double()).sum()) for p in spans)
+        assert float(z) == float(torch.tensor(want, dtype=torch.float64).to(dt)) and float(y) == max(0.0, float(z))
+    else:
+        for p in spans:
+            want = part(flat[0], p) * part(flat[1], p)
+            same("z", flat[3][p], want)
+            same("y", flat[2][p], want.clamp_(min=0))
+    del y, want
+    flat = flat[:2]
+    z.fill_(1.0)                     # half of dy is kept
+    z.view(-1)[::2] = -1.0 if which < 2 else 1.0
+    dy = values(M, N)
+    dx, dw = (torch.full(v.shape, float("nan"), dtype=dt, device="cuda") for v in (x, w))
+    db = torch.full((N,), float("nan"), dtype=dt, device="cuda")
+    ws = B.alloc_linear_workspace(d, B.PASS_BACKWARD)
+    print("backward", type, M, N, K, flush=True)
+    B.cct_linear_backward(d, x, w, z, dy, dx, dw, db, ws)
+    torch.cuda.synchronize()
+    del ws
+    dz, f = dy.view(-1), [v.reshape(-1) for v in (dx, dw, x, w)]
+    sums = [0.0, 0.0, 0.0]           # of dx, dw, dbias where each is one value
+    for p in spans:
+        v = part(dz, p) * (part(z.view(-1), p) > 0)
+        for i, other in ((0, f[3]), (1, f[2])):
+            term = v * part(other, p)
+            if f[i].numel() > 1:
+                same(("dx", "dw")[i], f[i][p], term.expand_as(f[i][p]))
+            else:
+                sums[i] += float(term.double().sum())
+        if N > 1:
+            same("dbias", db[p], v)
+        elif M > 1:
+            sums[2] += float(v.double().sum())
+        else:
+            sums[2] = float(v)
+    for i, got in ((0, dx), (1, dw), (2, db)):
+        if got.numel() == 1:
+            assert float(got) == float(torch.tensor(sums[i], dtype=torch.float64).to(dt)), i
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+def test_copied_rows_keep_their_smallest_numbers(B, type):
+    """Rows of 17 values are copied for the tiles: subnormal ones too, as they are."""
+    t, dt = consts(B, type)
+    M, N, K = 90, 40, 17
+    low = 2.0 ** (-133 if type == "bf16" else -24)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = (numbers(g, M, K, torch.float64, 3) * low).to(dt)
+    w = numbers(g, N, K, dt, 2) * 2.0 ** 12
+    d = B.make_linear_desc(M, N, K, t)
+    y = empty(M, N, dt)
+    names = profiled(B, lambda: B.cct_linear_forward(d, x, w, None, None, y, None, B.alloc_linear_workspace(d, B.PASS_FORWARD)))
+    assert any(n.startswith("ff_dz_kernel") for n in names)
+    same("y", y, x.double() @ w.double().t())
+    dy = torch.eye(M, N, device="cuda").to(dt)       # dw is x's first rows
+    dw = empty(N, K, dt)
+    B.cct_linear_backward(d, x, None, None, dy, None, dw, None, B.alloc_linear_workspace(d, B.PASS_BACKWARD))
+    same("dw", dw, x[:N])
