@@ -318,12 +318,13 @@ int cct_softmax_loss_backward(int32_t N, int32_t C, const float* prob, const int
 
 /*
  * Feed-forward blocks: matrix products with their activation and additions in one kernel, in training and in
- * serving.  (The paper's fully connected layers are cct_conv_* with K == H == W, fp32, bias only; these take 16-bit
- * tensors too, rows of any stride, and what lies around the product.)  x is M x K (M tokens or images), a weight is
+ * serving.  (The paper's fully connected layers are cct_conv_* with K == H == W, fp32, bias only, on the same memory;
+ * up to 64 images are up to a third faster there, 256 and more take the same time.  These take 16-bit tensors too, rows
+ * of any stride, what lies around the product, and give both gradients in one call.)  x is M x K (M tokens or images), a weight is
  * N x K, both with consecutive values along K; a row begins `ld` elements behind the one before (ld >= the row's
  * length; any element-aligned pointer and any such ld are accepted, rows that begin at multiples of 16 bytes are the
  * fastest).  All tensors of a call have the descriptor's type.  Sums are fp32 (the matrix cores'), activations are
- * computed in fp32, a result is rounded once.
+ * computed in fp32, a result is rounded once.  No output may overlap anything else, but for what is said at a call.
  */
 typedef enum { CCT_TYPE_F32 = 0, CCT_TYPE_BF16 = 1, CCT_TYPE_F16 = 2 } cct_type_t;
 typedef enum {
@@ -354,7 +355,7 @@ int cct_gated_workspace_bytes(const cct_gated_desc_t* desc, int32_t backward, si
 /*
  * z = x w^T + bias,  y = act(z) + residual.  bias (N values) and residual (M x N) may be NULL.  z may be NULL; a
  * training program keeps it for the backward pass (it is not needed there for CCT_ACT_NONE).  y may be the residual
- * itself (same pointer and ldr == ldy); nothing else may overlap.
+ * itself (same pointer and ldr == ldy).
  */
 int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
                        const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz,
@@ -363,7 +364,8 @@ int cct_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx
  * dz = dy * act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum of dz over its rows; the residual's gradient is dy.
  * Any of dx, dw, dbias may be NULL: it is not computed then, and w is not read without dx, x not without dw (both
  * may be NULL then).  z may be NULL for CCT_ACT_NONE.  Sums run in a fixed order (bit-reproducible).  16-bit types:
- * dz is rounded to the type before the products, as the matrix cores take it, and summed unrounded for dbias.
+ * dz is rounded to the type before the products, as the matrix cores take it (in fp16 a dz beyond 65504 is an infinity
+ * there), and summed unrounded for dbias.
  */
 int cct_linear_backward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* w, int64_t ldw,
                         const void* z, int64_t ldz, const void* dy, int64_t lddy, void* dx, int64_t lddx, void* dw,
@@ -378,7 +380,8 @@ int cct_gated_forward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, 
                       void* workspace, size_t workspace_bytes, void* hip_stream);
 /*
  * dg = dh * u * act'(g),  du = dh * act(g),  dx = dg wg + du wu (one sum),  dwg = dg^T x,  dwu = du^T x.
- * dx may be NULL, and dwg and dwu together.  16-bit types: dg and du are rounded to the type before the products.
+ * dx may be NULL, and dwg and dwu together.  16-bit types: dg and du are rounded to the type before the products
+ * (in fp16 beyond 65504 to an infinity: the caller's scale of dh decides).
  */
 int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx, const void* wg, int64_t ldwg,
                        const void* wu, int64_t ldwu, const void* g, int64_t ldg, const void* u, int64_t ldu,

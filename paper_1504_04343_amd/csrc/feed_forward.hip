@@ -152,10 +152,11 @@ GatedLayout gated_layout(const cct_gated_desc_t& d, bool backward) {
   return b;
 }
 
-// Whether a forward product runs on ff_rows.hip.  bf16, 4096 -> 4096: 16 rows 11.7 us there, 12.0 in tiles; 48 rows 22 and 14,
-// but tiles may need a copy of the weight first (three times its bytes): 64 rows 17 to 21 and 30.  Rows that begin between
-// multiples of four bytes take 44 there, so that more than 16 are copied: 62 rows of 10881 -> 2880 166 us there, 43 so.
-// fp32: 16 rows 22.6 us; 48 rows 41 there, 37 on ff_f32.hip; 64 rows of 4096 -> 16384 183 and 100.
+// Whether a forward product runs on ff_rows.hip.  4096 -> 4096, other weights in every call, us there and in tiles, bf16: 2 rows
+// 9.0 and 11.5, 16 rows 11.5 and 12.0, 32 rows 15.2 and 12.2, 64 rows 22.9 and 12.9; but tiles may need a copy of the weight
+// first (three times its bytes): 64 rows 26 and 31.  Rows that begin between multiples of four bytes: 16 rows 25.5 and 29, 32
+// rows 39.5 and 30.5, so that more than 16 are copied.  fp32: 16 rows 20.3 and 32.7, 32 rows 29.4 and 33.9 (16384 outputs
+// 102 and 97).
 bool few_rows(int M, int N, int type, bool in_place, bool words) {
   return always_rows(M, N, type) || (type != CCT_TYPE_F32 && ff_rows_fits(N, type) && M <= kFfRowsMost && words && !in_place);
 }

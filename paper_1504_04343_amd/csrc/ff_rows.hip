@@ -7,18 +7,20 @@
 // follows).  No LDS and no meeting in the loop; eight steps' loads are in flight per wave, and x comes from L2 the same way.  The waves' sums meet in LDS in a fixed
 // order.  fp32 runs on v_mfma_f32_16x16x4_f32, which memory outlasts.
 //
-// One row, bf16, weights from memory: 4096 x 4096 7.9 us (4.3 TB/s; 6.8 at the rate of a large copy), 16384 x 4096 25.6 (5.2
-// TB/s), gated 2 x 8192 x 4096 27.0 (5.0).  With two batches of four steps in turn 9.0, 29.1 and 29.8: the compiler waits
-// for all of a batch before it loads the next one into the same registers, so that they are only smaller; with sixteen waves
-// 8.0, 26.8 and 26.8.  fp32, eight and sixteen waves: 18.7 and 16.6, 56.7 and 52.0, 62.5 and 56.5 (4096 x 16384).
+// One row, bf16, other weights in every call, which come from memory: 4096 x 4096 8.9 us (3.8 TB/s; 6.8 at the rate of a large
+// copy), 16384 x 4096 26.5 (5.1 TB/s), gated 2 x 8192 x 4096 28.8 (4.7); the same weights again and again, which the 256 MiB
+// behind the L2s hold: 7.0 to 7.7, 22.6, 23.0 to 26.9.  fp32: 17.3, 54.3, 56.0.  What was tried (weights partly held):
+// two batches of four steps in turn 9.0, 29.1 and 29.8 for 7.9, 25.6 and 27.0: the compiler waits for all of a batch before it
+// loads the next one into the same registers, so that they are only smaller; sixteen waves 8.0, 26.8 and 26.8.  fp32, eight and
+// sixteen waves: 18.7 and 16.6, 56.7 and 52.0, 62.5 and 56.5 (4096 x 16384).
 //
 // Few columns of long rows leave most CUs idle: the contraction is then cut into splits, whose sums ff_join_kernel adds (64
 // outputs of 16384 inputs, bf16: 19.3 us on four CUs, 9.8 in eight splits).
 //
 // Any alignment: gfx950 loads 16 bytes at any address, at multiples of four as fast as at multiples of sixteen while memory is
 // the bound.  16-bit rows that begin between them (up to 16 rows of x; with more the caller has such weights copied) are loaded
-// from the words below and shifted: 4096 x 4096, bf16, rows 4097 apart, 1 / 16 rows of x: 16.1 / 19.4 us, loaded as they lie
-// 16.0 / 26.7, with a copy first 23 / 29.  A last step that is not whole is loaded value by value.
+// from the words below and shifted: 4096 x 4096, bf16, rows 4097 apart, 1 / 16 rows of x: 16.1 / 20.2 us (other weights in
+// every call 20.9 / 25.0), loaded as they lie 16.0 / 26.7, with a copy first 23 / 29.  A last step that is not whole is loaded value by value.
 #include <algorithm>
 
 #include "activation.h"

@@ -11,7 +11,7 @@
 // them.  Scaling and updating walk the lists from the end: what the norm read last is what the 256 MiB cache behind the
 // eight L2s still holds, and what is written, and the weights and moments, which nobody reads again soon, go past it
 // (nontemporal).  CaffeNet's 61 million fp32 gradients, us: norm 45 (5.4 TB/s), norm and scaling 117 (139 without, 141 from the
-// beginning too), norm and update 218 (266, 274): 5.7 TB/s of gradients read once, weights and moments.
+// beginning too), norm and update 218 (266, 274): 5.6 TB/s of gradients read once, weights and moments.
 //
 // The squares are summed in 64 bits: with 2^-53 per addition no order matters to the fp32 result, 3e38 squared does not
 // overflow, and the kernel waits for memory all the same (4 conversions and fused multiply-adds per 16 bytes).  Every
