@@ -79,7 +79,8 @@ bool ff_rows_fits(int N, int type);  // whether a launch takes so many columns
 long long ff_rows_part_bytes(int M, int N, int K, int type, int epilogue);
 int launch_ff_rows(const FfProduct& p, float* ws, hipStream_t st);
 // Whether the 16-bit product takes a matrix of `cols` consecutive values and rows `ld` apart in place: 16-byte loads, 256 rows
-// within 32-bit offsets (a copy's rows are as long as they are: ff_tile_plan chooses a tile that reaches them).  Rows that are no multiple of 8 values must be followed by zeros up to one, as copies are.
+// within 32-bit offsets (a copy's rows are as long as they are: ff_tile_plan chooses a tile that reaches them).  Rows that are
+// no multiple of 8 values must be followed by zeros up to one, as copies are.
 inline bool ff_in_place(const void* p, long long ld, long long cols) {
   return !((uintptr_t)p & 15) && ld % 8 == 0 && cols % 8 == 0 && ld < (1LL << 21);
 }

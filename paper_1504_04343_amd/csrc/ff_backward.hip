@@ -3,11 +3,12 @@
 //   gated   dg = dh u act'(g), du = dh act(g).
 // Each input is read once and each output written once; the rounding of dz, dg and du to 16 bits is the matrix cores', which
 // take no more of an operand (bf16 at most 2^-8 of a value, fp16 2^-11, as the operands themselves were rounded by; a gradient
-// then has sqrt(2) times the error that its own rounding makes).
+// then has sqrt(2) times the error that its own rounding makes; in fp16 what passes 65504 is an infinity).
 //
-// A workgroup takes 256 columns x 64 rows, or 8 where that leaves CUs idle (1531 x 1000: 5.3 us, 9.9 before), a thread 8
-// neighbouring columns of every eighth row: its column sums stay in registers, meet in LDS in a fixed order and leave as one
-// row of partial sums per workgroup, which ff_bias_sum.h adds in order.  Rows of any alignment; the outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
+// A workgroup takes 256 columns x 64 rows (more from 2^35 values on), or 8 where that leaves CUs idle (1531 x 1000: 5.3 us,
+// 9.9 before), a thread 8 neighbouring columns of every eighth row: its column sums stay in registers, meet in LDS in a fixed
+// order and leave as one row of partial sums per workgroup, which ff_bias_sum.h adds in order.  Rows of any alignment; the
+// outputs' rows are padded with zeros to a multiple of 8 values, which the products rely on.
 #include <algorithm>
 
 #include "activation.h"
