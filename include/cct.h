@@ -324,7 +324,8 @@ int cct_softmax_loss_backward(int32_t N, int32_t C, const float* prob, const int
  * (M tokens or images), a weight is N x K, both with consecutive values along K; a row begins `ld` elements behind the
  * one before (ld >= the row's length; any element-aligned pointer and any such ld are accepted, rows that begin at
  * multiples of 16 bytes are the fastest).  All tensors of a call have the descriptor's type.  Sums are fp32 (the
- * matrix cores'), activations are computed in fp32, a result is rounded once.  No output may overlap anything else, but for what is said at a call.
+ * matrix cores'), activations are computed in fp32, a result is rounded once.  No output may overlap anything else,
+ * but for what is said at a call.
  */
 typedef enum { CCT_TYPE_F32 = 0, CCT_TYPE_BF16 = 1, CCT_TYPE_F16 = 2 } cct_type_t;
 typedef enum {
