@@ -390,6 +390,49 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
                        int64_t lddwu, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * What stands between the blocks of a residual network, in one pass over the stream: a block's output b goes through its
+ * norm (`after`) and its gate onto the stream r, and the new stream through the norm (`before`) of the block that follows:
+ *   p = N_after(b),  s = r + scale * gate * p,  h = N_before(s)  (from the unrounded s).
+ * N(v) = n * w + c over the D values of a row, n = v / sqrt(mean(v^2) + eps) (CCT_NORM_RMS), the same of v - mean(v)
+ * (CCT_NORM_LAYER), or N(v) = v (CCT_NORM_NONE).  A row of the gate belongs to `gate_rows` consecutive rows of the stream
+ * (gate: ceil(M / gate_rows) x D): M for a gate that all share, 1 for one of each row's own.  All tensors have one type;
+ * everything is computed in fp32 and rounded once.  Matrices and their strides are as for cct_linear_*, vectors have D
+ * consecutive values.  M >= 0, D >= 1, gate_rows >= 1, eps >= 0, eps and scale finite (CCT_EINVAL); CCT_EUNSUPPORTED as above.
+ */
+typedef enum { CCT_NORM_NONE = 0, CCT_NORM_RMS = 1, CCT_NORM_LAYER = 2 } cct_norm_t;
+typedef struct {
+  int32_t M, D;
+  int32_t type;          /* cct_type_t */
+  int32_t before, after; /* cct_norm_t */
+  int32_t gate_rows;
+  float eps, scale;
+} cct_residual_norm_desc_t;
+/*
+ * NULL may be: b (no block yet: s = r; then gate, w_after and c_after must be NULL), gate (1), w_* (1), c_* (0), s or h
+ * where it is not wanted.  With CCT_NORM_NONE the norm's w and c, and for `before` also h, must be NULL.  s may be r itself
+ * (same pointer and ld).
+ */
+int cct_residual_norm_forward(const cct_residual_norm_desc_t* desc, const void* r, int64_t ldr, const void* b, int64_t ldb,
+                              const void* gate, int64_t ldgate, const void* w_after, const void* c_after,
+                              const void* w_before, const void* c_before, void* s, int64_t lds, void* h, int64_t ldh,
+                              void* hip_stream);
+/*
+ * Gradients from ds (the stream's, from what reads s) and dh (may one be NULL: zeros; dh only with `before`).  s is the
+ * stream that the forward call left (r where there is no b); nothing else is kept from it.  dr is the gradient of r.
+ * dw_* are sums of gradient * n over the rows, dc_* of the gradient, dgate of scale * p * dr over a gate row's rows.
+ * Any output may be NULL; those of b, the gate and a norm must be where there is none.  dr may be ds itself (same pointer
+ * and ld).  c_after is read for dgate only.  M == 0: dw_* and dc_* are zero.  Sums are fp32 and run in an order that
+ * depends on the descriptor alone.
+ */
+int cct_residual_norm_workspace_bytes(const cct_residual_norm_desc_t* desc, size_t* bytes);
+int cct_residual_norm_backward(const cct_residual_norm_desc_t* desc, const void* s, int64_t lds, const void* b, int64_t ldb,
+                               const void* gate, int64_t ldgate, const void* w_after, const void* c_after,
+                               const void* w_before, const void* ds, int64_t ldds, const void* dh, int64_t lddh, void* dr,
+                               int64_t lddr, void* db, int64_t lddb, void* dgate, int64_t lddgate, void* dw_after,
+                               void* dc_after, void* dw_before, void* dc_before, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/*
  * From gradients to new weights, over lists of tensors (host arrays; the tensors they name are contiguous device
  * memory, element-aligned).  The lists are read during the call only.
  *

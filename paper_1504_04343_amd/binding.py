@@ -29,6 +29,7 @@ PASS_FORWARD, PASS_BACKWARD_DATA, PASS_BACKWARD_WEIGHTS = 0, 1, 2
 PASS_BACKWARD = 3  # of the feed-forward operators, whose gradients are one call
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 OK, EINVAL, EWORKSPACE, EUNSUPPORTED, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5
 STATIC_SCRATCH_BYTES = 32 << 20
 
@@ -44,6 +45,7 @@ EXPORTS = [
     "cct_softmax_loss_backward", "cct_linear_workspace_bytes", "cct_gated_workspace_bytes",
     "cct_linear_forward", "cct_linear_backward", "cct_gated_forward", "cct_gated_backward",
     "cct_grad_norm_workspace_bytes", "cct_grad_norm", "cct_grad_scale", "cct_sgd_update",
+    "cct_residual_norm_forward", "cct_residual_norm_workspace_bytes", "cct_residual_norm_backward",
 ]
 
 
@@ -133,6 +135,18 @@ _lib.cct_grad_norm_workspace_bytes.argtypes = [_tp, _i32, ctypes.POINTER(_sz)]
 _lib.cct_grad_norm.argtypes = [_tp, _i32, _f32, _vp, _vp, _sz, _vp]
 _lib.cct_grad_scale.argtypes = [_tp, _i32, _vp, _tp, _vp]
 _lib.cct_sgd_update.argtypes = [_tp, _i32, _vp, _tp, _tp, _tp, _f32, _f32, _f32, _vp]
+
+
+class ResidualNormDesc(ctypes.Structure):
+    """cct_residual_norm_desc_t."""
+    _fields_ = [(k, ctypes.c_int32) for k in ("M", "D", "type", "before", "after", "gate_rows")] + \
+               [(k, ctypes.c_float) for k in ("eps", "scale")]
+
+
+_np = ctypes.POINTER(ResidualNormDesc)
+_lib.cct_residual_norm_forward.argtypes = [_np] + [_vp, _i64] * 3 + [_vp] * 4 + [_vp, _i64] * 2 + [_vp]
+_lib.cct_residual_norm_workspace_bytes.argtypes = [_np, ctypes.POINTER(_sz)]
+_lib.cct_residual_norm_backward.argtypes = [_np] + [_vp, _i64] * 3 + [_vp] * 3 + [_vp, _i64] * 5 + [_vp] * 4 + [_vp, _sz, _vp]
 
 
 class ProfileEntry(ctypes.Structure):
@@ -546,6 +560,53 @@ def cct_gated_backward(desc: GatedDesc, x, wg, wu, g, u, dh, dx, dwg, dwu, works
         *_mat(wu, "wu", F, K, dt, none), *_mat(g, "g", M, F, dt), *_mat(u, "u", M, F, dt), *_mat(dh, "dh", M, F, dt),
         *_mat(dx, "dx", M, K, dt, True), *_mat(dwg, "dwg", F, K, dt, True), *_mat(dwu, "dwu", F, K, dt, True),
         *_ws(workspace), _stream()), "cct_gated_backward")
+
+
+# ---- norms and gates on a residual stream -------------------------------------------------------
+
+def make_residual_norm_desc(M, D, type=TYPE_F32, before=NORM_RMS, after=NORM_NONE, gate_rows=1, eps=1e-6,
+                            scale=1.0) -> ResidualNormDesc:
+    return ResidualNormDesc(M, D, type, before, after, gate_rows, eps, scale)
+
+
+def cct_residual_norm_workspace_bytes(desc: ResidualNormDesc) -> int:
+    """Of the backward pass; the forward pass needs none."""
+    out = _sz()
+    _check(_lib.cct_residual_norm_workspace_bytes(ctypes.byref(desc), ctypes.byref(out)),
+           "cct_residual_norm_workspace_bytes")
+    return out.value
+
+
+def alloc_residual_norm_workspace(desc: ResidualNormDesc):
+    return torch.empty(cct_residual_norm_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+
+
+def _gate_count(desc):
+    return -(-desc.M // max(1, desc.gate_rows))
+
+
+def cct_residual_norm_forward(desc: ResidualNormDesc, r, b, gate, w_after, c_after, w_before, c_before, s, h) -> None:
+    """s = r + scale * gate * N_after(b), h = N_before(s); b, gate, the norms' vectors, and s or h may be None.  gate: a row
+    for each gate_rows rows of r."""
+    M, D, dt = desc.M, desc.D, _dtype_of(desc)
+    _check(_lib.cct_residual_norm_forward(
+        ctypes.byref(desc), *_mat(r, "r", M, D, dt), *_mat(b, "b", M, D, dt, True),
+        *_mat(gate, "gate", _gate_count(desc), D, dt, True), _vec(w_after, "w_after", D, dt),
+        _vec(c_after, "c_after", D, dt), _vec(w_before, "w_before", D, dt), _vec(c_before, "c_before", D, dt),
+        *_mat(s, "s", M, D, dt, True), *_mat(h, "h", M, D, dt, True), _stream()), "cct_residual_norm_forward")
+
+
+def cct_residual_norm_backward(desc: ResidualNormDesc, s, b, gate, w_after, c_after, w_before, ds, dh, dr, db, dgate,
+                               dw_after, dc_after, dw_before, dc_before, workspace) -> None:
+    """The gradients of r, b, the gate and the norms' vectors, each of which may be None, from those of s and h."""
+    M, D, dt, n = desc.M, desc.D, _dtype_of(desc), _gate_count(desc)
+    _check(_lib.cct_residual_norm_backward(
+        ctypes.byref(desc), *_mat(s, "s", M, D, dt, True), *_mat(b, "b", M, D, dt, True),
+        *_mat(gate, "gate", n, D, dt, True), _vec(w_after, "w_after", D, dt), _vec(c_after, "c_after", D, dt),
+        _vec(w_before, "w_before", D, dt), *_mat(ds, "ds", M, D, dt, True), *_mat(dh, "dh", M, D, dt, True),
+        *_mat(dr, "dr", M, D, dt, True), *_mat(db, "db", M, D, dt, True), *_mat(dgate, "dgate", n, D, dt, True),
+        _vec(dw_after, "dw_after", D, dt), _vec(dc_after, "dc_after", D, dt), _vec(dw_before, "dw_before", D, dt),
+        _vec(dc_before, "dc_before", D, dt), *_ws(workspace), _stream()), "cct_residual_norm_backward")
 
 
 # ---- gradient norm and weight update ------------------------------------------------------------

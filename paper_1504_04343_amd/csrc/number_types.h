@@ -52,6 +52,24 @@ __device__ __forceinline__ void store8(void* p, long long i, const f32x8& v) {
   *(typename Number<TYPE>::U8*)at = __builtin_convertvector(v, typename Number<TYPE>::V8);
 }
 
+// The first n of 8 values, zeros behind them.
+template <int TYPE>
+__device__ __forceinline__ f32x8 load_first(const void* p, long long i, int n) {
+  if (n >= 8) return load8<TYPE>(p, i);
+  f32x8 v = {};
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) v[e] = load1<TYPE>(p, i + e);
+  return v;
+}
+template <int TYPE>
+__device__ __forceinline__ void store_first(void* p, long long i, const f32x8& v, int n) {
+  if (n >= 8) return store8<TYPE>(p, i, v);
+#pragma unroll
+  for (int e = 0; e < 7; ++e)
+    if (e < n) store1<TYPE>(p, i + e, v[e]);
+}
+
 inline int type_bytes(int type) { return type == CCT_TYPE_F32 ? 4 : 2; }
 inline bool type_known(int type) { return type >= CCT_TYPE_F32 && type <= CCT_TYPE_F16; }
 
