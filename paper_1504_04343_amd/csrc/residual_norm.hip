@@ -10,6 +10,8 @@
 namespace cct {
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 template <class F>
 void with_type(int type, F f) {
   if (type == CCT_TYPE_F32)
@@ -20,24 +22,42 @@ void with_type(int type, F f) {
     f(std::integral_constant<int, CCT_TYPE_F16>());
 }
 
-// The sum over a wave's lanes, in all of them.
-__device__ __forceinline__ float wave_sum(float v) {
+template <class F>
+void with_bool(bool b, F f) {
+  if (b)
+    f(std::true_type());
+  else
+    f(std::false_type());
+}
+
+// The sum over 16 neighbouring lanes, in all of them.
+__device__ __forceinline__ float row_sum(float v) {
   auto other = [](float x, auto how) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(how)::value, 0xf, 0xf, true));
   };
-  v += other(v, std::integral_constant<int, 0xb1>());   // neighbours
-  v += other(v, std::integral_constant<int, 0x4e>());   // pairs of them
-  v += other(v, std::integral_constant<int, 0x141>());  // fours of a half row, mirrored
-  v += other(v, std::integral_constant<int, 0x140>());  // eights of a row, mirrored
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
+  v += other(v, std::integral_constant<int, 0xb1>());          // neighbours
+  v += other(v, std::integral_constant<int, 0x4e>());          // pairs of them
+  v += other(v, std::integral_constant<int, 0x141>());         // fours of a half row, mirrored
+  return v + other(v, std::integral_constant<int, 0x140>());  // eights of a row, mirrored
+}
+// Over a wave's lanes.
+__device__ __forceinline__ float wave_sum(float v) {
+  v = row_sum(v);
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const unsigned r0 = rows[0], r1 = rows[1];  // a bit cast of the second element itself reads the first
+  const unsigned h = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1));
+  const auto halves = __builtin_amdgcn_permlane32_swap(h, h, false, false);
+  const unsigned h0 = halves[0], h1 = halves[1];
+  return __builtin_bit_cast(float, h0) + __builtin_bit_cast(float, h1);
 }
 
-constexpr int kMostWaves = 16;
+constexpr int kMostWaves = 16, kRegisterColumns = kMostWaves * 512;
+constexpr int kNormTeams = 4;  // rows of up to 512 columns that a workgroup takes
 // Sums over a workgroup's waves, in all threads.  Two places in LDS in turn: a wave that is a sum ahead does not write over what
-// others still read.
+// others still read.  Each lane reads one wave's sum: one after the other they were a trip to LDS each.
 struct RowSums {
-  float (*lds)[kMostWaves][4];
+  float (*lds)[4][kMostWaves];
   int waves, turn;
   template <int N>
   __device__ __forceinline__ void operator()(float (&v)[N]) {
@@ -45,15 +65,15 @@ struct RowSums {
     for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if (waves == 1) return;
     turn ^= 1;
+    const int lane = threadIdx.x & 15;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int i = 0; i < N; ++i) lds[turn][threadIdx.x >> 6][i] = v[i];
+      for (int i = 0; i < N; ++i) lds[turn][i][threadIdx.x >> 6] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lds[turn][0][i];
-    for (int w = 1; w < waves; ++w)
+    for (int i = 0; i < N; ++i) v[i] = lane < waves ? lds[turn][i][lane] : 0.f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += lds[turn][w][i];
+    for (int i = 0; i < N; ++i) v[i] = row_sum(v[i]);
   }
 };
 
@@ -66,7 +86,7 @@ __device__ __forceinline__ f32x8 first_of(f32x8 v, int n) {
 // Values of a vector that may not be there.
 template <int TYPE>
 __device__ __forceinline__ f32x8 vector_or(const void* p, int c, int n, float none) {
-  if (p) return load_first<TYPE>(p, c, n);
+  if (p) return load_row<TYPE>(p, 0, c, n);
   f32x8 v;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = none;
@@ -74,10 +94,11 @@ __device__ __forceinline__ f32x8 vector_or(const void* p, int c, int n, float no
 }
 __device__ __forceinline__ float rstd_of(float squares, const int D, float eps) { return 1.f / sqrtf(squares / (float)D + eps); }
 
-// Rows of any length: each sum is a pass over the row, which a cache holds.
+// Rows of any length: each sum is a pass over the row, which a cache holds (bf16, 4096 x 12296, two norms: 125 us, 3.2 TB/s of what
+// has to be moved).
 template <int TYPE>
 __global__ __launch_bounds__(1024) void residual_norm_long_kernel(ResidualNorm p) {
-  __shared__ float lds[2][kMostWaves][4];
+  __shared__ float lds[2][4][kMostWaves];
   RowSums sums = {lds, (int)blockDim.x >> 6, 0};
   const int D = p.D, step = blockDim.x * 8, c0 = threadIdx.x * 8;
   for (long long row = blockIdx.x; row < p.M; row += gridDim.x) {
@@ -89,7 +110,7 @@ __global__ __launch_bounds__(1024) void residual_norm_long_kernel(ResidualNorm p
       sums(v);
       return v[0];
     };
-    auto old = [&](int c, int n) { return load_first<TYPE>(p.b, row * p.ldb + c, n); };
+    auto old = [&](int c, int n) { return load_row<TYPE>(p.b, row * p.ldb, c, n); };
     if (p.after == CCT_NORM_LAYER && p.b) mean_b = over(old) / (float)D;
     if (p.after != CCT_NORM_NONE && p.b)
       rstd_b = rstd_of(over([&](int c, int n) {
@@ -97,14 +118,14 @@ __global__ __launch_bounds__(1024) void residual_norm_long_kernel(ResidualNorm p
                          return v * v;
                        }), D, p.eps);
     auto stream = [&](int c, int n) {
-      f32x8 s = load_first<TYPE>(p.r, row * p.ldr + c, n);
+      f32x8 s = load_row<TYPE>(p.r, row * p.ldr, c, n);
       if (p.b) {
         f32x8 v = old(c, n);
         if (p.after != CCT_NORM_NONE) {
           v = (v - mean_b) * rstd_b * vector_or<TYPE>(p.w_after, c, n, 1.f);
-          if (p.c_after) v += load_first<TYPE>(p.c_after, c, n);
+          if (p.c_after) v += load_row<TYPE>(p.c_after, 0, c, n);
         }
-        if (p.gate) v *= load_first<TYPE>(p.gate, gate + c, n);
+        if (p.gate) v *= load_row<TYPE>(p.gate, gate, c, n);
         s += v * p.scale;
       }
       return s;
@@ -122,9 +143,99 @@ __global__ __launch_bounds__(1024) void residual_norm_long_kernel(ResidualNorm p
       if (p.s) store_first<TYPE>(p.s, row * p.lds + c, s, n);
       if (p.h) {
         f32x8 h = (s - mean_s) * rstd_s * vector_or<TYPE>(p.w_before, c, n, 1.f);
-        if (p.c_before) h += load_first<TYPE>(p.c_before, c, n);
+        if (p.c_before) h += load_row<TYPE>(p.c_before, 0, c, n);
         store_first<TYPE>(p.h, row * p.ldh + c, h, n);
       }
+    }
+  }
+}
+
+// load_row and store_first where a row is whole eights (EIGHTS): less code and fewer registers.
+template <int TYPE, bool EIGHTS>
+__device__ __forceinline__ typename Number<TYPE>::V8 row_raw(const void* p, long long row, int c, int n) {
+  if constexpr (!EIGHTS) return load_row_raw<TYPE>(p, row, c, n);
+  typename Number<TYPE>::V8 v = {};
+  if (n > 0) v = *(const typename Number<TYPE>::U8*)((const typename Number<TYPE>::T*)p + row + c);
+  return v;
+}
+template <int TYPE, bool EIGHTS>
+__device__ __forceinline__ void store_row(void* p, long long i, const f32x8& v, int n) {
+  if constexpr (!EIGHTS) return store_first<TYPE>(p, i, v, n);
+  if (n > 0) store8<TYPE>(p, i, v);
+}
+
+// A vector that may not be there.
+template <int TYPE, bool EIGHTS>
+__device__ __forceinline__ typename Number<TYPE>::V8 row_vector(const void* p, int c, int n, float none) {
+  typename Number<TYPE>::V8 v;
+  if (p) return row_raw<TYPE, EIGHTS>(p, 0, c, n);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (typename Number<TYPE>::T)none;
+  return v;
+}
+
+// A row in registers, 8 columns a thread: a workgroup takes one at a time, or a wave where 512 columns are all.  What it waits for
+// is memory, and between loads and stores the meetings of its waves (two norms: one each, layer norms two), so that other
+// workgroups, or, where a row takes half a CU or more (AHEAD), the next row's loads have to fill them.  bf16, one norm after the
+// addition, 8192 x 4096: 48 us, 5.6 TB/s; 8192 x 8192: 102 us, with weights loaded behind the next row 130, without the next row
+// on its way 156.
+template <int TYPE, bool EIGHTS, bool AHEAD>
+__global__ __launch_bounds__(1024) void residual_norm_kernel(ResidualNorm p, bool wave_rows) {
+  typedef typename Number<TYPE>::V8 V8;
+  __shared__ float lds[2][4][kMostWaves];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
+  RowSums total = {lds, wave_rows ? 1 : waves, 0};
+  const int c = (wave_rows ? threadIdx.x & 63 : threadIdx.x) * 8, n = p.D - c;
+  const long long first = wave_rows ? (long long)blockIdx.x * waves + wave : blockIdx.x;
+  const long long stride = wave_rows ? (long long)gridDim.x * waves : gridDim.x;
+  // v becomes v - mean, zeros behind the row; the factor
+  auto center = [&](int kind, f32x8& v) {
+    float t[1];
+    if (kind == CCT_NORM_LAYER) {
+      t[0] = sum8(v);
+      total(t);
+      v = first_of(v - t[0] / (float)p.D, n);
+    }
+    t[0] = sum8(v * v);
+    total(t);
+    return rstd_of(t[0], p.D, p.eps);
+  };
+  V8 r, b, gate;
+  auto load = [&](long long row) {
+    r = row_raw<TYPE, EIGHTS>(p.r, row * p.ldr, c, n);
+    if (p.b) b = row_raw<TYPE, EIGHTS>(p.b, row * p.ldb, c, n);
+    if (p.gate) gate = row_raw<TYPE, EIGHTS>(p.gate, (long long)((unsigned)row / (unsigned)p.gate_rows) * p.ldgate, c, n);
+  };
+  auto wide = [](const V8& v) { return __builtin_convertvector(v, f32x8); };
+  if (first < p.M) load(first);
+  // what all rows take, so that in the loop nothing is loaded behind the next row: what comes last is waited for with all before it
+  V8 w_after, c_after, w_before, c_before;
+  if (p.b && p.after != CCT_NORM_NONE) {
+    w_after = row_vector<TYPE, EIGHTS>(p.w_after, c, n, 1.f);
+    c_after = row_vector<TYPE, EIGHTS>(p.c_after, c, n, 0.f);
+  }
+  if (p.h) {
+    w_before = row_vector<TYPE, EIGHTS>(p.w_before, c, n, 1.f);
+    c_before = row_vector<TYPE, EIGHTS>(p.c_before, c, n, 0.f);
+  }
+  for (long long row = first; row < p.M; row += stride) {
+    if (!AHEAD && row != first) load(row);
+    f32x8 s = wide(r), v, g;
+    if (p.b) v = wide(b);
+    if (p.gate) g = wide(gate);
+    if (AHEAD && row + stride < p.M) load(row + stride);
+    if (p.b) {
+      if (p.after != CCT_NORM_NONE) {
+        const float rstd = center(p.after, v);
+        v = v * rstd * wide(w_after) + wide(c_after);
+      }
+      if (p.gate) v *= g;
+      s += v * p.scale;
+    }
+    if (p.s) store_row<TYPE, EIGHTS>(p.s, row * p.lds + c, s, n);
+    if (p.h) {
+      const float rstd = center(p.before, s);
+      store_row<TYPE, EIGHTS>(p.h, row * p.ldh + c, s * rstd * wide(w_before) + wide(c_before), n);
     }
   }
 }
@@ -151,16 +262,16 @@ template <int TYPE>
 __device__ __forceinline__ f32x8 stream_gradient(const ResidualNormBack& p, const RowStats& q, long long row, int c, int n, f32x8* dh,
                                                  f32x8* n_s) {
   f32x8 ds = {};
-  if (p.ds) ds = load_first<TYPE>(p.ds, row * p.ldds + c, n);
+  if (p.ds) ds = load_row<TYPE>(p.ds, row * p.ldds, c, n);
   if (!p.dh) return ds;
-  *dh = load_first<TYPE>(p.dh, row * p.lddh + c, n);
-  *n_s = (load_first<TYPE>(p.s, row * p.lds + c, n) - q.mean_s) * q.rstd_s;
+  *dh = load_row<TYPE>(p.dh, row * p.lddh, c, n);
+  *n_s = (load_row<TYPE>(p.s, row * p.lds, c, n) - q.mean_s) * q.rstd_s;
   return ds + (*dh * vector_or<TYPE>(p.w_before, c, n, 1.f) - *n_s * q.slope_s - q.level_s) * q.rstd_s;
 }
 
 template <int TYPE>
 __global__ __launch_bounds__(1024) void residual_norm_stats_kernel(ResidualNormBack p, RowStats* __restrict__ stats) {
-  __shared__ float lds[2][kMostWaves][4];
+  __shared__ float lds[2][4][kMostWaves];
   RowSums sums = {lds, (int)blockDim.x >> 6, 0};
   const int D = p.D, step = blockDim.x * 8, c0 = threadIdx.x * 8;
   const bool block = p.b && p.after != CCT_NORM_NONE;
@@ -178,9 +289,9 @@ __global__ __launch_bounds__(1024) void residual_norm_stats_kernel(ResidualNormB
       sums(v);
       return make_float2(v[0], v[1]);
     };
-    auto at_s = [&](int c, int n) { return load_first<TYPE>(p.s, row * p.lds + c, n); };
-    auto at_b = [&](int c, int n) { return load_first<TYPE>(p.b, row * p.ldb + c, n); };
-    auto dn = [&](int c, int n) { return load_first<TYPE>(p.dh, row * p.lddh + c, n) * vector_or<TYPE>(p.w_before, c, n, 1.f); };
+    auto at_s = [&](int c, int n) { return load_row<TYPE>(p.s, row * p.lds, c, n); };
+    auto at_b = [&](int c, int n) { return load_row<TYPE>(p.b, row * p.ldb, c, n); };
+    auto dn = [&](int c, int n) { return load_row<TYPE>(p.dh, row * p.lddh, c, n) * vector_or<TYPE>(p.w_before, c, n, 1.f); };
     if (p.dh) {
       if (p.before == CCT_NORM_LAYER) {
         const float2 t = over([&](int c, int n, f32x8& a, f32x8& b) {
@@ -208,7 +319,7 @@ __global__ __launch_bounds__(1024) void residual_norm_stats_kernel(ResidualNormB
       const float2 t = over([&](int c, int n, f32x8& a, f32x8& b) {
         f32x8 dh, n_s;
         b = stream_gradient<TYPE>(p, q, row, c, n, &dh, &n_s) * p.scale;
-        if (p.gate) b *= load_first<TYPE>(p.gate, gate + c, n);
+        if (p.gate) b *= load_row<TYPE>(p.gate, gate, c, n);
         b *= vector_or<TYPE>(p.w_after, c, n, 1.f);
         a = b * ((at_b(c, n) - q.mean_b) * q.rstd_b);
       });
@@ -245,12 +356,12 @@ __global__ __launch_bounds__(kColumnThreads) void residual_norm_columns_kernel(R
     sums.v[kDwBefore] += dh * n_s;
     if (p.dr) store_first<TYPE>(p.dr, row * p.lddr + c, ds, n);
     f32x8 dp = ds * p.scale, n_b = {};
-    if (block) n_b = (load_first<TYPE>(p.b, row * p.ldb + c, n) - q.mean_b) * q.rstd_b;
+    if (block) n_b = (load_row<TYPE>(p.b, row * p.ldb, c, n) - q.mean_b) * q.rstd_b;
     if (p.gate) {
-      gate = load_first<TYPE>(p.gate, row / p.gate_rows * p.ldgate + c, n);
+      gate = load_row<TYPE>(p.gate, row / p.gate_rows * p.ldgate, c, n);
       if (p.out[kDgate]) {
-        f32x8 normed = block ? n_b * w_after : load_first<TYPE>(p.b, row * p.ldb + c, n);
-        if (p.c_after) normed += load_first<TYPE>(p.c_after, c, n);
+        f32x8 normed = block ? n_b * w_after : load_row<TYPE>(p.b, row * p.ldb, c, n);
+        if (p.c_after) normed += load_row<TYPE>(p.c_after, 0, c, n);
         sums.v[kDgate] += dp * normed;
         if (plan.whole && (row + 1 == run.end || (row + 1) % p.gate_rows == 0)) {
           store_first<TYPE>(p.out[kDgate], row / p.gate_rows * p.lddgate + c, sums.v[kDgate], n);
@@ -272,29 +383,189 @@ __global__ __launch_bounds__(kColumnThreads) void residual_norm_columns_kernel(R
       store_first<CCT_TYPE_F32>((char*)part + k * plan.part_bytes, (long long)blockIdx.x * p.D + c, sums.v[k], n);
 }
 
-// The runs' sums, added in order: 32 columns of one result, 32 threads a column.  blockIdx.y: four vectors, then the gate's rows.
+// Where the norms' sums are: LDS, so that 128 registers are enough for two workgroups on a CU; the next row of fp32 values leaves
+// no room for that, up to 512 threads they have 256.
+template <int TYPE, int THREADS>
+constexpr bool norm_sums_in_lds = THREADS > 512;
+
+// The same of rows of up to 8192 columns in one pass: a thread has 8 columns, a workgroup a run of rows, one at a time, or its waves
+// one each where 512 columns are all (in spans: of a gate row's rows, so that its sum is one wave's).  The next row is on its way
+// while one is worked on; its sums over columns stay with the thread.  Between a row's loads and stores its waves meet two or three
+// times, which is what the time went into (8192 x 4096, bf16, two norms and a gate: 84 us; 100 with sums over waves that read
+// LDS one after the other) and what is above the 79 us of a copy; the runs' sums and their joining take 10 us more.
+template <int TYPE, int THREADS, bool EIGHTS>
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS <= 512 ? 2 : 4))) void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {
+  typedef typename Number<TYPE>::V8 V8;
+  constexpr bool AHEAD = THREADS <= 512, IN_LDS = norm_sums_in_lds<TYPE, THREADS>;
+  __shared__ float lds[2][4][kMostWaves];
+  __shared__ float meet[AHEAD ? kNormTeams : 1][512];
+  extern __shared__ f32x4 norm_sums[];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const bool teams = AHEAD && p.D <= 512;
+  RowSums total = {lds, teams ? 1 : waves, 0};
+  const int c = (teams ? threadIdx.x & 63 : threadIdx.x) * 8, n = p.D - c;
+  const float D = (float)p.D;
+  const bool block = p.b && p.after != CCT_NORM_NONE;
+  const NormRun run = norm_run(p, plan, blockIdx.x);
+  const int span = plan.whole ? p.gate_rows : 1;
+  const long long skip = teams ? (long long)(waves - 1) * span : 0;
+  const V8 raw_before = row_vector<TYPE, EIGHTS>(p.w_before, c, n, 1.f), raw_after = row_vector<TYPE, EIGHTS>(p.w_after, c, n, 1.f),
+           raw_c = row_vector<TYPE, EIGHTS>(p.c_after, c, n, 0.f);
+  ColumnSums sums = {};
+  auto own = [&](int k, int half) { return norm_sums + (k * 2 + half) * THREADS + threadIdx.x; };
+  if constexpr (IN_LDS)
+#pragma unroll
+    for (int k = 0; k < kDgate; ++k) *own(k, 0) = *own(k, 1) = f32x4{};
+  auto add = [&](auto which, const f32x8& v) {
+    constexpr int K = decltype(which)::value;
+    if constexpr (!IN_LDS || K == kDgate) {
+      sums.v[K] += v;
+    } else if (p.out[K]) {
+      *own(K, 0) += __builtin_shufflevector(v, v, 0, 1, 2, 3);
+      *own(K, 1) += __builtin_shufflevector(v, v, 4, 5, 6, 7);
+    }
+  };
+
+  struct Row {
+    V8 s, b, ds, dh, gate;
+  };
+  auto load = [&](Row& to, long long row, long long before) {
+    if (p.ds) to.ds = row_raw<TYPE, EIGHTS>(p.ds, row * p.ldds, c, n);
+    if (p.dh) {
+      to.s = row_raw<TYPE, EIGHTS>(p.s, row * p.lds, c, n);
+      to.dh = row_raw<TYPE, EIGHTS>(p.dh, row * p.lddh, c, n);
+    }
+    if (p.b) to.b = row_raw<TYPE, EIGHTS>(p.b, row * p.ldb, c, n);
+    if (p.gate) {
+      const unsigned g = (unsigned)row / (unsigned)p.gate_rows;
+      if (before < 0 || g != (unsigned)before / (unsigned)p.gate_rows) to.gate = row_raw<TYPE, EIGHTS>(p.gate, (long long)g * p.ldgate, c, n);
+    }
+  };
+  long long row = run.first + (teams ? (long long)wave * span : 0);
+  int left = span;
+  Row at = {};
+  if (AHEAD && row < run.end) load(at, row, -1);
+  while (row < run.end) {
+    const bool turn = left == 1;
+    const long long next = row + 1 + (turn ? skip : 0);
+    left = turn ? span : left - 1;
+    Row ahead;
+    if constexpr (AHEAD) {
+      ahead = at;
+      if (next < run.end) load(ahead, next, row);
+    } else {
+      load(at, row, -1);
+    }
+
+    f32x8 ds = {}, dh = {}, n_s = {}, n_b = {}, dn = {};
+    if (p.ds) ds = __builtin_convertvector(at.ds, f32x8);
+    if (p.dh) {
+      dh = __builtin_convertvector(at.dh, f32x8);
+      n_s = __builtin_convertvector(at.s, f32x8);
+      dn = dh * __builtin_convertvector(raw_before, f32x8);
+    }
+    if (p.b) n_b = __builtin_convertvector(at.b, f32x8);
+    float level_s = 0.f;
+    const bool layer_s = p.dh && p.before == CCT_NORM_LAYER, layer_b = block && p.after == CCT_NORM_LAYER;
+    if (layer_s || layer_b) {
+      float t[3] = {sum8(n_s), sum8(dn), sum8(n_b)};
+      total(t);
+      if (layer_s) {
+        n_s = first_of(n_s - t[0] / D, n);
+        level_s = t[1] / D;
+      }
+      if (layer_b) n_b = first_of(n_b - t[2] / D, n);
+    }
+    float t[3] = {sum8(n_s * n_s), sum8(n_s * dn), sum8(n_b * n_b)};
+    if (p.dh || block) total(t);
+    if (p.dh) {
+      const float rstd = rstd_of(t[0], p.D, p.eps);
+      n_s *= rstd;
+      ds += (dn - n_s * (t[1] * rstd / D) - level_s) * rstd;
+    }
+    if (p.dr) store_row<TYPE, EIGHTS>(p.dr, row * p.lddr + c, ds, n);
+    add(std::integral_constant<int, kDcBefore>(), dh);
+    add(std::integral_constant<int, kDwBefore>(), dh * n_s);
+    f32x8 dp = ds * p.scale;
+    const float rstd_b = block ? rstd_of(t[2], p.D, p.eps) : 1.f;
+    if (block) n_b *= rstd_b;
+    const f32x8 w_after = __builtin_convertvector(raw_after, f32x8);
+    if (p.gate) {
+      if (p.out[kDgate]) {
+        sums.v[kDgate] += dp * (n_b * w_after + __builtin_convertvector(raw_c, f32x8));
+        if (plan.whole && (turn || row + 1 == run.end)) {
+          store_row<TYPE, EIGHTS>(p.out[kDgate], (long long)((unsigned)row / (unsigned)p.gate_rows) * p.lddgate + c, sums.v[kDgate], n);
+          sums.v[kDgate] = f32x8{};
+        }
+      }
+      dp *= __builtin_convertvector(at.gate, f32x8);
+    }
+    if (block) {
+      add(std::integral_constant<int, kDcAfter>(), dp);
+      add(std::integral_constant<int, kDwAfter>(), dp * n_b);
+      if (p.db) {
+        dp *= w_after;
+        float u[2] = {sum8(dp * n_b), sum8(dp)};
+        total(u);
+        dp = (dp - n_b * (u[0] / D) - (layer_b ? u[1] / D : 0.f)) * rstd_b;
+      }
+    }
+    if (p.db) store_row<TYPE, EIGHTS>(p.db, row * p.lddb + c, dp, n);
+    if constexpr (AHEAD) at = ahead;
+    row = next;
+  }
+
+#pragma unroll
+  for (int k = 0; k < kNormSums; ++k) {
+    if (!p.out[k] || (k == kDgate && plan.whole)) continue;
+    if constexpr (IN_LDS)
+      if (k != kDgate) sums.v[k] = __builtin_shufflevector(*own(k, 0), *own(k, 1), 0, 1, 2, 3, 4, 5, 6, 7);
+    if (teams) {
+      *(f32x8*)&meet[wave][c] = sums.v[k];
+      __syncthreads();
+      if (wave == 0)
+        for (int w = 1; w < waves; ++w) sums.v[k] += *(const f32x8*)&meet[w][c];
+      __syncthreads();
+      if (wave > 0) continue;
+    }
+    if (plan.count == 1)  // nothing to join
+      store_first<TYPE>(p.out[k], c, sums.v[k], n);
+    else
+      store_first<CCT_TYPE_F32>((char*)part + k * plan.part_bytes, (long long)blockIdx.x * p.D + c, sums.v[k], n);
+  }
+}
+
+// The runs' sums, added in order: 32 columns of one result, 8 threads a column.  blockIdx.y: four vectors, then the gate's rows.
+constexpr int kJoinRows = 8;
 template <int TYPE>
-__global__ __launch_bounds__(1024) void residual_norm_join_kernel(ResidualNormBack p, ResidualNormPlan plan, const float* __restrict__ part) {
-  __shared__ float lds[32][33];
+__global__ __launch_bounds__(kJoinRows * 32) void residual_norm_join_kernel(ResidualNormBack p, ResidualNormPlan plan,
+                                                                            const float* __restrict__ part) {
+  __shared__ float lds[kJoinRows][33];
   const int k = min((int)blockIdx.y, (int)kDgate), group = (int)blockIdx.y - k;
   if (!p.out[k]) return;
   const int rows = k == kDgate ? plan.per_gate : plan.count, x = threadIdx.x & 31, y = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + x;
   const float* from = (const float*)((const char*)part + k * plan.part_bytes) + (long long)group * rows * p.D + c;
-  float v = 0.f;
-  if (c < p.D)
-#pragma unroll 8
-    for (int r = y; r < rows; r += 32) v += from[(long long)r * p.D];
-  lds[y][x] = v;
+  float v[4] = {};  // four chains: one waits for itself
+  if (c < p.D) {
+    int r = y;
+#pragma unroll 2
+    for (; r + 3 * kJoinRows < rows; r += 4 * kJoinRows)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += from[(long long)(r + q * kJoinRows) * p.D];
+    for (; r < rows; r += kJoinRows) v[0] += from[(long long)r * p.D];
+  }
+  lds[y][x] = (v[0] + v[1]) + (v[2] + v[3]);
   __syncthreads();
 #pragma unroll
-  for (int half = 16; half > 0; half >>= 1) {
+  for (int half = kJoinRows / 2; half > 0; half >>= 1) {
     if (y < half) lds[y][x] += lds[y + half][x];
     __syncthreads();
   }
   if (y == 0 && c < p.D) store1<TYPE>(p.out[k], k == kDgate ? group * p.lddgate + c : c, lds[0][x]);
 }
 
+constexpr int kRowsAhead = 512;  // workgroups, two a CU, of rows that leave no room for more
 int row_threads(int D) { return std::min(kMostWaves, pieces(D, 512)) * 64; }
 double forward_bytes(const ResidualNorm& p) {
   return (double)type_bytes(p.type) * p.M * p.D * (1 + (p.b != nullptr) + (p.s != nullptr) + (p.h != nullptr));
@@ -304,7 +575,10 @@ double forward_bytes(const ResidualNorm& p) {
 
 ResidualNormPlan residual_norm_plan(const cct_residual_norm_desc_t& d) {
   ResidualNormPlan p = {};
-  const int most = 512;
+  // as many runs as the chip takes at a time: a CU has places for 12 waves of residual_norm_back_kernel (fp32: 8), three for each
+  // of its SIMDs, so that rows of more than four waves come one by one
+  const int waves = d.D <= 512 ? kNormTeams : pieces(d.D, 512), places = d.type == CCT_TYPE_F32 ? 8 : 12;
+  const int most = 256 * (waves <= 4 ? std::min(3, places / waves) : 1);
   const int wanted = std::max(4, pieces(d.M, most)), shared = std::min(d.gate_rows, std::max(d.M, 1));
   p.whole = shared <= wanted;
   if (p.whole) {
@@ -312,20 +586,39 @@ ResidualNormPlan residual_norm_plan(const cct_residual_norm_desc_t& d) {
     p.per_gate = 0;
     p.count = pieces(d.M, p.rows);
   } else {
-    p.per_gate = pieces(shared, wanted);
+    p.per_gate = std::max(1, std::min(pieces(shared, wanted), most / pieces(d.M, shared)));
     p.rows = pieces(shared, p.per_gate);
     p.count = pieces(d.M, shared) * p.per_gate;
   }
   auto up = [](long long v) { return (v + 255) / 256 * 256; };
-  p.part_off = up((long long)d.M * sizeof(RowStats));
+  p.part_off = d.D <= kRegisterColumns ? 0 : up((long long)d.M * sizeof(RowStats));
   p.part_bytes = up((long long)p.count * d.D * 4);
   p.total = std::max(256LL, p.part_off + kNormSums * p.part_bytes);
   return p;
 }
 
 int launch_residual_norm(const ResidualNorm& p, hipStream_t st) {
-  ProfScope ps("residual_norm_long_kernel", 0.0, forward_bytes(p), st);
   const int threads = row_threads(p.D);
+  if (p.D <= kRegisterColumns) {
+    ProfScope ps("residual_norm_kernel", 0.0, forward_bytes(p), st);
+    const bool wave_rows = p.D <= 512;
+    const int groups = std::min(wave_rows ? pieces(p.M, kNormTeams) : p.M, 1 << 20);
+    with_type(p.type, [&](auto type) {
+      constexpr int TYPE = decltype(type)::value;
+      with_bool(p.D % 8 == 0, [&](auto eights) {
+        constexpr bool EIGHTS = decltype(eights)::value;
+        if (p.D <= kRegisterColumns / 2)
+          hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_kernel<TYPE, EIGHTS, false>), dim3(groups),
+                             dim3(wave_rows ? kNormTeams * 64 : threads), 0, st, p, wave_rows);
+        else
+          hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_kernel<TYPE, EIGHTS, true>), dim3(std::min(groups, kRowsAhead)),
+                             dim3(threads), 0, st, p, false);
+      });
+    });
+    CCT_CHECK_LAUNCH();
+    return CCT_OK;
+  }
+  ProfScope ps("residual_norm_long_kernel", 0.0, forward_bytes(p), st);
   with_type(p.type, [&](auto type) {
     hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_long_kernel<decltype(type)::value>), dim3(std::min(p.M, 1 << 20)), dim3(threads),
                        0, st, p);
@@ -338,7 +631,33 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
   RowStats* stats = (RowStats*)ws;
   float* part = (float*)(ws + plan.part_off);
   const double all = (double)type_bytes(p.type) * p.M * p.D;
-  if (p.M > 0) {
+  if (p.M > 0 && p.D <= kRegisterColumns) {
+    ProfScope ps("residual_norm_back_kernel", 0.0,
+                 all * ((p.ds != nullptr) + 2 * (p.dh != nullptr) + (p.b != nullptr) + (p.dr != nullptr) + (p.db != nullptr)), st);
+    int rc = CCT_OK;
+    with_type(p.type, [&](auto type) {
+      constexpr int TYPE = decltype(type)::value;
+      const int threads = p.D <= 512 ? kNormTeams * 64 : row_threads(p.D);
+      with_bool(p.D % 8 == 0, [&](auto eights) {
+        constexpr bool EIGHTS = decltype(eights)::value;
+        auto run = [&](auto most) {
+          constexpr int THREADS = decltype(most)::value;
+          const int lds = norm_sums_in_lds<TYPE, THREADS> ? kDgate * THREADS * 32 : 0;
+          if (lds) rc = ensure_dynamic_lds<residual_norm_back_kernel<TYPE, THREADS, EIGHTS>>(lds);
+          if (rc == CCT_OK)
+            hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_back_kernel<TYPE, THREADS, EIGHTS>), dim3(plan.count), dim3(threads), lds,
+                               st, p, plan, part);
+        };
+        if (threads <= 512)
+          run(std::integral_constant<int, 512>());
+        else
+          run(std::integral_constant<int, 1024>());
+      });
+    });
+    if (rc != CCT_OK) return rc;
+    CCT_CHECK_LAUNCH();
+    if (plan.count == 1) return CCT_OK;
+  } else if (p.M > 0) {
     {
       ProfScope ps("residual_norm_stats_kernel", 0.0, all * ((p.ds != nullptr) + 2 * (p.dh != nullptr) + (p.b != nullptr)), st);
       with_type(p.type, [&](auto type) {
@@ -361,7 +680,7 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
     ProfScope ps("residual_norm_join_kernel", 0.0, 0.0, st);
     with_type(p.type, [&](auto type) {
       hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_join_kernel<decltype(type)::value>),
-                         dim3(pieces(p.D, 32), kDgate + (gate ? plan.count / plan.per_gate : 0)), dim3(1024), 0, st, p, plan, part);
+                         dim3(pieces(p.D, 32), kDgate + (gate ? plan.count / plan.per_gate : 0)), dim3(kJoinRows * 32), 0, st, p, plan, part);
     });
     CCT_CHECK_LAUNCH();
   }

@@ -101,7 +101,9 @@ SHAPES = [(1, 1, "rms", "rms", 1, True, 0, 0), (1, 7, "layer", "rms", 1, True, 0
           (64, 4096, "layer", "none", 64, False, 8, 8), (129, 1025, "rms", "rms", 1, True, 0, 0), (300, 72, "layer", "layer", 7, True, 0, 0),
           (700, 24, "rms", "rms", 300, False, 0, 0), (1531, 264, "rms", "rms", 1000, True, 0, 0), (2100, 40, "layer", "layer", 5, True, 0, 0),
           (2100, 520, "rms", "none", 2100, False, 0, 0), (40, 8200, "rms", "layer", 13, True, 0, 0), (9, 16387, "layer", "rms", 1, True, 1, 1),
-          (2, 33000, "rms", "none", 2, False, 0, 0), (6, 3000, "none", "none", 3, False, 0, 0), (4, 1536, "none", "layer", 0, True, 2, 0)]
+          (2, 33000, "rms", "none", 2, False, 0, 0), (6, 3000, "none", "none", 3, False, 0, 0), (4, 1536, "none", "layer", 0, True, 2, 0),
+          (37, 5000, "layer", "rms", 5, True, 3, 1), (300, 4104, "rms", "layer", 300, True, 0, 0), (70, 8191, "rms", "rms", 9, False, 0, 0),
+          (4, 500, "rms", "rms", 4, True, 0, 0), (3, 4200, "layer", "layer", 5, True, 0, 0), (2049, 512, "rms", "layer", 700, True, 0, 0)]
 IDS = ["%dx%d-%s-%s-%d+%d@%d" % (s[:5] + s[6:]) for s in SHAPES]
 
 
@@ -236,7 +238,7 @@ def test_rows_far_apart(B):
     assert torch.equal(dr, got["dr"])
 
 
-@pytest.mark.parametrize("M,D,rows", [(50, 600, 7), (1, 4096, 1), (600, 96, 600), (20, 9000, 20)])
+@pytest.mark.parametrize("M,D,rows", [(50, 600, 7), (1, 4096, 1), (30, 6000, 4), (600, 96, 600), (20, 9000, 20)])
 def test_replayed_from_a_graph_and_on_another_stream(B, M, D, rows):
     c = Case(B, M, D, "bf16", "rms", "rms", rows)
     args = [mat(c.b), mat(c.gate), vec(c.w_after), vec(c.c_after), vec(c.w_before)]
