@@ -433,6 +433,60 @@ int cct_residual_norm_backward(const cct_residual_norm_desc_t* desc, const void*
                                void* hip_stream);
 
 /*
+ * Microscaled 4-bit floating point (the e2m1 format of the Open Compute Project's MX specification): 32 consecutive values of a
+ * row are a block that shares a power of two; each is one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times that.
+ *   codes: 4 bits a value, its sign above its number in this list; byte i of a row holds value 2i in the lower half and value
+ *     2i + 1 in the upper one.  A row is ceil(cols / 32) whole blocks of 16 bytes; values behind the row's end are zeros (a
+ *     product multiplies whole blocks).  codes and ld_codes (bytes) are multiples of 16.
+ *   scales: a byte for each block, its power of two's exponent + 127; 255: the block is NaN.  A row is ceil(cols / 32) bytes,
+ *     with room for a multiple of 4; scales and ld_scales (bytes) are multiples of 4.
+ * cct_mx_quantize: the exponent is floor(log2(m)) - 2 for the block's largest size m, at least -127 (also for a block of zeros);
+ * x / 2^exponent is rounded to the nearest, ties to even, at most 6.  A block that holds an infinity or a NaN is NaN. 
+ * cct_mx_dequantize: the values, rounded to the type of x (fp32 and bf16: exact; fp16: infinities beyond its range).
+ * rows >= 0, cols >= 1; x as for cct_linear_*; the same CCT_EUNSUPPORTED.
+ */
+int cct_mx_quantize(int32_t rows, int32_t cols, int32_t type, const void* x, int64_t ldx, void* codes, int64_t ld_codes,
+                    void* scales, int64_t ld_scales, void* hip_stream);
+int cct_mx_dequantize(int32_t rows, int32_t cols, int32_t type, const void* codes, int64_t ld_codes, const void* scales,
+                      int64_t ld_scales, void* x, int64_t ldx, void* hip_stream);
+/*
+ * cct_linear_forward of a microscaled weight (N x K) and a microscaled x: z = x w^T + bias, y = act(z) + residual.  Products are
+ * exact, sums fp32, bias, residual, y and z have the descriptor's type.  x_scales NULL: x (M x K, the descriptor's type, ldx in
+ * values) is quantised into the workspace first, as cct_mx_quantize does; else x is codes (ldx in bytes), x_scales their
+ * scales.  `quantize`: whether the workspace has room for that.  Everything else is as for cct_linear_forward.
+ */
+int cct_mx_linear_workspace_bytes(const cct_linear_desc_t* desc, int32_t quantize, size_t* bytes);
+int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* x_scales, int64_t ldxs,
+                          const void* w, int64_t ldw, const void* w_scales, int64_t ldws, const void* bias,
+                          const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A layer of experts for a few tokens (serving: a batch of sequences, one token each).  Expert e is a gated block of weights
+ * wg[e], wu[e] (F x D) and wd[e] (D x F); token t goes to the `chosen` experts of largest logit:
+ *   logit[t][e] = x[t] . router[e]  (router: experts x D; summed in 64 bits, rounded to 32; ties go to the lower e, NaN come
+ *   last),
+ *   weight = exp(logit - max) / sum of that over the chosen experts (normalize != 0) or all of them,
+ *   h = act(x[t] wg[e]^T) * (x[t] wu[e]^T),   y[t] = sum over the chosen e of weight * (h wd[e]^T) + residual[t].
+ * Experts that no token chooses are not read.  The weights of consecutive experts lie `e` values apart (wg_e >= F rows' extent;
+ * any element-aligned address and distance), their rows `ld`.  Sums are fp32; h keeps 16 bits or more (fp16: an infinity beyond
+ * 65504).  residual (tokens x D), chosen_out (tokens x chosen int32, largest logit first) and weights_out (fp32) may be NULL;
+ * these two are contiguous.  y may be the residual itself.
+ * 0 <= tokens, 1 <= chosen <= experts, D, F >= 1 (CCT_EINVAL); CCT_EUNSUPPORTED: more than 64 tokens, 512 experts or 16
+ * chosen ones, matrices as above.  Results do not depend on the order of workgroups.
+ */
+typedef struct {
+  int32_t tokens, experts, chosen, D, F;
+  int32_t type, activation;
+  int32_t normalize;
+} cct_moe_desc_t;
+int cct_moe_workspace_bytes(const cct_moe_desc_t* desc, size_t* bytes);
+int cct_moe_forward(const cct_moe_desc_t* desc, const void* x, int64_t ldx, const void* router, int64_t ldrouter, const void* wg,
+                    int64_t ldwg, int64_t wg_e, const void* wu, int64_t ldwu, int64_t wu_e, const void* wd, int64_t ldwd,
+                    int64_t wd_e, const void* residual, int64_t ldr, void* y, int64_t ldy, int32_t* chosen_out,
+                    float* weights_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * From gradients to new weights, over lists of tensors (host arrays; the tensors they name are contiguous device
  * memory, element-aligned).  The lists are read during the call only.
  *

@@ -46,6 +46,8 @@ EXPORTS = [
     "cct_linear_forward", "cct_linear_backward", "cct_gated_forward", "cct_gated_backward",
     "cct_grad_norm_workspace_bytes", "cct_grad_norm", "cct_grad_scale", "cct_sgd_update",
     "cct_residual_norm_forward", "cct_residual_norm_workspace_bytes", "cct_residual_norm_backward",
+    "cct_mx_quantize", "cct_mx_dequantize", "cct_mx_linear_workspace_bytes", "cct_mx_linear_forward",
+    "cct_moe_workspace_bytes", "cct_moe_forward",
 ]
 
 
@@ -147,6 +149,22 @@ _np = ctypes.POINTER(ResidualNormDesc)
 _lib.cct_residual_norm_forward.argtypes = [_np] + [_vp, _i64] * 3 + [_vp] * 4 + [_vp, _i64] * 2 + [_vp]
 _lib.cct_residual_norm_workspace_bytes.argtypes = [_np, ctypes.POINTER(_sz)]
 _lib.cct_residual_norm_backward.argtypes = [_np] + [_vp, _i64] * 3 + [_vp] * 3 + [_vp, _i64] * 5 + [_vp] * 4 + [_vp, _sz, _vp]
+
+
+_lib.cct_mx_quantize.argtypes = [_i32, _i32, _i32] + [_vp, _i64] * 3 + [_vp]
+_lib.cct_mx_dequantize.argtypes = [_i32, _i32, _i32] + [_vp, _i64] * 3 + [_vp]
+_lib.cct_mx_linear_workspace_bytes.argtypes = [_lp, _i32, ctypes.POINTER(_sz)]
+_lib.cct_mx_linear_forward.argtypes = [_lp] + [_vp, _i64] * 4 + [_vp] + [_vp, _i64] * 3 + [_vp, _sz, _vp]
+
+
+class MoeDesc(ctypes.Structure):
+    """cct_moe_desc_t."""
+    _fields_ = [(k, ctypes.c_int32) for k in ("tokens", "experts", "chosen", "D", "F", "type", "activation", "normalize")]
+
+
+_mp = ctypes.POINTER(MoeDesc)
+_lib.cct_moe_workspace_bytes.argtypes = [_mp, ctypes.POINTER(_sz)]
+_lib.cct_moe_forward.argtypes = [_mp] + [_vp, _i64] * 2 + [_vp, _i64, _i64] * 3 + [_vp, _i64] * 2 + [_vp, _vp, _vp, _sz, _vp]
 
 
 class ProfileEntry(ctypes.Structure):
@@ -607,6 +625,119 @@ def cct_residual_norm_backward(desc: ResidualNormDesc, s, b, gate, w_after, c_af
         *_mat(dr, "dr", M, D, dt, True), *_mat(db, "db", M, D, dt, True), *_mat(dgate, "dgate", n, D, dt, True),
         _vec(dw_after, "dw_after", D, dt), _vec(dc_after, "dc_after", D, dt), _vec(dw_before, "dw_before", D, dt),
         _vec(dc_before, "dc_before", D, dt), *_ws(workspace), _stream()), "cct_residual_norm_backward")
+
+
+# ---- microscaled 4-bit floating point -------------------------------------------------------------
+
+class MxMatrix:
+    """A matrix in microscaled 4-bit floating point: codes (rows x 16 bytes for each 32 columns) and scales (rows x a multiple
+    of 4 bytes, one for each 32 columns), uint8 tensors on the GPU, allocated here where they are not given."""
+
+    def __init__(self, rows, cols, codes=None, scales=None):
+        self.rows, self.cols = rows, cols
+        blocks = -(-cols // 32)
+        shapes = ((rows, blocks * 16), (rows, -(-blocks // 4) * 4))
+        given = [torch.empty(s, dtype=torch.uint8, device="cuda") if t is None else t for t, s in
+                 zip((codes, scales), shapes)]
+        self.codes, self.scales = given
+        self.codes_at, self.scales_at = (_mat(t, n, *s, torch.uint8) for t, n, s in
+                                         zip(given, ("codes", "scales"), shapes))
+
+
+def _mx(m, name, rows, cols):
+    if not isinstance(m, MxMatrix):
+        raise TypeError("%s must be an MxMatrix" % name)
+    if (m.rows, m.cols) != (rows, cols):
+        raise ValueError("%s is %d x %d, expected %d x %d" % (name, m.rows, m.cols, rows, cols))
+    return (*m.codes_at, *m.scales_at)
+
+
+def _type_of(t, name):
+    if not isinstance(t, torch.Tensor) or t.dtype not in _DTYPES or t.dim() != 2:
+        raise TypeError("%s must be a matrix of fp32, bf16 or fp16" % name)
+    return _DTYPES.index(t.dtype)
+
+
+def cct_mx_quantize(x, mx: MxMatrix) -> None:
+    """x (fp32, bf16 or fp16) rounded to microscaled 4 bits."""
+    ty = _type_of(x, "x")
+    _check(_lib.cct_mx_quantize(mx.rows, mx.cols, ty, *_mat(x, "x", mx.rows, mx.cols, x.dtype),
+                                *_mx(mx, "mx", mx.rows, mx.cols), _stream()), "cct_mx_quantize")
+
+
+def cct_mx_dequantize(mx: MxMatrix, x) -> None:
+    """The values of mx in x's type."""
+    ty = _type_of(x, "x")
+    _check(_lib.cct_mx_dequantize(mx.rows, mx.cols, ty, *_mx(mx, "mx", mx.rows, mx.cols),
+                                  *_mat(x, "x", mx.rows, mx.cols, x.dtype), _stream()), "cct_mx_dequantize")
+
+
+def cct_mx_linear_workspace_bytes(desc: LinearDesc, quantize: bool) -> int:
+    out = _sz()
+    _check(_lib.cct_mx_linear_workspace_bytes(ctypes.byref(desc), int(quantize), ctypes.byref(out)),
+           "cct_mx_linear_workspace_bytes")
+    return out.value
+
+
+def alloc_mx_linear_workspace(desc: LinearDesc, quantize: bool = True):
+    return torch.empty(cct_mx_linear_workspace_bytes(desc, quantize), dtype=torch.uint8, device="cuda")
+
+
+def cct_mx_linear_forward(desc: LinearDesc, x, w: MxMatrix, bias, residual, y, z, workspace) -> None:
+    """y = act(x w^T + bias) + residual; x is an MxMatrix, or a tensor that is quantised first."""
+    M, N, K, dt = desc.M, desc.N, desc.K, _dtype_of(desc)
+    at = _mx(x, "x", M, K) if isinstance(x, MxMatrix) else (*_mat(x, "x", M, K, dt), None, 0)
+    _check(_lib.cct_mx_linear_forward(
+        ctypes.byref(desc), *at, *_mx(w, "w", N, K), _vec(bias, "bias", N, dt),
+        *_mat(residual, "residual", M, N, dt, True), *_mat(y, "y", M, N, dt), *_mat(z, "z", M, N, dt, True),
+        *_ws(workspace), _stream()), "cct_mx_linear_forward")
+
+
+# ---- experts ----------------------------------------------------------------------------------------
+
+def make_moe_desc(tokens, experts, chosen, D, F, type=TYPE_F32, activation=ACT_SILU, normalize=True) -> MoeDesc:
+    return MoeDesc(tokens, experts, chosen, D, F, type, activation, int(normalize))
+
+
+def cct_moe_workspace_bytes(desc: MoeDesc) -> int:
+    out = _sz()
+    _check(_lib.cct_moe_workspace_bytes(ctypes.byref(desc), ctypes.byref(out)), "cct_moe_workspace_bytes")
+    return out.value
+
+
+def alloc_moe_workspace(desc: MoeDesc):
+    return torch.empty(cct_moe_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+
+
+def _experts(t, name, E, rows, cols, dtype):
+    """Address, row stride and expert stride of a tensor of matrices."""
+    if not isinstance(t, torch.Tensor) or t.shape != (E, rows, cols):
+        raise ValueError("%s must be a tensor of shape %s" % (name, (E, rows, cols)))
+    at, ld = _mat(t[0], name, rows, cols, dtype)
+    apart = t.stride(0) if E > 1 else rows * ld
+    if E > 1 and apart < (rows - 1) * ld + cols:
+        raise TypeError("%s has experts that overlap" % name)
+    return at, ld, apart
+
+
+def _out(t, name, shape, dtype):
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or t.shape != shape or \
+            not t.is_contiguous():
+        raise TypeError("%s must be a contiguous %s GPU tensor of shape %s" % (name, dtype, shape))
+    return t.data_ptr()
+
+
+def cct_moe_forward(desc: MoeDesc, x, router, wg, wu, wd, residual, y, chosen, weights, workspace) -> None:
+    """y = the chosen experts' weighted sum (+ residual); chosen (int32) and weights (fp32), tokens x chosen, may be None.
+    wg, wu: experts x F x D, wd: experts x D x F."""
+    T, E, k, D, F, dt = desc.tokens, desc.experts, desc.chosen, desc.D, desc.F, _dtype_of(desc)
+    _check(_lib.cct_moe_forward(
+        ctypes.byref(desc), *_mat(x, "x", T, D, dt), *_mat(router, "router", E, D, dt), *_experts(wg, "wg", E, F, D, dt),
+        *_experts(wu, "wu", E, F, D, dt), *_experts(wd, "wd", E, D, F, dt), *_mat(residual, "residual", T, D, dt, True),
+        *_mat(y, "y", T, D, dt), _out(chosen, "chosen", (T, k), torch.int32), _out(weights, "weights", (T, k), torch.float32),
+        *_ws(workspace), _stream()), "cct_moe_forward")
 
 
 # ---- gradient norm and weight update ------------------------------------------------------------

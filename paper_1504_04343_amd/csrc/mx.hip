@@ -1,0 +1,142 @@
+// The microscaled 4-bit operators' entry points (cct_mx_*): checks of arguments, workspaces, and which kernels a product runs on.
+#include "mx.h"
+
+#include <algorithm>
+
+#include "activation.h"
+#include "number_types.h"
+
+namespace cct {
+namespace {
+
+bool rows_ok(const void* p, long long ld, long long rows, long long cols, int align) {
+  return p && !((uintptr_t)p & (align - 1)) && ld >= 0 && (rows <= 1 || ld >= cols);
+}
+bool matrix_ok(const void* p, long long ld, long long rows, long long cols, int type) { return rows_ok(p, ld, rows, cols, type_bytes(type)); }
+bool mx_ok(const void* codes, long long ldc, const void* scales, long long lds, int rows, int cols) {
+  return rows_ok(codes, ldc, rows, mx_code_bytes(cols), 16) && ldc % 16 == 0 && rows_ok(scales, lds, rows, mx_scale_bytes(cols), 4) &&
+         lds % 4 == 0;
+}
+// As the 16- and 32-bit products' sizes; codes are smaller.
+int sizes_ok(int rows, int cols, int type) {
+  if (rows < 0 || cols < 1 || !type_known(type)) return CCT_EINVAL;
+  return std::max(rows, cols) <= 0x7fffff00 && (long long)rows * cols <= (1LL << 38) / type_bytes(type) ? CCT_OK : CCT_EUNSUPPORTED;
+}
+int product_ok(const cct_linear_desc_t& d) {
+  if (d.N < 1 || !activation_known(d.activation)) return CCT_EINVAL;
+  const int a = sizes_ok(d.M, d.K, d.type), b = sizes_ok(d.N, d.K, d.type), c = sizes_ok(d.M, d.N, d.type);
+  return a != CCT_OK ? a : b != CCT_OK ? b : c;
+}
+
+struct MxLayout {
+  long long codes, scales, part, total;
+};
+MxLayout layout_of(const cct_linear_desc_t& d, bool quantize) {
+  MxLayout b = {};
+  auto take = [&](long long bytes) {
+    const long long at = b.total;
+    b.total += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  b.codes = take(quantize ? d.M * mx_code_bytes(d.K) : 0);
+  b.scales = take(quantize ? d.M * mx_scale_bytes(d.K) : 0);
+  b.part = take(d.M > 0 ? mx_plan(d.M, d.N, d.K, d.type).part_bytes : 0);
+  b.total = std::max(b.total, 256LL);
+  return b;
+}
+
+}  // namespace
+
+// Few columns of long rows leave most CUs idle: splits of 32 steps (a turn of a workgroup's waves) or more.
+MxPlan mx_plan(int M, int N, int K, int type) {
+  MxPlan plan = {kNoTile, 1, pieces(mx_blocks(K), 4), 0};
+  const long long groups = (long long)pieces(N, 16) * pieces(M, M <= 16 ? 16 : M <= 32 ? 32 : 64);
+  if (groups <= 64 && plan.steps >= 128) {
+    const int splits = (int)std::min(128 / groups, plan.steps / 32LL);
+    plan.steps = pieces(plan.steps, splits);
+    plan.splits = pieces(pieces(mx_blocks(K), 4), plan.steps);
+  }
+  if (plan.splits > 1) plan.part_bytes = 4LL * plan.splits * M * ((N + 3) / 4 * 4);
+  return plan;
+}
+
+}  // namespace cct
+
+using namespace cct;
+
+extern "C" {
+
+int cct_mx_quantize(int32_t rows, int32_t cols, int32_t type, const void* x, int64_t ldx, void* codes, int64_t ld_codes,
+                    void* scales, int64_t ld_scales, void* hip_stream) {
+  const int rc = sizes_ok(rows, cols, type);
+  if (rc != CCT_OK || rows == 0) return rc;
+  if (!matrix_ok(x, ldx, rows, cols, type) || !mx_ok(codes, ld_codes, scales, ld_scales, rows, cols)) return CCT_EINVAL;
+  return launch_mx_quantize(rows, cols, type, x, ldx, (unsigned char*)codes, ld_codes, (unsigned char*)scales, ld_scales,
+                            (hipStream_t)hip_stream);
+}
+
+int cct_mx_dequantize(int32_t rows, int32_t cols, int32_t type, const void* codes, int64_t ld_codes, const void* scales,
+                      int64_t ld_scales, void* x, int64_t ldx, void* hip_stream) {
+  const int rc = sizes_ok(rows, cols, type);
+  if (rc != CCT_OK || rows == 0) return rc;
+  if (!matrix_ok(x, ldx, rows, cols, type) || !mx_ok(codes, ld_codes, scales, ld_scales, rows, cols)) return CCT_EINVAL;
+  return launch_mx_dequantize(rows, cols, type, {(const unsigned char*)codes, ld_codes, (const unsigned char*)scales, ld_scales}, x,
+                              ldx, (hipStream_t)hip_stream);
+}
+
+int cct_mx_linear_workspace_bytes(const cct_linear_desc_t* desc, int32_t quantize, size_t* bytes) {
+  if (!desc || !bytes) return CCT_EINVAL;
+  const int rc = product_ok(*desc);
+  if (rc != CCT_OK) return rc;
+  *bytes = (size_t)layout_of(*desc, quantize != 0).total;
+  return CCT_OK;
+}
+
+int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* x_scales, int64_t ldxs,
+                          const void* w, int64_t ldw, const void* w_scales, int64_t ldws, const void* bias,
+                          const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz, void* workspace,
+                          size_t workspace_bytes, void* hip_stream) {
+  if (!desc) return CCT_EINVAL;
+  const cct_linear_desc_t& d = *desc;
+  int rc = product_ok(d);
+  if (rc != CCT_OK) return rc;
+  if (d.M == 0) return CCT_OK;
+  const bool quantize = !x_scales;
+  if (quantize ? !matrix_ok(x, ldx, d.M, d.K, d.type) : !mx_ok(x, ldx, x_scales, ldxs, d.M, d.K)) return CCT_EINVAL;
+  if (!mx_ok(w, ldw, w_scales, ldws, d.N, d.K) || !matrix_ok(y, ldy, d.M, d.N, d.type) || ((uintptr_t)bias & (type_bytes(d.type) - 1)) ||
+      (residual && !matrix_ok(residual, ldr, d.M, d.N, d.type)) || (z && !matrix_ok(z, ldz, d.M, d.N, d.type)))
+    return CCT_EINVAL;
+  const MxLayout b = layout_of(d, quantize);
+  if (!workspace || ((uintptr_t)workspace & 255)) return CCT_EINVAL;
+  if (workspace_bytes < (size_t)b.total) return CCT_EWORKSPACE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  unsigned char* ws = (unsigned char*)workspace;
+  MxProduct a = {};
+  a.blocks = mx_blocks(d.K);
+  a.w = {(const unsigned char*)w, ldw, (const unsigned char*)w_scales, ldws};
+  a.x = {(const unsigned char*)x, ldx, (const unsigned char*)x_scales, ldxs};
+  if (quantize) {
+    a.x = {ws + b.codes, mx_code_bytes(d.K), ws + b.scales, mx_scale_bytes(d.K)};
+    rc = launch_mx_quantize(d.M, d.K, d.type, x, ldx, ws + b.codes, a.x.ldc, ws + b.scales, a.x.lds, st);
+    if (rc != CCT_OK) return rc;
+  }
+  FfProduct& p = a.p;
+  p.M = d.M;
+  p.N = d.N;
+  p.K = d.K;
+  p.type = d.type;
+  p.activation = d.activation;
+  p.segments = 1;
+  p.epilogue = kFfLinear;
+  p.bias = bias;
+  p.residual = residual;
+  p.ldr = ldr;
+  p.out = y;
+  p.ldo = ldy;
+  p.z = z;
+  p.ldz = ldz;
+  const MxPlan plan = mx_plan(d.M, d.N, d.K, d.type);
+  return launch_mx_rows(a, plan, (float*)(ws + b.part), st);
+}
+
+}  // extern "C"
