@@ -223,6 +223,83 @@ struct TileEpilogue {
   static constexpr int BYTES = WM * WN * EROWS * PITCH * 4;
 };
 
+// A workgroup's sums on their way out: block j, i of a wave has columns row_b(j) and rows i * 16 of it; `apart`: they are one split's.
+template <int TYPE, int BM, int BN, int WM, int WN, int EPI>
+__device__ __forceinline__ void finish_tile(const FfProduct& p, const FfPart& part, bool apart, int split, int m0, int n0,
+                                            const f32x4 (&acc)[BN / WN / 16][BM / WM / 16]) {
+  constexpr int RB = BM / WM / 16, CB = BN / WN / 16, PARTS = EPI == kFfGated ? 2 : 1;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char tile_smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  constexpr int OUT = CB / PARTS;  // blocks of columns of the result
+  if (apart) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      const int m = m0 + wm * (BM / WM) + i * 16 + (lane & 15);
+#pragma unroll
+      for (int j = 0; j < OUT; ++j) {
+        const int n = n0 + wn * (BN / PARTS / WN) + j * 16 + (lane >> 4) * 4;
+        if (m >= p.M || n >= p.N) continue;
+        float* to = part.p + ((long long)split * PARTS * p.M + m) * part.ld + n;
+        *(f32x4*)to = acc[j][i];
+        if constexpr (PARTS == 2) *(f32x4*)(to + (long long)p.M * part.ld) = acc[j + OUT][i];
+      }
+    }
+    return;
+  }
+  // Through LDS, EROWS rows of a wave at a time: a lane then has 8 neighbouring columns, stores are whole rows of the wave's
+  // columns, and the code stands once and not for every block.  The residual's rows are asked for in front of that, all at
+  // once: one by one they were a trip to memory each (4096 x 4096 x 4096 with a residual 119 us, 104 without).
+  typedef TileEpilogue<BM, BN, WM, WN> Ep;
+  typedef typename Number<TYPE>::V8 V8;
+  constexpr int COLS = OUT * 16, PER = COLS / 8, STEPS = Ep::EROWS * PER / 64, DOWN = 64 / PER;  // lanes of a row; rows of a step
+  static_assert(STEPS * 64 == Ep::EROWS * PER, "whole steps");
+  __syncthreads();
+  float* mine = (float*)tile_smem + wave * (Ep::EROWS * Ep::PITCH);
+  const int row = lane / PER, c = lane % PER * 8, n = n0 + wn * COLS + c;
+  const bool ahead = EPI == kFfLinear && p.residual && n + 8 <= p.N;
+#pragma unroll
+  for (int half = 0; half < BM / WM / Ep::EROWS; ++half) {
+    constexpr int IB = Ep::EROWS / 16;
+    const int m1 = m0 + wm * (BM / WM) + half * Ep::EROWS + row;
+    V8 res[STEPS] = {};
+    if (ahead)
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s)
+        if (m1 + s * DOWN < p.M)
+          res[s] = *(const typename Number<TYPE>::U8*)((const typename Number<TYPE>::T*)p.residual + (m1 + s * DOWN) * p.ldr + n);
+#pragma unroll
+    for (int i = 0; i < IB; ++i)
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+        *(f32x4*)(mine + (i * 16 + (lane & 15)) * Ep::PITCH + j * 16 + (lane >> 4) * 4) = acc[j][half * IB + i];
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int s = 0; s < STEPS; ++s) {
+      const int m = m1 + s * DOWN;
+      if (m >= p.M || n >= p.N) continue;
+      float v[8], u[8], r[8];
+      V8 rs = res[0];  // a step's, chosen by comparing: an index would put them into memory
+#pragma unroll
+      for (int q = 1; q < STEPS; ++q) rs = s == q ? res[q] : rs;
+      const float* from = mine + (row + s * DOWN) * Ep::PITCH + c;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = from[e];
+        u[e] = PARTS == 2 ? from[COLS + e] : 0.f;
+        r[e] = (float)rs[e];
+      }
+      if (ahead)
+        finish<TYPE, EPI>(p, m, n, v, u, &r);
+      else
+        finish<TYPE, EPI>(p, m, n, v, u);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // BM x BN results (kFfGated: BM x BN / 2 of each product) with WM x WN waves; RING stages in LDS; SPLIT: the sums go to `part`,
 // always or if it says so.
 enum { kWhole, kSplit, kEither };
@@ -341,73 +418,7 @@ __device__ __forceinline__ void compute_tile(const FfProduct& p, int tiles_m, in
 #undef CCT_MEET
   __builtin_amdgcn_s_waitcnt(0x0f70);  // the empty loads write LDS too
 
-  constexpr int OUT = CB / PARTS;  // blocks of columns of the result
-  if (SPLIT == kSplit || (SPLIT == kEither && part.splits > 1)) {
-#pragma unroll
-    for (int i = 0; i < RB; ++i) {
-      const int m = m0 + wm * (BM / WM) + i * 16 + (lane & 15);
-#pragma unroll
-      for (int j = 0; j < OUT; ++j) {
-        const int n = n0 + row_b(j) + (lane >> 4) * 4;
-        if (m >= p.M || n >= p.N) continue;
-        float* to = part.p + ((long long)split * PARTS * p.M + m) * part.ld + n;
-        *(f32x4*)to = acc[j][i];
-        if constexpr (PARTS == 2) *(f32x4*)(to + (long long)p.M * part.ld) = acc[j + OUT][i];
-      }
-    }
-    return;
-  }
-  // Through LDS, EROWS rows of a wave at a time: a lane then has 8 neighbouring columns, stores are whole rows of the wave's
-  // columns, and the code stands once and not for every block.  The residual's rows are asked for in front of that, all at
-  // once: one by one they were a trip to memory each (4096 x 4096 x 4096 with a residual 119 us, 104 without).
-  typedef TileEpilogue<BM, BN, WM, WN> Ep;
-  typedef typename Number<TYPE>::V8 V8;
-  constexpr int COLS = OUT * 16, PER = COLS / 8, STEPS = Ep::EROWS * PER / 64, DOWN = 64 / PER;  // lanes of a row; rows of a step
-  static_assert(STEPS * 64 == Ep::EROWS * PER, "whole steps");
-  __syncthreads();
-  float* mine = (float*)tile_smem + wave * (Ep::EROWS * Ep::PITCH);
-  const int row = lane / PER, c = lane % PER * 8, n = n0 + wn * COLS + c;
-  const bool ahead = EPI == kFfLinear && p.residual && n + 8 <= p.N;
-#pragma unroll
-  for (int half = 0; half < BM / WM / Ep::EROWS; ++half) {
-    constexpr int IB = Ep::EROWS / 16;
-    const int m1 = m0 + wm * (BM / WM) + half * Ep::EROWS + row;
-    V8 res[STEPS] = {};
-    if (ahead)
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s)
-        if (m1 + s * DOWN < p.M)
-          res[s] = *(const typename Number<TYPE>::U8*)((const typename Number<TYPE>::T*)p.residual + (m1 + s * DOWN) * p.ldr + n);
-#pragma unroll
-    for (int i = 0; i < IB; ++i)
-#pragma unroll
-      for (int j = 0; j < CB; ++j)
-        *(f32x4*)(mine + (i * 16 + (lane & 15)) * Ep::PITCH + j * 16 + (lane >> 4) * 4) = acc[j][half * IB + i];
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int s = 0; s < STEPS; ++s) {
-      const int m = m1 + s * DOWN;
-      if (m >= p.M || n >= p.N) continue;
-      float v[8], u[8], r[8];
-      V8 rs = res[0];  // a step's, chosen by comparing: an index would put them into memory
-#pragma unroll
-      for (int q = 1; q < STEPS; ++q) rs = s == q ? res[q] : rs;
-      const float* from = mine + (row + s * DOWN) * Ep::PITCH + c;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = from[e];
-        u[e] = PARTS == 2 ? from[COLS + e] : 0.f;
-        r[e] = (float)rs[e];
-      }
-      if (ahead)
-        finish<TYPE, EPI>(p, m, n, v, u, &r);
-      else
-        finish<TYPE, EPI>(p, m, n, v, u);
-    }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-  }
+  finish_tile<TYPE, BM, BN, WM, WN, EPI>(p, part, SPLIT == kSplit || (SPLIT == kEither && part.splits > 1), split, m0, n0, acc);
 }
 
 template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool AX, bool BX, int EPI, int SPLIT>

@@ -23,14 +23,16 @@ int launch_mx_dequantize(int rows, int cols, int type, const MxMatrix& m, void* 
 struct MxProduct {
   FfProduct p;
   MxMatrix x, w;
-  int blocks;  // of a row
+  int blocks;     // of a row
+  bool quantize;  // x are values yet, in rows of x.ldc (up to kMxQuantizeRows rows on mx_rows.hip)
 };
+constexpr int kMxQuantizeRows = 4;
 // How it runs: kNoTile: mx_rows.hip; splits of the contraction, of so many steps of 128 values (rows) or stages of 256 (tiles).
 struct MxPlan {
   int tile, splits, steps;
   long long part_bytes;
 };
-MxPlan mx_plan(int M, int N, int K, int type);
+MxPlan mx_plan(int M, int N, int K);
 int launch_mx_rows(const MxProduct& p, const MxPlan& plan, float* part, hipStream_t st);
 int launch_mx_tile(const MxProduct& p, const MxPlan& plan, float* part, hipStream_t st);
 

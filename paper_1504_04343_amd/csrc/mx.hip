@@ -40,24 +40,66 @@ MxLayout layout_of(const cct_linear_desc_t& d, bool quantize) {
   };
   b.codes = take(quantize ? d.M * mx_code_bytes(d.K) : 0);
   b.scales = take(quantize ? d.M * mx_scale_bytes(d.K) : 0);
-  b.part = take(d.M > 0 ? mx_plan(d.M, d.N, d.K, d.type).part_bytes : 0);
+  b.part = take(d.M > 0 ? mx_plan(d.M, d.N, d.K).part_bytes : 0);
   b.total = std::max(b.total, 256LL);
   return b;
 }
 
 }  // namespace
 
+namespace {
+
+constexpr int kCus = 256;
+// A tile: its workgroups on a CU, and us a stage takes where the CUs are full of them, and one alone.
+struct MxTileCost {
+  int tile, bm, bn, threads, per_cu;
+  double full, alone;
+};
+constexpr MxTileCost kMxTiles[] = {{kTile256, 256, 256, 512, 1, 2.2, 1.9}, {kTile128, 128, 128, 256, 2, 1.35, 0.95}, {kTile64x128, 64, 128, 256, 3, 1.3, 0.58}};
+constexpr double kLaunchMicros = 3.0, kJoinMicros = 3.0, kJoinBytesPerMicro = 3.0e6, kAround = 2.0;
+
 // Few columns of long rows leave most CUs idle: splits of 32 steps (a turn of a workgroup's waves) or more.
-MxPlan mx_plan(int M, int N, int K, int type) {
-  MxPlan plan = {kNoTile, 1, pieces(mx_blocks(K), 4), 0};
+MxPlan rows_plan(int M, int N, int K) {
+  const int steps = pieces(mx_blocks(K), 4);
+  MxPlan plan = {kNoTile, 1, steps, 0};
   const long long groups = (long long)pieces(N, 16) * pieces(M, M <= 16 ? 16 : M <= 32 ? 32 : 64);
-  if (groups <= 64 && plan.steps >= 128) {
-    const int splits = (int)std::min(128 / groups, plan.steps / 32LL);
-    plan.steps = pieces(plan.steps, splits);
-    plan.splits = pieces(pieces(mx_blocks(K), 4), plan.steps);
+  if (groups <= 64 && steps >= 128) {
+    const int splits = (int)std::min(128 / groups, steps / 32LL);
+    plan.steps = pieces(steps, splits);
+    plan.splits = pieces(steps, plan.steps);
   }
-  if (plan.splits > 1) plan.part_bytes = 4LL * plan.splits * M * ((N + 3) / 4 * 4);
   return plan;
+}
+// us of it: the weight from memory, or both operands of every workgroup of 16 columns from L2 (48 x 16384 x 4096: 27, in tiles of
+// 64 x 128 14), or what a turn takes at least.
+double rows_micros(int M, int N, int K, const MxPlan& plan) {
+  const double row = K * 17.0 / 32, wide = pieces(N, 16), high = pieces(M, 64);
+  const double bytes = wide * (16 * high + M) * row;
+  return 4.5 + std::max(std::max((double)N * row / 5.0e6, bytes / 7.5e6), (0.8 + 0.6 * (M <= 16 ? 1 : M <= 32 ? 2 : 4)) * pieces(plan.steps, 32)) + (plan.splits > 1 ? kJoinMicros : 0.0);
+}
+
+}  // namespace
+
+MxPlan mx_plan(int M, int N, int K) {
+  MxPlan best = rows_plan(M, N, K);
+  double least = rows_micros(M, N, K, best);
+  const int stages = pieces(mx_blocks(K), 8);
+  for (const MxTileCost& c : kMxTiles) {
+    const long long tiles = (long long)pieces(M, c.bm) * pieces(N, c.bn);
+    for (int splits = 1; splits <= (c.tile == kTile256 ? 1 : 16) && splits <= std::max(1, stages / 4); ++splits) {
+      const int each = pieces(stages, splits), have = pieces(stages, each);
+      const long long groups = tiles * have, slots = (long long)kCus * c.per_cu, rest = groups % slots;
+      if (groups * c.threads > kMostThreads) continue;
+      double us = ((double)(groups / slots) * c.full + (rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full)) * (each + kAround) + kLaunchMicros;
+      if (have > 1) us += kJoinMicros + 8.0 * have * M * N / kJoinBytesPerMicro;
+      if (us < least) {
+        least = us;
+        best = {c.tile, have, each, 0};
+      }
+    }
+  }
+  if (best.splits > 1) best.part_bytes = 4LL * best.splits * M * ((N + 3) / 4 * 4);
+  return best;
 }
 
 }  // namespace cct
@@ -111,15 +153,20 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
   if (workspace_bytes < (size_t)b.total) return CCT_EWORKSPACE;
   hipStream_t st = (hipStream_t)hip_stream;
   unsigned char* ws = (unsigned char*)workspace;
+  MxPlan plan = mx_plan(d.M, d.N, d.K);
   MxProduct a = {};
   a.blocks = mx_blocks(d.K);
   a.w = {(const unsigned char*)w, ldw, (const unsigned char*)w_scales, ldws};
   a.x = {(const unsigned char*)x, ldx, (const unsigned char*)x_scales, ldxs};
-  if (quantize) {
+  a.quantize = quantize && plan.tile == kNoTile && d.M <= kMxQuantizeRows;
+  if (quantize && !a.quantize) {
     a.x = {ws + b.codes, mx_code_bytes(d.K), ws + b.scales, mx_scale_bytes(d.K)};
     rc = launch_mx_quantize(d.M, d.K, d.type, x, ldx, ws + b.codes, a.x.ldc, ws + b.scales, a.x.lds, st);
     if (rc != CCT_OK) return rc;
   }
+  // a tile's offsets have 32 bits, of 256 rows
+  constexpr long long kMost = 1 << 23;
+  if (plan.tile != kNoTile && std::max(std::max(a.x.ldc, a.w.ldc), std::max(a.x.lds, a.w.lds)) >= kMost) plan = {kNoTile, 1, 0, 0};
   FfProduct& p = a.p;
   p.M = d.M;
   p.N = d.N;
@@ -135,8 +182,7 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
   p.ldo = ldy;
   p.z = z;
   p.ldz = ldz;
-  const MxPlan plan = mx_plan(d.M, d.N, d.K, d.type);
-  return launch_mx_rows(a, plan, (float*)(ws + b.part), st);
+  return plan.tile == kNoTile ? launch_mx_rows(a, plan, (float*)(ws + b.part), st) : launch_mx_tile(a, plan, (float*)(ws + b.part), st);
 }
 
 }  // extern "C"

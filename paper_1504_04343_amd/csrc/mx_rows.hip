@@ -19,7 +19,8 @@ namespace {
 
 constexpr int NW = 8, kBatch = 4;
 
-template <int TYPE, int RM, bool SPLIT>
+// QUANTIZE: x are values (x.codes, x.ldc of them), which every workgroup rounds for itself.
+template <int TYPE, int RM, bool SPLIT, bool QUANTIZE>
 __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart part) {
   const FfProduct& p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lo = lane & 15, q = lane >> 4;
@@ -36,7 +37,7 @@ __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart pa
 #pragma unroll
       for (int i = 0; i < RM; ++i) {
         const long long r = min((long long)m0 + i * 16 + lo, p.M - 1LL);
-        xc[i] = a.x.codes + r * a.x.ldc;
+        xc[i] = a.x.codes + (QUANTIZE ? 0 : r * a.x.ldc);
         xs[i] = a.x.scales + r * a.x.lds;
       }
       f32x4 acc[RM];
@@ -44,45 +45,51 @@ __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart pa
       for (int i = 0; i < RM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       struct Turn {
         i32x4 w[kBatch], ws, x[RM][kBatch], xs[RM];
+        typename Number<TYPE>::V8 v[QUANTIZE ? kBatch : 1][4];
       };
       auto load = [&](Turn& t, int s0) {
         t.ws = mx_scales4(ws, s0, a.blocks);
+        if constexpr (!QUANTIZE)
 #pragma unroll
-        for (int i = 0; i < RM; ++i) t.xs[i] = mx_scales4(xs[i], s0, a.blocks);
+          for (int i = 0; i < RM; ++i) t.xs[i] = mx_scales4(xs[i], s0, a.blocks);
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-          const long long at = 16LL * min((s0 + j) * 4 + q, a.blocks - 1);
-          t.w[j] = *(const i32x4*)(wc + at);
+          const int block = min((s0 + j) * 4 + q, a.blocks - 1);
+          t.w[j] = *(const i32x4*)(wc + 16LL * block);
+          if constexpr (QUANTIZE) {
 #pragma unroll
-          for (int i = 0; i < RM; ++i) t.x[i][j] = *(const i32x4*)(xc[i] + at);
+            for (int c = 0; c < 4; ++c) {
+              const int col = block * kMxBlock + c * 8;
+              t.v[j][c] = load_row_raw<TYPE>(a.x.codes, min((long long)m0 + lo, p.M - 1LL) * a.x.ldc, col, p.K - col);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < RM; ++i) t.x[i][j] = *(const i32x4*)(xc[i] + 16LL * block);
+          }
         }
       };
       auto multiply = [&](const Turn& t, int s0) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
+          i32x4 own = {};
+          int own_scale = 127;
+          if constexpr (QUANTIZE) own = mx_quantize_block<TYPE>(t.v[j], &own_scale);
           const bool live = s0 + j < end && (s0 + j) * 4 + q < a.blocks;
           const i32x4 w = live ? t.w[j] : i32x4{0, 0, 0, 0};
           const int sw = live ? (int)((unsigned)t.ws[j] >> (8 * q)) : 127;
 #pragma unroll
-          for (int i = 0; i < RM; ++i)
-            acc[i] = mx_mfma<0, 0>(w, live ? t.x[i][j] : i32x4{0, 0, 0, 0}, acc[i], sw, live ? (int)((unsigned)t.xs[i][j] >> (8 * q)) : 127);
+          for (int i = 0; i < RM; ++i) {
+            const i32x4 x = QUANTIZE ? own : t.x[i][j];
+            const int sx = QUANTIZE ? own_scale : (int)((unsigned)t.xs[i][j] >> (8 * q));
+            acc[i] = mx_mfma<0, 0>(w, live ? x : i32x4{0, 0, 0, 0}, acc[i], sw, live ? sx : 127);
+          }
         }
       };
-      constexpr bool AHEAD = RM < 4;  // else the registers have no room
-      Turn now;
-      int s = first + wave * kBatch;
-      if (AHEAD && s < end) load(now, s);
-      for (; s < end; s += NW * kBatch) {
-        if constexpr (AHEAD) {
-          Turn then = now;
-          if (s + NW * kBatch < end) load(then, s + NW * kBatch);
-          __builtin_amdgcn_sched_barrier(0);
-          multiply(now, s);
-          now = then;
-        } else {
-          load(now, s);
-          multiply(now, s);
-        }
+      for (int s = first + wave * kBatch; s < end; s += NW * kBatch) {
+        Turn t;
+        load(t, s);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(t, s);
       }
       __syncthreads();
 #pragma unroll
@@ -107,20 +114,23 @@ __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart pa
 template <int TYPE>
 void launch(const MxProduct& a, const MxPlan& plan, float* ws, hipStream_t st) {
   const FfPart part = {ws, (a.p.N + 3) / 4 * 4, plan.splits, plan.steps};
-  auto run = [&](auto rm) {
+  auto run = [&](auto rm, auto quantize) {
     constexpr int RM = decltype(rm)::value;
+    constexpr bool QUANTIZE = decltype(quantize)::value;
     const dim3 grid(std::min(pieces(a.p.N, 16), 1 << 16), std::min(pieces(a.p.M, RM * 16), 64), plan.splits);
     if (plan.splits > 1)
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_rows_kernel<TYPE, RM, true>), grid, dim3(NW * 64), 0, st, a, part);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_rows_kernel<TYPE, RM, true, QUANTIZE>), grid, dim3(NW * 64), 0, st, a, part);
     else
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_rows_kernel<TYPE, RM, false>), grid, dim3(NW * 64), 0, st, a, part);
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(mx_rows_kernel<TYPE, RM, false, QUANTIZE>), grid, dim3(NW * 64), 0, st, a, part);
   };
-  if (a.p.M <= 16)
-    run(std::integral_constant<int, 1>());
+  if (a.p.M <= 16 && a.quantize)
+    run(std::integral_constant<int, 1>(), std::true_type());
+  else if (a.p.M <= 16)
+    run(std::integral_constant<int, 1>(), std::false_type());
   else if (a.p.M <= 32)
-    run(std::integral_constant<int, 2>());
+    run(std::integral_constant<int, 2>(), std::false_type());
   else
-    run(std::integral_constant<int, 4>());
+    run(std::integral_constant<int, 4>(), std::false_type());
   if (plan.splits > 1) launch_join<TYPE, kFfLinear>(a.p, part, st);
 }
 

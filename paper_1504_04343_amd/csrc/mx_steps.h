@@ -2,6 +2,7 @@
 // block l / 16 of row l % 16 (16 bytes) and its scale in byte BY of a register.
 #pragma once
 #include "gemm_common.h"
+#include "number_types.h"
 
 namespace cct {
 namespace {
@@ -26,6 +27,50 @@ __device__ __forceinline__ i32x4 mx_scales4(const unsigned char* row, int s0, in
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = *(const int*)(row + 4LL * min(s0 + j, words - 1));
   return v;
+}
+
+// A block of a row of values (four chunks of 8, zeros behind the row's end) as mx_quantize_kernel rounds it: its codes, its scale.
+template <int TYPE>
+__device__ __forceinline__ i32x4 mx_quantize_block(const typename Number<TYPE>::V8 (&v)[4], int* scale) {
+  unsigned most = 0;
+  if constexpr (TYPE == CCT_TYPE_F32) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = max(most, __builtin_bit_cast(unsigned, (float)v[q][e]) & 0x7fffffffu);
+  } else {  // sizes of 16-bit values compare as whole numbers too, two at a time
+    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+    u16x8 m = __builtin_bit_cast(u16x8, v[0]) & (unsigned short)0x7fff;
+#pragma unroll
+    for (int q = 1; q < 4; ++q) m = __builtin_elementwise_max(m, (u16x8)(__builtin_bit_cast(u16x8, v[q]) & (unsigned short)0x7fff));
+    unsigned short t = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = max(t, m[e]);
+    most = TYPE == CCT_TYPE_BF16 ? (unsigned)t << 16 : __builtin_bit_cast(unsigned, (float)__builtin_bit_cast(_Float16, t));
+  }
+  const unsigned field = most >> 23;
+  *scale = field == 255 ? 255 : max((int)field - 2, 0);
+  const float s = __builtin_bit_cast(float, (unsigned)*scale << 23);
+  i32x4 codes;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    unsigned c = 0;
+    auto two = [&](auto byte) {
+      constexpr int B = decltype(byte)::value;
+      if constexpr (TYPE == CCT_TYPE_F32)
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[q][2 * B], v[q][2 * B + 1], s, B);
+      else if constexpr (TYPE == CCT_TYPE_BF16)
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_shufflevector(v[q], v[q], 2 * B, 2 * B + 1), s, B);
+      else
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_shufflevector(v[q], v[q], 2 * B, 2 * B + 1), s, B);
+    };
+    two(std::integral_constant<int, 0>());
+    two(std::integral_constant<int, 1>());
+    two(std::integral_constant<int, 2>());
+    two(std::integral_constant<int, 3>());
+    codes[q] = field == 255 ? 0 : (int)c;
+  }
+  return codes;
 }
 
 }  // namespace

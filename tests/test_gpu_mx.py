@@ -169,6 +169,37 @@ def test_whole_numbers(B, M):
     assert torch.equal(y.cpu().double(), xv @ wv.t())
 
 
+PLANS = [(3, 160, 1000, "mx_rows_kernel"), (16, 24, 40000, "mx_rows_kernel"), (300, 200, 1100, "mx_tile_kernel<64x128, 1 splits>"),
+         (40, 16384, 4000, "mx_tile_kernel<64x128, 1 splits>"), (300, 200, 10880, "mx_tile_kernel<64x128, 9 splits>"),
+         (1500, 1500, 4100, "mx_tile_kernel<128x128, 1 splits>"), (1030, 1000, 20000, "mx_tile_kernel<128x128, 3 splits>"),
+         (4096, 4090, 1500, "mx_tile_kernel<256x256, 1 splits>"), (7000, 8000, 200, "mx_tile_kernel<256x256, 1 splits>")]
+
+
+@pytest.mark.parametrize("M,N,K,kernel", PLANS)
+def test_every_plan(B, M, N, K, kernel):
+    """Which kernel ran, and whole numbers, whose sums are exact: terms of up to 144 * 4, at most 40000 of them."""
+    g = torch.Generator().manual_seed(M)
+    (xc, xs, _), (wc, ws, _) = operand(g, M, K, 1, 3), operand(g, N, K, 1, 2)   # multiples of 1: halves times two or more
+    x, w = given(B, xc, xs, K, 1), given(B, wc, ws, K)
+    residual = torch.randint(-9, 9, (M, N), generator=g).float()
+    B.cct_profile_enable(True)
+    try:
+        y, _ = run(B, "f32", "none", x, w, None, residual, False, M, N, K)
+        names = [e["name"] for e in B.cct_profile_read() if e["name"].startswith("mx")]
+    finally:
+        B.cct_profile_enable(False)
+    assert len(names) == 1 and names[0].startswith(kernel), names
+    values = [torch.empty(r, K, device="cuda") for r in (M, N)]
+    for m, v in zip((x, w), values):
+        B.cct_mx_dequantize(m, v)
+    assert torch.equal(y.double(), values[0].double() @ values[1].double().t() + residual.double().cuda())
+    # rows too far apart for a tile's offsets
+    if M <= 300 and N <= 200:
+        far = torch.empty((N - 1) * (1 << 23) + w.codes.shape[1], dtype=torch.uint8, device="cuda").as_strided(w.codes.shape, (1 << 23, 1))
+        far.copy_(w.codes)
+        assert torch.equal(y, run(B, "f32", "none", x, B.MxMatrix(N, K, far, w.scales), None, residual, False, M, N, K)[0])
+
+
 @pytest.mark.parametrize("M", [1, 40, 200, 600])
 def test_scales_from_end_to_end(B, M):
     """Products far up and far down: results in fp32's range are right to the sum's bound, or what its smallest numbers lose."""
