@@ -473,8 +473,8 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
  * product (fp16: an infinity beyond 65504).  residual (tokens x D), chosen_out (tokens x chosen int32, largest logit first) and weights_out (fp32) may be NULL;
  * these two are contiguous.  y may be the residual itself.
  * 0 <= tokens, 1 <= chosen <= experts, D, F >= 1 (CCT_EINVAL); CCT_EUNSUPPORTED: more than 64 tokens, 512 experts, 16
- * chosen ones or 2^24 features, matrices as above.  Results are bit-reproducible; which experts the other
- * tokens choose decides in which order a token's sums run.
+ * chosen ones or 2^24 features, matrices as above.  Results are bit-reproducible, and a token's do not
+ * depend on the other tokens' values.
  */
 typedef struct {
   int32_t tokens, experts, chosen, D, F;

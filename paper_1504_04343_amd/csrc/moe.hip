@@ -1,25 +1,27 @@
 // A layer of experts for a few tokens (cct_moe_forward), which is bound by reading the weights of the experts that some token
-// chooses, each once.  Four launches:
+// chooses, each once.  Launches:
 //   moe_logits_kernel  a workgroup an expert and up to 8 tokens: the router's sums in 64 bits, so that which expert is chosen does
 //                      not hang on their order (products of 16-bit values are exact);
-//   moe_route_kernel   one workgroup: a wave a token, its chosen experts by rounds of a largest key, their weights; the list of
-//                      experts that are used, and for each the rows of h of its tokens;
-//   moe_gated_kernel   16 columns of both gate and up of one used expert and all its tokens: weight * act(g) * u, kept as two 16-bit
-//                      terms (16 bits of a value in bf16, 22 in fp16; fp32 as it is), which the next product multiplies both;
-//   moe_down_kernel    16 columns of y and all tokens, the contraction over all used experts' features.
+//   moe_route_kernel   one workgroup: a wave a token, its chosen experts by rounds of a largest key, their weights; then the experts
+//                      that are used, and for each the rows of h of its tokens (a single token: every wave of the next kernel
+//                      chooses for itself, which takes less than a launch);
+//   moe_gated_kernel   16 columns of both gate and up of one used expert and its tokens: weight * act(g) * u, kept as two 16-bit
+//                      terms (16 bits of a value in bf16, 22 in fp16; fp32 as it is), both of which the next product multiplies;
+//   moe_down_kernel    16 columns of one used expert's results and its tokens, or of all experts' for a single token;
+//   moe_join_kernel    (more than one token) a token's results added in the order of its choice, and the residual.
 // The two products are those of few rows (ff_rows.hip): weights go from memory into the registers of the matrix cores, waves take
-// steps in turn, their sums meet in LDS in a fixed order.  A token that an expert is not for keeps its sum: zeros in its place
-// would turn an infinite weight into NaN.
+// steps in turn, their sums meet in LDS in a fixed order.  A token's results do not depend on the other tokens.
 #include <algorithm>
 
 #include "activation.h"
 #include "ff_step.h"
 #include "ff_tile.h"
+#include "wave_ops.h"
 
 namespace cct {
 namespace {
 
-constexpr int kMostTokens = 64, kMostExperts = 512, kMostChosen = 16;
+constexpr int kMostTokens = 64, kMostExperts = 512, kMostChosen = 16, kMostPairs = kMostTokens * kMostChosen;
 
 struct MoeMatrix {
   const void* p;
@@ -32,10 +34,13 @@ struct Moe {
   MoeMatrix wg, wu, wd;
   // in the workspace
   float* logits;    // T x E
-  int* used;        // number of used experts, then their numbers
-  short* rows;      // for each used expert and token its row of h, or -1
-  float* weight;    // of each row of h
+  short* chosen;    // T x k
+  float* weight;    // of each of these
+  int* slot;        // for each used expert its number and its tokens'; -1 behind them
+  short* rows;      // kMostTokens for each: its tokens' rows (token * k + place among its chosen ones), the last again
   void *h, *h_low;  // T k rows of Fp values: the terms; fp32: h alone
+  float* part;      // T k rows of Dp results
+  int Dp;
   int32_t* chosen_out;
   float* weights_out;
 };
@@ -55,88 +60,99 @@ __global__ __launch_bounds__(256) void moe_logits_kernel(Moe a) {
         for (int i = 0; i < 8; ++i) sum[t] = fma((double)w[i], (double)x[i], sum[t]);
       }
   }
+  // eight sums over 64 lanes: halves of the lanes keep halves of the sums, then one is left in each lane
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int half = kLogitTokens / 2, off = 32; half > 0; half /= 2, off /= 2)
+#pragma unroll
+    for (int t = 0; t < half; ++t) {
+      const bool upper = lane & off;
+      const double give = upper ? sum[t] : sum[t + half], keep = upper ? sum[t + half] : sum[t];
+      sum[t] = keep + __shfl_xor(give, off, 64);
+    }
+#pragma unroll
+  for (int off = 32 / kLogitTokens; off > 0; off >>= 1) sum[0] += __shfl_xor(sum[0], off, 64);
   __shared__ double sums[4][kLogitTokens];
-#pragma unroll
-  for (int t = 0; t < kLogitTokens; ++t) {
-    if (t >= tokens) break;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum[t] += __shfl_xor(sum[t], off, 64);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6][t] = sum[t];
-  }
+  if (lane % (64 / kLogitTokens) == 0) sums[threadIdx.x >> 6][lane / (64 / kLogitTokens)] = sum[0];
   __syncthreads();
   const int t = threadIdx.x;
   if (t < tokens) a.logits[(long long)(t0 + t) * a.E + e] = (float)((sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t]));
 }
 
-// Keys that order logits as numbers, the largest first, equal ones by the lower expert, NaN behind all others.
-__device__ __forceinline__ unsigned long long logit_key(float v, int e) {
-  v = v == 0.f ? 0.f : v;  // -0 is 0
-  const unsigned b = __builtin_bit_cast(unsigned, v), up = v != v ? 0u : b >> 31 ? ~b : b | 0x80000000u;
-  return (unsigned long long)up << 32 | (0xffffffffu - (unsigned)e);
+// The chosen experts of a token, one wave: lane j < k has the j-th, largest logit first, equal ones by the lower expert, NaN last,
+// and its weight.
+constexpr int kOwn = kMostExperts / 64;
+__device__ __forceinline__ void select_experts(const Moe& a, int t, int lane, int* which, float* weight) {
+  // logits as whole numbers of the same order; 1: NaN, 0: not there or chosen already
+  unsigned key[kOwn];
+  float logit[kOwn];
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int e = i * 64 + lane;
+    logit[i] = e < a.E ? a.logits[(long long)t * a.E + e] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const float v = logit[i] == 0.f ? 0.f : logit[i];  // -0 is 0
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    key[i] = i * 64 + lane >= a.E ? 0u : v != v ? 1u : b >> 31 ? ~b : b | 0x80000000u;
+  }
+  float most = 0.f, mine = 0.f;
+  *which = 0;
+  for (int j = 0; j < a.k; ++j) {
+    unsigned best = key[0], first = 0xffffffffu;
+#pragma unroll
+    for (int i = 1; i < kOwn; ++i)
+      if (i * 64 < a.E) best = max(best, key[i]);
+    best = wave_max(best);
+#pragma unroll
+    for (int i = kOwn - 1; i >= 0; --i)
+      if (i * 64 < a.E) first = key[i] == best ? (unsigned)(i * 64 + lane) : first;
+    first = wave_min(first);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (i * 64 < a.E && (unsigned)(i * 64 + lane) == first) key[i] = 0;
+    const float value = best == 1u ? NAN : __builtin_bit_cast(float, best >> 31 ? best ^ 0x80000000u : ~best);
+    if (j == 0) most = value;
+    if (lane == j) {
+      mine = value;
+      *which = (int)first;
+    }
+  }
+  const float own = expf(mine - most);
+  float sum = 0.f;
+  if (a.normalize) {
+    sum = lane < a.k ? own : 0.f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) sum += i * 64 + lane < a.E ? expf(logit[i] - most) : 0.f;
+  }
+  *weight = own / wave_sum(sum);
 }
-constexpr int kRouteThreads = 1024, kOwn = kMostExperts / 64;
+__device__ __forceinline__ void write_selected(const Moe& a, int t, int lane, int which, float weight) {
+  if (lane >= a.k) return;
+  const int i = t * a.k + lane;
+  a.chosen[i] = (short)which;
+  a.weight[i] = weight;
+  if (a.chosen_out) a.chosen_out[i] = which;
+  if (a.weights_out) a.weights_out[i] = weight;
+}
+constexpr int kRouteThreads = 1024;
 __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(Moe a) {
-  __shared__ short chosen[kMostTokens][kMostChosen];
+  __shared__ short chosen[kMostPairs];
   __shared__ unsigned long long tokens_of[kMostExperts];
-  __shared__ int used[kMostExperts], count;
+  __shared__ int used[kMostExperts], total;
+  __shared__ short row_of[kRouteThreads / 64][kMostTokens];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int e = threadIdx.x; e < a.E; e += kRouteThreads) tokens_of[e] = 0;
   __syncthreads();
   for (int t = wave; t < a.T; t += kRouteThreads / 64) {
-    unsigned long long key[kOwn];  // 0: not there, or chosen
-    float logit[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int e = i * 64 + lane;
-      logit[i] = e < a.E ? a.logits[(long long)t * a.E + e] : -INFINITY;
-      key[i] = e < a.E ? logit_key(logit[i], e) : 0;
-    }
-    float most = 0.f, mine = 0.f;  // the largest logit; lane j: of the j-th chosen expert
-    int which = 0;
-    for (int j = 0; j < a.k; ++j) {
-      unsigned long long best = key[0];
-      float value = logit[0];
-#pragma unroll
-      for (int i = 1; i < kOwn; ++i)
-        if (key[i] > best) {
-          best = key[i];
-          value = logit[i];
-        }
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) {
-        const unsigned long long other = __shfl_xor(best, off, 64);
-        const float theirs = __shfl_xor(value, off, 64);
-        if (other > best) {
-          best = other;
-          value = theirs;
-        }
-      }
-      const int e = (int)(0xffffffffu - (unsigned)best);
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i)
-        if (key[i] == best) key[i] = 0;
-      if (j == 0) most = value;
-      if (lane == j) {
-        mine = value;
-        which = e;
-      }
-    }
-    const float own = expf(mine - most);
-    float sum = 0.f;
-    if (a.normalize) {
-      sum = lane < a.k ? own : 0.f;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i) sum += i * 64 + lane < a.E ? expf(logit[i] - most) : 0.f;
-    }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    int which;
+    float weight;
+    select_experts(a, t, lane, &which, &weight);
+    write_selected(a, t, lane, which, weight);
     if (lane < a.k) {
-      const float w = own / sum;
-      chosen[t][lane] = (short)which;
-      a.weight[t * a.k + lane] = w;
-      if (a.chosen_out) a.chosen_out[t * a.k + lane] = which;
-      if (a.weights_out) a.weights_out[t * a.k + lane] = w;
+      chosen[t * a.k + lane] = (short)which;
       atomicOr(&tokens_of[which], 1ull << t);
     }
   }
@@ -146,23 +162,28 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(Moe a) {
     for (int e0 = 0; e0 < a.E; e0 += 64) {
       const bool in = e0 + lane < a.E && tokens_of[min(e0 + lane, a.E - 1)] != 0;
       const unsigned long long who = __ballot(in);
-      if (in) {
-        const int at = n + __popcll(who & ((1ull << lane) - 1));
-        used[at] = e0 + lane;
-        a.used[1 + at] = e0 + lane;
-      }
+      if (in) used[n + __popcll(who & ((1ull << lane) - 1))] = e0 + lane;
       n += __popcll(who);
     }
-    if (lane == 0) a.used[0] = count = n;
+    if (lane == 0) total = n;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < count * a.T; i += kRouteThreads) {
-    const int s = i / a.T, t = i - s * a.T, e = used[s];
-    int row = -1;
-    if (tokens_of[e] >> t & 1)
-      for (int j = 0; j < a.k; ++j)
-        if (chosen[t][j] == e) row = t * a.k + j;
-    a.rows[i] = (short)row;
+  for (int s = wave; s < a.slots; s += kRouteThreads / 64) {
+    const int e = s < total ? used[s] : -1;
+    const unsigned long long tokens = e < 0 ? 0 : tokens_of[e];
+    const int n = __popcll(tokens);
+    if (lane == 0) {
+      a.slot[2 * s] = e;
+      a.slot[2 * s + 1] = n;
+    }
+    if (tokens >> lane & 1) {
+      int j = 0;
+      while (j < a.k - 1 && chosen[lane * a.k + j] != e) ++j;
+      row_of[wave][__popcll(tokens & ((1ull << lane) - 1))] = (short)(lane * a.k + j);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (n > 0) a.rows[s * kMostTokens + lane] = row_of[wave][min(lane, n - 1)];
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -186,180 +207,264 @@ __device__ __forceinline__ void store_terms(const Moe& a, long long at, const fl
   }
 }
 
-constexpr int kGatedWaves = 8;
-// RM: blocks of 16 tokens that an expert may have
-template <int TYPE, int RM>
-__global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
-  typedef Step<TYPE> S;
-  typedef typename S::V V;
-  constexpr int NW = kGatedWaves, BATCH = RM == 4 ? 4 : 8;
-  __shared__ short token[kMostTokens], place[kMostTokens];
-  __shared__ int tokens;
-  __shared__ f32x4 sums[NW][2 * RM][64];
-  const int slot = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int e = a.used[1 + slot];
-  if (slot >= a.used[0]) return;
-  if (wave == 0) {
-    const int row = lane < a.T ? a.rows[slot * a.T + lane] : -1;
-    const unsigned long long who = __ballot(row >= 0);
-    if (row >= 0) {
-      const int at = __popcll(who & ((1ull << lane) - 1));
-      token[at] = (short)lane;
-      place[at] = (short)row;
-    }
-    if (lane == 0) tokens = __popcll(who);
-  }
-  __syncthreads();
-  const int n = tokens, f0 = blockIdx.x * 16, lo = lane & 15, kq = (lane >> 4) * S::CH;
-  const long long f = min(f0 + lo, a.F - 1), g_at = e * a.wg.e + f * a.wg.ld, u_at = e * a.wu.e + f * a.wu.ld;
-  long long x_at[RM];
-#pragma unroll
-  for (int i = 0; i < RM; ++i) x_at[i] = token[min(i * 16 + lo, n - 1)] * a.ldx;
-  f32x4 acc[2][RM];
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int i = 0; i < RM; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int whole = a.D / S::K;
-  V w[BATCH][2], x[BATCH][RM];
-  for (int s0 = wave; s0 < whole; s0 += BATCH * NW) {
-    // steps past the last one load it again and multiply zeros
-#pragma unroll
-    for (int q = 0; q < BATCH; ++q) {
-      const long long k = (long long)min(s0 + q * NW, whole - 1) * S::K + kq;
-      w[q][0] = S::load(a.wg.p, g_at + k);
-      w[q][1] = S::load(a.wu.p, u_at + k);
-#pragma unroll
-      for (int i = 0; i < RM; ++i)
-        if (i == 0 || i * 16 < n) x[q][i] = S::load(a.x, x_at[i] + k);
-    }
-    __builtin_amdgcn_sched_barrier(0);  // the loads in front of it are not moved behind
-#pragma unroll
-    for (int q = 0; q < BATCH; ++q) {
-      const bool live = s0 + q * NW < whole;
-#pragma unroll
-      for (int i = 0; i < RM; ++i)
-        if (i == 0 || i * 16 < n) {
-          const V xv = live ? x[q][i] : V{};
-#pragma unroll
-          for (int b = 0; b < 2; ++b) acc[b][i] = S::mfma(live ? w[q][b] : V{}, xv, acc[b][i]);
-        }
-    }
-  }
-  if (a.D % S::K && whole % NW == wave) {
-    const int k = whole * S::K + kq, left = max(0, min(S::CH, a.D - k));
-    const V wv[2] = {S::part(a.wg.p, g_at + k, left), S::part(a.wu.p, u_at + k, left)};
-#pragma unroll
-    for (int i = 0; i < RM; ++i)
-      if (i == 0 || i * 16 < n) {
-        const V xv = S::part(a.x, x_at[i] + k, left);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) acc[b][i] = S::mfma(wv[b], xv, acc[b][i]);
-      }
-  }
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int i = 0; i < RM; ++i) sums[wave][b * RM + i][lane] = acc[b][i];
-  __syncthreads();
-  for (int i = wave; i < RM; i += NW) {
-    const int m = i * 16 + lo, at = f0 + (lane >> 4) * 4;
-    if (m >= n) continue;
-    float g[4], u[4];
-    f32x4 s[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      s[b] = sums[0][b * RM + i][lane];
-#pragma unroll
-      for (int q = 1; q < NW; ++q) s[b] += sums[q][b * RM + i][lane];
+// What is left of a row of n values from column k on, as a step's operand: behind the row's end zeros.
+template <int TYPE>
+__device__ __forceinline__ typename Step<TYPE>::V row_tail(const void* p, long long row, int k, int n) {
+  if constexpr (TYPE == CCT_TYPE_F32) {
+    typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+    const float* at = (const float*)p + row;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (k + 4 <= n) return *(const f32x4u*)(at + k);
+    if (k >= n) return v;
+    if (n >= 4) {  // with those in front of them: one load
+      const f32x4 u = *(const f32x4u*)(at + n - 4);
+      return n - k == 1 ? f32x4{u[3], 0.f, 0.f, 0.f} : n - k == 2 ? f32x4{u[2], u[3], 0.f, 0.f} : f32x4{u[1], u[2], u[3], 0.f};
     }
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      g[c] = s[0][c];
-      u[c] = s[1][c];
-    }
-    activate<true>(a.activation, g, u);
-    const int row = place[m];
-    const float weight = a.weight[row];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) g[c] = at + c < a.F ? g[c] * weight : 0.f;  // zeros up to whole steps
-    store_terms<TYPE>(a, (long long)row * a.Fp + at, g);
+    for (int e = 0; e < 3; ++e)
+      if (k + e < n) v[e] = at[k + e];
+    return v;
+  } else {
+    return __builtin_bit_cast(typename Step<TYPE>::V, load_row_raw<TYPE>(p, row, k, n - k));
   }
 }
 
-constexpr int kDownWaves = 16;
-template <int TYPE, int RM>
-__global__ __launch_bounds__(kDownWaves * 64) void moe_down_kernel(Moe a, FfProduct p) {
+constexpr int kGatedWaves = 8;
+// RM: blocks of 16 tokens that are multiplied at once; ONE: a single token, whose experts are not chosen yet
+template <int TYPE, int RM, bool ONE>
+__global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
-  constexpr int NW = kDownWaves, TERMS = TYPE == CCT_TYPE_F32 ? 1 : 2, BATCH = RM == 4 ? 2 : RM == 2 ? 4 : 8;
+  constexpr int NW = kGatedWaves, BATCH = ONE ? 8 : 4;
   extern __shared__ __attribute__((aligned(16))) unsigned char moe_smem[];
-  f32x4(*sums)[RM][64] = (f32x4(*)[RM][64])moe_smem;        // [NW]
-  int* experts = (int*)(moe_smem + NW * RM * 1024);          // [slots]
-  short* rows = (short*)(experts + a.slots);                 // [slots][T]
+  f32x4(*sums)[2 * RM][64] = (f32x4(*)[2 * RM][64])moe_smem;  // [NW]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int count = a.used[0];
-  for (int i = threadIdx.x; i < a.slots; i += NW * 64) experts[i] = a.used[1 + i];
-  for (int i = threadIdx.x; i < a.slots * a.T; i += NW * 64) rows[i] = a.rows[i];
-  __syncthreads();
-  const int n0 = blockIdx.x * 16, lo = lane & 15, kq = (lane >> 4) * S::CH;
-  const long long w_row = min(n0 + lo, a.D - 1) * a.wd.ld;
-  f32x4 acc[RM];
+  const int slot = blockIdx.y, lo = lane & 15;
+  int e, all = 1, row[RM];  // the expert, its tokens, their rows of h
+  float weight[RM];
+  if constexpr (ONE) {
+    int which;
+    float of;
+    select_experts(a, 0, lane, &which, &of);
+    if (blockIdx.x == 0 && slot == 0 && wave == 0) write_selected(a, 0, lane, which, of);
+    e = __builtin_amdgcn_readlane(which, slot);
+    row[0] = slot;
+    weight[0] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, of), slot));
+  } else {
+    e = a.slot[2 * slot];
+    all = a.slot[2 * slot + 1];
 #pragma unroll
-  for (int i = 0; i < RM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int whole = a.F / S::K, total = count * whole;
-  V w[BATCH], h[BATCH][RM][TERMS];
-  short row[BATCH][RM];
-  auto fetch = [&](int q, int slot, long long k) {
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      const int t = i * 16 + lo;
-      row[q][i] = t < a.T ? rows[slot * a.T + t] : (short)-1;
-      const long long at = max((int)row[q][i], 0) * (long long)a.Fp + k;
-      h[q][i][0] = S::load(a.h, at);
-      if constexpr (TERMS == 2) h[q][i][1] = S::load(a.h_low, at);
-    }
-  };
-  auto multiply = [&](int q, const V& wv, bool live) {
-#pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      f32x4 s = acc[i];
-#pragma unroll
-      for (int t = 0; t < TERMS; ++t) s = S::mfma(wv, h[q][i][t], s);
-      if (live && row[q][i] >= 0) acc[i] = s;  // else the token's sum stays as it is
-    }
-  };
-  for (int s0 = wave; s0 < total; s0 += BATCH * NW) {
-#pragma unroll
-    for (int q = 0; q < BATCH; ++q) {
-      const int step = min(s0 + q * NW, total - 1), slot = step / whole;
-      const long long k = (long long)(step - slot * whole) * S::K + kq;
-      w[q] = S::load(a.wd.p, experts[slot] * a.wd.e + w_row + k);
-      fetch(q, slot, k);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int q = 0; q < BATCH; ++q) multiply(q, w[q], s0 + q * NW < total);
+    for (int i = 0; i < RM; ++i) row[i] = a.rows[slot * kMostTokens + i * 16 + lo];
+    if (e < 0) return;
   }
-  if (a.F % S::K)
-    for (int slot = wave; slot < count; slot += NW) {
+  const int f0 = blockIdx.x * 16, kq = (lane >> 4) * S::CH;
+  const long long f = min(f0 + lo, a.F - 1), g_at = e * a.wg.e + f * a.wg.ld, u_at = e * a.wu.e + f * a.wu.ld;
+  for (int m0 = 0; m0 < all; m0 += RM * 16) {
+    const int n = all - m0;
+    if constexpr (!ONE) {
+      if (m0 > 0) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RM; ++i) row[i] = a.rows[slot * kMostTokens + m0 + i * 16 + lo];
+      }
+#pragma unroll
+      for (int i = 0; i < RM; ++i) weight[i] = a.weight[row[i]];
+    }
+    long long x_at[RM];
+#pragma unroll
+    for (int i = 0; i < RM; ++i) x_at[i] = ONE ? 0 : row[i] / a.k * a.ldx;
+    f32x4 acc[2][RM];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < RM; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int whole = a.D / S::K;
+    V w[BATCH][2], x[BATCH][RM];
+    for (int s0 = wave; s0 < whole; s0 += BATCH * NW) {
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) {
+        if (s0 + q * NW >= whole) break;
+        const long long k = (long long)(s0 + q * NW) * S::K + kq;
+        w[q][0] = S::load(a.wg.p, g_at + k);
+        w[q][1] = S::load(a.wu.p, u_at + k);
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+          if (i == 0 || i * 16 < n) x[q][i] = i * 16 + lo < n ? S::load(a.x, x_at[i] + k) : V{};  // lanes without a token ask for nothing
+      }
+      __builtin_amdgcn_sched_barrier(0);  // the loads in front of it are not moved behind
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) {
+        if (s0 + q * NW >= whole) break;
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+          if (i == 0 || i * 16 < n)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) acc[b][i] = S::mfma(w[q][b], x[q][i], acc[b][i]);
+      }
+    }
+    if (a.D % S::K && whole % NW == wave) {
       const int k = whole * S::K + kq;
-      w[0] = S::part(a.wd.p, experts[slot] * a.wd.e + w_row + k, max(0, min(S::CH, a.F - k)));
-      fetch(0, slot, k);
-      multiply(0, w[0], true);
+      const V wv[2] = {row_tail<TYPE>(a.wg.p, g_at, k, a.D), row_tail<TYPE>(a.wu.p, u_at, k, a.D)};
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+        if (i == 0 || i * 16 < n) {
+          const V xv = row_tail<TYPE>(a.x, x_at[i], k, a.D);
+#pragma unroll
+          for (int b = 0; b < 2; ++b) acc[b][i] = S::mfma(wv[b], xv, acc[b][i]);
+        }
     }
 #pragma unroll
-  for (int i = 0; i < RM; ++i) sums[wave][i][lane] = acc[i];
-  __syncthreads();
-  for (int i = wave; i < RM; i += NW) {
-    f32x4 s = sums[0][i][lane];
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int q = 1; q < NW; ++q) s += sums[q][i][lane];
-    const int m = i * 16 + lo, n = n0 + (lane >> 4) * 4;
-    if (m >= a.T || n >= a.D) continue;
-    float v[4] = {s[0], s[1], s[2], s[3]}, u[4] = {};
-    finish<TYPE, kFfLinear>(p, m, n, v, u);
+      for (int i = 0; i < RM; ++i) sums[wave][b * RM + i][lane] = acc[b][i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      const int at = f0 + (lane >> 4) * 4;
+      if (wave != i || i * 16 + lo >= n) continue;
+      float g[4], u[4];
+      f32x4 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        s[b] = sums[0][b * RM + i][lane];
+#pragma unroll
+        for (int q = 1; q < NW; ++q) s[b] += sums[q][b * RM + i][lane];
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        g[c] = s[0][c];
+        u[c] = s[1][c];
+      }
+      activate<true>(a.activation, g, u);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) g[c] = at + c < a.F ? g[c] * weight[i] : 0.f;  // zeros up to whole steps
+      store_terms<TYPE>(a, (long long)row[i] * a.Fp + at, g);
+    }
   }
+}
+
+// The down product.  ONE: a single token, whose chosen experts' features are one contraction; else an expert and its tokens, whose
+// results go to `part`.
+template <int TYPE, int RM, bool ONE>
+__global__ __launch_bounds__((ONE ? 16 : 8) * 64) void moe_down_kernel(Moe a, FfProduct p) {
+  typedef Step<TYPE> S;
+  typedef typename S::V V;
+  constexpr int NW = ONE ? 16 : 8, TERMS = TYPE == CCT_TYPE_F32 ? 1 : 2, BATCH = ONE ? 8 : RM == 4 ? 2 : 4;
+  static_assert(!ONE || RM == 1, "one token");
+  extern __shared__ __attribute__((aligned(16))) unsigned char moe_smem[];
+  f32x4(*sums)[RM][64] = (f32x4(*)[RM][64])moe_smem;  // [NW]
+  __shared__ short chosen[ONE ? kMostChosen : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lo = lane & 15;
+  int e = 0, all = 1, row[RM] = {};
+  if constexpr (ONE) {
+    if ((int)threadIdx.x < a.k) chosen[threadIdx.x] = a.chosen[threadIdx.x];
+    __syncthreads();
+  } else {
+    e = a.slot[2 * blockIdx.y];
+    all = a.slot[2 * blockIdx.y + 1];
+#pragma unroll
+    for (int i = 0; i < RM; ++i) row[i] = a.rows[blockIdx.y * kMostTokens + i * 16 + lo];
+    if (e < 0) return;
+  }
+  const int count = ONE ? a.k : 1;  // experts
+  const int n0 = blockIdx.x * 16, kq = (lane >> 4) * S::CH;
+  const long long w_row = min(n0 + lo, a.D - 1) * a.wd.ld;
+  for (int m0 = 0; m0 < all; m0 += RM * 16) {
+    const int n = all - m0;
+    if (m0 > 0) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < RM; ++i) row[i] = a.rows[blockIdx.y * kMostTokens + m0 + i * 16 + lo];
+    }
+    long long h_at[RM];
+#pragma unroll
+    for (int i = 0; i < RM; ++i) h_at[i] = row[i] * (long long)a.Fp;
+    f32x4 acc[RM];
+#pragma unroll
+    for (int i = 0; i < RM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int whole = a.F / S::K, total = count * whole;
+    V w[BATCH], h[BATCH][RM][TERMS];
+    auto fetch = [&](int q, int slot, long long k) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+        if (i == 0 || i * 16 < n) {
+          const bool there = i * 16 + lo < n;  // lanes without a token ask for nothing
+          const long long at = h_at[i] + (ONE ? slot * (long long)a.Fp : 0) + k;
+          h[q][i][0] = there ? S::load(a.h, at) : V{};
+          if constexpr (TERMS == 2) h[q][i][1] = there ? S::load(a.h_low, at) : V{};
+        }
+    };
+    auto multiply = [&](int q, const V& wv) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i)
+        if (i == 0 || i * 16 < n)
+#pragma unroll
+          for (int t = 0; t < TERMS; ++t) acc[i] = S::mfma(wv, h[q][i][t], acc[i]);
+    };
+    auto expert = [&](int slot) { return (ONE ? (int)chosen[slot] : e) * a.wd.e; };
+    for (int s0 = wave; s0 < total; s0 += BATCH * NW) {
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) {
+        const int step = s0 + q * NW, slot = ONE ? step / whole : 0;
+        if (step >= total) break;
+        const long long k = (long long)(step - slot * whole) * S::K + kq;
+        w[q] = S::load(a.wd.p, expert(slot) + w_row + k);
+        fetch(q, slot, k);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) {
+        if (s0 + q * NW >= total) break;
+        multiply(q, w[q]);
+      }
+    }
+    if (a.F % S::K)
+      for (int slot = (total + wave) % NW; slot < count; slot += NW) {
+        const int k = whole * S::K + kq;
+        w[0] = row_tail<TYPE>(a.wd.p, expert(slot) + w_row, k, a.F);
+        fetch(0, slot, k);
+        multiply(0, w[0]);
+      }
+#pragma unroll
+    for (int i = 0; i < RM; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      const int m = i * 16 + lo, c = n0 + (lane >> 4) * 4;
+      if (wave != i || m >= n || c >= a.D) continue;
+      f32x4 s = sums[0][i][lane];
+#pragma unroll
+      for (int q = 1; q < NW; ++q) s += sums[q][i][lane];
+      if constexpr (ONE) {
+        float v[4] = {s[0], s[1], s[2], s[3]}, u[4] = {};
+        finish<TYPE, kFfLinear>(p, m, c, v, u);
+      } else {
+        *(f32x4*)(a.part + row[i] * (long long)a.Dp + c) = s;
+      }
+    }
+  }
+}
+
+// A thread takes 4 columns of a token.
+template <int TYPE>
+__global__ __launch_bounds__(256) void moe_join_kernel(Moe a, FfProduct p) {
+  const int t = blockIdx.y, c = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4;
+  if (c >= a.D) return;
+  const float* from = a.part + (long long)t * a.k * a.Dp + c;
+  f32x4 s = *(const f32x4*)from;
+#pragma unroll 4
+  for (int j = 1; j < a.k; ++j) s += *(const f32x4*)(from + (long long)j * a.Dp);
+  float v[4] = {s[0], s[1], s[2], s[3]}, u[4] = {};
+  finish<TYPE, kFfLinear>(p, t, c, v, u);
+}
+
+template <auto KERNEL, class... ARGS>
+int launch_with_lds(dim3 grid, int threads, int lds, hipStream_t st, ARGS... args) {
+  const int rc = ensure_dynamic_lds<KERNEL>(lds);
+  if (rc != CCT_OK) return rc;
+  hipLaunchKernelGGL(KERNEL, grid, dim3(threads), lds, st, args...);
+  CCT_CHECK_LAUNCH();
+  return CCT_OK;
 }
 
 template <int TYPE, int RM>
@@ -370,28 +475,39 @@ int launch(const Moe& a, const FfProduct& p, hipStream_t st) {
     hipLaunchKernelGGL(HIP_KERNEL_NAME(moe_logits_kernel<TYPE>), dim3(a.E, pieces(a.T, kLogitTokens)), dim3(256), 0, st, a);
     CCT_CHECK_LAUNCH();
   }
-  {
+  if (a.T > 1) {
     ProfScope ps("moe_route_kernel", 0.0, 4.0 * a.T * a.E, st);
     hipLaunchKernelGGL(moe_route_kernel, dim3(1), dim3(kRouteThreads), 0, st, a);
     CCT_CHECK_LAUNCH();
   }
+  int rc;
   {
     ProfScope ps("moe_gated_kernel", 4.0 * pairs * a.D * a.F, 2.0 * size * a.slots * (double)a.D * a.F, st);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(moe_gated_kernel<TYPE, RM>), dim3(a.Fp / 16, a.slots), dim3(kGatedWaves * 64), 0, st, a);
-    CCT_CHECK_LAUNCH();
+    const dim3 grid(a.Fp / 16, a.slots);
+    constexpr int lds = kGatedWaves * 2 * RM * 1024;
+    rc = a.T == 1 ? launch_with_lds<moe_gated_kernel<TYPE, 1, true>>(grid, kGatedWaves * 64, lds, st, a)
+                           : launch_with_lds<moe_gated_kernel<TYPE, RM, false>>(grid, kGatedWaves * 64, lds, st, a);
+    if (rc != CCT_OK) return rc;
   }
-  constexpr auto down = moe_down_kernel<TYPE, RM>;
-  const int most = kDownWaves * RM * 1024 + kMostExperts * (4 + 2 * RM * 16);
-  const int rc = ensure_dynamic_lds<down>(most);
-  if (rc != CCT_OK) return rc;
-  ProfScope ps("moe_down_kernel", 2.0 * pairs * a.D * a.F, size * a.slots * (double)a.D * a.F, st);
-  hipLaunchKernelGGL(down, dim3(pieces(a.D, 16)), dim3(kDownWaves * 64), kDownWaves * RM * 1024 + a.slots * (4 + 2 * a.T), st, a, p);
+  const int tiles = pieces(a.D, 16);
+  {
+    ProfScope ps("moe_down_kernel", 2.0 * pairs * a.D * a.F, size * a.slots * (double)a.D * a.F, st);
+    rc = a.T == 1 ? launch_with_lds<moe_down_kernel<TYPE, 1, true>>(dim3(tiles), 1024, 16 * 1024, st, a, p)
+                  : launch_with_lds<moe_down_kernel<TYPE, RM, false>>(dim3(tiles, a.slots), 512, 8 * RM * 1024, st, a, p);
+    if (rc != CCT_OK || a.T == 1) return rc;
+  }
+  ProfScope ps("moe_join_kernel", 0.0, 4.0 * pairs * a.D + size * a.T * (double)a.D, st);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(moe_join_kernel<TYPE>), dim3(pieces(a.Dp / 4, 256), a.T), dim3(256), 0, st, a, p);
   CCT_CHECK_LAUNCH();
   return CCT_OK;
 }
 template <int TYPE>
 int launch(const Moe& a, const FfProduct& p, hipStream_t st) {
-  return a.T <= 16 ? launch<TYPE, 1>(a, p, st) : a.T <= 32 ? launch<TYPE, 2>(a, p, st) : launch<TYPE, 4>(a, p, st);
+  // blocks of 16 tokens that a workgroup takes at once: more of an expert's come in further passes over its weights, from a cache, so
+  // that there is room for twice the tokens that an expert has on average (37 tokens, 3 of 24 experts, gated: in one block 35 us, in
+  // four, which leave half the loads in flight, 46)
+  const int most = std::min(a.T, pieces(2 * a.T * a.k, a.E));
+  return most <= 16 ? launch<TYPE, 1>(a, p, st) : most <= 32 ? launch<TYPE, 2>(a, p, st) : launch<TYPE, 4>(a, p, st);
 }
 
 int dims_ok(const cct_moe_desc_t& d) {
@@ -422,11 +538,14 @@ long long lay_out(const cct_moe_desc_t& d, char* ws, Moe* a) {
   a->activation = d.activation;
   a->normalize = d.normalize;
   a->logits = (float*)take(4LL * a->T * a->E);
-  a->used = (int*)take(4LL * (1 + a->slots));
-  a->rows = (short*)take(2LL * a->slots * a->T);
+  a->chosen = (short*)take(2LL * a->T * a->k);
   a->weight = (float*)take(4LL * a->T * a->k);
+  a->slot = (int*)take(8LL * a->slots);
+  a->rows = (short*)take(2LL * kMostTokens * a->slots);
   a->h = take((long long)type_bytes(d.type) * a->T * a->k * a->Fp);
   a->h_low = take(d.type == CCT_TYPE_F32 ? 0 : 2LL * a->T * a->k * a->Fp);
+  a->Dp = (d.D + 3) / 4 * 4;
+  a->part = (float*)take(d.tokens <= 1 ? 0 : 4LL * a->T * a->k * a->Dp);
   return std::max(total, 256LL);
 }
 

@@ -6,6 +6,7 @@
 
 #include "feed_forward.h"
 #include "residual_norm.h"
+#include "wave_ops.h"
 
 namespace cct {
 namespace {
@@ -28,28 +29,6 @@ void with_bool(bool b, F f) {
     f(std::true_type());
   else
     f(std::false_type());
-}
-
-// The sum over 16 neighbouring lanes, in all of them.
-__device__ __forceinline__ float row_sum(float v) {
-  auto other = [](float x, auto how) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(how)::value, 0xf, 0xf, true));
-  };
-  v += other(v, std::integral_constant<int, 0xb1>());          // neighbours
-  v += other(v, std::integral_constant<int, 0x4e>());          // pairs of them
-  v += other(v, std::integral_constant<int, 0x141>());         // fours of a half row, mirrored
-  return v + other(v, std::integral_constant<int, 0x140>());  // eights of a row, mirrored
-}
-// Over a wave's lanes.
-__device__ __forceinline__ float wave_sum(float v) {
-  v = row_sum(v);
-  const unsigned u = __builtin_bit_cast(unsigned, v);
-  const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  const unsigned r0 = rows[0], r1 = rows[1];  // a bit cast of the second element itself reads the first
-  const unsigned h = __builtin_bit_cast(unsigned, __builtin_bit_cast(float, r0) + __builtin_bit_cast(float, r1));
-  const auto halves = __builtin_amdgcn_permlane32_swap(h, h, false, false);
-  const unsigned h0 = halves[0], h1 = halves[1];
-  return __builtin_bit_cast(float, h0) + __builtin_bit_cast(float, h1);
 }
 
 constexpr int kMostWaves = 16, kRegisterColumns = kMostWaves * 512;
