@@ -27,9 +27,11 @@ struct MxProduct {
   bool quantize;  // x are values yet, in rows of x.ldc (up to kMxQuantizeRows rows on mx_rows.hip)
 };
 constexpr int kMxQuantizeRows = 4;
-// How it runs: kNoTile: mx_rows.hip; splits of the contraction, of so many steps of 128 values (rows) or stages of 256 (tiles).
+// How it runs: kNoTile: mx_rows.hip; splits of the contraction, of so many steps of 128 values (rows) or stages of 256 (tiles);
+// deep: tiles of 64 x 64 that hold four stages, not two.
 struct MxPlan {
   int tile, splits, steps;
+  bool deep;
   long long part_bytes;
 };
 MxPlan mx_plan(int M, int N, int K);

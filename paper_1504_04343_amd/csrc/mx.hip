@@ -50,18 +50,26 @@ MxLayout layout_of(const cct_linear_desc_t& d, bool quantize) {
 namespace {
 
 constexpr int kCus = 256;
-// A tile: its workgroups on a CU, and us a stage takes where the CUs are full of them, and one alone.
+// A tile: its workgroups on a CU, and us a stage takes where the CUs are full of them, and one alone, measured on products of 64 to 8192
+// rows.  Stages of small tiles are mostly waiting, so that they do best where no CU has many (256 x 4096 x 4096: in tiles of 128 18 us, of
+// 64 x 128 12, of 64 10, and 9.5 with four stages; 48 x 16384 x 4096: 17.6, 14.0, 12.2 and 9.6; 8192 x 8192 x 8192: 348, 436, 524 and 576).
 struct MxTileCost {
-  int tile, bm, bn, threads, per_cu;
-  double full, alone;
+  int tile;
+  bool deep;
+  int bm, bn, threads, per_cu;
+  double full, alone, around;  // what stands around a contraction, in stages
 };
-constexpr MxTileCost kMxTiles[] = {{kTile256, 256, 256, 512, 1, 2.2, 1.9}, {kTile128, 128, 128, 256, 2, 1.35, 0.95}, {kTile64x128, 64, 128, 256, 3, 1.3, 0.58}};
-constexpr double kLaunchMicros = 3.0, kJoinMicros = 3.0, kJoinBytesPerMicro = 3.0e6, kAround = 2.0;
+constexpr MxTileCost kMxTiles[] = {{kTile256, false, 256, 256, 512, 1, 2.2, 1.9, 2},
+                                   {kTile128, false, 128, 128, 256, 2, 1.35, 0.95, 2},
+                                   {kTile64x128, false, 64, 128, 256, 3, 1.25, 0.6, 2},
+                                   {kTile64, false, 64, 64, 256, 4, 1.02, 0.5, 2},
+                                   {kTile64, true, 64, 64, 256, 2, 0.56, 0.36, 4}};
+constexpr double kLaunchMicros = 3.0, kJoinMicros = 3.0, kJoinBytesPerMicro = 3.0e6;
 
 // Few columns of long rows leave most CUs idle: splits of 32 steps (a turn of a workgroup's waves) or more.
 MxPlan rows_plan(int M, int N, int K) {
   const int steps = pieces(mx_blocks(K), 4);
-  MxPlan plan = {kNoTile, 1, steps, 0};
+  MxPlan plan = {kNoTile, 1, steps, false, 0};
   const long long groups = (long long)pieces(N, 16) * pieces(M, M <= 16 ? 16 : M <= 32 ? 32 : 64);
   if (groups <= 64 && steps >= 128) {
     const int splits = (int)std::min(128 / groups, steps / 32LL);
@@ -90,11 +98,12 @@ MxPlan mx_plan(int M, int N, int K) {
       const int each = pieces(stages, splits), have = pieces(stages, each);
       const long long groups = tiles * have, slots = (long long)kCus * c.per_cu, rest = groups % slots;
       if (groups * c.threads > kMostThreads) continue;
-      double us = ((double)(groups / slots) * c.full + (rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full)) * (each + kAround) + kLaunchMicros;
+      double us = ((double)(groups / slots) * c.full + (rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full)) * (each + c.around) + kLaunchMicros;
+      if (M <= kMxQuantizeRows) us += kLaunchMicros;  // of x's codes, if it has none yet: the choice is the same for both
       if (have > 1) us += kJoinMicros + 8.0 * have * M * N / kJoinBytesPerMicro;
       if (us < least) {
         least = us;
-        best = {c.tile, have, each, 0};
+        best = {c.tile, have, each, c.deep, 0};
       }
     }
   }
@@ -166,7 +175,7 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
   }
   // a tile's offsets have 32 bits, of 256 rows
   constexpr long long kMost = 1 << 23;
-  if (plan.tile != kNoTile && std::max(std::max(a.x.ldc, a.w.ldc), std::max(a.x.lds, a.w.lds)) >= kMost) plan = {kNoTile, 1, 0, 0};
+  if (plan.tile != kNoTile && std::max(std::max(a.x.ldc, a.w.ldc), std::max(a.x.lds, a.w.lds)) >= kMost) plan = {kNoTile, 1, 0, false, 0};
   FfProduct& p = a.p;
   p.M = d.M;
   p.N = d.N;

@@ -103,6 +103,8 @@ __global__ __launch_bounds__(kThreads) void mx_dequantize_kernel(MxJob j, const 
 MxJob job_of(int rows, int cols, long long ldx, long long ldc, long long lds, dim3* grid) {
   MxJob j = {rows, cols, 4 * mx_blocks(cols), 4, ldx, ldc, lds};
   while (j.wide < kThreads && j.wide < j.chunks) j.wide *= 2;
+  // rows a little longer than that leave most threads of their last workgroup idle: half as wide (2049 columns: 256 and 4 chunks)
+  while (j.wide > 64 && pieces(j.chunks, j.wide / 2) * (j.wide / 2) < pieces(j.chunks, j.wide) * j.wide * 7 / 8) j.wide /= 2;
   const int across = pieces(j.chunks, j.wide);
   const long long most = std::min(65535LL, std::max(1LL, kMostThreads / kThreads / across));
   *grid = dim3(across, (unsigned)std::min(most, (long long)pieces(rows, kThreads / j.wide * kRows)));

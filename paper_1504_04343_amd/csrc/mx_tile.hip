@@ -62,7 +62,7 @@ __device__ __forceinline__ void end_scales(int q, int left, int (&s)[N]) {
   }
 }
 
-template <int TYPE, int BM, int BN, int WM, int WN, bool SPLIT>
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool SPLIT>
 __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))) void mx_tile_kernel(MxProduct a, int tiles_m, int tiles_n,
                                                                                                       FfPart part) {
   constexpr int NW = WM * WN, RB = BM / WM / 16, CB = BN / WN / 16;
@@ -70,6 +70,8 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   typedef TileOperand<BN, NW, false> OpB;
   constexpr int STAGE = OpA::BYTES + OpB::BYTES, SCALES = (BM + BN) * 16, UNITS = (BM + BN) / 64;  // loads of scales: one of a wave
   static_assert(UNITS <= NW && BM % 64 == 0, "one load");
+  static_assert((RING & (RING - 1)) == 0, "places of a ring");  // of as many pairs of stages the scales, those in use and those ahead
+
   extern __shared__ __attribute__((aligned(1024))) unsigned char tile_smem[];
 
   const FfProduct& p = a.p;
@@ -100,14 +102,14 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   long long sc_bytes = (sc_rows - 1) * sm.lds + ((a.blocks + 3) & ~3) - first * kStageBlocks;  // to the last row's end
   int loaded = 0;
   auto load = [&]() {
-    unsigned char* st = tile_smem + (loaded & 1) * STAGE;
+    unsigned char* st = tile_smem + (loaded & (RING - 1)) * STAGE;
     const int left = loaded < stages ? (a.blocks - (first + loaded) * kStageBlocks) * 8 : 0;
     opa.template load<1>(st, wave, ca, left);
     opb.template load<1>(st + OpA::BYTES, wave, cb, left);
     if ((loaded & 1) == 0) {
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(sc_from), 0,
                                                                          left > 0 ? (int)min(sc_bytes, 0x7fffffffLL) : 0, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(tile_smem + 2 * STAGE + (loaded >> 1 & 1) * SCALES + unit * 1024), 16, (int)sc_at, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(tile_smem + RING * STAGE + (loaded >> 1 & (RING - 1)) * SCALES + unit * 1024), 16, (int)sc_at, 0, 0, 0);
       sc_from += 2 * kStageBlocks;
       sc_bytes -= 2 * kStageBlocks;
     }
@@ -125,14 +127,14 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   s16x8 fa[2][RB], fb[2][CB];
   int sa[RB / 2], sb[CB / 2];
   auto read = [&](int set, int h, int t) {
-    const unsigned char* st = tile_smem + (t & 1) * STAGE;
+    const unsigned char* st = tile_smem + (t & (RING - 1)) * STAGE;
 #pragma unroll
     for (int j = 0; j < CB; ++j) fb[set][j] = OpB::read(st + OpA::BYTES, lane, wn * (BN / WN) + j * 16, h);
 #pragma unroll
     for (int i = 0; i < RB; ++i) fa[set][i] = OpA::read(st, lane, wm * (BM / WM) + i * 16, h);
   };
   auto scales = [&](int t, int (&to_a)[RB / 2], int (&to_b)[CB / 2]) {
-    const unsigned char* sc = tile_smem + 2 * STAGE + (t >> 1 & 1) * SCALES + (t & 1) * 8;
+    const unsigned char* sc = tile_smem + RING * STAGE + (t >> 1 & (RING - 1)) * SCALES + (t & 1) * 8;
     read_scales<RB>(sc + wm * (BM / WM) * 16, lane, to_a);
     read_scales<CB>(sc + (BM + wn * (BN / WN)) * 16, lane, to_b);
   };
@@ -160,9 +162,9 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   asm volatile("" ::: "memory");                                                \
   __builtin_amdgcn_s_barrier();                                                 \
   asm volatile("" ::: "memory")
-  load();
-  load();
-  CCT_MEET(L);
+  static_assert((RING - 1) * L < 64, "vmcnt has six bits");
+  for (int q = 0; q < RING; ++q) load();
+  CCT_MEET((RING - 1) * L);  // (loads of scales are some more: this waits for a little more than it must)
   read(0, 0, 0);
   scales(0, sa, sb);
   for (int t = 0; t < stages; ++t) {
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     }
     read(1, 1, t);
     multiply(0, false);
-    CCT_MEET(0);
+    CCT_MEET((RING - 2) * L);
     load();
     int na[RB / 2], nb[CB / 2];
     scales(t + 1, na, nb);
@@ -189,10 +191,10 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
   finish_tile<TYPE, BM, BN, WM, WN, kFfLinear>(p, part, SPLIT, split, m0, n0, acc);
 }
 
-template <int TYPE, int BM, int BN, int WM, int WN, bool SPLIT>
+template <int TYPE, int BM, int BN, int WM, int WN, int RING, bool SPLIT>
 int launch_one(const MxProduct& a, const FfPart& part, hipStream_t st) {
-  constexpr int ring = 2 * (BM + BN) * (128 + 16), out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
-  constexpr auto kernel = mx_tile_kernel<TYPE, BM, BN, WM, WN, SPLIT>;
+  constexpr int ring = RING * (BM + BN) * (128 + 16), out = TileEpilogue<BM, BN, WM, WN>::BYTES, lds = ring > out ? ring : out;
+  constexpr auto kernel = mx_tile_kernel<TYPE, BM, BN, WM, WN, RING, SPLIT>;
   const int rc = ensure_dynamic_lds<kernel>(lds);
   if (rc != CCT_OK) return rc;
   const int tiles_m = pieces(a.p.M, BM), tiles_n = pieces(a.p.N, BN);
@@ -201,19 +203,20 @@ int launch_one(const MxProduct& a, const FfPart& part, hipStream_t st) {
   return CCT_OK;
 }
 
+template <int TYPE, bool SPLIT>
+int launch_planned(const MxProduct& a, const MxPlan& plan, const FfPart& part, hipStream_t st) {
+  switch (plan.tile) {
+    case kTile128: return launch_one<TYPE, 128, 128, 2, 2, 2, SPLIT>(a, part, st);
+    case kTile64x128: return launch_one<TYPE, 64, 128, 2, 2, 2, SPLIT>(a, part, st);
+    default: return plan.deep ? launch_one<TYPE, 64, 64, 2, 2, 4, SPLIT>(a, part, st) : launch_one<TYPE, 64, 64, 2, 2, 2, SPLIT>(a, part, st);
+  }
+}
 template <int TYPE>
 int launch(const MxProduct& a, const MxPlan& plan, float* ws, hipStream_t st) {
   const FfPart part = {ws, (a.p.N + 3) / 4 * 4, plan.splits, plan.steps};
-  int rc;
-  if (plan.splits == 1) switch (plan.tile) {
-      case kTile256: return launch_one<TYPE, 256, 256, 2, 4, false>(a, part, st);
-      case kTile128: return launch_one<TYPE, 128, 128, 2, 2, false>(a, part, st);
-      default: return launch_one<TYPE, 64, 128, 2, 2, false>(a, part, st);
-    }
-  if (plan.tile == kTile128)
-    rc = launch_one<TYPE, 128, 128, 2, 2, true>(a, part, st);
-  else
-    rc = launch_one<TYPE, 64, 128, 2, 2, true>(a, part, st);
+  if (plan.tile == kTile256) return launch_one<TYPE, 256, 256, 2, 4, 2, false>(a, part, st);
+  if (plan.splits == 1) return launch_planned<TYPE, false>(a, plan, part, st);
+  const int rc = launch_planned<TYPE, true>(a, plan, part, st);
   if (rc != CCT_OK) return rc;
   launch_join<TYPE, kFfLinear>(a.p, part, st);
   CCT_CHECK_LAUNCH();
@@ -226,7 +229,8 @@ int launch_mx_tile(const MxProduct& a, const MxPlan& plan, float* part, hipStrea
   const double mn = (double)a.p.M * a.p.N, k = (double)a.p.K;
   ProfScope ps(2.0 * mn * k,
                (a.p.M + (double)a.p.N) * k * 17 / 32 + type_bytes(a.p.type) * mn * (1 + (a.p.residual != nullptr) + (a.p.z != nullptr)), st,
-               "mx_tile_kernel<%s, %d splits>", plan.tile == kTile256 ? "256x256" : plan.tile == kTile128 ? "128x128" : "64x128", plan.splits);
+               "mx_tile_kernel<%s, %d splits, %d stages>", plan.tile == kTile256 ? "256x256" : plan.tile == kTile128 ? "128x128" : plan.tile == kTile64x128 ? "64x128" : "64x64",
+               plan.splits, plan.deep ? 4 : 2);
   if (a.p.type == CCT_TYPE_F32) return launch<CCT_TYPE_F32>(a, plan, part, st);
   return a.p.type == CCT_TYPE_BF16 ? launch<CCT_TYPE_BF16>(a, plan, part, st) : launch<CCT_TYPE_F16>(a, plan, part, st);
 }

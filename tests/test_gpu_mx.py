@@ -169,10 +169,13 @@ def test_whole_numbers(B, M):
     assert torch.equal(y.cpu().double(), xv @ wv.t())
 
 
-PLANS = [(3, 160, 1000, "mx_rows_kernel"), (16, 24, 40000, "mx_rows_kernel"), (300, 200, 1100, "mx_tile_kernel<64x128, 1 splits>"),
-         (40, 16384, 4000, "mx_tile_kernel<64x128, 1 splits>"), (300, 200, 10880, "mx_tile_kernel<64x128, 9 splits>"),
-         (1500, 1500, 4100, "mx_tile_kernel<128x128, 1 splits>"), (1030, 1000, 20000, "mx_tile_kernel<128x128, 3 splits>"),
-         (4096, 4090, 1500, "mx_tile_kernel<256x256, 1 splits>"), (7000, 8000, 200, "mx_tile_kernel<256x256, 1 splits>")]
+PLANS = [(3, 160, 1000, "mx_rows_kernel"), (16, 24, 40000, "mx_rows_kernel"),
+         (300, 200, 1100, "mx_tile_kernel<64x64, 1 splits, 4 stages>"), (40, 16384, 4000, "mx_tile_kernel<64x64, 1 splits, 4 stages>"),
+         (300, 200, 10880, "mx_tile_kernel<64x64, 9 splits, 4 stages>"), (1000, 1000, 200, "mx_tile_kernel<64x64, 1 splits, 2 stages>"),
+         (4182, 1, 13105, "mx_tile_kernel<64x64, 13 splits, 2 stages>"), (2100, 2100, 1100, "mx_tile_kernel<64x128, 1 splits, 2 stages>"),
+         (70, 1814, 19797, "mx_tile_kernel<64x128, 8 splits, 2 stages>"), (1500, 1500, 4100, "mx_tile_kernel<128x128, 1 splits, 2 stages>"),
+         (1030, 1000, 20000, "mx_tile_kernel<128x128, 3 splits, 2 stages>"), (4096, 4090, 1500, "mx_tile_kernel<256x256, 1 splits, 2 stages>"),
+         (7000, 8000, 200, "mx_tile_kernel<256x256, 1 splits, 2 stages>")]
 
 
 @pytest.mark.parametrize("M,N,K,kernel", PLANS)
@@ -188,7 +191,7 @@ def test_every_plan(B, M, N, K, kernel):
         names = [e["name"] for e in B.cct_profile_read() if e["name"].startswith("mx")]
     finally:
         B.cct_profile_enable(False)
-    assert len(names) == 1 and names[0].startswith(kernel), names
+    assert names == [kernel]
     values = [torch.empty(r, K, device="cuda") for r in (M, N)]
     for m, v in zip((x, w), values):
         B.cct_mx_dequantize(m, v)
