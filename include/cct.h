@@ -396,8 +396,9 @@ int cct_gated_backward(const cct_gated_desc_t* desc, const void* x, int64_t ldx,
  * N(v) = n * w + c over the D values of a row, n = v / sqrt(mean(v^2) + eps) (CCT_NORM_RMS), the same of v - mean(v)
  * (CCT_NORM_LAYER), or N(v) = v (CCT_NORM_NONE).  A row of the gate belongs to `gate_rows` consecutive rows of the stream
  * (gate: ceil(M / gate_rows) x D): M for a gate that all share, 1 for one of each row's own.  All tensors have one type;
- * everything is computed in fp32 and rounded once.  Matrices and their strides are as for cct_linear_*, vectors have D
- * consecutive values.  M >= 0, D >= 1, gate_rows >= 1, eps >= 0, eps and scale finite (CCT_EINVAL); CCT_EUNSUPPORTED as above.
+ * everything is computed in fp32 and rounded once (a mean of squares beyond fp32 is an infinity: n is 0 there).  Matrices
+ * and their strides are as for cct_linear_*, vectors have D consecutive values.  M >= 0, D >= 1, gate_rows >= 1, eps >= 0,
+ * eps and scale finite (CCT_EINVAL); CCT_EUNSUPPORTED as above.
  */
 typedef enum { CCT_NORM_NONE = 0, CCT_NORM_RMS = 1, CCT_NORM_LAYER = 2 } cct_norm_t;
 typedef struct {
@@ -421,8 +422,8 @@ int cct_residual_norm_forward(const cct_residual_norm_desc_t* desc, const void* 
  * stream that the forward call left (r where there is no b); nothing else is kept from it.  dr is the gradient of r.
  * dw_* are sums of gradient * n over the rows, dc_* of the gradient, dgate of scale * p * dr over a gate row's rows.
  * Any output may be NULL; those of b, the gate and a norm must be where there is none.  dr may be ds itself (same pointer
- * and ld).  c_after is read for dgate only.  M == 0: dw_* and dc_* are zero.  Sums are fp32 and run in an order that
- * depends on the descriptor alone.
+ * and ld).  c_after is read for dgate only, b for dgate and for what goes through its norm.  M == 0: dw_* and
+ * dc_* are zero.  Sums are fp32 and run in an order that depends on the descriptor alone.
  */
 int cct_residual_norm_workspace_bytes(const cct_residual_norm_desc_t* desc, size_t* bytes);
 int cct_residual_norm_backward(const cct_residual_norm_desc_t* desc, const void* s, int64_t lds, const void* b, int64_t ldb,
@@ -441,7 +442,7 @@ int cct_residual_norm_backward(const cct_residual_norm_desc_t* desc, const void*
  *   scales: a byte for each block, its power of two's exponent + 127; 255: the block is NaN.  A row is ceil(cols / 32) bytes,
  *     with room for a multiple of 4; scales and ld_scales (bytes) are multiples of 4.
  * cct_mx_quantize: the exponent is floor(log2(m)) - 2 for the block's largest size m, at least -127 (also for a block of zeros);
- * x / 2^exponent is rounded to the nearest, ties to even, at most 6.  A block that holds an infinity or a NaN is NaN. 
+ * x / 2^exponent is rounded to the nearest, ties to even, at most 6.  A block that holds an infinity or a NaN is NaN.
  * cct_mx_dequantize: the values, rounded to the type of x (fp32 and bf16: exact; fp16: infinities beyond its range).
  * rows >= 0, cols >= 1; x as for cct_linear_*; the same CCT_EUNSUPPORTED.
  */
@@ -470,11 +471,11 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
  *   h = act(x[t] wg[e]^T) * (x[t] wu[e]^T),   y[t] = sum over the chosen e of weight * (h wd[e]^T) + residual[t].
  * Experts that no token chooses are not read.  The weights of consecutive experts lie `e` values apart (wg_e >= F rows' extent;
  * any element-aligned address and distance), their rows `ld`.  Sums are fp32; weight * h keeps 16 bits or more for the last
- * product (fp16: an infinity beyond 65504).  residual (tokens x D), chosen_out (tokens x chosen int32, largest logit first) and weights_out (fp32) may be NULL;
- * these two are contiguous.  y may be the residual itself.
+ * product (fp16: an infinity beyond 65504).  residual (tokens x D), chosen_out (tokens x chosen int32, largest logit first) and
+ * weights_out (fp32) may be NULL; these two are contiguous.  y may be the residual itself.
  * 0 <= tokens, 1 <= chosen <= experts, D, F >= 1 (CCT_EINVAL); CCT_EUNSUPPORTED: more than 64 tokens, 512 experts, 16
- * chosen ones or 2^24 features, matrices as above.  Results are bit-reproducible, and a token's do not
- * depend on the other tokens' values.
+ * chosen ones or 2^24 features, matrices as above.  Results are bit-reproducible, and a token's do not depend on the other
+ * tokens' values.
  */
 typedef struct {
   int32_t tokens, experts, chosen, D, F;

@@ -711,13 +711,24 @@ def alloc_moe_workspace(desc: MoeDesc):
 
 def _experts(t, name, E, rows, cols, dtype):
     """Address, row stride and expert stride of a tensor of matrices."""
-    if not isinstance(t, torch.Tensor) or t.shape != (E, rows, cols):
-        raise ValueError("%s must be a tensor of shape %s" % (name, (E, rows, cols)))
-    at, ld = _mat(t[0], name, rows, cols, dtype)
-    apart = t.stride(0) if E > 1 else rows * ld
-    if E > 1 and apart < (rows - 1) * ld + cols:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a torch tensor on the GPU" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    if t.shape != (E, rows, cols):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), (E, rows, cols)))
+    apart, ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise TypeError("%s must have consecutive values along a row" % name)
+    if rows <= 1:
+        ld = cols
+    elif ld < cols:
+        raise TypeError("%s has rows that overlap" % name)
+    if E <= 1:
+        apart = rows * ld
+    elif apart < (rows - 1) * ld + cols:
         raise TypeError("%s has experts that overlap" % name)
-    return at, ld, apart
+    return t.data_ptr(), ld, apart
 
 
 def _out(t, name, shape, dtype):

@@ -320,10 +320,10 @@ template <int TYPE>
 __global__ __launch_bounds__(kColumnThreads) void residual_norm_columns_kernel(ResidualNormBack p, ResidualNormPlan plan,
                                                                               const RowStats* __restrict__ stats,
                                                                               float* __restrict__ part) {
-  const long long c8 = ((long long)blockIdx.y * kColumnThreads + threadIdx.x) * 8;
+  const long long c8 = ((long long)blockIdx.x * kColumnThreads + threadIdx.x) * 8;
   if (c8 >= p.D) return;
   const int c = (int)c8, n = p.D - c;
-  const NormRun run = norm_run(p, plan, blockIdx.x);
+  const NormRun run = norm_run(p, plan, blockIdx.y);
   ColumnSums sums = {};
   const f32x8 w_after = vector_or<TYPE>(p.w_after, c, n, 1.f);
   const bool block = p.b && p.after != CCT_NORM_NONE;
@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kColumnThreads) void residual_norm_columns_kernel(R
 #pragma unroll
   for (int k = 0; k < kNormSums; ++k)
     if (p.out[k] && !(k == kDgate && plan.whole))
-      store_first<CCT_TYPE_F32>((char*)part + k * plan.part_bytes, (long long)blockIdx.x * p.D + c, sums.v[k], n);
+      store_first<CCT_TYPE_F32>((char*)part + k * plan.part_bytes, (long long)blockIdx.y * p.D + c, sums.v[k], n);
 }
 
 // Where the norms' sums are: LDS, so that 128 registers are enough for two workgroups on a CU; the next row of fp32 values leaves
@@ -523,25 +523,27 @@ __global__ __launch_bounds__(kJoinRows * 32) void residual_norm_join_kernel(Resi
   const int k = min((int)blockIdx.y, (int)kDgate), group = (int)blockIdx.y - k;
   if (!p.out[k]) return;
   const int rows = k == kDgate ? plan.per_gate : plan.count, x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + x;
-  const float* from = (const float*)((const char*)part + k * plan.part_bytes) + (long long)group * rows * p.D + c;
-  float v[4] = {};  // four chains: one waits for itself
-  if (c < p.D) {
-    int r = y;
+  for (long long c = blockIdx.x * 32LL + x; c - x < p.D; c += gridDim.x * 32LL) {
+    const float* from = (const float*)((const char*)part + k * plan.part_bytes) + (long long)group * rows * p.D + c;
+    float v[4] = {};  // four chains: one waits for itself
+    if (c < p.D) {
+      int r = y;
 #pragma unroll 2
-    for (; r + 3 * kJoinRows < rows; r += 4 * kJoinRows)
+      for (; r + 3 * kJoinRows < rows; r += 4 * kJoinRows)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] += from[(long long)(r + q * kJoinRows) * p.D];
-    for (; r < rows; r += kJoinRows) v[0] += from[(long long)r * p.D];
-  }
-  lds[y][x] = (v[0] + v[1]) + (v[2] + v[3]);
-  __syncthreads();
+        for (int q = 0; q < 4; ++q) v[q] += from[(long long)(r + q * kJoinRows) * p.D];
+      for (; r < rows; r += kJoinRows) v[0] += from[(long long)r * p.D];
+    }
+    lds[y][x] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
 #pragma unroll
-  for (int half = kJoinRows / 2; half > 0; half >>= 1) {
-    if (y < half) lds[y][x] += lds[y + half][x];
+    for (int half = kJoinRows / 2; half > 0; half >>= 1) {
+      if (y < half) lds[y][x] += lds[y + half][x];
+      __syncthreads();
+    }
+    if (y == 0 && c < p.D) store1<TYPE>(p.out[k], k == kDgate ? group * p.lddgate + c : c, lds[0][x]);
     __syncthreads();
   }
-  if (y == 0 && c < p.D) store1<TYPE>(p.out[k], k == kDgate ? group * p.lddgate + c : c, lds[0][x]);
 }
 
 constexpr int kRowsAhead = 512;  // workgroups, two a CU, of rows that leave no room for more
@@ -649,7 +651,7 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
                  all * ((p.ds != nullptr) + 2 * (p.dh != nullptr) + (p.b != nullptr) + (p.dr != nullptr) + (p.db != nullptr)), st);
     with_type(p.type, [&](auto type) {
       hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_columns_kernel<decltype(type)::value>),
-                         dim3(plan.count, pieces(p.D, kColumnThreads * 8)), dim3(kColumnThreads), 0, st, p, plan, stats, part);
+                         dim3(pieces(p.D, kColumnThreads * 8), plan.count), dim3(kColumnThreads), 0, st, p, plan, stats, part);
     });
     CCT_CHECK_LAUNCH();
   }
@@ -659,7 +661,7 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
     ProfScope ps("residual_norm_join_kernel", 0.0, 0.0, st);
     with_type(p.type, [&](auto type) {
       hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_join_kernel<decltype(type)::value>),
-                         dim3(pieces(p.D, 32), kDgate + (gate ? plan.count / plan.per_gate : 0)), dim3(kJoinRows * 32), 0, st, p, plan, part);
+                         dim3(std::min(pieces(p.D, 32), 1 << 20), kDgate + (gate ? plan.count / plan.per_gate : 0)), dim3(kJoinRows * 32), 0, st, p, plan, part);
     });
     CCT_CHECK_LAUNCH();
   }

@@ -158,6 +158,33 @@ def test_product(B, type, shape):
     ff.check("y", a, expect(act, mx.values(*mx.quantize(v), K), wv, bias, residual, dt)[0])
 
 
+@pytest.mark.parametrize("type", list(ff.TYPES))
+@pytest.mark.parametrize("M", [1, 4, 5])
+def test_what_is_quantised_on_the_way(B, type, M):
+    """A product with the identity gives the values that x was rounded to, also where the workgroups that multiply round it: rows of
+    every scale of the type, its smallest numbers, infinities and NaN."""
+    K, dt = 96, ff.TYPES[type]
+    g = torch.Generator().manual_seed(M)
+    code = torch.eye(K).byte() * 2                        # 1.0
+    eye = given(B, code, torch.full((K, 3), 127, dtype=torch.uint8), K)
+    lo, hi = dict(f32=(-149, 125), bf16=(-133, 125), f16=(-24, 13))[type]
+    for e in range(lo, hi, 7):
+        # up to just below 8 times 2^e, so that every rounding is met; a row of the middles between neighbours
+        x = torch.ldexp((torch.rand(M, K, generator=g) * 16 - 8).double(), torch.tensor(e)).to(dt)
+        x[M - 1, :15] = torch.ldexp(torch.tensor([4, .25, .75, 1.25, 1.75, 2.5, 3.5, 5, 6, 7, .5, 1, 1.5, 2, 3]).double(), torch.tensor(e)).to(dt)
+        x[0, 64:] = 0
+        y, _ = run(B, type, "none", ff.to_gpu(x), eye, None, None, False, M, K, K, 0, True)
+        want = mx.values(*mx.quantize(x), K)
+        # (what is below fp32's normal numbers may be lost in the sum of its products)
+        off = (y.cpu().double() - want).abs()
+        assert bool((off <= (2.0 ** -126 if type != "f16" else 0.0)).all()), e
+    x = ff.rand(g, M, K, dt)
+    x[0, 5], x[M - 1, 70] = float("inf"), float("nan")
+    y = run(B, type, "none", ff.to_gpu(x), eye, None, None, False, M, K, K, 0, True)[0].cpu()
+    assert torch.isnan(y[0]).all() and torch.isnan(y[M - 1]).all()        # 0 * NaN
+    assert M < 3 or torch.equal(y[1:M - 1].double(), mx.values(*mx.quantize(x), K)[1:M - 1])
+
+
 @pytest.mark.parametrize("M", [1, 20, 300])
 def test_whole_numbers(B, M):
     """Sums of whole numbers below 2^24 are exact, whatever their order."""

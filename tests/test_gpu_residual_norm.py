@@ -238,6 +238,27 @@ def test_rows_far_apart(B):
     assert torch.equal(dr, got["dr"])
 
 
+def test_rows_of_134_million_columns(B):
+    """More columns than a launch's second and third dimension take workgroups of them: against 64 bits on the GPU."""
+    D = 65535 * 2048 + 1000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r, w, ds, dh = (torch.randn(1, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(4))
+    d = B.make_residual_norm_desc(1, D, B.TYPE_BF16, B.NORM_RMS)
+    h, dr, dw = (torch.full_like(r, float("nan")) for _ in range(3))
+    B.cct_residual_norm_forward(d, r, None, None, None, None, w[0], None, None, h)
+    B.cct_residual_norm_backward(d, r, None, None, None, None, w[0], ds, dh, dr, None, None, None, None, dw[0], None,
+                                 B.alloc_residual_norm_workspace(d))
+    v, e, u = r.double(), dh.double(), w.double()
+    rstd = 1 / ((v * v).mean() + 1e-6).sqrt()
+    n = v * rstd
+    # A thread adds 16384 times, its workgroup 10 more: a sum is off by 16400 x 2^-24 < 2^-9.99 of its terms' sizes, rstd by half of
+    # that, n slope by 2.5 times that: all below 2^-8.6.  The result's rounding is half a step of bf16.
+    slope, most = (e * u * n).mean(), (e * u * n).abs().mean()
+    for got, want, size in ((h, n * u, (n * u).abs()), (dw, e * n, (e * n).abs()),
+                            (dr, ds.double() + (e * u - n * slope) * rstd, ((e * u).abs() + n.abs() * most) * rstd)):
+        assert bool(((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -8.6 * (1 + 2.0 ** -8) * size + 1e-30).all())
+
+
 @pytest.mark.parametrize("M,D,rows", [(50, 600, 7), (1, 4096, 1), (30, 6000, 4), (600, 96, 600), (20, 9000, 20)])
 def test_replayed_from_a_graph_and_on_another_stream(B, M, D, rows):
     c = Case(B, M, D, "bf16", "rms", "rms", rows)
