@@ -454,7 +454,8 @@ int cct_mx_dequantize(int32_t rows, int32_t cols, int32_t type, const void* code
  * cct_linear_forward of a microscaled weight (N x K) and a microscaled x: z = x w^T + bias, y = act(z) + residual.  Products are
  * exact, sums fp32, bias, residual, y and z have the descriptor's type.  x_scales NULL: x (M x K, the descriptor's type, ldx in
  * values) is quantised into the workspace first, as cct_mx_quantize does; else x is codes (ldx in bytes), x_scales their
- * scales.  `quantize`: whether the workspace has room for that.  Everything else is as for cct_linear_forward.
+ * scales.  `quantize`: whether the workspace has room for that.  16-bit types: act(z) is good to 2^-16 of it before it is
+ * rounded.  Everything else is as for cct_linear_forward.
  */
 int cct_mx_linear_workspace_bytes(const cct_linear_desc_t* desc, int32_t quantize, size_t* bytes);
 int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t ldx, const void* x_scales, int64_t ldxs,

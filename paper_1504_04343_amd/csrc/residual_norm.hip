@@ -370,8 +370,10 @@ constexpr bool norm_sums_in_lds = THREADS > 512;
 // The same of rows of up to 8192 columns in one pass: a thread has 8 columns, a workgroup a run of rows, one at a time, or its waves
 // one each where 512 columns are all (in spans: of a gate row's rows, so that its sum is one wave's).  The next row is on its way
 // while one is worked on; its sums over columns stay with the thread.  Between a row's loads and stores its waves meet two or three
-// times, which is what the time went into (8192 x 4096, bf16, two norms and a gate: 84 us; 100 with sums over waves that read
-// LDS one after the other) and what is above the 79 us of a copy; the runs' sums and their joining take 10 us more.
+// times, which is what the time went into (8192 x 4096, bf16, two norms and a gate: 84 to 100 us by
+// card, 79 at a copy's rate; 15 more with sums over waves that read LDS one after the other); the runs' sums and their joining take
+// 6 to 10 us more.  1531 x 2049 fp16, layer norms, a gate row for 37: 35 us, 5 for each of a workgroup's seven rows: five waves, of which
+// a CU has one workgroup, wait for the sums (three meetings) with nothing beside them.
 template <int TYPE, int THREADS, bool EIGHTS>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS <= 512 ? 2 : 4))) void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {
   typedef typename Number<TYPE>::V8 V8;
@@ -515,6 +517,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
 }
 
 // The runs' sums, added in order: 32 columns of one result, 8 threads a column.  blockIdx.y: four vectors, then the gate's rows.
+// Bound by the trip to memory (256 runs of 4096 columns, five results, 21 MB: 5 us).
 constexpr int kJoinRows = 8;
 template <int TYPE>
 __global__ __launch_bounds__(kJoinRows * 32) void residual_norm_join_kernel(ResidualNormBack p, ResidualNormPlan plan,

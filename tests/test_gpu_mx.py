@@ -185,6 +185,33 @@ def test_what_is_quantised_on_the_way(B, type, M):
     assert M < 3 or torch.equal(y[1:M - 1].double(), mx.values(*mx.quantize(x), K)[1:M - 1])
 
 
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("act", ff.ACTS)
+@pytest.mark.parametrize("M", [1, 300])
+def test_activations_of_all_numbers(B, type, act, M):
+    """Of every number of the type: a product of zeros, and the number as bias."""
+    dt, N = ff.TYPES[type], 65536
+    z = torch.arange(N, dtype=torch.int32).to(torch.uint16).view(dt)
+    zeros = lambda rows: given(B, torch.zeros(rows, 32, dtype=torch.uint8), torch.full((rows, 1), 127, dtype=torch.uint8), 32)
+    y, _ = run(B, type, act, zeros(M), zeros(N), z, None, False, M, N, 32)
+    y = y.cpu()
+    assert torch.equal(y.view(torch.int16), y[:1].view(torch.int16).expand(M, N)) or act != "none" and \
+        torch.equal(y.nan_to_num(1.0), y[:1].nan_to_num(1.0).expand(M, N))
+    y, z = y[:1], z.double().view(1, N)
+    plus, bad = z == float("inf"), torch.isnan(z)
+    assert bool((y[plus] == float("inf")).all()) and bool(torch.isnan(y[bad]).all())
+    there = torch.isfinite(z)
+    z = z[there].view(1, -1)
+    # 1 + erf and 1 + tanh have nothing of the left tails in 64 bits: erfc and the logistic function do
+    if act == "gelu":
+        a = z * 0.5 * torch.special.erfc(-z * 0.5 ** 0.5)
+    elif act == "gelu_tanh":
+        a = z * torch.sigmoid(2 * 0.7978845608028654 * (z + 0.044715 * z ** 3))
+    else:
+        a = ff.act64(act, z)[0]
+    ff.check("y", y[there].view(1, -1), ff.rounded(a, ff.ACT_ERR * a.abs(), dt))
+
+
 @pytest.mark.parametrize("M", [1, 20, 300])
 def test_whole_numbers(B, M):
     """Sums of whole numbers below 2^24 are exact, whatever their order."""
