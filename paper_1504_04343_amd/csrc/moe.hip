@@ -12,12 +12,12 @@
 // The two products are those of few rows (ff_rows.hip): weights go from memory into the registers of the matrix cores, waves take
 // steps in turn, their sums meet in LDS in a fixed order.  A token's results do not depend on the other tokens.
 //
-// us of each kernel, bf16 (the last fp16):                                             logits route gated down join   weights
-//   1 token, 2 of 16 experts, 4096 -> 8192                                                5      -    56   31   -     403 MB
-//   16 tokens, 4 of 64 experts, 2048 -> 2048                                              7      7   130   75   5    1038 MB
-//   37 tokens, 3 of 24 experts, 1000 -> 1531, rows at odd distances                       7     10    39   32   5     219 MB
-// The products run at 4.9 to 5.3 TB/s where there are weights enough to fill the chip; what is in front of and behind them are launches.
-// Rows at odd addresses take two requests for each load.
+// us of each kernel, bf16 (the last fp16):                                        logits route gated down join   weights
+//   1 token, 2 of 16 experts, 4096 -> 8192                                             5     -    56   31    -    403 MB
+//   16 tokens, 4 of 64 experts, 2048 -> 2048                                           7     7   130   75    5   1038 MB
+//   37 tokens, 3 of 24 experts, 1000 -> 1531, rows at odd distances                    7    10    37   30    5    219 MB
+// The products read at 4.6 to 5.3 TB/s where there are weights enough to fill the chip; what is in front of and behind them are launches.
+// Of the last line's workgroups, two or three rounds of which fill the chip, each waits for its tokens' numbers, weights and sums in turn.
 #include <algorithm>
 
 #include "activation.h"
@@ -214,25 +214,27 @@ __device__ __forceinline__ void store_terms(const Moe& a, long long at, const fl
   }
 }
 
-// What is left of a row of n values from column k on, as a step's operand: behind the row's end zeros.
+// A step's operand from column k on of a row of n values, zeros behind its end: as it comes (of the last columns those that end with
+// the row), and brought into place, which waits for it.
 template <int TYPE>
-__device__ __forceinline__ typename Step<TYPE>::V row_tail(const void* p, long long row, int k, int n) {
+__device__ __forceinline__ typename Step<TYPE>::V tail_raw(const void* p, long long row, int k, int n) {
+  typedef Step<TYPE> S;
+  if (n >= S::CH) return S::load(p, row + min(k, n - S::CH));
+  return S::part(p, row, k == 0 ? n : 0);
+}
+template <int TYPE>
+__device__ __forceinline__ typename Step<TYPE>::V tail_settled(typename Step<TYPE>::V v, int k, int n) {
+  typedef Step<TYPE> S;
+  const int left = n - k;
+  if (left >= S::CH || n < S::CH) return v;
+  if (left <= 0) return typename S::V{};
   if constexpr (TYPE == CCT_TYPE_F32) {
-    typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-    const float* at = (const float*)p + row;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (k + 4 <= n) return *(const f32x4u*)(at + k);
-    if (k >= n) return v;
-    if (n >= 4) {  // with those in front of them: one load
-      const f32x4 u = *(const f32x4u*)(at + n - 4);
-      return n - k == 1 ? f32x4{u[3], 0.f, 0.f, 0.f} : n - k == 2 ? f32x4{u[2], u[3], 0.f, 0.f} : f32x4{u[1], u[2], u[3], 0.f};
-    }
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-      if (k + e < n) v[e] = at[k + e];
+    const int by = S::CH - left;
+    if (by & 1) v = f32x4{v[1], v[2], v[3], 0.f};
+    if (by & 2) v = f32x4{v[2], v[3], 0.f, 0.f};
     return v;
   } else {
-    return __builtin_bit_cast(typename Step<TYPE>::V, load_row_raw<TYPE>(p, row, k, n - k));
+    return move_down(v, S::CH - left);
   }
 }
 
@@ -285,40 +287,37 @@ __global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < RM; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int whole = a.D / S::K;
+    const int whole = a.D / S::K, steps = (a.D + S::K - 1) / S::K;  // the last one may end within
     V w[BATCH][2], x[BATCH][RM];
-    for (int s0 = wave; s0 < whole; s0 += BATCH * NW) {
+    for (int s0 = wave; s0 < steps; s0 += BATCH * NW) {
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
-        if (s0 + q * NW >= whole) break;
-        const long long k = (long long)(s0 + q * NW) * S::K + kq;
-        w[q][0] = S::load(a.wg.p, g_at + k);
-        w[q][1] = S::load(a.wu.p, u_at + k);
+        const int step = s0 + q * NW, k = step * S::K + kq;
+        if (step >= steps) break;
+        auto operand = [&](const void* p, long long at) { return step < whole ? S::load(p, at + k) : tail_raw<TYPE>(p, at, k, a.D); };
+        w[q][0] = operand(a.wg.p, g_at);
+        w[q][1] = operand(a.wu.p, u_at);
 #pragma unroll
         for (int i = 0; i < RM; ++i)
-          if (i == 0 || i * 16 < n) x[q][i] = i * 16 + lo < n ? S::load(a.x, x_at[i] + k) : V{};  // lanes without a token ask for nothing
+          if (i == 0 || i * 16 < n) x[q][i] = i * 16 + lo < n ? operand(a.x, x_at[i]) : V{};  // lanes without a token ask for nothing
       }
       __builtin_amdgcn_sched_barrier(0);  // the loads in front of it are not moved behind
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
-        if (s0 + q * NW >= whole) break;
+        const int step = s0 + q * NW, k = step * S::K + kq;
+        if (step >= steps) break;
+        if (step >= whole) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) w[q][b] = tail_settled<TYPE>(w[q][b], k, a.D);
+#pragma unroll
+          for (int i = 0; i < RM; ++i) x[q][i] = tail_settled<TYPE>(x[q][i], k, a.D);
+        }
 #pragma unroll
         for (int i = 0; i < RM; ++i)
           if (i == 0 || i * 16 < n)
 #pragma unroll
             for (int b = 0; b < 2; ++b) acc[b][i] = S::mfma(w[q][b], x[q][i], acc[b][i]);
       }
-    }
-    if (a.D % S::K && whole % NW == wave) {
-      const int k = whole * S::K + kq;
-      const V wv[2] = {row_tail<TYPE>(a.wg.p, g_at, k, a.D), row_tail<TYPE>(a.wu.p, u_at, k, a.D)};
-#pragma unroll
-      for (int i = 0; i < RM; ++i)
-        if (i == 0 || i * 16 < n) {
-          const V xv = row_tail<TYPE>(a.x, x_at[i], k, a.D);
-#pragma unroll
-          for (int b = 0; b < 2; ++b) acc[b][i] = S::mfma(wv[b], xv, acc[b][i]);
-        }
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -389,49 +388,37 @@ __global__ __launch_bounds__((ONE ? 16 : 8) * 64) void moe_down_kernel(Moe a, Ff
     f32x4 acc[RM];
 #pragma unroll
     for (int i = 0; i < RM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int whole = a.F / S::K, total = count * whole;
+    const int whole = a.F / S::K, steps = (a.F + S::K - 1) / S::K, total = count * steps;  // an expert's last step may end within
     V w[BATCH], h[BATCH][RM][TERMS];
-    auto fetch = [&](int q, int slot, long long k) {
-#pragma unroll
-      for (int i = 0; i < RM; ++i)
-        if (i == 0 || i * 16 < n) {
-          const bool there = i * 16 + lo < n;  // lanes without a token ask for nothing
-          const long long at = h_at[i] + (ONE ? slot * (long long)a.Fp : 0) + k;
-          h[q][i][0] = there ? S::load(a.h, at) : V{};
-          if constexpr (TERMS == 2) h[q][i][1] = there ? S::load(a.h_low, at) : V{};
-        }
-    };
-    auto multiply = [&](int q, const V& wv) {
-#pragma unroll
-      for (int i = 0; i < RM; ++i)
-        if (i == 0 || i * 16 < n)
-#pragma unroll
-          for (int t = 0; t < TERMS; ++t) acc[i] = S::mfma(wv, h[q][i][t], acc[i]);
-    };
-    auto expert = [&](int slot) { return (ONE ? (int)chosen[slot] : e) * a.wd.e; };
     for (int s0 = wave; s0 < total; s0 += BATCH * NW) {
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
-        const int step = s0 + q * NW, slot = ONE ? step / whole : 0;
-        if (step >= total) break;
-        const long long k = (long long)(step - slot * whole) * S::K + kq;
-        w[q] = S::load(a.wd.p, expert(slot) + w_row + k);
-        fetch(q, slot, k);
+        const int at = s0 + q * NW, slot = ONE ? at / steps : 0, step = at - slot * steps, k = step * S::K + kq;
+        if (at >= total) break;
+        const long long row_of_w = (ONE ? (int)chosen[slot] : e) * a.wd.e + w_row;
+        w[q] = step < whole ? S::load(a.wd.p, row_of_w + k) : tail_raw<TYPE>(a.wd.p, row_of_w, k, a.F);
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+          if (i == 0 || i * 16 < n) {
+            const bool there = i * 16 + lo < n;  // lanes without a token ask for nothing
+            const long long h_of = h_at[i] + (ONE ? slot * (long long)a.Fp : 0) + k;
+            h[q][i][0] = there ? S::load(a.h, h_of) : V{};
+            if constexpr (TERMS == 2) h[q][i][1] = there ? S::load(a.h_low, h_of) : V{};
+          }
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
-        if (s0 + q * NW >= total) break;
-        multiply(q, w[q]);
+        const int at = s0 + q * NW, step = ONE ? at % steps : at;
+        if (at >= total) break;
+        if (step >= whole) w[q] = tail_settled<TYPE>(w[q], step * S::K + kq, a.F);
+#pragma unroll
+        for (int i = 0; i < RM; ++i)
+          if (i == 0 || i * 16 < n)
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) acc[i] = S::mfma(w[q], h[q][i][t], acc[i]);
       }
     }
-    if (a.F % S::K)
-      for (int slot = (total + wave) % NW; slot < count; slot += NW) {
-        const int k = whole * S::K + kq;
-        w[0] = row_tail<TYPE>(a.wd.p, expert(slot) + w_row, k, a.F);
-        fetch(0, slot, k);
-        multiply(0, w[0]);
-      }
 #pragma unroll
     for (int i = 0; i < RM; ++i) sums[wave][i][lane] = acc[i];
     __syncthreads();

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_kernel(MxJob j, const vo
 #pragma unroll
     for (int q = 0; q < kRows; ++q) {
       const long long row = r0 + q * down;
-      const f32x8 v = __builtin_convertvector(raw[q], f32x8);
+      const f32x8 v = __builtin_convertvector(settle_row<TYPE>(raw[q], c, n), f32x8);
       unsigned most = 0;  // sizes compare as whole numbers, infinities and NaN above all others
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = max(most, __builtin_bit_cast(unsigned, (float)v[e]) & 0x7fffffffu);

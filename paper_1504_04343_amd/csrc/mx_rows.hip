@@ -29,6 +29,7 @@ __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart pa
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lo = lane & 15, q = lane >> 4;
   const int steps = pieces(a.blocks, 4), tiles = pieces(p.N, 16), tall = pieces(p.M, RM * 16);
   const int split = SPLIT ? blockIdx.z : 0;
+  const bool eights = p.K % 8 == 0;
   const int first = SPLIT ? split * part.stages : 0, end = SPLIT ? min(steps, first + part.stages) : steps;
   __shared__ f32x4 sums[NW][RM][64];
   for (int mb = blockIdx.y; mb < tall; mb += gridDim.y)
@@ -63,7 +64,12 @@ __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart pa
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
               const int col = block * kMxBlock + c * 8;
-              t.v[j][c] = load_row_raw<TYPE>(a.x.codes, min((long long)m0 + lo, p.M - 1LL) * a.x.ldc, col, p.K - col);
+              const long long row = min((long long)m0 + lo, p.M - 1LL) * a.x.ldc;
+              if (eights)  // less between the loads and their use
+                t.v[j][c] = col < p.K ? *(const typename Number<TYPE>::U8*)((const typename Number<TYPE>::T*)a.x.codes + row + col)
+                                      : typename Number<TYPE>::V8{};
+              else
+                t.v[j][c] = load_row_raw<TYPE>(a.x.codes, row, col, p.K - col);
             }
           } else {
 #pragma unroll
@@ -71,12 +77,20 @@ __global__ __launch_bounds__(NW * 64) void mx_rows_kernel(MxProduct a, FfPart pa
           }
         }
       };
-      auto multiply = [&](const Turn& t, int s0) {
+      auto multiply = [&](Turn& t, int s0) {
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
           i32x4 own = {};
           int own_scale = 127;
-          if constexpr (QUANTIZE) own = mx_quantize_block<TYPE>(t.v[j], &own_scale);
+          if constexpr (QUANTIZE) {
+            if (!eights)
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const int col = min((s0 + j) * 4 + q, a.blocks - 1) * kMxBlock + c * 8;
+                t.v[j][c] = settle_row<TYPE>(t.v[j][c], col, p.K - col);
+              }
+            own = mx_quantize_block<TYPE>(t.v[j], &own_scale);
+          }
           const bool live = s0 + j < end && (s0 + j) * 4 + q < a.blocks;
           const i32x4 w = live ? t.w[j] : i32x4{0, 0, 0, 0};
           const int sw = live ? (int)((unsigned)t.ws[j] >> (8 * q)) : 127;

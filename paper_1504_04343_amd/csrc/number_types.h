@@ -72,24 +72,29 @@ __device__ __forceinline__ V8 move_down(V8 v, int by) {
     return v;
   }
 }
-// 8 values from column c on of a row that begins at `row` and has c + n values; zeros behind its end.  The last ones come with
-// those in front of them: one by one they were up to 7 trips to memory (a backward pass of norms, 1531 x 2049: 53 us for 30).
+// 8 values from column c on of a row that begins at `row` and has c + n values, zeros behind its end: as they come from memory
+// (of a row's last columns the eight that end with it), and brought into place, which waits for them.  One by one the last values were up
+// to 7 trips to memory, in place as they come one for each load (backward pass of norms, 1531 x 2049: 53, 41 and 39 us).
 template <int TYPE>
 __device__ __forceinline__ typename Number<TYPE>::V8 load_row_raw(const void* p, long long row, int c, int n) {
-  typedef typename Number<TYPE>::V8 V8;
-  const auto* at = (const typename Number<TYPE>::T*)p + row + c;
-  V8 v = {};
-  if (n >= 8) return *(const typename Number<TYPE>::U8*)at;
-  if (n <= 0) return v;
-  if (c > 0) return move_down<V8>(*(const typename Number<TYPE>::U8*)(at + n - 8), 8 - n);
+  const auto* at = (const typename Number<TYPE>::T*)p + row;
+  if (c + n >= 8) return *(const typename Number<TYPE>::U8*)(at + min(c, c + n - 8));
+  typename Number<TYPE>::V8 v = {};
+  if (c == 0)
 #pragma unroll
-  for (int e = 0; e < 7; ++e)
-    if (e < n) v[e] = at[e];
+    for (int e = 0; e < 7; ++e)
+      if (e < n) v[e] = at[e];
   return v;
 }
 template <int TYPE>
+__device__ __forceinline__ typename Number<TYPE>::V8 settle_row(typename Number<TYPE>::V8 v, int c, int n) {
+  if (n >= 8 || c + n < 8) return v;
+  if (n <= 0) return typename Number<TYPE>::V8{};
+  return move_down(v, 8 - n);
+}
+template <int TYPE>
 __device__ __forceinline__ f32x8 load_row(const void* p, long long row, int c, int n) {
-  return __builtin_convertvector(load_row_raw<TYPE>(p, row, c, n), f32x8);
+  return __builtin_convertvector(settle_row<TYPE>(load_row_raw<TYPE>(p, row, c, n), c, n), f32x8);
 }
 // The first n of 8 values.
 template <int TYPE>

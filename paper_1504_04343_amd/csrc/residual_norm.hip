@@ -129,13 +129,18 @@ __global__ __launch_bounds__(1024) void residual_norm_long_kernel(ResidualNorm p
   }
 }
 
-// load_row and store_first where a row is whole eights (EIGHTS): less code and fewer registers.
+// load_row_raw, settle_row and store_first where a row is whole eights (EIGHTS): less code and fewer registers.
 template <int TYPE, bool EIGHTS>
 __device__ __forceinline__ typename Number<TYPE>::V8 row_raw(const void* p, long long row, int c, int n) {
   if constexpr (!EIGHTS) return load_row_raw<TYPE>(p, row, c, n);
   typename Number<TYPE>::V8 v = {};
   if (n > 0) v = *(const typename Number<TYPE>::U8*)((const typename Number<TYPE>::T*)p + row + c);
   return v;
+}
+template <int TYPE, bool EIGHTS>
+__device__ __forceinline__ f32x8 settled(const typename Number<TYPE>::V8& v, int c, int n) {
+  if constexpr (EIGHTS) return __builtin_convertvector(v, f32x8);
+  return __builtin_convertvector(settle_row<TYPE>(v, c, n), f32x8);
 }
 template <int TYPE, bool EIGHTS>
 __device__ __forceinline__ void store_row(void* p, long long i, const f32x8& v, int n) {
@@ -147,7 +152,10 @@ __device__ __forceinline__ void store_row(void* p, long long i, const f32x8& v, 
 template <int TYPE, bool EIGHTS>
 __device__ __forceinline__ typename Number<TYPE>::V8 row_vector(const void* p, int c, int n, float none) {
   typename Number<TYPE>::V8 v;
-  if (p) return row_raw<TYPE, EIGHTS>(p, 0, c, n);
+  if (p) {
+    v = row_raw<TYPE, EIGHTS>(p, 0, c, n);
+    return EIGHTS ? v : settle_row<TYPE>(v, c, n);
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (typename Number<TYPE>::T)none;
   return v;
@@ -199,9 +207,9 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(ResidualNorm p, boo
   }
   for (long long row = first; row < p.M; row += stride) {
     if (!AHEAD && row != first) load(row);
-    f32x8 s = wide(r), v, g;
-    if (p.b) v = wide(b);
-    if (p.gate) g = wide(gate);
+    f32x8 s = settled<TYPE, EIGHTS>(r, c, n), v, g;
+    if (p.b) v = settled<TYPE, EIGHTS>(b, c, n);
+    if (p.gate) g = settled<TYPE, EIGHTS>(gate, c, n);
     if (AHEAD && row + stride < p.M) load(row + stride);
     if (p.b) {
       if (p.after != CCT_NORM_NONE) {
@@ -370,10 +378,10 @@ constexpr bool norm_sums_in_lds = THREADS > 512;
 // The same of rows of up to 8192 columns in one pass: a thread has 8 columns, a workgroup a run of rows, one at a time, or its waves
 // one each where 512 columns are all (in spans: of a gate row's rows, so that its sum is one wave's).  The next row is on its way
 // while one is worked on; its sums over columns stay with the thread.  Between a row's loads and stores its waves meet two or three
-// times, which is what the time went into (8192 x 4096, bf16, two norms and a gate: 84 to 100 us by
-// card, 79 at a copy's rate; 15 more with sums over waves that read LDS one after the other); the runs' sums and their joining take
-// 6 to 10 us more.  1531 x 2049 fp16, layer norms, a gate row for 37: 35 us, 5 for each of a workgroup's seven rows: five waves, of which
-// a CU has one workgroup, wait for the sums (three meetings) with nothing beside them.
+// times, which is what the time went into (8192 x 4096, bf16, two norms and a gate: 84 to 100 us by card, 79 at a copy's rate; 15
+// more with sums over waves that read LDS one after the other); the runs' sums and their joining take 6 to 10 us more.  1531 x 2049
+// fp16, layer norms, a gate row for 37: 33 us, 2048 columns 21: five waves, of which a CU takes one workgroup (two do not start
+// together: 41), wait for one another with nothing beside them.
 template <int TYPE, int THREADS, bool EIGHTS>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS <= 512 ? 2 : 4))) void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {
   typedef typename Number<TYPE>::V8 V8;
@@ -439,13 +447,13 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
     }
 
     f32x8 ds = {}, dh = {}, n_s = {}, n_b = {}, dn = {};
-    if (p.ds) ds = __builtin_convertvector(at.ds, f32x8);
+    if (p.ds) ds = settled<TYPE, EIGHTS>(at.ds, c, n);
     if (p.dh) {
-      dh = __builtin_convertvector(at.dh, f32x8);
-      n_s = __builtin_convertvector(at.s, f32x8);
+      dh = settled<TYPE, EIGHTS>(at.dh, c, n);
+      n_s = settled<TYPE, EIGHTS>(at.s, c, n);
       dn = dh * __builtin_convertvector(raw_before, f32x8);
     }
-    if (p.b) n_b = __builtin_convertvector(at.b, f32x8);
+    if (p.b) n_b = settled<TYPE, EIGHTS>(at.b, c, n);
     float level_s = 0.f;
     const bool layer_s = p.dh && p.before == CCT_NORM_LAYER, layer_b = block && p.after == CCT_NORM_LAYER;
     if (layer_s || layer_b) {
@@ -479,7 +487,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
           sums.v[kDgate] = f32x8{};
         }
       }
-      dp *= __builtin_convertvector(at.gate, f32x8);
+      dp *= settled<TYPE, EIGHTS>(at.gate, c, n);
     }
     if (block) {
       add(std::integral_constant<int, kDcAfter>(), dp);
@@ -664,7 +672,8 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
     ProfScope ps("residual_norm_join_kernel", 0.0, 0.0, st);
     with_type(p.type, [&](auto type) {
       hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_join_kernel<decltype(type)::value>),
-                         dim3(std::min(pieces(p.D, 32), 1 << 20), kDgate + (gate ? plan.count / plan.per_gate : 0)), dim3(kJoinRows * 32), 0, st, p, plan, part);
+                         dim3(std::min(pieces(p.D, 32), 1 << 20), kDgate + (gate ? plan.count / plan.per_gate : 0)),
+                         dim3(kJoinRows * 32), 0, st, p, plan, part);
     });
     CCT_CHECK_LAUNCH();
   }
