@@ -32,12 +32,13 @@ void with_bool(bool b, F f) {
 }
 
 constexpr int kMostWaves = 16, kRegisterColumns = kMostWaves * 512;
-constexpr int kNormTeams = 4;  // rows of up to 512 columns that a workgroup takes
+constexpr int kNormTeams = 4;  // rows of up to 512 columns that a workgroup takes at a time
 // Sums over a workgroup's waves, in all threads.  Two places in LDS in turn: a wave that is a sum ahead does not write over what
 // others still read.  Each lane reads one wave's sum: one after the other they were a trip to LDS each.
 struct RowSums {
   float (*lds)[4][kMostWaves];
   int waves, turn;
+  int first = 0;  // of the workgroup's waves
   template <int N>
   __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
@@ -50,7 +51,7 @@ struct RowSums {
       for (int i = 0; i < N; ++i) lds[turn][i][threadIdx.x >> 6] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lane < waves ? lds[turn][i][lane] : 0.f;
+    for (int i = 0; i < N; ++i) v[i] = lane < waves ? lds[turn][i][first + lane] : 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = row_sum(v[i]);
   }
@@ -372,32 +373,33 @@ __global__ __launch_bounds__(kColumnThreads) void residual_norm_columns_kernel(R
 
 // Where the norms' sums are: LDS, so that 128 registers are enough for two workgroups on a CU; the next row of fp32 values leaves
 // no room for that, up to 512 threads they have 256.
-template <int TYPE, int THREADS>
-constexpr bool norm_sums_in_lds = THREADS > 512;
+template <int THREADS>
+constexpr bool norm_sums_in_lds = THREADS == 1024;
 
-// The same of rows of up to 8192 columns in one pass: a thread has 8 columns, a workgroup a run of rows, one at a time, or its waves
-// one each where 512 columns are all (in spans: of a gate row's rows, so that its sum is one wave's).  The next row is on its way
-// while one is worked on; its sums over columns stay with the thread.  Between a row's loads and stores its waves meet two or three
-// times, which is what the time went into (8192 x 4096, bf16, two norms and a gate: 84 to 100 us by card, 79 at a copy's rate; 15
-// more with sums over waves that read LDS one after the other); the runs' sums and their joining take 6 to 10 us more.  1531 x 2049
-// fp16, layer norms, a gate row for 37: 33 us, 2048 columns 21: five waves, of which a CU takes one workgroup (two do not start
-// together: 41), wait for one another with nothing beside them.
+// The same of rows of up to 8192 columns in one pass: a thread has 8 columns, a workgroup a run of rows, one at a time, or as many as
+// it has teams of waves for a row each (in spans: of a gate row's rows, so that its sum is one team's): four of one wave where 512
+// columns are all, two of five or six.  The next row is on its way while one is worked on; its sums over columns stay with the thread.
+// Between a row's loads and stores its waves meet two or three times, which is what the time went into (8192 x 4096, bf16, two norms
+// and a gate: 84 to 100 us by card, 79 at a copy's rate; 15 more with sums over waves that read LDS one after the other); the runs'
+// sums and their joining take 6 to 10 us more.  Two teams, since a CU starts no second workgroup of five waves: 8192 x 2560 89 -> 67 us,
+// 1531 x 2049 fp16 with layer norms 39 -> 34 (two such workgroups a CU in the plan: 46).
 template <int TYPE, int THREADS, bool EIGHTS>
-__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS <= 512 ? 2 : 4))) void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {
+__global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS / 256 < 2 ? 2 : THREADS / 256)))
+void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {
   typedef typename Number<TYPE>::V8 V8;
-  constexpr bool AHEAD = THREADS <= 512, IN_LDS = norm_sums_in_lds<TYPE, THREADS>;
+  constexpr bool IN_LDS = norm_sums_in_lds<THREADS>, AHEAD = !IN_LDS;
   __shared__ float lds[2][4][kMostWaves];
-  __shared__ float meet[AHEAD ? kNormTeams : 1][512];
+  __shared__ __attribute__((aligned(16))) float meet[THREADS == 512 ? (kNormTeams - 1) * 512 : THREADS == 768 ? 6 * 512 : 1];
   extern __shared__ f32x4 norm_sums[];
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const bool teams = AHEAD && p.D <= 512;
-  RowSums total = {lds, teams ? 1 : waves, 0};
-  const int c = (teams ? threadIdx.x & 63 : threadIdx.x) * 8, n = p.D - c;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = (p.D + 511) >> 9;  // of a team
+  const int teams = AHEAD ? (int)(blockDim.x >> 6) / waves : 1, team = AHEAD ? wave / waves : 0, thread = threadIdx.x - team * waves * 64;
+  RowSums total = {lds, waves, 0, team * waves};
+  const int c = thread * 8, n = p.D - c;
   const float D = (float)p.D;
   const bool block = p.b && p.after != CCT_NORM_NONE;
   const NormRun run = norm_run(p, plan, blockIdx.x);
   const int span = plan.whole ? p.gate_rows : 1;
-  const long long skip = teams ? (long long)(waves - 1) * span : 0;
+  const long long begin = (long long)team * span, skip = (long long)(teams - 1) * span;
   const V8 raw_before = row_vector<TYPE, EIGHTS>(p.w_before, c, n, 1.f), raw_after = row_vector<TYPE, EIGHTS>(p.w_after, c, n, 1.f),
            raw_c = row_vector<TYPE, EIGHTS>(p.c_after, c, n, 0.f);
   ColumnSums sums = {};
@@ -430,12 +432,12 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
       if (before < 0 || g != (unsigned)before / (unsigned)p.gate_rows) to.gate = row_raw<TYPE, EIGHTS>(p.gate, (long long)g * p.ldgate, c, n);
     }
   };
-  long long row = run.first + (teams ? (long long)wave * span : 0);
+  long long row = run.first + begin;
   int left = span;
   Row at = {};
   if (AHEAD && row < run.end) load(at, row, -1);
-  while (row < run.end) {
-    const bool turn = left == 1;
+  while (row - begin < run.end) {  // all teams as often as the first one, for their meetings
+    const bool live = row < run.end, turn = left == 1;
     const long long next = row + 1 + (turn ? skip : 0);
     left = turn ? span : left - 1;
     Row ahead;
@@ -472,15 +474,17 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
       n_s *= rstd;
       ds += (dn - n_s * (t[1] * rstd / D) - level_s) * rstd;
     }
-    if (p.dr) store_row<TYPE, EIGHTS>(p.dr, row * p.lddr + c, ds, n);
-    add(std::integral_constant<int, kDcBefore>(), dh);
-    add(std::integral_constant<int, kDwBefore>(), dh * n_s);
+    if (live) {
+      if (p.dr) store_row<TYPE, EIGHTS>(p.dr, row * p.lddr + c, ds, n);
+      add(std::integral_constant<int, kDcBefore>(), dh);
+      add(std::integral_constant<int, kDwBefore>(), dh * n_s);
+    }
     f32x8 dp = ds * p.scale;
     const float rstd_b = block ? rstd_of(t[2], p.D, p.eps) : 1.f;
     if (block) n_b *= rstd_b;
     const f32x8 w_after = __builtin_convertvector(raw_after, f32x8);
     if (p.gate) {
-      if (p.out[kDgate]) {
+      if (p.out[kDgate] && live) {
         sums.v[kDgate] += dp * (n_b * w_after + __builtin_convertvector(raw_c, f32x8));
         if (plan.whole && (turn || row + 1 == run.end)) {
           store_row<TYPE, EIGHTS>(p.out[kDgate], (long long)((unsigned)row / (unsigned)p.gate_rows) * p.lddgate + c, sums.v[kDgate], n);
@@ -490,8 +494,10 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
       dp *= settled<TYPE, EIGHTS>(at.gate, c, n);
     }
     if (block) {
-      add(std::integral_constant<int, kDcAfter>(), dp);
-      add(std::integral_constant<int, kDwAfter>(), dp * n_b);
+      if (live) {
+        add(std::integral_constant<int, kDcAfter>(), dp);
+        add(std::integral_constant<int, kDwAfter>(), dp * n_b);
+      }
       if (p.db) {
         dp *= w_after;
         float u[2] = {sum8(dp * n_b), sum8(dp)};
@@ -499,7 +505,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
         dp = (dp - n_b * (u[0] / D) - (layer_b ? u[1] / D : 0.f)) * rstd_b;
       }
     }
-    if (p.db) store_row<TYPE, EIGHTS>(p.db, row * p.lddb + c, dp, n);
+    if (p.db && live) store_row<TYPE, EIGHTS>(p.db, row * p.lddb + c, dp, n);
     if constexpr (AHEAD) at = ahead;
     row = next;
   }
@@ -509,13 +515,13 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS
     if (!p.out[k] || (k == kDgate && plan.whole)) continue;
     if constexpr (IN_LDS)
       if (k != kDgate) sums.v[k] = __builtin_shufflevector(*own(k, 0), *own(k, 1), 0, 1, 2, 3, 4, 5, 6, 7);
-    if (teams) {
-      *(f32x8*)&meet[wave][c] = sums.v[k];
+    if (AHEAD && teams > 1) {
+      if (team > 0) *(f32x8*)&meet[((team - 1) * waves * 64 + thread) * 8] = sums.v[k];
       __syncthreads();
-      if (wave == 0)
-        for (int w = 1; w < waves; ++w) sums.v[k] += *(const f32x8*)&meet[w][c];
+      if (team == 0)
+        for (int t = 1; t < teams; ++t) sums.v[k] += *(const f32x8*)&meet[((t - 1) * waves * 64 + thread) * 8];
       __syncthreads();
-      if (wave > 0) continue;
+      if (team > 0) continue;
     }
     if (plan.count == 1)  // nothing to join
       store_first<TYPE>(p.out[k], c, sums.v[k], n);
@@ -629,21 +635,22 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
     int rc = CCT_OK;
     with_type(p.type, [&](auto type) {
       constexpr int TYPE = decltype(type)::value;
-      const int threads = p.D <= 512 ? kNormTeams * 64 : row_threads(p.D);
+      const int waves = pieces(p.D, 512), teams = p.D <= 512 ? kNormTeams : TYPE != CCT_TYPE_F32 && (waves == 5 || waves == 6) ? 2 : 1;
+      const int threads = teams * waves * 64;
       with_bool(p.D % 8 == 0, [&](auto eights) {
         constexpr bool EIGHTS = decltype(eights)::value;
         auto run = [&](auto most) {
           constexpr int THREADS = decltype(most)::value;
-          const int lds = norm_sums_in_lds<TYPE, THREADS> ? kDgate * THREADS * 32 : 0;
+          const int lds = norm_sums_in_lds<THREADS> ? kDgate * THREADS * 32 : 0;
           if (lds) rc = ensure_dynamic_lds<residual_norm_back_kernel<TYPE, THREADS, EIGHTS>>(lds);
           if (rc == CCT_OK)
             hipLaunchKernelGGL(HIP_KERNEL_NAME(residual_norm_back_kernel<TYPE, THREADS, EIGHTS>), dim3(plan.count), dim3(threads), lds,
                                st, p, plan, part);
         };
-        if (threads <= 512)
-          run(std::integral_constant<int, 512>());
-        else
-          run(std::integral_constant<int, 1024>());
+        if (threads <= 512) return run(std::integral_constant<int, 512>());
+        if constexpr (TYPE != CCT_TYPE_F32)
+          if (teams == 2) return run(std::integral_constant<int, 768>());
+        run(std::integral_constant<int, 1024>());
       });
     });
     if (rc != CCT_OK) return rc;

@@ -103,7 +103,10 @@ SHAPES = [(1, 1, "rms", "rms", 1, True, 0, 0), (1, 7, "layer", "rms", 1, True, 0
           (2100, 520, "rms", "none", 2100, False, 0, 0), (40, 8200, "rms", "layer", 13, True, 0, 0), (9, 16387, "layer", "rms", 1, True, 1, 1),
           (2, 33000, "rms", "none", 2, False, 0, 0), (6, 3000, "none", "none", 3, False, 0, 0), (4, 1536, "none", "layer", 0, True, 2, 0),
           (37, 5000, "layer", "rms", 5, True, 3, 1), (300, 4104, "rms", "layer", 300, True, 0, 0), (70, 8191, "rms", "rms", 9, False, 0, 0),
-          (4, 500, "rms", "rms", 4, True, 0, 0), (3, 4200, "layer", "layer", 5, True, 0, 0), (2049, 512, "rms", "layer", 700, True, 0, 0)]
+          (4, 500, "rms", "rms", 4, True, 0, 0), (3, 4200, "layer", "layer", 5, True, 0, 0), (2049, 512, "rms", "layer", 700, True, 0, 0),
+          # two rows at a time: runs that end in the first, in the second and within a gate row
+          (2, 2300, "layer", "rms", 1, True, 0, 0), (301, 2500, "layer", "layer", 3, True, 5, 1), (1100, 2560, "rms", "rms", 1100, False, 0, 0),
+          (1027, 2816, "rms", "layer", 2, True, 8, 0), (205, 2049, "layer", "layer", 37, True, 3, 3), (13, 2568, "none", "rms", 6, True, 0, 0)]
 IDS = ["%dx%d-%s-%s-%d+%d@%d" % (s[:5] + s[6:]) for s in SHAPES]
 
 
