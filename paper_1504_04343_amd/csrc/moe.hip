@@ -7,8 +7,9 @@
 //                      chooses for itself, which takes less than a launch);
 //   moe_gated_kernel   16 columns of both gate and up of one used expert and its tokens: weight * act(g) * u, kept as two 16-bit
 //                      terms (16 bits of a value in bf16, 22 in fp16; fp32 as it is), both of which the next product multiplies;
-//   moe_down_kernel    16 columns of one used expert's results and its tokens, or of all experts' for a single token;
-//   moe_join_kernel    (more than one token) a token's results added in the order of its choice, and the residual.
+//   moe_down_kernel    16 columns of one used expert's results and its tokens, or of all experts' for a single token (where that
+//                      keeps the chip busy);
+//   moe_join_kernel    (unless a workgroup had all experts') a token's results added in the order of its choice, and the residual.
 // The two products are those of few rows (ff_rows.hip): weights go from memory into the registers of the matrix cores, waves take
 // steps in turn, their sums meet in LDS in a fixed order.  A token's results do not depend on the other tokens.
 //
@@ -238,13 +239,12 @@ __device__ __forceinline__ typename Step<TYPE>::V tail_settled(typename Step<TYP
   }
 }
 
-constexpr int kGatedWaves = 8;
-// RM: blocks of 16 tokens that are multiplied at once; ONE: a single token, whose experts are not chosen yet
-template <int TYPE, int RM, bool ONE>
-__global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
+// RM: blocks of 16 tokens that are multiplied at once; ONE: a single token, whose experts are not chosen yet; NW: waves
+template <int TYPE, int RM, bool ONE, int NW>
+__global__ __launch_bounds__(NW * 64) void moe_gated_kernel(Moe a) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
-  constexpr int NW = kGatedWaves, BATCH = ONE ? 8 : 4;
+  constexpr int BATCH = ONE ? 8 : 4;
   extern __shared__ __attribute__((aligned(16))) unsigned char moe_smem[];
   f32x4(*sums)[2 * RM][64] = (f32x4(*)[2 * RM][64])moe_smem;  // [NW]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -255,7 +255,14 @@ __global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
     int which;
     float of;
     select_experts(a, 0, lane, &which, &of);
-    if (blockIdx.x == 0 && slot == 0 && wave == 0) write_selected(a, 0, lane, which, of);
+    if (blockIdx.x == 0 && slot == 0 && wave == 0) {
+      write_selected(a, 0, lane, which, of);
+      if (lane < a.k) {
+        a.slot[2 * lane] = which;
+        a.slot[2 * lane + 1] = 1;
+      }
+      for (int j = 0; j < a.k; ++j) a.rows[j * kMostTokens + lane] = (short)j;
+    }
     e = __builtin_amdgcn_readlane(which, slot);
     row[0] = slot;
     weight[0] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, of), slot));
@@ -327,7 +334,7 @@ __global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
 #pragma unroll
     for (int i = 0; i < RM; ++i) {
       const int at = f0 + (lane >> 4) * 4;
-      if (wave != i || i * 16 + lo >= n) continue;
+      if (wave != i % NW || i * 16 + lo >= n) continue;
       float g[4], u[4];
       f32x4 s[2];
 #pragma unroll
@@ -351,11 +358,11 @@ __global__ __launch_bounds__(kGatedWaves * 64) void moe_gated_kernel(Moe a) {
 
 // The down product.  ONE: a single token, whose chosen experts' features are one contraction; else an expert and its tokens, whose
 // results go to `part`.
-template <int TYPE, int RM, bool ONE>
-__global__ __launch_bounds__((ONE ? 16 : 8) * 64) void moe_down_kernel(Moe a, FfProduct p) {
+template <int TYPE, int RM, bool ONE, int NW>
+__global__ __launch_bounds__(NW * 64) void moe_down_kernel(Moe a, FfProduct p) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
-  constexpr int NW = ONE ? 16 : 8, TERMS = TYPE == CCT_TYPE_F32 ? 1 : 2, BATCH = ONE ? 8 : RM == 4 ? 2 : 4;
+  constexpr int TERMS = TYPE == CCT_TYPE_F32 ? 1 : 2, BATCH = ONE ? 8 : RM == 4 ? 2 : 4;
   static_assert(!ONE || RM == 1, "one token");
   extern __shared__ __attribute__((aligned(16))) unsigned char moe_smem[];
   f32x4(*sums)[RM][64] = (f32x4(*)[RM][64])moe_smem;  // [NW]
@@ -425,7 +432,7 @@ __global__ __launch_bounds__((ONE ? 16 : 8) * 64) void moe_down_kernel(Moe a, Ff
 #pragma unroll
     for (int i = 0; i < RM; ++i) {
       const int m = i * 16 + lo, c = n0 + (lane >> 4) * 4;
-      if (wave != i || m >= n || c >= a.D) continue;
+      if (wave != i % NW || m >= n || c >= a.D) continue;
       f32x4 s = sums[0][i][lane];
 #pragma unroll
       for (int q = 1; q < NW; ++q) s += sums[q][i][lane];
@@ -461,6 +468,18 @@ int launch_with_lds(dim3 grid, int threads, int lds, hipStream_t st, ARGS... arg
   return CCT_OK;
 }
 
+// Waves that a contraction of so many steps feeds (16 tokens, 8 of 64 experts, 1024 -> 512, bf16: 61 us, with eight always 67; 39, 8 of 99,
+// 2648 -> 141: 103 and 131; from 32 steps on eight are the fastest: 2 of 16, 4096 -> 8192: 89 us, with four 109).
+template <class F>
+void with_waves(int steps, F f) {
+  if (steps <= 8)
+    f(std::integral_constant<int, 2>());
+  else if (steps <= 24)
+    f(std::integral_constant<int, 4>());
+  else
+    f(std::integral_constant<int, 8>());
+}
+
 template <int TYPE, int RM>
 int launch(const Moe& a, const FfProduct& p, hipStream_t st) {
   const double size = type_bytes(TYPE), pairs = (double)a.T * a.k;
@@ -478,17 +497,26 @@ int launch(const Moe& a, const FfProduct& p, hipStream_t st) {
   {
     ProfScope ps("moe_gated_kernel", 4.0 * pairs * a.D * a.F, 2.0 * size * a.slots * (double)a.D * a.F, st);
     const dim3 grid(a.Fp / 16, a.slots);
-    constexpr int lds = kGatedWaves * 2 * RM * 1024;
-    rc = a.T == 1 ? launch_with_lds<moe_gated_kernel<TYPE, 1, true>>(grid, kGatedWaves * 64, lds, st, a)
-                           : launch_with_lds<moe_gated_kernel<TYPE, RM, false>>(grid, kGatedWaves * 64, lds, st, a);
+    with_waves(pieces(a.D, Step<TYPE>::K), [&](auto waves) {
+      constexpr int NW = decltype(waves)::value, lds = NW * 2 * 1024;
+      rc = a.T == 1 ? launch_with_lds<moe_gated_kernel<TYPE, 1, true, NW>>(grid, NW * 64, lds, st, a)
+                    : launch_with_lds<moe_gated_kernel<TYPE, RM, false, NW>>(grid, NW * 64, lds * RM, st, a);
+    });
     if (rc != CCT_OK) return rc;
   }
   const int tiles = pieces(a.D, 16);
   {
     ProfScope ps("moe_down_kernel", 2.0 * pairs * a.D * a.F, size * a.slots * (double)a.D * a.F, st);
-    rc = a.T == 1 ? launch_with_lds<moe_down_kernel<TYPE, 1, true>>(dim3(tiles), 1024, 16 * 1024, st, a, p)
-                  : launch_with_lds<moe_down_kernel<TYPE, RM, false>>(dim3(tiles, a.slots), 512, 8 * RM * 1024, st, a, p);
-    if (rc != CCT_OK || a.T == 1) return rc;
+    const int steps = pieces(a.F, Step<TYPE>::K);
+    // a single token's experts one after the other, unless that leaves half of the CUs idle for longer than a join takes (a step of a
+    // workgroup 0.045 us; 8 of 32 experts, 1024 -> 4096 and back: 64 us, 95 one after the other)
+    if (a.T == 1 && (tiles > 128 || (a.k - 1) * steps < 128))
+      return launch_with_lds<moe_down_kernel<TYPE, 1, true, 16>>(dim3(tiles), 1024, 16 * 1024, st, a, p);
+    with_waves(steps, [&](auto waves) {
+      constexpr int NW = decltype(waves)::value;
+      rc = launch_with_lds<moe_down_kernel<TYPE, RM, false, NW>>(dim3(tiles, a.slots), NW * 64, NW * RM * 1024, st, a, p);
+    });
+    if (rc != CCT_OK) return rc;
   }
   ProfScope ps("moe_join_kernel", 0.0, 4.0 * pairs * a.D + size * a.T * (double)a.D, st);
   hipLaunchKernelGGL(HIP_KERNEL_NAME(moe_join_kernel<TYPE>), dim3(pieces(a.Dp / 4, 256), a.T), dim3(256), 0, st, a, p);
@@ -539,7 +567,7 @@ long long lay_out(const cct_moe_desc_t& d, char* ws, Moe* a) {
   a->h = take((long long)type_bytes(d.type) * a->T * a->k * a->Fp);
   a->h_low = take(d.type == CCT_TYPE_F32 ? 0 : 2LL * a->T * a->k * a->Fp);
   a->Dp = (d.D + 3) / 4 * 4;
-  a->part = (float*)take(d.tokens <= 1 ? 0 : 4LL * a->T * a->k * a->Dp);
+  a->part = (float*)take(4LL * a->T * a->k * a->Dp);
   return std::max(total, 256LL);
 }
 

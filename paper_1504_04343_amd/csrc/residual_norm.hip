@@ -382,7 +382,7 @@ constexpr bool norm_sums_in_lds = THREADS == 1024;
 // Between a row's loads and stores its waves meet two or three times, which is what the time went into (8192 x 4096, bf16, two norms
 // and a gate: 84 to 100 us by card, 79 at a copy's rate; 15 more with sums over waves that read LDS one after the other); the runs'
 // sums and their joining take 6 to 10 us more.  Two teams, since a CU starts no second workgroup of five waves: 8192 x 2560 89 -> 67 us,
-// 1531 x 2049 fp16 with layer norms 39 -> 34 (two such workgroups a CU in the plan: 46).
+// 1531 x 2049 fp16 with layer norms 39 -> 34 (two such workgroups a CU in the plan were 49 for 41 then).
 template <int TYPE, int THREADS, bool EIGHTS>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS / 256 < 2 ? 2 : THREADS / 256)))
 void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {

@@ -73,7 +73,9 @@ class Case:
 SHAPES = [(1, 1, 1, 1, 1, 0, 0), (1, 4, 2, 7, 3, 0, 0), (1, 8, 2, 256, 512, 0, 0), (2, 3, 3, 33, 100, 1, 1), (3, 16, 4, 1000, 515, 0, 0),
           (5, 64, 8, 72, 40, 8, 0), (16, 8, 2, 128, 264, 0, 2), (17, 6, 2, 136, 96, 0, 0), (16, 20, 3, 2049, 31, 0, 0), (32, 4, 1, 64, 520, 3, 1),
           (33, 2, 2, 48, 72, 0, 0), (64, 7, 3, 96, 130, 64, 8), (64, 1, 1, 40, 24, 0, 0), (50, 512, 16, 24, 16, 0, 0), (64, 130, 5, 31, 33, 5, 0),
-          (9, 256, 1, 64, 64, 0, 0)]
+          (9, 256, 1, 64, 64, 0, 0),
+          # a token's experts side by side; contractions of 2, 4 and 8 waves, of whole steps or not
+          (1, 6, 5, 72, 1100, 0, 0), (1, 9, 3, 513, 2100, 1, 1), (35, 3, 2, 520, 250, 0, 0), (64, 2, 1, 300, 700, 3, 0), (20, 5, 2, 768, 32, 0, 0)]
 
 
 @pytest.mark.parametrize("type", list(ff.TYPES))
@@ -161,7 +163,7 @@ def test_experts_far_apart(B, type):
     assert torch.equal(y, want)
 
 
-@pytest.mark.parametrize("T,E,k,D,F", [(1, 16, 2, 512, 768), (40, 12, 3, 100, 50), (16, 64, 4, 256, 256)])
+@pytest.mark.parametrize("T,E,k,D,F", [(1, 16, 2, 512, 768), (1, 8, 3, 256, 2100), (40, 12, 3, 100, 50), (16, 64, 4, 256, 256)])
 def test_replayed_from_a_graph_and_on_another_stream(B, T, E, k, D, F):
     c = Case(T, E, k, D, F, "bf16", residual=True, seed=8)
     d = c.desc(B)
