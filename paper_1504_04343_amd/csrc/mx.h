@@ -24,9 +24,12 @@ struct MxProduct {
   FfProduct p;
   MxMatrix x, w;
   int blocks;     // of a row
-  bool quantize;  // x are values yet, in rows of x.ldc (up to kMxQuantizeRows rows on mx_rows.hip)
+  bool quantize;  // x are values yet, in rows of x.ldc (mx_rows.hip, where mx_quantizes says so)
 };
-constexpr int kMxQuantizeRows = 4;
+// Whether the workgroups that multiply quantise x as well, each all of it: a launch (3.5 us) less, as long as every CU has one of them
+// (16 columns) and rows are not too long (one row, weights from memory, and with a launch for x: 4096 x 4096 7.4 and 10.7 us, 4096 x
+// 8192 10.6 and 10.7, 2048 x 16384 17.8 and 12.3, 5120 x 5120 14.4 and 10.9, 8192 x 4096 11.5 and 10.7, 14144 x 8960 42 and 19).
+inline bool mx_quantizes(int M, int N, int K) { return M <= 4 && N <= 4096 && K <= 8192; }
 // How it runs: kNoTile: mx_rows.hip; splits of the contraction, of so many steps of 128 values (rows) or stages of 256 (tiles);
 // deep: tiles of 64 x 64 that hold four stages, not two.
 struct MxPlan {

@@ -83,7 +83,8 @@ MxPlan rows_plan(int M, int N, int K) {
 double rows_micros(int M, int N, int K, const MxPlan& plan) {
   const double row = K * 17.0 / 32, wide = pieces(N, 16), high = pieces(M, 64);
   const double bytes = wide * (16 * high + M) * row;
-  return 4.5 + std::max(std::max((double)N * row / 5.0e6, bytes / 7.5e6), (0.8 + 0.6 * (M <= 16 ? 1 : M <= 32 ? 2 : 4)) * pieces(plan.steps, 32)) + (plan.splits > 1 ? kJoinMicros : 0.0);
+  const double turns = (M <= 16 ? 1.0 : M <= 32 ? 2.0 : 3.2) * pieces(plan.steps, 32);
+  return std::max(2.0 + (double)N * row / 5.0e6, 4.5 + std::max(bytes / 7.5e6, turns)) + (plan.splits > 1 ? kJoinMicros : 0.0);
 }
 
 }  // namespace
@@ -99,7 +100,7 @@ MxPlan mx_plan(int M, int N, int K) {
       const long long groups = tiles * have, slots = (long long)kCus * c.per_cu, rest = groups % slots;
       if (groups * c.threads > kMostThreads) continue;
       double us = ((double)(groups / slots) * c.full + (rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full)) * (each + c.around) + kLaunchMicros;
-      if (M <= kMxQuantizeRows) us += kLaunchMicros;  // of x's codes, if it has none yet: the choice is the same for both
+      if (mx_quantizes(M, N, K)) us += kLaunchMicros;  // of x's codes, if it has none yet: the choice is the same for both
       if (have > 1) us += kJoinMicros + 8.0 * have * M * N / kJoinBytesPerMicro;
       if (us < least) {
         least = us;
@@ -167,7 +168,7 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
   a.blocks = mx_blocks(d.K);
   a.w = {(const unsigned char*)w, ldw, (const unsigned char*)w_scales, ldws};
   a.x = {(const unsigned char*)x, ldx, (const unsigned char*)x_scales, ldxs};
-  a.quantize = quantize && plan.tile == kNoTile && d.M <= kMxQuantizeRows;
+  a.quantize = quantize && plan.tile == kNoTile && mx_quantizes(d.M, d.N, d.K);
   if (quantize && !a.quantize) {
     a.x = {ws + b.codes, mx_code_bytes(d.K), ws + b.scales, mx_scale_bytes(d.K)};
     rc = launch_mx_quantize(d.M, d.K, d.type, x, ldx, ws + b.codes, a.x.ldc, ws + b.scales, a.x.lds, st);
