@@ -79,12 +79,14 @@ MxPlan rows_plan(int M, int N, int K) {
   return plan;
 }
 // us of it: the weight from memory, or both operands of every workgroup of 16 columns from L2 (48 x 16384 x 4096: 27, in tiles of
-// 64 x 128 14), or what a turn takes at least.
+// 64 x 128 14), or what a turn takes at least, or a workgroup itself (6148 x 2954 x 16: 18 000 of them 181, in tiles 26).
 double rows_micros(int M, int N, int K, const MxPlan& plan) {
   const double row = K * 17.0 / 32, wide = pieces(N, 16), high = pieces(M, 64);
   const double bytes = wide * (16 * high + M) * row;
+  const int blocks = M <= 16 ? 1 : M <= 32 ? 2 : 4;
   const double turns = (M <= 16 ? 1.0 : M <= 32 ? 2.0 : 3.2) * pieces(plan.steps, 32);
-  return std::max(2.0 + (double)N * row / 5.0e6, 4.5 + std::max(bytes / 7.5e6, turns)) + (plan.splits > 1 ? kJoinMicros : 0.0);
+  const double each = 0.002 * (1 + blocks) * wide * pieces(M, 16 * blocks);
+  return std::max(std::max(2.0 + (double)N * row / 5.0e6, 3.0 + each), 4.5 + std::max(bytes / 7.5e6, turns)) + (plan.splits > 1 ? kJoinMicros : 0.0);
 }
 
 }  // namespace

@@ -564,6 +564,10 @@ __global__ __launch_bounds__(kJoinRows * 32) void residual_norm_join_kernel(Resi
 }
 
 constexpr int kRowsAhead = 512;  // workgroups, two a CU, of rows that leave no room for more
+int norm_teams(int D, int type) {
+  const int waves = pieces(D, 512);
+  return waves == 1 ? kNormTeams : type != CCT_TYPE_F32 && (waves == 5 || waves == 6) ? 2 : 1;
+}
 int row_threads(int D) { return std::min(kMostWaves, pieces(D, 512)) * 64; }
 double forward_bytes(const ResidualNorm& p) {
   return (double)type_bytes(p.type) * p.M * p.D * (1 + (p.b != nullptr) + (p.s != nullptr) + (p.h != nullptr));
@@ -577,7 +581,10 @@ ResidualNormPlan residual_norm_plan(const cct_residual_norm_desc_t& d) {
   // of its SIMDs, so that rows of more than four waves come one by one
   const int waves = d.D <= 512 ? kNormTeams : pieces(d.D, 512), places = d.type == CCT_TYPE_F32 ? 8 : 12;
   const int most = 256 * (waves <= 4 ? std::min(3, places / waves) : 1);
-  const int wanted = std::max(4, pieces(d.M, most)), shared = std::min(d.gate_rows, std::max(d.M, 1));
+  // (four rows a run at least, so that the runs' sums are little beside the rows, unless that leaves CUs idle: 4 x 6464 fp32 27 -> 16 us;
+  // two rows are a run, which has nothing to join: 12.7 us, 15.5 as two)
+  const int fewest = std::min(4, std::max(norm_teams(d.D, d.type), d.M <= 2 ? 2 : pieces(d.M, 256)));
+  const int wanted = std::max(fewest, pieces(d.M, most)), shared = std::min(d.gate_rows, std::max(d.M, 1));
   p.whole = shared <= wanted;
   if (p.whole) {
     p.rows = pieces(wanted, shared) * shared;
@@ -635,8 +642,7 @@ int launch_residual_norm_back(const ResidualNormBack& p, const ResidualNormPlan&
     int rc = CCT_OK;
     with_type(p.type, [&](auto type) {
       constexpr int TYPE = decltype(type)::value;
-      const int waves = pieces(p.D, 512), teams = p.D <= 512 ? kNormTeams : TYPE != CCT_TYPE_F32 && (waves == 5 || waves == 6) ? 2 : 1;
-      const int threads = teams * waves * 64;
+      const int teams = norm_teams(p.D, TYPE), threads = teams * pieces(p.D, 512) * 64;
       with_bool(p.D % 8 == 0, [&](auto eights) {
         constexpr bool EIGHTS = decltype(eights)::value;
         auto run = [&](auto most) {
