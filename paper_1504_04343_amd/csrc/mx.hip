@@ -86,7 +86,8 @@ double rows_micros(int M, int N, int K, const MxPlan& plan) {
   const int blocks = M <= 16 ? 1 : M <= 32 ? 2 : 4;
   const double turns = (M <= 16 ? 1.0 : M <= 32 ? 2.0 : 3.2) * pieces(plan.steps, 32);
   const double each = 0.002 * (1 + blocks) * wide * pieces(M, 16 * blocks);
-  return std::max(std::max(2.0 + (double)N * row / 5.0e6, 3.0 + each), 4.5 + std::max(bytes / 7.5e6, turns)) + (plan.splits > 1 ? kJoinMicros : 0.0);
+  const double us = std::max(std::max(2.0 + (double)N * row / 5.0e6, 3.0 + each), 4.5 + std::max(bytes / 7.5e6, turns));
+  return us + (plan.splits > 1 ? kJoinMicros : 0.0);
 }
 
 }  // namespace
@@ -101,7 +102,8 @@ MxPlan mx_plan(int M, int N, int K) {
       const int each = pieces(stages, splits), have = pieces(stages, each);
       const long long groups = tiles * have, slots = (long long)kCus * c.per_cu, rest = groups % slots;
       if (groups * c.threads > kMostThreads) continue;
-      double us = ((double)(groups / slots) * c.full + (rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full)) * (each + c.around) + kLaunchMicros;
+      const double last = rest == 0 ? 0.0 : rest <= kCus ? c.alone : c.full;
+      double us = ((double)(groups / slots) * c.full + last) * (each + c.around) + kLaunchMicros;
       if (mx_quantizes(M, N, K)) us += kLaunchMicros;  // of x's codes, if it has none yet: the choice is the same for both
       if (have > 1) us += kJoinMicros + 8.0 * have * M * N / kJoinBytesPerMicro;
       if (us < least) {

@@ -114,7 +114,8 @@ __global__ __launch_bounds__(WM* WN * 64) __attribute__((amdgpu_waves_per_eu(2))
     if ((loaded & 1) == 0) {
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(sc_from), 0,
                                                                          left > 0 ? (int)min(sc_bytes, 0x7fffffffLL) : 0, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(tile_smem + RING * STAGE + (loaded >> 1 & (RING - 1)) * SCALES + unit * 1024), 16, (int)sc_at, 0, 0, 0);
+      unsigned char* to = tile_smem + RING * STAGE + (loaded >> 1 & (RING - 1)) * SCALES + unit * 1024;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)to, 16, (int)sc_at, 0, 0, 0);
       sc_from += 2 * kStageBlocks;
       sc_bytes -= 2 * kStageBlocks;
     }
@@ -234,7 +235,8 @@ int launch_mx_tile(const MxProduct& a, const MxPlan& plan, float* part, hipStrea
   const double mn = (double)a.p.M * a.p.N, k = (double)a.p.K;
   ProfScope ps(2.0 * mn * k,
                (a.p.M + (double)a.p.N) * k * 17 / 32 + type_bytes(a.p.type) * mn * (1 + (a.p.residual != nullptr) + (a.p.z != nullptr)), st,
-               "mx_tile_kernel<%s, %d splits, %d stages>", plan.tile == kTile256 ? "256x256" : plan.tile == kTile128 ? "128x128" : plan.tile == kTile64x128 ? "64x128" : "64x64",
+               "mx_tile_kernel<%s, %d splits, %d stages>",
+               plan.tile == kTile256 ? "256x256" : plan.tile == kTile128 ? "128x128" : plan.tile == kTile64x128 ? "64x128" : "64x64",
                plan.splits, plan.deep ? 4 : 2);
   if (a.p.type == CCT_TYPE_F32) return launch<CCT_TYPE_F32>(a, plan, part, st);
   return a.p.type == CCT_TYPE_BF16 ? launch<CCT_TYPE_BF16>(a, plan, part, st) : launch<CCT_TYPE_F16>(a, plan, part, st);

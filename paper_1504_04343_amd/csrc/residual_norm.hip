@@ -578,7 +578,7 @@ double forward_bytes(const ResidualNorm& p) {
 ResidualNormPlan residual_norm_plan(const cct_residual_norm_desc_t& d) {
   ResidualNormPlan p = {};
   // as many runs as the chip takes at a time: a CU has places for 12 waves of residual_norm_back_kernel (fp32: 8), three for each
-  // of its SIMDs, so that rows of more than four waves come one by one
+  // of its SIMDs; of workgroups of more than four waves one
   const int waves = d.D <= 512 ? kNormTeams : pieces(d.D, 512), places = d.type == CCT_TYPE_F32 ? 8 : 12;
   const int most = 256 * (waves <= 4 ? std::min(3, places / waves) : 1);
   // (four rows a run at least, so that the runs' sums are little beside the rows, unless that leaves CUs idle: 4 x 6464 fp32 27 -> 16 us;
