@@ -473,6 +473,8 @@ void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float*
       const float rstd = rstd_of(t[0], p.D, p.eps);
       n_s *= rstd;
       ds += (dn - n_s * (t[1] * rstd / D) - level_s) * rstd;
+      // the level is subtracted behind the row's end too, where nothing may come from: without a gate and w_after db's mean would hold it
+      if (layer_s) ds = first_of(ds, n);
     }
     if (live) {
       if (p.dr) store_row<TYPE, EIGHTS>(p.dr, row * p.lddr + c, ds, n);

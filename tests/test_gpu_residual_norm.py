@@ -174,6 +174,24 @@ def test_parts_that_are_not_there(B, D):
                 ff.check(k, got[k], want[k])
 
 
+@pytest.mark.parametrize("type", list(ff.TYPES))
+@pytest.mark.parametrize("D", [24, 512, 520, 768, 1000, 2049, 2560, 4100, 8185, 9000])
+def test_layer_norms_without_weights_or_gate(B, D, type):
+    """Nothing but the norms themselves, whose level (the mean of dh, far from zero here) must not reach columns that a row has not."""
+    for none in (("w_after", "c_after", "w_before", "c_before"), ("w_after", "c_after"), ("w_before", "c_before")):
+        c = Case(B, 9, D, type, "layer", "layer", gate=False, seed=D)
+        for n in none:
+            setattr(c, n, None)
+        c.dh = (c.dh.float() + 1.5).to(c.dt)
+        got, want = c.forward(), c.forward64()
+        back, want_back = c.backward(), c.backward64()
+        for k in got:
+            ff.check(k, got[k], want[k])
+        for k in back:
+            ff.check(k, back[k], want_back[k])
+        assert torch.equal(back["db"], c.backward(("db",))["db"])
+
+
 def test_b_is_not_needed_without_its_norm(B):
     c = Case(B, 6, 100, "f32", "rms", "none", rows=2)
     want = c.backward64()
