@@ -471,9 +471,9 @@ int cct_mx_linear_forward(const cct_linear_desc_t* desc, const void* x, int64_t 
  *   weight = exp(logit - max) / sum of that over the chosen experts (normalize != 0) or all of them,
  *   h = act(x[t] wg[e]^T) * (x[t] wu[e]^T),   y[t] = sum over the chosen e of weight * (h wd[e]^T) + residual[t].
  * Experts that no token chooses are not read.  The weights of consecutive experts lie `e` values apart (wg_e >= F rows' extent;
- * any element-aligned address and distance), their rows `ld`.  Sums are fp32; weight * h keeps 16 bits or more for the last
- * product (fp16: an infinity beyond 65504).  residual (tokens x D), chosen_out (tokens x chosen int32, largest logit first) and
- * weights_out (fp32) may be NULL; these two are contiguous.  y may be the residual itself.
+ * any element-aligned address and distance), their rows `ld`.  Sums are fp32, and so is weight * h in the last product, whatever
+ * the type (beside 16-bit weights the last bits of numbers below 2^-110 are lost).  residual (tokens x D), chosen_out (tokens x
+ * chosen int32, largest logit first) and weights_out (fp32) may be NULL; these two are contiguous.  y may be the residual itself.
  * 0 <= tokens, 1 <= chosen <= experts, D, F >= 1 (CCT_EINVAL); CCT_EUNSUPPORTED: more than 64 tokens, 512 experts, 16
  * chosen ones or 2^24 features, matrices as above.  Results are bit-reproducible, and a token's do not depend on the other
  * tokens' values.

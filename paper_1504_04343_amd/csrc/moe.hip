@@ -5,8 +5,7 @@
 //   moe_route_kernel   one workgroup: a wave a token, its chosen experts by rounds of a largest key, their weights; then the experts
 //                      that are used, and for each the rows of h of its tokens (a single token: every wave of the next kernel
 //                      chooses for itself, which takes less than a launch);
-//   moe_gated_kernel   16 columns of both gate and up of one used expert and its tokens: weight * act(g) * u, kept as two 16-bit
-//                      terms (16 bits of a value in bf16, 22 in fp16; fp32 as it is), both of which the next product multiplies;
+//   moe_gated_kernel   16 columns of both gate and up of one used expert and its tokens: weight * act(g) * u, in fp32;
 //   moe_down_kernel    16 columns of one used expert's results and its tokens, or of all experts' for a single token (where that
 //                      keeps the chip busy);
 //   moe_join_kernel    (unless a workgroup had all experts') a token's results added in the order of its choice, and the residual.
@@ -14,9 +13,9 @@
 // steps in turn, their sums meet in LDS in a fixed order.  A token's results do not depend on the other tokens.
 //
 // us of each kernel, bf16 (the last fp16):                                        logits route gated down join   weights
-//   1 token, 2 of 16 experts, 4096 -> 8192                                             5     -    56   31    -    403 MB
-//   16 tokens, 4 of 64 experts, 2048 -> 2048                                           7     7   130   75    5   1038 MB
-//   37 tokens, 3 of 24 experts, 1000 -> 1531, rows at odd distances                    7    10    37   30    5    219 MB
+//   1 token, 2 of 16 experts, 4096 -> 8192                                             5     -    54   31    -    403 MB
+//   16 tokens, 4 of 64 experts, 2048 -> 2048                                           7     7   130   76    5   1038 MB
+//   37 tokens, 3 of 24 experts, 1000 -> 1531, rows at odd distances                    7    10    35   34    5    219 MB
 // The products read at 4.6 to 5.3 TB/s where there are weights enough to fill the chip; what is in front of and behind them are launches.
 // Of the last line's workgroups, two or three rounds of which fill the chip, each waits for its tokens' numbers, weights and sums in turn.
 #include <algorithm>
@@ -24,6 +23,7 @@
 #include "activation.h"
 #include "ff_step.h"
 #include "ff_tile.h"
+#include "split_bf16.h"
 #include "wave_ops.h"
 
 namespace cct {
@@ -46,7 +46,8 @@ struct Moe {
   float* weight;    // of each of these
   int* slot;        // for each used expert its number and its tokens'; -1 behind them
   short* rows;      // kMostTokens for each: its tokens' rows (token * k + place among its chosen ones), the last again
-  void *h, *h_low;  // T k rows of Fp values: the terms; fp32: h alone
+  float* h;         // T k rows of Fp values
+  short* terms;     // a single token's, 16-bit types: three rows for each of them
   float* part;      // T k rows of Dp results
   int Dp;
   int32_t* chosen_out;
@@ -195,23 +196,78 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(Moe a) {
   }
 }
 
-// Four neighbouring values of a row of h.
+// h is fp32 in the second product too.  Beside 16-bit weights it is three bf16 numbers, each the eight leading bits of what is left, which
+// together are the 24 bits of fp32 over its whole range (of numbers below 2^-110 the last bits are lost); an fp16 weight is two.  Two
+// 16-bit terms of h were 16 bits in bf16, and in fp16 ended at 2^-24: 8 bits of a value of 1e-5, an infinity beyond 65504.  Values are
+// split behind their load: terms in memory are half as much again for every workgroup to read (64 tokens, one expert, 4096 -> 8192:
+// 184 us, split in registers 150).  Not a single token's, which are few: they lie beside h, and a term is a column of the product (2 of 16
+// experts, 4096 -> 8192: 91.4 and 89.4 us, fp16 93.1 and 90.3).
 template <int TYPE>
-__device__ __forceinline__ void store_terms(const Moe& a, long long at, const float (&v)[4]) {
-  if constexpr (TYPE == CCT_TYPE_F32) {
-    *(f32x4*)((float*)a.h + at) = f32x4{v[0], v[1], v[2], v[3]};
-  } else {
-    typedef typename Number<TYPE>::T T;
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    T4 high, low;
+constexpr int kWeightTerms = TYPE == CCT_TYPE_F16 ? 2 : 1;
+__device__ __forceinline__ float leading(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+// The eight leading bits of values as bf16; v keeps the rest.
+template <int N>
+__device__ __forceinline__ void take_leading(float (&v)[N], unsigned (&to)[N / 2]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      high[e] = (T)v[e];
-      const float rest = v[e] - (float)high[e];
-      low[e] = (T)(fabsf((float)high[e]) < INFINITY ? rest : 0.f);  // an infinity is one term
+  for (int e = 0; e < N / 2; ++e) {
+    to[e] = __builtin_amdgcn_perm(__float_as_uint(v[2 * e + 1]), __float_as_uint(v[2 * e]), 0x07060302u);
+    v[2 * e] -= leading(v[2 * e]);
+    v[2 * e + 1] -= leading(v[2 * e + 1]);
+  }
+}
+__device__ __forceinline__ s16x8 next_term(float (&v)[8]) {
+  unsigned to[4];
+  take_leading(v, to);
+  return __builtin_bit_cast(s16x8, u32x4{to[0], to[1], to[2], to[3]});
+}
+template <int TYPE>
+__device__ __forceinline__ void weight_terms(s16x8 w, s16x8 (&to)[kWeightTerms<TYPE>]) {
+  if constexpr (TYPE == CCT_TYPE_F16) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)__builtin_bit_cast(f16x8, w)[e];
+    to[0] = next_term(v);
+    to[1] = next_term(v);
+  } else {
+    to[0] = w;
+  }
+}
+
+// What a lane has of h in a step, beside its weights; TERMS: it is one of its terms.
+template <int TYPE, bool TERMS>
+struct HStep {
+  typedef float V __attribute__((ext_vector_type(Step<TYPE>::CH)));
+};
+template <int TYPE>
+struct HStep<TYPE, true> {
+  typedef s16x8 V;
+};
+template <int TYPE, bool TERMS, int RM>
+__device__ __forceinline__ void multiply_h(typename Step<TYPE>::V w, const typename HStep<TYPE, TERMS>::V (&h)[RM], int tokens, f32x4 (&acc)[RM]) {
+  if constexpr (TYPE == CCT_TYPE_F32) {
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+      if (i == 0 || i * 16 < tokens) acc[i] = Step<TYPE>::mfma(w, h[i], acc[i]);
+  } else {
+    s16x8 wt[kWeightTerms<TYPE>];
+    weight_terms<TYPE>(w, wt);
+    auto add = [&](s16x8 term, f32x4& to) {
+#pragma unroll
+      for (int q = 0; q < kWeightTerms<TYPE>; ++q) to = tile_mfma<CCT_TYPE_BF16>(wt[q], term, to);
+    };
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      if (i > 0 && i * 16 >= tokens) continue;
+      if constexpr (TERMS) {
+        add(h[i], acc[i]);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = h[i][e];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) add(next_term(v), acc[i]);
+      }
     }
-    *(T4*)((T*)a.h + at) = high;
-    *(T4*)((T*)a.h_low + at) = low;
   }
 }
 
@@ -351,18 +407,31 @@ __global__ __launch_bounds__(NW * 64) void moe_gated_kernel(Moe a) {
       activate<true>(a.activation, g, u);
 #pragma unroll
       for (int c = 0; c < 4; ++c) g[c] = at + c < a.F ? g[c] * weight[i] : 0.f;  // zeros up to whole steps
-      store_terms<TYPE>(a, (long long)row[i] * a.Fp + at, g);
+      *(f32x4*)(a.h + (long long)row[i] * a.Fp + at) = f32x4{g[0], g[1], g[2], g[3]};
+      if constexpr (ONE && TYPE != CCT_TYPE_F32)
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          unsigned term[2];
+          take_leading(g, term);
+          typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+          *(u32x2*)(a.terms + ((long long)row[i] * 3 + t) * a.Fp + at) = u32x2{term[0], term[1]};
+        }
     }
   }
 }
 
 // The down product.  ONE: a single token, whose chosen experts' features are one contraction; else an expert and its tokens, whose
-// results go to `part`.
+// results go to `part`.  A sum that is not finite may be one by the terms alone (0 times an infinite weight): it is formed again, of
+// the values, in fp32.  One block of tokens has three steps on their way and five waves a SIMD: 16 tokens, 4 of 64 experts, 2048 ->
+// 2048, 221 us, four steps and four waves 228 to 231.
 template <int TYPE, int RM, bool ONE, int NW>
-__global__ __launch_bounds__(NW * 64) void moe_down_kernel(Moe a, FfProduct p) {
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(ONE ? 4 : RM == 1 ? 5 : 2)))
+void moe_down_kernel(Moe a, FfProduct p) {
   typedef Step<TYPE> S;
   typedef typename S::V V;
-  constexpr int TERMS = TYPE == CCT_TYPE_F32 ? 1 : 2, BATCH = ONE ? 8 : RM == 4 ? 2 : 4;
+  constexpr bool TERMS = ONE && TYPE != CCT_TYPE_F32;  // of h are there: lanes 0 to 2 of 16 have one each
+  typedef typename HStep<TYPE, TERMS>::V H;
+  constexpr int BATCH = ONE ? 8 : RM == 4 ? 2 : RM == 1 ? 3 : 4;
   static_assert(!ONE || RM == 1, "one token");
   extern __shared__ __attribute__((aligned(16))) unsigned char moe_smem[];
   f32x4(*sums)[RM][64] = (f32x4(*)[RM][64])moe_smem;  // [NW]
@@ -396,7 +465,8 @@ __global__ __launch_bounds__(NW * 64) void moe_down_kernel(Moe a, FfProduct p) {
 #pragma unroll
     for (int i = 0; i < RM; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int whole = a.F / S::K, steps = (a.F + S::K - 1) / S::K, total = count * steps;  // an expert's last step may end within
-    V w[BATCH], h[BATCH][RM][TERMS];
+    V w[BATCH];
+    H h[BATCH][RM];
     for (int s0 = wave; s0 < total; s0 += BATCH * NW) {
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
@@ -405,13 +475,13 @@ __global__ __launch_bounds__(NW * 64) void moe_down_kernel(Moe a, FfProduct p) {
         const long long row_of_w = (ONE ? (int)chosen[slot] : e) * a.wd.e + w_row;
         w[q] = step < whole ? S::load(a.wd.p, row_of_w + k) : tail_raw<TYPE>(a.wd.p, row_of_w, k, a.F);
 #pragma unroll
-        for (int i = 0; i < RM; ++i)
-          if (i == 0 || i * 16 < n) {
-            const bool there = i * 16 + lo < n;  // lanes without a token ask for nothing
-            const long long h_of = h_at[i] + (ONE ? slot * (long long)a.Fp : 0) + k;
-            h[q][i][0] = there ? S::load(a.h, h_of) : V{};
-            if constexpr (TERMS == 2) h[q][i][1] = there ? S::load(a.h_low, h_of) : V{};
-          }
+        for (int i = 0; i < RM; ++i) {  // lanes without a token ask for nothing
+          if (i > 0 && i * 16 >= n) continue;
+          if constexpr (TERMS)
+            h[q][i] = lo < 3 ? *(const H*)(a.terms + (slot * 3LL + lo) * a.Fp + k) : H{};
+          else
+            h[q][i] = i * 16 + lo < n ? *(const H*)(a.h + h_at[i] + (ONE ? slot * (long long)a.Fp : 0) + k) : H{};
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -419,11 +489,7 @@ __global__ __launch_bounds__(NW * 64) void moe_down_kernel(Moe a, FfProduct p) {
         const int at = s0 + q * NW, step = ONE ? at % steps : at;
         if (at >= total) break;
         if (step >= whole) w[q] = tail_settled<TYPE>(w[q], step * S::K + kq, a.F);
-#pragma unroll
-        for (int i = 0; i < RM; ++i)
-          if (i == 0 || i * 16 < n)
-#pragma unroll
-            for (int t = 0; t < TERMS; ++t) acc[i] = S::mfma(w[q], h[q][i][t], acc[i]);
+        multiply_h<TYPE, TERMS, RM>(w[q], h[q], n, acc);
       }
     }
 #pragma unroll
@@ -432,10 +498,39 @@ __global__ __launch_bounds__(NW * 64) void moe_down_kernel(Moe a, FfProduct p) {
 #pragma unroll
     for (int i = 0; i < RM; ++i) {
       const int m = i * 16 + lo, c = n0 + (lane >> 4) * 4;
-      if (wave != i % NW || m >= n || c >= a.D) continue;
+      if (wave != i % NW) continue;
+      const bool live = m < n && c < a.D;
       f32x4 s = sums[0][i][lane];
 #pragma unroll
       for (int q = 1; q < NW; ++q) s += sums[q][i][lane];
+      if constexpr (TERMS)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] += __shfl_down(s[r], 1, 64) + __shfl_down(s[r], 2, 64);
+      if constexpr (TYPE != CCT_TYPE_F32) {
+#pragma unroll 1
+        for (int r = 0; r < 4; ++r) {
+          const float v = r == 0 ? s[0] : r == 1 ? s[1] : r == 2 ? s[2] : s[3];
+          const bool again = live && c + r < a.D && !finite(v);
+          if (!__any(again)) continue;
+          struct Result {
+            long long w, h;
+          };
+          const float exact = fp32_sum(
+              again, count * a.F,
+              [&](int of) {
+                return Result{(n0 + (of >> 4) * 4 + r) * a.wd.ld, __shfl(row[i], of & 15, 64) * (long long)a.Fp};
+              },
+              [&](const Result& to, int k, float* x, float* y) {
+                const int slot = ONE ? k / a.F : 0, f = k - slot * a.F;
+                *x = load1<TYPE>(a.wd.p, (ONE ? (int)chosen[slot] : e) * a.wd.e + to.w + f);
+                *y = a.h[to.h + slot * (long long)a.Fp + f];
+                return true;
+              });
+#pragma unroll
+          for (int q = 0; q < 4; ++q) s[q] = again && q == r ? exact : s[q];
+        }
+      }
+      if (!live) continue;
       if constexpr (ONE) {
         float v[4] = {s[0], s[1], s[2], s[3]}, u[4] = {};
         finish<TYPE, kFfLinear>(p, m, c, v, u);
@@ -564,8 +659,8 @@ long long lay_out(const cct_moe_desc_t& d, char* ws, Moe* a) {
   a->weight = (float*)take(4LL * a->T * a->k);
   a->slot = (int*)take(8LL * a->slots);
   a->rows = (short*)take(2LL * kMostTokens * a->slots);
-  a->h = take((long long)type_bytes(d.type) * a->T * a->k * a->Fp);
-  a->h_low = take(d.type == CCT_TYPE_F32 ? 0 : 2LL * a->T * a->k * a->Fp);
+  a->h = (float*)take(4LL * a->T * a->k * a->Fp);
+  a->terms = (short*)take(a->T == 1 && d.type != CCT_TYPE_F32 ? 6LL * a->k * a->Fp : 0);
   a->Dp = (d.D + 3) / 4 * 4;
   a->part = (float*)take(4LL * a->T * a->k * a->Dp);
   return std::max(total, 256LL);
