@@ -371,8 +371,9 @@ __global__ __launch_bounds__(kColumnThreads) void residual_norm_columns_kernel(R
       store_first<CCT_TYPE_F32>((char*)part + k * plan.part_bytes, (long long)blockIdx.y * p.D + c, sums.v[k], n);
 }
 
-// Where the norms' sums are: LDS, so that 128 registers are enough for two workgroups on a CU; the next row of fp32 values leaves
-// no room for that, up to 512 threads they have 256.
+// Where the norms' sums are: LDS, where a workgroup may be of up to sixteen waves: four on a SIMD leave a thread 128 registers, too few
+// for the sums and a row, so that the next row is not on its way either.  The sums take 128 KiB, one workgroup a CU, which is what
+// the plan counts on.  Up to 512 threads have 256 registers.
 template <int THREADS>
 constexpr bool norm_sums_in_lds = THREADS == 1024;
 
