@@ -1,6 +1,8 @@
-// SiLU and GELU to within 2^-19 of the value (GELU_TANH 2^-16 far down, where its argument's roundings are that), for results that are
-// rounded to 16 bits (by 2^-8 and 2^-11).  An epilogue of 8192 x 8192 results: SiLU 17 us, GELU 28, GELU_TANH 24; activation.h's, with
-// branches for far arguments and divisions good to the last place, 87, 57 and 65.
+// SiLU to within 2^-21 of the value, GELU 2^-19.7 (2^-18.8 at -13, by its power's constant), GELU_TANH 2^-20.5 around zero and 2^-16 far
+// down, where its argument's roundings are that; on all bf16 and fp16 numbers 2^-22.9, 2^-20.9 and 2^-18.1.  activation.h's GELU has 2^-22
+// around zero and 2^-16.4 at -13.  For results that are rounded to 16 bits (by 2^-8 and 2^-11): an epilogue of 8192 x 8192 of them takes
+// 17 to 25 us by card with SiLU, 28 to 38 with GELU, 24 to 34 with GELU_TANH; activation.h's, with branches for far arguments and
+// divisions good to the last place, 87, 57 and 65 on the first.
 #pragma once
 #include "activation.h"
 
@@ -34,16 +36,18 @@ __device__ __forceinline__ float gelu_tanh_near(float z) {
   return z * __builtin_ldexpf(__builtin_amdgcn_rcpf(1.f + __builtin_ldexpf(e.m, k)), k - e.k);
 }
 
-// z Phi(z).  With a = |z| and t = 1 / (1 + 0.27 a), Phi(-a) = exp(-a^2 / 2) t G(t), G the polynomial of degree 6 that is closest to it,
-// relative, over 0 <= a <= 20 (within 1.3e-6; a least-squares fit reweighted by its own errors, to the function in 64 bits).
+// z Phi(z).  With a = |z| and t = 1 / (1 + 0.31 a), Phi(-a) = exp(-a^2 / 2) t G(t), G the polynomial of degree 7 that is closest to it,
+// relative, over 0 <= a <= 20 (within 1.7e-7; a least-squares fit reweighted by its own errors, to the function in 64 bits).  One of
+// degree 6 is within 1.3e-6, 2^-19.4 of GELU, and takes as long.
 __device__ __forceinline__ float gelu_near(float z) {
-  constexpr float G[] = {0.107676625f, 0.10856124f, 0.0923238099f, 0.118718855f, -0.0255898498f, 0.159367070f, -0.0610583499f};
+  constexpr float G[] = {0.123655595f, 0.124079123f, 0.107661881f,  0.110446729f,
+                         -0.0154997231f, 0.155677781f, -0.141939357f, 0.0359180607f};
   const float a = fminf(__builtin_fabsf(z), 20.f), s = a * a;
   const Power e = power(s, 0.721347520f, __builtin_fmaf(a, a, -s));
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, 0.27f, 1.f));
-  float q = G[6];
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(a, 0.31f, 1.f));
+  float q = G[7];
 #pragma unroll
-  for (int i = 5; i >= 0; --i) q = __builtin_fmaf(q, t, G[i]);
+  for (int i = 6; i >= 0; --i) q = __builtin_fmaf(q, t, G[i]);
   q = __builtin_ldexpf(q * t * e.m, e.k);
   return z * (z < 0.f ? q : 1.f - q);
 }

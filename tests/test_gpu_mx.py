@@ -212,6 +212,32 @@ def test_activations_of_all_numbers(B, type, act, M):
     ff.check("y", y[there].view(1, -1), ff.rounded(a, ff.ACT_ERR * a.abs(), dt))
 
 
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("act,least,bound", [("silu", -60.0, 2.0 ** -21), ("gelu", -4.0, 2.0 ** -19.7), ("gelu_tanh", -1.0, 2.0 ** -20.5)],
+                         ids=["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("M", [1, 300])
+def test_activations_before_they_are_rounded(B, type, act, least, bound, M):
+    """The rounded activation as a residual that is taken away leaves act(z)'s own digits.  In units of 2^-23, a place of the hardware's
+    exp2 and reciprocal at the most, half of one an operation's rounding: SiLU 1 of each, 1 + e, the product and the power's argument:
+    3.2, 2^-21.3.  GELU: the polynomial 1.4, t (1.5 places at a = 3.2, where the function goes with its power 1.84; 1 of power 2.6 at
+    a = 0) 2.8, Horner's steps 1, exp2 1.5 with its argument, whose constant is short of 0.9 at a = 4, three products 1.5: 9.1, 2^-19.8.
+    GELU_TANH down to -1: an argument of 1.7 with two roundings and its constant's 1.8, the rest as SiLU: 5, 2^-20.6."""
+    dt, N = ff.TYPES[type], 65536
+    z = torch.arange(N, dtype=torch.int32).to(torch.uint16).view(dt)
+    z = z.masked_fill(~torch.isfinite(z), 0.0)
+    v = z.double()
+    if act == "gelu":
+        a = v * 0.5 * torch.special.erfc(-v * 0.5 ** 0.5)
+    else:
+        a = v * torch.sigmoid(v if act == "silu" else 2 * 0.7978845608028654 * (v + 0.044715 * v ** 3))
+    near = -a.to(dt)
+    zeros = lambda rows: given(B, torch.zeros(rows, 32, dtype=torch.uint8), torch.full((rows, 1), 127, dtype=torch.uint8), 32)
+    y, _ = run(B, type, act, zeros(M), zeros(N), z, near.expand(M, N).contiguous(), False, M, N, 32)
+    there = (v >= least) & (a.abs() > 2.0 ** -100)
+    value = (a + near.double())[there].expand(M, -1)
+    ff.check("y", y[:, there.cuda()], ff.rounded(value, bound * a[there].abs().expand(M, -1), dt))
+
+
 @pytest.mark.parametrize("M", [1, 20, 300])
 def test_whole_numbers(B, M):
     """Sums of whole numbers below 2^24 are exact, whatever their order."""
