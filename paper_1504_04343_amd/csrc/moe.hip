@@ -12,11 +12,12 @@
 // The two products are those of few rows (ff_rows.hip): weights go from memory into the registers of the matrix cores, waves take
 // steps in turn, their sums meet in LDS in a fixed order.  A token's results do not depend on the other tokens.
 //
-// us of each kernel, bf16 (the last fp16):                                        logits route gated down join   weights
-//   1 token, 2 of 16 experts, 4096 -> 8192                                             5     -    54   31    -    403 MB
-//   16 tokens, 4 of 64 experts, 2048 -> 2048                                           7     7   130   76    5   1038 MB
+// us of each kernel (within 2 %), bf16 (the last fp16):                          logits route gated down join   weights
+//   1 token, 2 of 16 experts, 4096 -> 8192                                             5     -    53   31    -    403 MB
+//   16 tokens, 4 of 64 experts, 2048 -> 2048                                           7     7   131   76    5   1038 MB
 //   37 tokens, 3 of 24 experts, 1000 -> 1531, rows at odd distances                    7    10    35   34    5    219 MB
-// The products read at 4.6 to 5.3 TB/s where there are weights enough to fill the chip; what is in front of and behind them are launches.
+// The products read at 4.6 to 5.4 TB/s (fp32 too: 16 tokens, 4 of 64, 2048 -> 1024, 213 us in all) where there are weights enough to
+// fill the chip; what is in front of and behind them are launches.
 // Of the last line's workgroups, two or three rounds of which fill the chip, each waits for its tokens' numbers, weights and sums in turn.
 #include <algorithm>
 

@@ -6,7 +6,8 @@
 // load a lane, every second stage; a lane reads a stage's words (four blocks a step) of its rows and keeps its own blocks' bytes,
 // two rows' and two steps' to a register.
 //
-// 8192 x 8192 x 8192: 276 to 300 us by card, 3.7 to 4.0 PFLOP/s.  The instructions alone, in a loop on registers, reach 9.3 PFLOP/s
+// 8192 x 8192 x 8192: 276 to 300 us by card, 3.7 to 4.0 PFLOP/s, in calls that follow one another on the same codes; with bias and GELU
+// 318 to 330, and about 355 in a kernel trace, where each launch stands alone.  The instructions alone, in a loop on registers, reach 9.3 PFLOP/s
 // on zeros and 6.2 to 7.0 on random codes (the card's clock falls); what keeps a tile of 256 x 256 from that is LDS, which a stage
 // asks for 24 KiB x 8 waves of operands and gives 64 KiB of new ones, as long as its matrix instructions take.  Without loads 245 of
 // then 311 us, without LDS reads 274, without scales 289, without waves meeting 288.  Slower: scales in loads of 4 bytes (298), a ring

@@ -165,7 +165,7 @@ __device__ __forceinline__ typename Number<TYPE>::V8 row_vector(const void* p, i
 // A row in registers, 8 columns a thread: a workgroup takes one at a time, or a wave where 512 columns are all.  What it waits for
 // is memory, and between loads and stores the meetings of its waves (two norms: one each, layer norms two), so that other
 // workgroups, or, where a row takes half a CU or more (AHEAD), the next row's loads have to fill them.  bf16, one norm after the
-// addition, 8192 x 4096: 48 us, 5.6 TB/s; 8192 x 8192: 102 us, with weights loaded behind the next row 130, without the next row
+// addition, 8192 x 4096: 48 us, 5.6 TB/s (fp32 95, 5.7); 8192 x 8192: 102 us, with weights loaded behind the next row 130, without the next row
 // on its way 156.
 template <int TYPE, bool EIGHTS, bool AHEAD>
 __global__ __launch_bounds__(1024) void residual_norm_kernel(ResidualNorm p, bool wave_rows) {
@@ -381,9 +381,10 @@ constexpr bool norm_sums_in_lds = THREADS == 1024;
 // it has teams of waves for a row each (in spans: of a gate row's rows, so that its sum is one team's): four of one wave where 512
 // columns are all, two of five or six.  The next row is on its way while one is worked on; its sums over columns stay with the thread.
 // Between a row's loads and stores its waves meet two or three times, which is what the time went into (8192 x 4096, bf16, two norms
-// and a gate: 84 to 100 us by card, 79 at a copy's rate; 15 more with sums over waves that read LDS one after the other); the runs'
-// sums and their joining take 6 to 10 us more.  Two teams, since a CU starts no second workgroup of five waves: 8192 x 2560 89 -> 67 us,
-// 1531 x 2049 fp16 with layer norms 39 -> 34 (two such workgroups a CU in the plan were 49 for 41 then).
+// and a gate: 84 to 93 us by card in calls that follow one another, 103 to 108 in a kernel trace, where each launch stands alone; 79 at
+// a copy's rate; 15 more with sums over waves that read LDS one after the other); the runs' sums and their joining take 6 to 10 us
+// more.  Two teams, since a CU starts no second workgroup of five waves: 8192 x 2560 89 -> 67 us, 1531 x 2049 fp16 with layer norms 39
+// -> 34 (two such workgroups a CU in the plan were 49 for 41 then).
 template <int TYPE, int THREADS, bool EIGHTS>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS / 256 < 2 ? 2 : THREADS / 256)))
 void residual_norm_back_kernel(ResidualNormBack p, ResidualNormPlan plan, float* __restrict__ part) {
